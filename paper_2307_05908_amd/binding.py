@@ -1,4 +1,4 @@
-"""ctypes binding of libppd (include/ppd.h, include/ppd_measure.h): argument marshalling only.
+"""ctypes binding of libppd (include/ppd.h, include/ppd_measure.h, include/ppd_layers.h): argument marshalling only.
 
 Every step of the decode path runs in the HIP kernels behind the C ABI; this
 module turns torch device tensors into the pointer tables the library takes
@@ -49,10 +49,26 @@ class Stats(ctypes.Structure):
                  "weight_bytes", "kv_bytes")]
 
 
+class PagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int64) for n in ("k_page", "k_pos", "k_head", "v_page", "v_pos", "v_head")] + \
+               [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")]
+
+
+class PagedBatch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q_start", "kv_len", "pages")] + [("pages_stride", ctypes.c_int64)] + \
+               [(n, ctypes.c_int32) for n in ("max_pages", "n_seqs", "n_tokens")]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
 EXPORTS = ("ppd_create", "ppd_reset", "ppd_prefill", "ppd_step", "plain_greedy_step", "ppd_get_logits",
            "ppd_get_early_logits", "ppd_get_stats", "ppd_set_profiling", "ppd_set_graphs", "ppd_set_sampling", "ppd_get_kernel_time",
            "ppd_time_ffn_in", "ppd_get_chain_rounds", "ppd_set_chain_wait", "ppd_stream_read_probe", "ppd_early_topk", "ppd_early_topk_noalloc", "ppd_destroy",
-           "ppd_strerror", "ppd_last_hip_error")
+           "ppd_strerror", "ppd_last_hip_error",
+           "ppd_paged_append", "ppd_paged_attention", "ppd_paged_attention_workspace", "ppd_verify_drafts", "ppd_verify_drafts_workspace")
 
 _lib = None
 
@@ -88,6 +104,13 @@ def load_library() -> ctypes.CDLL:
     lib.ppd_stream_read_probe.argtypes = [vp, ctypes.c_uint64, ci, ctypes.POINTER(ctypes.c_double)]
     lib.ppd_early_topk.argtypes = [ci, ci, ci, ctypes.c_float, ci, vp, vp, vp, vp, ci, vp, vp, vp, vp]
     lib.ppd_early_topk_noalloc.argtypes = lib.ppd_early_topk.argtypes
+    cp, bp, rp = ctypes.POINTER(PagedCache), ctypes.POINTER(PagedBatch), ctypes.POINTER(Rows)
+    cl, cu, cf = ctypes.c_int64, ctypes.c_uint64, ctypes.c_float
+    lib.ppd_paged_append.argtypes = [cp, bp, ci, rp, rp, rp, rp, vp, vp, cf, ci, cf, vp]
+    lib.ppd_paged_attention.argtypes = [cp, bp, ci, rp, rp, vp, cf, ci, vp, cu, vp]
+    lib.ppd_paged_attention_workspace.argtypes = [cp, bp, ci, ctypes.POINTER(cu)]
+    lib.ppd_verify_drafts.argtypes = [ci, ci, ci, ci, vp, vp, vp, cl, vp, cl, vp, vp, vp, vp, vp, cu, vp]
+    lib.ppd_verify_drafts_workspace.argtypes = [ci, ci, ci, ci, ctypes.POINTER(cu)]
     lib.ppd_destroy.argtypes = [vp]
     lib.ppd_destroy.restype = None
     lib.ppd_strerror.argtypes = [ci]
@@ -160,6 +183,164 @@ def ppd_early_topk_noalloc(h, norm_g, norm_b, head, k, norm, norm_eps=1e-5, want
     """The same through the entry point that allocates nothing (fixed scratch array in the library; asynchronous:
     the outputs are complete once the stream's work has run).  The output tensors are the caller's, made here."""
     return _early_topk_call("ppd_early_topk_noalloc", h, norm_g, norm_b, head, k, norm, norm_eps, want_logits, stream)
+
+
+# ---- operators on paged keys and values (include/ppd_layers.h)
+def _dtype_code(t) -> int:
+    import torch
+    codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    if t.dtype not in codes:
+        raise ValueError(f"float32, bfloat16 or float16 expected, not {t.dtype}")
+    return codes[t.dtype]
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _on_device(first, others, stream, call):
+    """call(stream) with the tensors' device as the current one and what it allocates on the stream that it works on.  Tensors that
+    another stream than the current one reads or writes are not given away before that stream is done with them."""
+    import torch
+    dev = first.device
+    _need(dev.type == "cuda" and all(t is None or t.device == dev for t in others), "all tensors on one GPU")
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _on_device(first, others, stream, call)
+    cur = torch.cuda.current_stream()
+    if stream is None or stream == cur:
+        return call(ctypes.c_void_p(cur.cuda_stream))
+    _need(stream.device == dev, "the stream is another GPU's")
+    for t in (first, *others):
+        if t is not None:
+            t.record_stream(stream)
+    with torch.cuda.stream(stream):
+        return call(ctypes.c_void_p(stream.cuda_stream))
+
+
+def _paged_args(k_cache, v_cache, pages, q_start, kv_len, n_tokens):
+    import torch
+    _need(k_cache.dim() == 4 and k_cache.shape == v_cache.shape and k_cache.dtype == v_cache.dtype,
+          "k_cache, v_cache: [n_pages, page_size, n_kv_heads, head_dim] of one type")
+    ks, vs = k_cache.stride(), v_cache.stride()
+    _need(ks[3] == 1 and vs[3] == 1, "head_dim must be contiguous")
+    i32 = torch.int32
+    _need(pages.dtype == i32 and q_start.dtype == i32 and kv_len.dtype == i32, "pages, q_start, kv_len: int32")
+    n = kv_len.numel()
+    _need(pages.dim() == 2 and pages.shape[0] == n and q_start.numel() == n + 1, "pages [n_seqs, max_pages], q_start [n_seqs + 1], kv_len [n_seqs]")
+    _need(q_start.is_contiguous() and kv_len.is_contiguous() and (pages.shape[1] < 2 or pages.stride(1) == 1), "contiguous index arrays")
+    shape = k_cache.shape
+    c = PagedCache(k_cache.data_ptr(), v_cache.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], shape[0], shape[1], shape[2], shape[3], _dtype_code(k_cache))
+    b = PagedBatch(q_start.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), pages.stride(0), pages.shape[1], n, n_tokens)
+    return c, b
+
+
+def _rows(t, like, what, n_tokens, heads=None) -> Rows:
+    _need(t.dim() == 3 and t.shape[0] == n_tokens and t.shape[2] == like.shape[3] and t.dtype == like.dtype and (heads is None or t.shape[1] == heads),
+          f"{what}: [n_tokens, heads, head_dim] of the cache's type")
+    s = t.stride()
+    _need(s[2] == 1, f"{what}: head_dim must be contiguous")
+    return Rows(t.data_ptr(), s[0], s[1])
+
+
+def ppd_paged_append(k_cache, v_cache, pages, q_start, kv_len, q, k, v, q_gain=None, k_gain=None, norm_eps=1e-5, rotary_dim=0,
+                     rope_theta=10000.0, q_out=None, stream=None):
+    """Queries and keys of a ragged batch normalised per head (where a gain is given) and rotated, keys and values written to their
+    pages.  q [n_tokens, n_heads, head_dim] (None: keys and values only), k and v [n_tokens, n_kv_heads, head_dim].  Returns q_out
+    (made here if not given, without contents where a row belongs to no sequence; may be q itself).  Asynchronous."""
+    import torch
+    lib = load_library()
+
+    def call(st):
+        n = k.shape[0]
+        c, b = _paged_args(k_cache, v_cache, pages, q_start, kv_len, n)
+        kr, vr = _rows(k, k_cache, "k", n, c.n_kv_heads), _rows(v, k_cache, "v", n, c.n_kv_heads)
+        out, qr, outr, heads = q_out, None, None, 0
+        if q is not None:
+            qr, heads = _rows(q, k_cache, "q", n), q.shape[1]
+            if out is None:
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            outr = _rows(out, k_cache, "q_out", n, heads)
+        for g in (q_gain, k_gain):
+            _need(g is None or (g.dtype == k_cache.dtype and g.numel() == c.head_dim and g.is_contiguous()), "gains: [head_dim] of the cache's type")
+        rc = lib.ppd_paged_append(c, b, heads, qr, outr, kr, vr, None if q_gain is None else q_gain.data_ptr(),
+                                  None if k_gain is None else k_gain.data_ptr(), norm_eps, rotary_dim, rope_theta, st)
+        if rc != 0:
+            raise PPDError(rc, "ppd_paged_append", lib.ppd_last_hip_error(None))
+        return out
+
+    return _on_device(k_cache, (v_cache, pages, q_start, kv_len, q, k, v, q_gain, k_gain, q_out), stream, call)
+
+
+def ppd_paged_attention(q, k_cache, v_cache, pages, q_start, kv_len, scale=None, window=0, out=None, want_lse=False, workspace=None, stream=None):
+    """Attention of a ragged batch's new tokens over their sequences' pages: (out [n_tokens, n_heads, head_dim], lse float32
+    [n_tokens, n_heads] or None).  scale None: 1 / sqrt(head_dim).  out, and workspace (a uint8 tensor), are made here if not given; rows
+    of no sequence keep what out holds (a new one holds nothing there).  Asynchronous."""
+    import torch
+    lib = load_library()
+
+    def call(st):
+        n = q.shape[0]
+        c, b = _paged_args(k_cache, v_cache, pages, q_start, kv_len, n)
+        qr, heads = _rows(q, k_cache, "q", n), q.shape[1]
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        outr = _rows(o, k_cache, "out", n, heads)
+        lse = torch.empty((n, heads), dtype=torch.float32, device=q.device) if want_lse else None
+        need = ctypes.c_uint64()
+        rc = lib.ppd_paged_attention_workspace(c, b, heads, need)
+        w = workspace
+        if rc == 0 and w is None and need.value:
+            w = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+        if rc == 0:
+            rc = lib.ppd_paged_attention(c, b, heads, qr, outr, None if lse is None else lse.data_ptr(),
+                                         c.head_dim ** -0.5 if scale is None else scale, window, None if w is None else w.data_ptr(),
+                                         0 if w is None else w.numel() * w.element_size(), st)
+        if rc != 0:
+            raise PPDError(rc, "ppd_paged_attention", lib.ppd_last_hip_error(None))
+        return o, lse
+
+    return _on_device(q, (k_cache, v_cache, pages, q_start, kv_len, out, workspace), stream, call)
+
+
+def ppd_verify_drafts(target_logits, ids, row_start, uniform, draft_logits=None, temperature=None, tokens=None, accepted=None, workspace=None,
+                      stream=None):
+    """Drafted tokens against the target model's logits: (tokens int32 [n_rows], accepted int32 [n_seqs]).  target_logits and
+    draft_logits [n_rows, vocab], ids int32 [n_rows], row_start int32 [n_seqs + 1], uniform float32 [n_rows, 2], temperature float32
+    [n_seqs] (0: arg max).  tokens, accepted and workspace (a uint8 tensor) are made here if not given.  Asynchronous."""
+    import torch
+    lib = load_library()
+
+    def call(st):
+        i32, f32 = torch.int32, torch.float32
+        z, d = target_logits, draft_logits
+        _need(z.dim() == 2 and (z.shape[1] < 2 or z.stride(1) == 1), "target_logits: [n_rows, vocab], vocab contiguous")
+        n, vocab = z.shape
+        _need(d is None or (d.shape == z.shape and d.dtype == z.dtype and (vocab < 2 or d.stride(1) == 1)), "draft_logits: as target_logits")
+        seqs = row_start.numel() - 1
+        _need(ids.dtype == i32 and ids.numel() == n and row_start.dtype == i32 and seqs >= 1, "ids int32 [n_rows], row_start int32 [n_seqs + 1]")
+        _need(uniform.dtype == f32 and uniform.numel() == 2 * n, "uniform: float32 [n_rows, 2]")
+        _need(temperature is None or (temperature.dtype == f32 and temperature.numel() == seqs), "temperature: float32 [n_seqs]")
+        t = torch.empty(n, dtype=i32, device=z.device) if tokens is None else tokens
+        a = torch.empty(seqs, dtype=i32, device=z.device) if accepted is None else accepted
+        _need(t.dtype == i32 and t.numel() == n and a.dtype == i32 and a.numel() == seqs, "tokens int32 [n_rows], accepted int32 [n_seqs]")
+        _need(all(x is None or x.is_contiguous() for x in (ids, row_start, uniform, temperature, t, a)), "contiguous arrays")
+        need = ctypes.c_uint64()
+        code = _dtype_code(z)
+        rc = lib.ppd_verify_drafts_workspace(seqs, n, vocab, code, need)
+        w = workspace
+        if rc == 0 and w is None and need.value:
+            w = torch.empty(need.value, dtype=torch.uint8, device=z.device)
+        if rc == 0:
+            rc = lib.ppd_verify_drafts(seqs, n, vocab, code, row_start.data_ptr(), ids.data_ptr(), z.data_ptr(), z.stride(0) if n > 1 else vocab,
+                                       None if d is None else d.data_ptr(), 0 if d is None else d.stride(0) if n > 1 else vocab,
+                                       None if temperature is None else temperature.data_ptr(), uniform.data_ptr(), t.data_ptr(), a.data_ptr(),
+                                       None if w is None else w.data_ptr(), 0 if w is None else w.numel() * w.element_size(), st)
+        if rc != 0:
+            raise PPDError(rc, "ppd_verify_drafts", lib.ppd_last_hip_error(None))
+        return t, a
+
+    return _on_device(target_logits, (ids, row_start, uniform, draft_logits, temperature, tokens, accepted, workspace), stream, call)
 
 
 class PPD:

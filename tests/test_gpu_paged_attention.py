@@ -1,0 +1,341 @@
+"""ppd_paged_attention against 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paged_common import HALF_STEP, TINY, Batch, attention64
+from paper_2307_05908_amd import binding
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+TYPES = [F32, BF16, F16]
+
+
+def call(d, **kw):
+    return binding.ppd_paged_attention(d.q, d.k_cache, d.v_cache, d.pages, d.q_start, d.kv_len, want_lse=True, **kw)
+
+
+def limits(b, ref, lse, size, reach):
+    """How far (out, lse) may be off.  A score: head_dim products and sums in fp32, and the scale: (hd + 4) half steps of the largest
+    sum of products.  It goes through exp2 with two more roundings of its size and four of its own.  The sums over n positions: n half
+    steps.  A weight's relative error counts twice (numerator and denominator).  Weights are rounded to the values' type for their product
+    with them (not for their sum), and so is the result."""
+    n = max(b.kv) if b.kv else 0
+    w = (b.hd + 8) * reach + n + 16
+    w = w * 2.0 ** -24
+    once = 0.0 if b.dtype == F32 else HALF_STEP[b.dtype]
+    return size * (2 * w[..., None] + once) + ref.abs() * HALF_STEP[b.dtype] * (1 + 2.0 ** -9) + TINY[b.dtype], w + lse.abs() * 2.0 ** -23
+
+
+def check(b, scale=None, window=0, d=None, ref=None):
+    d = b.cuda() if d is None else d
+    out, lse = call(d, scale=scale, window=window, out=torch.full_like(d.q, 7.0))
+    torch.cuda.synchronize()
+    o, z = out.cpu().double(), lse.cpu().double()
+    ref64, lse64, size, reach = attention64(b, scale, window) if ref is None else ref
+    r = b.rows
+    tol, ltol = limits(b, ref64, lse64, size, reach)
+    gone = torch.isinf(lse64[:r])
+    assert torch.equal(torch.isinf(z[:r]) & (z[:r] < 0), gone)
+    assert (o[:r][gone] == 0).all()
+    assert ((z[:r] - lse64[:r]).abs()[~gone] <= ltol[:r][~gone]).all(), float((z[:r] - lse64[:r]).abs()[~gone].max())
+    bad = (o[:r] - ref64[:r]).abs() > tol[:r]
+    assert not bad.any() and not o[:r].isnan().any(), (bad.nonzero()[:5], o[:r][bad][:5], ref64[:r][bad][:5])
+    assert (o[r:] == 7.0).all()                                        # rows of no sequence
+    return out, lse
+
+
+SHAPES = {
+    "one": ([1], [1]),
+    "token": ([1], [333]),
+    "tokens": ([1, 1, 1, 0, 1], [1, 64, 65, 30, 700]),
+    "drafts": ([4, 3, 1, 5], [4, 130, 17, 64]),
+    "runs": ([16, 17, 0, 33, 2], [16, 80, 5, 33, 300]),
+    "chunk": ([130, 1], [257, 90]),
+    "prompt": ([200], [200]),
+}
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("shape", list(SHAPES))
+@pytest.mark.parametrize("heads,kv_heads", [(2, 2), (6, 2), (8, 1)])
+def test_types_heads_and_lengths(dtype, hd, shape, heads, kv_heads):
+    new, kv = SHAPES[shape]
+    check(Batch(new, kv, heads, kv_heads, hd, dtype, seed=len(shape), pad=2))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (3, 1), (5, 5), (16, 1), (32, 2), (21, 3), (40, 4), (70, 2)])
+def test_shared_heads(dtype, heads, kv_heads):
+    check(Batch([1, 3, 11], [50, 70, 140], heads, kv_heads, 64, dtype, seed=heads))
+
+
+@pytest.mark.parametrize("page", [1, 3, 8, 16, 20, 64, 100, 256])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_pages(page, dtype):
+    check(Batch([1, 40, 3], [90, 130, 200], 4, 2, 128, dtype, page=page, seed=page))
+
+
+@pytest.mark.parametrize("layout", ["phkd", "pkhd", "hpkd", "khpd"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_orders_of_the_cache(layout, dtype):
+    check(Batch([1, 40, 3], [90, 130, 200], 4, 2, 128, dtype, layout=layout))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("window", [1, 2, 16, 63, 64, 65, 100, 1000])
+def test_windows(dtype, window):
+    b = Batch([1, 40, 3, 150], [190, 130, 200, 333], 4, 2, 64, dtype, seed=window)
+    check(b, window=window)
+    # pages that no row's window reaches any more are given back
+    for s, (m, x) in enumerate(zip(b.new, b.kv)):
+        b.pages[s, :max(0, x - m - window + 1) // b.page] = -1
+    check(b, window=window)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_scales(dtype):
+    for scale in (1e-6, 0.03, 1.0, 5.0):
+        check(Batch([2, 30], [70, 100], 4, 4, 64, dtype), scale=scale)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("hd", [64, 128])
+def test_every_position_has_its_part(dtype, hd):
+    """Equal scores: the log sum is the log of the number of positions seen, which no lost or doubled one leaves as it is; and one score
+    far above the others gives that position's value, bit for bit."""
+    b = Batch([1, 4, 70, 1], [1000, 513, 300, 64], 4, 2, hd, dtype)
+    b.q.zero_()
+    _, lse = check(b)
+    at = [x - m + i for m, x in zip(b.new, b.kv) for i in range(m)]
+    count = torch.tensor([[float(p + 1)] for p in at])
+    assert (torch.exp(lse.cpu()[:b.rows].double()) - count).abs().max() < 0.1
+    rng = np.random.default_rng(1)
+    b = Batch([1, 4, 70, 1], [1000, 513, 300, 64], 4, 2, hd, dtype)
+    b.k_cache *= 0
+    b.q.zero_()
+    want = torch.empty(b.rows, 4, hd, dtype=dtype)
+    row = 0
+    axis = {}
+    for s, (m, x) in enumerate(zip(b.new, b.kv)):
+        picks = rng.choice(x, size=hd, replace=x < hd)               # component c of the keys marks position picks[c]
+        for c, p in enumerate(picks):
+            b.k_cache[b.slot(s, int(p))][:, c] = 60.0
+        for i in range(m):
+            seen = [c for c, p in enumerate(picks) if p <= x - m + i and list(picks).count(p) == 1]
+            for h in range(4):
+                if seen:
+                    c = seen[rng.integers(len(seen))]
+                    b.q[row, h, c] = 60.0
+                    want[row, h] = b.v_cache[b.slot(s, int(picks[c]))][h // 2]
+                else:
+                    want[row, h] = float("nan")
+            row += 1
+    out, _ = call(b.cuda(), scale=1.0)
+    some = ~want.isnan().any(-1)
+    assert some.sum() > 150 and torch.equal(out.cpu()[:b.rows][some], want[some])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_that_see_nothing(dtype):
+    b = Batch([5, 3, 70, 2], [2, 0, 60, 40], 4, 2, 64, dtype, spare=8)        # kv below the rows: the first ones have no position
+    b.pages[3, :] = -1                                                        # a sequence without any page
+    check(b)
+    b = Batch([1, 1], [0, 33], 4, 2, 64, dtype)
+    check(b)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_pages_that_are_not_there(dtype):
+    """Holes, numbers that are no page's, lengths behind the table."""
+    b = Batch([3, 70, 1, 2], [200, 170, 300, 90], 4, 2, 128, dtype, spare=4)
+    b.pages[0, 3], b.pages[0, 11], b.pages[1, 0], b.pages[1, 5] = -1, b.n_pages, 2 ** 31 - 1, -2 ** 31
+    b.pages = b.pages[:, :15].contiguous()
+    check(b)
+    b.kv_len[2] = 2 ** 31 - 1                                                 # far behind its pages: all of them are seen
+    b.kv[2] = 15 * 16 + 1
+    b.kv_len[3] = -5
+    b.kv[3] = 0
+    check(b)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_what_is_not_seen_has_no_part(dtype, hd, bad):
+    """NaN and infinities in free slots, in other sequences' pages, outside the window and in later tokens."""
+    b = Batch([1, 60, 4, 140], [90, 77, 30, 140], 4, 2, hd, dtype)
+    ref = attention64(b)
+    d = b.cuda()
+    used = torch.zeros(b.n_pages, b.page, dtype=torch.bool)
+    for s in range(4):
+        for p in range(b.kv[s]):
+            used[b.slot(s, p)] = True
+    d.k_cache[~used.cuda()] = bad
+    d.v_cache[~used.cuda()] = bad
+    check(b, d=d, ref=ref)
+    # the last tokens of the two runs, and one in the middle: rows before them are as they were
+    for s, back in ((1, 1), (1, 40), (3, 1), (3, 100)):
+        slot = b.slot(s, b.kv[s] - back)
+        d.k_cache[slot], d.v_cache[slot] = bad, bad
+    out, lse = call(d)
+    first, tol, ltol = b.rows - 140 - 4 - 60, *limits(b, *ref)
+    for lo, hi in ((0, first + 60 - 40), (first + 60, first + 64), (first + 64, first + 64 + 40)):
+        assert ((out.cpu().double() - ref[0]).abs() <= tol)[lo:hi].all()
+        assert ((lse.cpu().double() - ref[1]).abs() <= ltol)[lo:hi].all()
+    late = out[first + 60 - 40:first + 60].cpu()
+    assert late.isnan().any(-1).all() if math.isnan(bad) else True
+    # outside the window
+    b = Batch([1, 60, 4, 140], [90, 77, 30, 140], 4, 2, hd, dtype)
+    ref = attention64(b, window=20)
+    d = b.cuda()
+    slot = b.slot(3, 50)
+    d.k_cache[slot], d.v_cache[slot] = bad, bad
+    out, lse = call(d, window=20)
+    tol, ltol = limits(b, *ref)
+    clean = [r for r in range(b.rows) if not (r >= 65 and 50 <= r - 65 < 70)]
+    assert ((out.cpu().double() - ref[0]).abs() <= tol)[clean].all() and ((lse.cpu().double() - ref[1]).abs() <= ltol)[clean].all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_one_infinite_value_is_one_infinite_component(dtype):
+    b = Batch([1, 40], [90, 60], 2, 2, 64, dtype)
+    d = b.cuda()
+    for s, p in ((0, 17), (1, 50)):
+        d.v_cache[b.slot(s, p)][0, 5] = math.inf
+    out, _ = call(d)
+    clean, _, _, _ = attention64(b)
+    o = out.cpu().double()
+    hit = torch.zeros_like(o, dtype=torch.bool)
+    hit[0, 0, 5] = True
+    hit[1 + 30:, 0, 5] = True                                                 # positions 20 .. 59: from 50 on
+    assert torch.isinf(o[hit]).all() and torch.isfinite(o[~hit]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_long_and_split(dtype):
+    """Few rows over many positions (cut into parts and joined), alone and beside short sequences."""
+    check(Batch([1], [4100], 8, 2, 128, dtype, page=64))
+    check(Batch([4, 1, 1, 2], [3000, 5, 1, 700], 4, 1, 64, dtype, page=32))
+    check(Batch([20, 1], [2500, 2000], 4, 4, 128, dtype, page=16), window=1500)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_many_sequences(dtype):
+    rng = np.random.default_rng(5)
+    new = rng.integers(0, 4, 150)
+    check(Batch(new.tolist(), (new + rng.integers(0, 120, 150)).tolist(), 4, 2, 64, dtype, pad=5))
+    check(Batch([1] * 300, rng.integers(1, 50, 300).tolist(), 2, 2, 64, dtype))
+
+
+def test_prompts_beside_tokens():
+    check(Batch([1, 300, 1, 0, 64, 1, 5], [400, 300, 20, 7, 200, 1, 90], 8, 2, 128, BF16, pad=3))
+    check(Batch([1, 300, 1, 0, 64, 1, 5], [400, 300, 20, 7, 200, 1, 90], 8, 8, 64, F16, pad=3), window=50)
+
+
+def test_strided_rows():
+    b = Batch([3, 20], [50, 60], 4, 2, 128, BF16)
+    d = b.cuda()
+    ref, _ = call(d)
+    whole = torch.zeros((b.n, 9, 128), dtype=BF16, device="cuda")
+    whole[:, 2:6] = d.q
+    out = torch.full((4, b.n, 128), 3.0, dtype=BF16, device="cuda").transpose(0, 1)
+    got, _ = binding.ppd_paged_attention(whole[:, 2:6], d.k_cache, d.v_cache, d.pages, d.q_start, d.kv_len, out=out)
+    assert got is out and torch.equal(got, ref)
+    # keys and values in one tensor, as pages of both
+    both = torch.stack([d.k_cache, d.v_cache], 1)
+    got, _ = binding.ppd_paged_attention(d.q, both[:, 0], both[:, 1], d.pages, d.q_start, d.kv_len)
+    assert torch.equal(got, ref)
+    # a table that is part of a wider one
+    wide = torch.full((2, 100), 3, dtype=torch.int32, device="cuda")
+    wide[:, :d.pages.shape[1]] = d.pages
+    got, _ = binding.ppd_paged_attention(d.q, d.k_cache, d.v_cache, wide[:, :d.pages.shape[1]], d.q_start, d.kv_len)
+    assert torch.equal(got, ref)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_same_bits_every_time_and_for_equal_sequences(dtype):
+    b = Batch([1, 3, 40, 1], [2000, 800, 90, 1500], 8, 2, 128, dtype).cuda()
+    out, lse = call(b)
+    for _ in range(5):
+        o, z = call(b)
+        assert torch.equal(o, out) and torch.equal(z, lse)
+
+
+def test_offsets_beyond_32_bits():
+    n_pages = (1 << 31) // (64 * 8 * 128) + 40
+    for dtype in (BF16, F32):
+        b = Batch([3, 50], [150, 130], 16, 8, 128, dtype, page=32)
+        far = torch.zeros((n_pages, 64, 8, 128), dtype=dtype, device="cuda")
+        d = b.cuda()
+        kc, vc = far[:, :32], far[:, 32:]
+        move = torch.arange(n_pages - 2 * b.n_pages, n_pages, 2)[:b.n_pages]
+        kc[move.cuda()], vc[move.cuda()] = d.k_cache, d.v_cache
+        ref, rl = call(d)
+        d.pages = torch.where(d.pages >= 0, move.int().cuda()[d.pages.clamp(min=0).long()], -1)
+        d.k_cache, d.v_cache = kc, vc
+        out, lse = call(d)
+        assert torch.equal(out, ref) and torch.equal(lse, rl)
+        del far, kc, vc, d
+        torch.cuda.empty_cache()
+
+
+def test_streams_replays_and_growing_lengths():
+    """Captured once for a table's worth of positions; lengths grow from replay to replay, two graphs live side by side."""
+    b = Batch([2, 1, 1], [40, 700, 3], 8, 2, 128, BF16, extra_pages=4, spare=30).cuda()
+    free = [p for p in range(b.n_pages) if p not in b.pages.flatten().tolist()]
+    for s in range(3):
+        for i in range(b.pages.shape[1]):
+            if int(b.pages[s, i]) < 0 and free:
+                b.pages[s, i] = free.pop()
+    c = Batch([20, 30], [900, 30], 8, 2, 128, BF16, seed=5).cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    ref, _ = call(b)
+    got, _ = call(b, stream=side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(ref, got)
+    graphs = []
+    for x in (b, c):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = call(x)
+        graphs.append((g, x, out))
+    for i in range(4):
+        for g, x, (out, lse) in graphs:
+            x.kv_len += 1 if x is b else 0
+            x.q.copy_(torch.randn_like(x.q))
+            g.replay()
+            o, z = out.clone(), lse.clone()
+            torch.cuda.synchronize()
+            want, wz = call(x)
+            assert torch.equal(o, want) and torch.equal(z, wz)
+
+
+def test_a_workspace_of_the_callers():
+    import ctypes
+    b = Batch([1, 2], [3000, 90], 4, 2, 128, BF16).cuda()
+    ref, _ = call(b)
+    c, bb = binding._paged_args(b.k_cache, b.v_cache, b.pages, b.q_start, b.kv_len, b.n)
+    need = ctypes.c_uint64()
+    assert binding.load_library().ppd_paged_attention_workspace(c, bb, 4, need) == 0
+    if need.value:
+        w = torch.full((need.value + 64,), 0xff, dtype=torch.uint8, device="cuda")
+        got, _ = call(b, workspace=w[:need.value])
+        torch.cuda.synchronize()
+        assert torch.equal(got, ref) and bool((w[need.value:] == 0xff).all())
+        with pytest.raises(binding.PPDError) as e:
+            call(b, workspace=w[:need.value - 1])
+        assert e.value.code == -1
+
+
+def test_nothing_to_do():
+    b = Batch([0, 0], [5, 0], 4, 2, 64, BF16).cuda()
+    out, lse = call(b)
+    assert out.shape == (0, 4, 64) and lse.shape == (0, 4)
+    b = Batch([0, 0], [5, 0], 4, 2, 64, BF16, pad=3)
+    check(b)

@@ -1,0 +1,323 @@
+"""ppd_verify_drafts against the rule in 64 bits, row by row on the host."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2307_05908_amd import binding
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def softmax64(z, t):
+    z = np.where(np.isnan(z), -np.inf, z.astype(np.float64))
+    top = z.max()
+    if top == -np.inf:
+        return np.zeros_like(z)
+    with np.errstate(invalid="ignore"):
+        e = np.where(z == top, 1.0, np.exp((z - top) / t))
+    return e / e.sum()
+
+
+def rule(drafts, ids, z, zd, temp, u):
+    """(tokens, accepted, how near a number came to a border: cases nearer than sums in another order can move it are left out)"""
+    n = sum(drafts) + len(drafts)
+    tokens, accepted, near = np.full(n, -1), np.zeros(len(drafts), int), 1.0
+    row = 0
+    for s, m in enumerate(drafts):
+        for i in range(m + 1):
+            r, last = row + i, i == m
+            d = None if last else int(ids[r + 1])
+            real = d is not None and 0 <= d < z.shape[1]
+            if temp[s] <= 0 or math.isnan(temp[s]):
+                zz = np.where(np.isnan(z[r]), -np.inf, z[r])
+                choice, take = int(np.argmax(zz)), False
+                take = real and d == choice and zz[choice] > -np.inf
+            else:
+                p = softmax64(z[r], temp[s])
+                q = np.zeros_like(p)
+                if not last:
+                    if zd is not None:
+                        q = softmax64(zd[r], temp[s])
+                    elif real:
+                        q[d] = 1.0
+                take = real and u[r, 0] * q[d] < p[d]
+                if real and p[d] > 0:
+                    near = min(near, abs(u[r, 0] * q[d] - p[d]) / p[d])
+                left = np.maximum(p - q, 0)
+                # p and q that are equal but for their last digits leave nothing but noise
+                left = left if left.sum() > 0 else p
+                upto = np.cumsum(left)
+                choice = int(np.searchsorted(upto, u[r, 1] * upto[-1], side="right")) if upto[-1] > 0 else 0
+                if choice == len(p):
+                    choice = int(np.nonzero(left)[0][-1])
+                if not take and upto[-1] > 0:
+                    near = min(near, np.abs(upto - u[r, 1] * upto[-1]).min() / upto[-1])
+            if take:
+                tokens[r], accepted[s] = d, accepted[s] + 1
+            else:
+                tokens[r] = choice
+                break
+        row += m + 1
+    return tokens, accepted, near
+
+
+def make(drafts, vocab, dtype, seed, with_draft=True, temp=None, agree=0.5, kept=0):
+    g = torch.Generator().manual_seed(seed)
+    n = sum(drafts) + len(drafts)
+    z = 3 * torch.randn(n, vocab, generator=g)
+    zd = z + agree * torch.randn(n, vocab, generator=g)
+    if kept:
+        for x in (z, zd):
+            x[x < torch.topk(x, min(kept, vocab), dim=1).values[:, -1:]] = -math.inf
+    z, zd = z.to(dtype), zd.to(dtype)
+    t = torch.full((len(drafts),), 0.8) if temp is None else torch.tensor(temp, dtype=torch.float32)
+    per_row = torch.repeat_interleave(t, torch.tensor([d + 1 for d in drafts])).clamp(min=0)[:, None].nan_to_num()
+    noise = -torch.log(-torch.log(torch.rand(n, vocab, generator=g).clamp(1e-9, 1 - 1e-6)))
+    drawn = torch.argmax(zd.float() + (noise * per_row if with_draft else 0), 1).int()
+    ids = torch.cat([torch.zeros(1, dtype=torch.int32), drawn[:-1]])
+    u = torch.rand(n, 2, generator=g)
+    start = torch.tensor(np.concatenate([[0], np.cumsum([d + 1 for d in drafts])]), dtype=torch.int32)
+    return dict(drafts=drafts, ids=ids, z=z, zd=zd if with_draft else None, t=t, u=u, start=start)
+
+
+def call(c, **kw):
+    up = lambda x: None if x is None else x.cuda()  # noqa: E731
+    return binding.ppd_verify_drafts(up(c["z"]), up(c["ids"]), up(c["start"]), up(c["u"]), draft_logits=up(c["zd"]), temperature=up(c["t"]), **kw)
+
+
+def check(c):
+    z, zd = c["z"].float().numpy(), None if c["zd"] is None else c["zd"].float().numpy()
+    temp = c["t"].numpy().astype(np.float64) if c["t"] is not None else np.ones(len(c["drafts"]))
+    tokens, accepted, near = rule(c["drafts"], c["ids"].numpy(), z, zd, temp, c["u"].numpy().astype(np.float64))
+    # 64-bit sums over 2^17 terms in any order are within 2^17 * 2^-53 = 2^-36 of each other
+    assert near > 2.0 ** -35, "the inputs are at a border"
+    t, a = call(c)
+    np.testing.assert_array_equal(a.cpu().numpy(), accepted)
+    np.testing.assert_array_equal(t.cpu().numpy(), tokens)
+    return accepted
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [1, 2, 3, 63, 64, 65, 255, 1000, 1021, 4096, 4097, 8191, 32000])
+@pytest.mark.parametrize("with_draft", [True, False])
+def test_vocabularies_and_types(dtype, vocab, with_draft):
+    c = make([3, 0, 5, 1, 8], vocab, dtype, vocab, with_draft, temp=[0.8, 1.0, 0.3, 2.0, 0.0])
+    if vocab <= 3 and not with_draft:
+        c["ids"] %= vocab
+    check(c)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_large_vocabularies(dtype):
+    check(make([4, 2], 131072 + 13, dtype, 1))
+    check(make([0], 50272, dtype, 2))
+    check(make([1, 3], 300001, dtype, 3, temp=[0.0, 1.0]))
+
+
+def test_accepting_and_rejecting_everywhere():
+    """Drafters from near to far: every number of taken drafts occurs."""
+    seen = set()
+    for seed, agree in enumerate((0.0, 0.05, 0.3, 1.0, 3.0)):
+        c = make([6] * 40, 500, torch.float32, seed, agree=agree)
+        seen |= set(check(c).tolist()) if agree else set()
+        if not agree:                                   # the same distribution: every draft is taken whatever u is
+            t, a = call(c)
+            assert (a == 6).all()
+    assert seen == set(range(7))
+
+
+@pytest.mark.parametrize("kept", [1, 2, 50])
+def test_filtered_logits(kept):
+    for with_draft in (True, False):
+        check(make([4, 3, 6] * 4, 777, torch.float32, kept, with_draft, kept=kept))
+        check(make([4, 3, 6] * 4, 5000, torch.bfloat16, kept, with_draft, kept=kept, agree=2.0))
+
+
+def test_no_temperature_and_all_greedy():
+    c = make([4, 0, 2], 3001, torch.float32, 9, temp=[1.0] * 3)
+    a = check(c)
+    c["t"] = None
+    np.testing.assert_array_equal(check(c), a)
+    check(make([4, 0, 2, 7], 3001, torch.float32, 9, temp=[0.0, -1.0, math.nan, 0.0], agree=0.02))
+    check(make([4, 0, 2, 7], 3001, torch.bfloat16, 9, False, temp=[0.0] * 4, agree=0.02))       # many ties
+
+
+def test_small_and_large_temperatures():
+    check(make([3] * 5, 1000, torch.float32, 4, temp=[1e-3, 1e-30, 1e-42, 50.0, 1e30]))
+
+
+def test_equal_logits_are_drawn_by_id():
+    """Where all weights are equal the token is floor(u * vocab); the greedy choice is token 0."""
+    v = 4096
+    c = make([0] * 64, v, torch.float32, 3, temp=[1.0] * 64)
+    c["z"].zero_()
+    c["u"][:, 1] = (torch.arange(64) / 64)              # exactly on borders: the sums are exact, "exceeds" decides
+    t, _ = call(c)
+    np.testing.assert_array_equal(t.cpu().numpy(), np.arange(64) * (v // 64))
+    c["t"] = torch.zeros(64)
+    t, _ = call(c)
+    assert (t == 0).all()
+
+
+def test_random_numbers_at_their_ends():
+    c = make([2, 2, 2, 2], 1000, torch.float32, 8, kept=20)
+    for value in (0.0, 1.0 - 2.0 ** -24):
+        c["u"][:] = value
+        z = c["z"].numpy()
+        t, a = call(c)
+        t, a = t.cpu().numpy(), a.cpu().numpy()
+        for s in range(4):
+            r = 3 * s + a[s]
+            assert np.isfinite(z[r, t[r]])              # never a token that was filtered out
+        if value == 0.0:
+            assert (a == 2).all() or not np.isfinite(z[[r for s in range(4) for r in (3 * s, 3 * s + 1)], :][:, 0]).all()
+    for value in (1.0, 2.0, -1.0, math.nan, math.inf):  # no result of the rule, but tokens of the vocabulary
+        c["u"][:] = value
+        t, a = call(c)
+        t = t.cpu().numpy()
+        assert ((t >= -1) & (t < 1000)).all()
+
+
+def test_logits_without_a_distribution():
+    v = 700
+    c = make([2, 2, 2, 2, 2, 2], v, torch.float32, 2, temp=[1.0, 1.0, 1.0, 0.0, 1.0, 1.0])
+    c["z"][0] = -math.inf                               # nothing left: no draft is taken, token 0
+    c["z"][3] = math.nan
+    c["z"][6, 100] = math.inf                           # one +inf: that token
+    c["ids"][7] = 100
+    c["z"][7, 5] = math.nan                             # a NaN among others: as if filtered out
+    c["z"][9] = -math.inf
+    c["zd"][12] = -math.inf                             # a drafter without a distribution: a draft of any probability is taken
+    c["zd"][15, 3:5] = math.inf
+    c["ids"][16] = 4
+    tokens, accepted, _ = rule(c["drafts"], c["ids"].numpy(), c["z"].numpy(), c["zd"].numpy(), c["t"].numpy().astype(float), c["u"].numpy().astype(float))
+    t, a = call(c)
+    np.testing.assert_array_equal(a.cpu().numpy(), accepted)
+    np.testing.assert_array_equal(t.cpu().numpy(), tokens)
+    assert tokens[0] == 0 and tokens[3] == 0 and tokens[6] == 100 and accepted[2] >= 1 and tokens[9] == 0 and accepted[4] >= 1
+
+
+def test_drafts_outside_the_vocabulary():
+    for with_draft in (True, False):
+        for bad in (-1, 500, 2 ** 31 - 1, -2 ** 31):
+            c = make([3, 3], 500, torch.float32, 6, with_draft)
+            c["ids"][2] = bad
+            c["ids"][5] = bad
+            check(c)
+
+
+def test_sequences_without_rows_and_padded_rows():
+    c = make([3, 2], 900, torch.bfloat16, 5)
+    ref, acc, _ = rule(c["drafts"], c["ids"].numpy(), c["z"].float().numpy(), c["zd"].float().numpy(), c["t"].numpy().astype(float), c["u"].numpy().astype(float))
+    pad = lambda x: torch.cat([x, x[:3]])  # noqa: E731
+    c["z"], c["zd"], c["ids"], c["u"] = (pad(c[n]) for n in ("z", "zd", "ids", "u"))
+    c["start"] = torch.tensor([0, 0, 4, 4, 7, 7], dtype=torch.int32)
+    c["t"] = torch.full((5,), 0.8)
+    tokens = torch.full((10,), 77, dtype=torch.int32, device="cuda")
+    t, a = call(c, tokens=tokens)
+    np.testing.assert_array_equal(a.cpu().numpy(), [0, acc[0], 0, acc[1], 0])
+    np.testing.assert_array_equal(t.cpu().numpy(), ref.tolist() + [77] * 3)
+    # nothing but empty sequences, with and without rows
+    c["start"] = torch.zeros(6, dtype=torch.int32)
+    t, a = call(c, tokens=tokens.fill_(5))
+    assert (a == 0).all() and (t == 5).all()
+    z = torch.empty((0, 900), device="cuda")
+    t, a = binding.ppd_verify_drafts(z, torch.empty(0, dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda"), torch.empty((0, 2), device="cuda"))
+    assert t.numel() == 0 and (a == 0).all()
+
+
+def test_bounds_outside_the_rows():
+    """row_start that reaches behind the rows, or before them: what is there counts, nothing else is touched."""
+    c = make([3, 2], 300, torch.float32, 5)
+    c["start"] = torch.tensor([-4, 4, 1000], dtype=torch.int32)
+    ref, acc, _ = rule(c["drafts"], c["ids"].numpy(), c["z"].numpy(), c["zd"].numpy(), c["t"].numpy().astype(float), c["u"].numpy().astype(float))
+    t, a = call(c)
+    np.testing.assert_array_equal(a.cpu().numpy(), acc)
+    np.testing.assert_array_equal(t.cpu().numpy(), ref)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_strides_and_offsets(dtype):
+    """Rows of any alignment, from a wider tensor."""
+    for vocab, off in ((1001, 1), (1001, 3), (4095, 5), (640, 8)):
+        c = make([3, 2, 4], vocab, dtype, vocab + off)
+        ref, acc, _ = rule(c["drafts"], c["ids"].numpy(), c["z"].float().numpy(), c["zd"].float().numpy(), c["t"].numpy().astype(float), c["u"].numpy().astype(float))
+        wide = [torch.full((12, vocab + 17), math.nan, dtype=dtype, device="cuda") for _ in range(2)]
+        for w, x in zip(wide, (c["z"], c["zd"])):
+            w[:, off:off + vocab] = x.cuda()
+        t, a = binding.ppd_verify_drafts(wide[0][:, off:off + vocab], c["ids"].cuda(), c["start"].cuda(), c["u"].cuda(), draft_logits=wide[1][:, off:off + vocab],
+                                         temperature=c["t"].cuda())
+        np.testing.assert_array_equal(a.cpu().numpy(), acc)
+        np.testing.assert_array_equal(t.cpu().numpy(), ref)
+
+
+def test_long_and_many():
+    check(make([70, 0, 130], 257, torch.float32, 1, agree=0.1))
+    check(make(np.random.default_rng(0).integers(0, 4, 700).tolist(), 100, torch.bfloat16, 2))
+
+
+def test_the_emitted_tokens_have_the_targets_distribution():
+    """The rule's point.  40000 sequences of one draft over 12 tokens: the first emitted token's counts against p, within 5 standard
+    deviations of a binomial count each (a correct rule fails one of the 12 in about 10^5 runs; the numbers are fixed)."""
+    v, n = 12, 4000
+    g = torch.Generator().manual_seed(11)
+    z, zd = 1.5 * torch.randn(v, generator=g), 1.5 * torch.randn(v, generator=g)
+    counts = np.zeros(v)
+    for part in range(10):
+        drawn = torch.multinomial(torch.softmax(zd.double(), 0), n, replacement=True, generator=g).int()
+        ids = torch.stack([torch.zeros(n, dtype=torch.int32), drawn], 1).flatten()
+        rows = torch.arange(n + 1, dtype=torch.int32) * 2
+        t, _ = binding.ppd_verify_drafts(z.repeat(2 * n, 1).cuda(), ids.cuda(), rows.cuda(), torch.rand(2 * n, 2, generator=g).cuda(), draft_logits=zd.repeat(2 * n, 1).cuda())
+        counts += np.bincount(t.cpu().numpy()[::2], minlength=v)
+    p = torch.softmax(z.double(), 0).numpy()
+    assert (np.abs(counts - 10 * n * p) <= 5 * np.sqrt(10 * n * p * (1 - p))).all()
+
+
+def test_rows_beyond_32_bits():
+    """The last rows lie more than 2^32 bytes into the logits."""
+    v = 131072
+    n = (1 << 33) // (4 * v) + 8
+    z = torch.zeros((n, v), device="cuda")
+    c = make([3, 3], v, torch.float32, 3)
+    z[-8:] = c["z"].cuda()
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")
+    ids[-8:] = c["ids"].cuda()
+    u = torch.zeros((n, 2), device="cuda")
+    u[-8:] = c["u"].cuda()
+    start = torch.tensor([n - 8, n - 4, n], dtype=torch.int32, device="cuda")
+    t, a = binding.ppd_verify_drafts(z, ids, start, u, temperature=c["t"].cuda())
+    c["zd"] = None
+    ref, acc, _ = rule(c["drafts"], c["ids"].numpy(), c["z"].numpy(), None, c["t"].numpy().astype(float), c["u"].numpy().astype(float))
+    np.testing.assert_array_equal(a.cpu().numpy(), acc)
+    np.testing.assert_array_equal(t[-8:].cpu().numpy(), ref)
+
+
+def test_streams_and_replays():
+    cs = [make([4, 2, 0, 7], 20000, torch.float32, 4), make([1, 5], 3001, torch.float32, 5)]
+    dev = [{k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in c.items()} for c in cs]
+    run = lambda d, **kw: binding.ppd_verify_drafts(d["z"], d["ids"], d["start"], d["u"], draft_logits=d["zd"], temperature=d["t"], **kw)  # noqa: E731
+    refs = [[x.clone() for x in run(d)] for d in dev]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out = run(dev[0], stream=side)
+    side.synchronize()
+    assert torch.equal(out[0], refs[0][0]) and torch.equal(out[1], refs[0][1])
+    graphs = []
+    for d in dev:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = run(d)
+        graphs.append((g, out))
+    for i in range(4):
+        for (g, out), d in zip(graphs, dev):
+            d["u"].copy_(torch.rand_like(d["u"]))
+            for x in out:
+                x.fill_(-7)
+            g.replay()
+            got = [x.clone() for x in out]
+            want = run(d)
+            torch.cuda.synchronize()
+            assert all(torch.equal(x, y) for x, y in zip(got, want))

@@ -1,113 +1,475 @@
 // ppd_paged_attention: attention of ragged runs of new tokens over paged keys and values.
+//
+// For a key/value head its group of query heads is as many rows for each new token: row r of a sequence is token r / group, head
+// r % group of the group, and a tile is 16 rows that read the same keys and values.  Scores are computed transposed, S^T = K Q^T: in a
+// matrix product's result a lane then has one row (column r of S^T) and four positions in turn, so a row's maximum and sum stay in a
+// lane but for one exchange of four lanes, and the weights are, as they lie in the registers, the right operand of O^T = V^T P^T.
 #include "ppd_layers_common.h"
 
 #include <math.h>
 
+#include <type_traits>
+
 using namespace ppd;
 
 namespace {
+
+constexpr int ROWS = 16;              // rows of a tile
+constexpr int PLAN_BLOCK = 64;        // positions that lengths are cut by
+constexpr int SPLIT_WAVES = 4;
 
 struct PagedAttnArgs {
   Batch b;
   const void* q; void* out; float* lse; const void *kc, *vc;
   int64_t q_tok, q_head, o_tok, o_head;
   int64_t kc_page, kc_pos, kc_head, vc_page, vc_pos, vc_head;
-  int heads, kv_heads, window;
-  float scale;
+  int heads, kv_heads, group, window;
+  float to_log2;                      // scale * log2(e): a score's exponent of two
+  int want, least;                    // parts per key/value head to aim at; blocks of a part at least (0: one part each)
+  float* part_o; float2* part_ml;     // [item][kv_heads][ROWS][head_dim], [item][kv_heads][ROWS]
+  int2* plan;                         // [n_seqs]: first item of a sequence, parts of its tiles
 };
 
-template <typename T> __device__ __forceinline__ float elem(const void* p, int64_t i);
-template <> __device__ __forceinline__ float elem<float>(const void* p, int64_t i) { return ((const float*)p)[i]; }
-template <> __device__ __forceinline__ float elem<bf16_t>(const void* p, int64_t i) { return bf16_to_f32(((const uint16_t*)p)[i]); }
-template <> __device__ __forceinline__ float elem<f16_t>(const void* p, int64_t i) { return (float)((const _Float16*)p)[i]; }
-__device__ __forceinline__ void put(float* p, float v) { *p = v; }
-__device__ __forceinline__ void put(bf16_t* p, float v) { p->v = f32_to_bf16(v); }
-__device__ __forceinline__ void put(f16_t* p, float v) { *(_Float16*)p = (_Float16)v; }
+// ---- element types as matrix operands
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 
-// One workgroup for a row and a query head; a wave takes every fourth position, a running maximum and sum, then the four are joined.
+__device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c, bf16_t) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c, f16_t) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// two numbers rounded to the type, side by side, and what the rounding left of them
+__device__ __forceinline__ uint32_t pair(float a, float b, bf16_t) { const bf16x2 v = {(__bf16)a, (__bf16)b}; return __builtin_bit_cast(uint32_t, v); }
+__device__ __forceinline__ void rest(uint32_t p, float& a, float& b, bf16_t) { a -= __uint_as_float(p << 16); b -= __uint_as_float(p & 0xffff0000u); }
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pair(float a, float b, f16_t) { const f16x2 v = {(_Float16)a, (_Float16)b}; return __builtin_bit_cast(uint32_t, v); }
+__device__ __forceinline__ void rest(uint32_t p, float& a, float& b, f16_t) { const f16x2 v = __builtin_bit_cast(f16x2, p); a -= (float)v.x; b -= (float)v.y; }
+// the largest of the numbers' magnitudes, as bits, and whether it is infinite or no number
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+template <typename T> __device__ __forceinline__ uint32_t largest(uint32_t m, u32x4 v, T) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if constexpr (sizeof(T) == 4) m = max(m, v[e] & 0x7fffffffu);
+    else m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), __builtin_bit_cast(u16x2, v[e] & 0x7fff7fffu)));
+  return m;
+}
+__device__ __forceinline__ bool endless(uint32_t m, bf16_t) { return m >= 0x7f800000u || (m & 0xffffu) >= 0x7f80u; }
+__device__ __forceinline__ bool endless(uint32_t m, f16_t) { return m >= 0x7c000000u || (m & 0xffffu) >= 0x7c00u; }
+__device__ __forceinline__ bool endless(uint32_t m, float) { return m >= 0x7f800000u; }
+template <typename T> __device__ __forceinline__ typename Quad<T>::raw quad_out(f32x4 v) {
+  if constexpr (sizeof(T) == 4) return Quad<T>::narrow(v);
+  else return (u32x2){pair(v.x, v.y, T()), pair(v.z, v.w, T())};
+}
+
+// ---- what a workgroup does: a part of the positions of one tile of one sequence
+struct Item {
+  int s, rows0, n, pos0;   // the sequence, its first row of the tensors, its tokens, the first one's position
+  int tile, part, parts;
+  int lo, hi;              // positions of the part, lo a multiple of PLAN_BLOCK
+};
+
+struct SeqPlan { int tiles, blocks, parts; SeqRows r; };
+__device__ __forceinline__ void seq_plan(const PagedAttnArgs& a, int s, SeqPlan& p) {
+  p.tiles = p.blocks = 0;
+  p.r = {0, 0, 0};
+  if (s >= a.b.n_seqs) return;
+  p.r = seq_rows(a.b, s);
+  if (p.r.rows == 0) return;
+  p.tiles = (int)(((int64_t)p.r.rows * a.group + ROWS - 1) / ROWS);
+  const int hi = min(p.r.pos0 + p.r.rows, a.b.room), lo = a.window > 0 ? max(p.r.pos0 - a.window + 1, 0) & -PLAN_BLOCK : 0;
+  p.blocks = max(1, (hi - lo + PLAN_BLOCK - 1) / PLAN_BLOCK);
+}
+__device__ __forceinline__ int scan_up(int v, int lane) {
+#pragma unroll
+  for (int o = 1; o < WAVE; o <<= 1) { const int u = __shfl_up(v, o, WAVE); if (lane >= o) v += u; }
+  return v;
+}
+// Every wave makes the plan for itself, from the lengths on the device: all tiles' blocks of positions together are cut into about
+// `want` parts of equal length, a tile at its own ends.  (The sum is in fp32, one order: every wave has the same; its error is far below
+// the one item that the grid has to spare.)  False: there is no such item.
+__device__ bool find_item(const PagedAttnArgs& a, int idx, bool tell, int lane, Item& it) {
+  SeqPlan p;
+  int len = 1;
+  if (a.least > 0) {
+    float all = 0.f;
+    for (int s = 0; s < a.b.n_seqs; s += WAVE) {
+      seq_plan(a, s + lane, p);
+      all += wave_sum((float)p.tiles * (float)p.blocks);
+    }
+    len = max(a.least, (int)ceilf(all / (float)a.want));
+  }
+  int before = 0;
+  bool found = false;
+  for (int s = 0; s < a.b.n_seqs; s += WAVE) {
+    if (a.b.n_seqs > WAVE || a.least == 0) seq_plan(a, s + lane, p);
+    p.parts = a.least > 0 ? (p.blocks + len - 1) / len : p.blocks > 0;
+    const int items = p.tiles * p.parts, upto = before + scan_up(items, lane);
+    if (tell && s + lane < a.b.n_seqs) a.plan[s + lane] = make_int2(upto - items, p.parts);
+    const unsigned long long past = __ballot(upto > idx);
+    if (!found && past) {
+      const int w = __builtin_ctzll(past);
+      const int r = idx - __builtin_amdgcn_readlane(upto - items, w);
+      it.s = s + w;
+      it.parts = __builtin_amdgcn_readlane(p.parts, w);
+      it.rows0 = __builtin_amdgcn_readlane(p.r.row0, w);
+      it.n = __builtin_amdgcn_readlane(p.r.rows, w);
+      it.pos0 = __builtin_amdgcn_readlane(p.r.pos0, w);
+      it.tile = r / it.parts;
+      it.part = r % it.parts;
+      found = true;
+      if (!tell) break;
+    }
+    before = __builtin_amdgcn_readlane(upto, 63);
+  }
+  if (!found) return false;
+  const int first = (int)((int64_t)it.tile * ROWS / a.group), last = min((int)(((int64_t)it.tile * ROWS + ROWS - 1) / a.group), it.n - 1);
+  const int hi = min(it.pos0 + last + 1, a.b.room), lo = a.window > 0 ? max(it.pos0 + first - a.window + 1, 0) & -PLAN_BLOCK : 0;
+  const int blocks = (max(hi - lo, 0) + PLAN_BLOCK - 1) / PLAN_BLOCK, per = (blocks + it.parts - 1) / it.parts;
+  it.lo = lo + min(it.part * per, blocks) * PLAN_BLOCK;
+  it.hi = min(hi, lo + min((it.part + 1) * per, blocks) * PLAN_BLOCK);
+  return true;
+}
+
+// ---- few rows, many positions: bound by the stream of keys and values
+// A wave has every fourth step of BP positions of its part to itself: keys straight into registers as the left operand, values through
+// registers into LDS rows of its own, from where the transposing reads (fp32: plain ones) make them the left operand of the second product.
+// The next step's are requested before this one's arithmetic; nothing waits at a barrier until the four waves' results are joined.
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
-  constexpr int E = HD / WAVE;
-  __shared__ float sm[4], sl[4], so[4][HD];
-  const int row = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+struct Split {
+  static constexpr int SZ = sizeof(T) == 4 ? 4 : 2, BP = SZ == 4 ? 16 : 32, NT = BP / 16;
+  static constexpr int NK = HD * SZ / 64;                 // 16-byte pieces of a key per lane
+  static constexpr int LPR = HD * SZ / 16, RPI = WAVE / LPR, NV = BP / RPI;
+  static constexpr int STRIDE = HD * SZ + (SZ == 4 ? 16 : 32);   // of a row of values in LDS: no two rows of an operand on the same banks
+  static constexpr int WAVE_LDS = BP * STRIDE;
+  static constexpr int OUT_LDS = ROWS * (HD + 4) * 4 + ROWS * 8; // a wave's results: sums (rows 16 bytes longer than they are), maxima and totals
+  static constexpr int LDS = SPLIT_WAVES * (WAVE_LDS > OUT_LDS ? WAVE_LDS : OUT_LDS);
+};
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256, 2) void paged_split_kernel(PagedAttnArgs a) {
+  using C = Split<T, HD>;
+  __shared__ __align__(16) char lds[C::LDS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = blockIdx.y, row = lane & 15, quad = lane >> 4;
+  Item it;
+  if (!find_item(a, blockIdx.x, blockIdx.x == 0 && kvh == 0 && wave == 0 && a.least > 0, lane, it)) return;
+  const int all_rows = it.n * a.group;
+  const int r = it.tile * ROWS + row, rc = min(r, all_rows - 1), tok = rc / a.group, head = kvh * a.group + rc % a.group;
+  const int pos = r < all_rows ? it.pos0 + tok : -1;                          // what the lane's row sees ends there
+  const int from = a.window > 0 ? pos - a.window + 1 : 0;
+  const int tok_first = it.tile * ROWS / a.group, tok_last = min((it.tile * ROWS + ROWS - 1) / a.group, it.n - 1);
+  const int all_see_to = it.pos0 + tok_first, all_see_from = a.window > 0 ? it.pos0 + tok_last - a.window + 1 : 0;
+  u32x4 q[C::NK];
+  {
+    const char* p = (const char*)a.q + ((int64_t)(it.rows0 + tok) * a.q_tok + (int64_t)head * a.q_head) * C::SZ + quad * 16;
+#pragma unroll
+    for (int i = 0; i < C::NK; ++i) {
+      q[i] = *(const u32x4*)(p + i * 64);
+      if (C::SZ == 4)                                     // fp32 queries take the scale along: the largest score's weight is 1 to the bit then
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[i][e] = __float_as_uint(__uint_as_float(q[i][e]) * a.to_log2);
+    }
+  }
+  const float to_log2 = C::SZ == 4 ? 1.0f : a.to_log2;
+  char* const mine = lds + wave * C::WAVE_LDS;
+  const char* const kbase = (const char*)a.kc + (int64_t)kvh * a.kc_head * C::SZ + quad * 16;
+  const char* const vbase = (const char*)a.vc + (int64_t)kvh * a.vc_head * C::SZ + (lane % C::LPR) * 16;
+  const int steps = (it.hi - it.lo + C::BP - 1) / C::BP;
+  // the page (or -1) and slot of position lo + step * BP + (lane % BP)
+  auto place = [&](int step, int& page, int& slot) {
+    const int p = it.lo + step * C::BP + (lane & (C::BP - 1));
+    page = step < steps && p < it.hi ? page_of(a.b, it.s, p) : -1;
+    slot = (int)((unsigned)p % (unsigned)a.b.page_size);
+  };
+  u32x4 k[C::NT][C::NK], v[C::NV];
+  uint32_t there = 0;                                     // a bit for each of the step's positions that has a page
+  auto request = [&](int page, int slot) {
+    there = (uint32_t)__ballot(page >= 0) & (uint32_t)((1ull << C::BP) - 1);
+    const int pg = max(page, 0), sl = page >= 0 ? slot : 0;      // what has no page is read from where there is something, and not used
+    const int64_t ko = ((int64_t)pg * a.kc_page + (int64_t)sl * a.kc_pos) * C::SZ, vo = ((int64_t)pg * a.vc_page + (int64_t)sl * a.vc_pos) * C::SZ;
+#pragma unroll
+    for (int t = 0; t < C::NT; ++t) {
+      const char* p = kbase + __shfl(ko, 16 * t + row, WAVE);
+#pragma unroll
+      for (int i = 0; i < C::NK; ++i) k[t][i] = *(const u32x4*)(p + i * 64);
+    }
+#pragma unroll
+    for (int i = 0; i < C::NV; ++i) v[i] = *(const u32x4*)(vbase + __shfl(vo, i * C::RPI + lane / C::LPR, WAVE));
+  };
+  f32x4 o[HD / 16];
+#pragma unroll
+  for (int i = 0; i < HD / 16; ++i) o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;                           // the row's maximum (of scores times to_log2; the same in its four lanes) and the lane's part of the sum
+  int page, slot;
+  int step = wave;
+  place(step, page, slot);
+  if (step < steps) request(page, slot);
+  place(step + SPLIT_WAVES, page, slot);
+  for (; step < steps; step += SPLIT_WAVES) {
+    const int base = it.lo + step * C::BP;
+    const uint32_t have = there;
+    const bool whole = have == (uint32_t)((1ull << C::BP) - 1) && base + C::BP - 1 <= all_see_to && base >= all_see_from;
+    f32x4 s[C::NT];
+#pragma unroll
+    for (int t = 0; t < C::NT; ++t) {
+      s[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < C::NK; ++i) {
+        if constexpr (C::SZ == 2) s[t] = mma16(k[t][i], q[i], s[t], T());
+        else
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[t][i][e]), __uint_as_float(q[i][e]), s[t], 0, 0, 0);
+      }
+    }
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < C::NV; ++i) {
+      const int at = i * C::RPI + lane / C::LPR;
+      u32x4 w = v[i];
+      if (!whole && !((have >> at) & 1)) w = (u32x4){0u, 0u, 0u, 0u};
+      most = largest(most, w, T());
+      *(u32x4*)(mine + at * C::STRIDE + (lane % C::LPR) * 16) = w;
+    }
+    if (step + SPLIT_WAVES < steps) request(page, slot);
+    place(step + 2 * SPLIT_WAVES, page, slot);
+    const bool odd = __ballot(endless(most, T())) != 0;
+    if (!whole) {
+#pragma unroll
+      for (int t = 0; t < C::NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int at = 16 * t + 4 * quad + e, p = base + at;
+          if (!((have >> at) & 1) || p > pos || p < from) s[t][e] = -INFINITY;
+        }
+    }
+    // running maximum: joined and sums rescaled only where it grows for some row
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < C::NT; ++t) top = fmaxf(top, fmaxf(fmaxf(s[t].x, s[t].y), fmaxf(s[t].z, s[t].w)));
+    top *= to_log2;
+    if (__ballot(top > m)) {
+      top = fmaxf(top, __shfl_xor(top, 16, WAVE));
+      top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+      const float mn = fmaxf(m, top), keep = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= keep;
+#pragma unroll
+      for (int i = 0; i < HD / 16; ++i) o[i] *= keep;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int t = 0; t < C::NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { s[t][e] = __builtin_amdgcn_exp2f(fmaf(s[t][e], to_log2, -ref)); l += s[t][e]; }
+    if constexpr (C::SZ == 2) {
+      // Weights in two terms of the type: the rounding of one alone is as large as the output's own.  Beside infinite values one: what is left
+      // of a weight may be zero or negative, and so that no weight above zero becomes one, half floats go no lower than their smallest number.
+      if (sizeof(T) == 2 && std::is_same<T, f16_t>::value && odd)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[t][e] = s[t][e] > 0.f ? fmaxf(s[t][e], 0x1p-24f) : s[t][e];
+      u32x4 hi, lo;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        hi[2 * t] = pair(s[t].x, s[t].y, T()); hi[2 * t + 1] = pair(s[t].z, s[t].w, T());
+        float x = s[t].x, y = s[t].y, z = s[t].z, w = s[t].w;
+        rest(hi[2 * t], x, y, T()); rest(hi[2 * t + 1], z, w, T());
+        lo[2 * t] = pair(x, y, T()); lo[2 * t + 1] = pair(z, w, T());
+      }
+      const char* src = mine + (4 * quad + (row >> 2)) * C::STRIDE + (row & 3) * 8;
+#pragma unroll
+      for (int i = 0; i < HD / 16; ++i) {
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(src + i * 32));
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(src + 16 * C::STRIDE + i * 32));
+        const u32x2 xu = __builtin_bit_cast(u32x2, x), yu = __builtin_bit_cast(u32x2, y);
+        const u32x4 vt = {xu.x, xu.y, yu.x, yu.y};
+        if (odd && whole) o[i] = mma16(vt, hi, o[i], T());
+        else if (odd) {
+          // a value that is no number, or infinite, among positions that not every row sees: position by position, kept where it is seen
+          for (int p = 0; p < 32; ++p) {
+            u32x4 only = {0u, 0u, 0u, 0u};
+            const int e = (p >> 4) * 4 + (p & 3);
+            if (((p >> 2) & 3) == quad) {
+#pragma unroll
+              for (int z = 0; z < 4; ++z) if (z == e / 2) only[z] = vt[z] & (e & 1 ? 0xffff0000u : 0xffffu);
+            }
+            const f32x4 n = mma16(only, hi, o[i], T());
+            if (((have >> p) & 1) && base + p <= pos && base + p >= from) o[i] = n;
+          }
+        } else {
+          o[i] = mma16(vt, hi, o[i], T());
+          o[i] = mma16(vt, lo, o[i], T());
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < HD / 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = *(const float*)(mine + (4 * quad + e) * C::STRIDE + (16 * i + row) * 4);
+          if (!whole && odd) {
+            for (int c = 0; c < 4; ++c) {
+              const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x4f32(c == quad ? x : 0.f, s[0][e], o[i], 0, 0, 0);
+              const int p = 4 * c + e;
+              if (((have >> p) & 1) && base + p <= pos && base + p >= from) o[i] = n;
+            }
+          } else o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, s[0][e], o[i], 0, 0, 0);
+        }
+    }
+  }
+  l += __shfl_xor(l, 16, WAVE);
+  l += __shfl_xor(l, 32, WAVE);
+  // ---- the four waves' results
+  __syncthreads();
+  float* const so = (float*)(lds + wave * C::OUT_LDS);
+#pragma unroll
+  for (int i = 0; i < HD / 16; ++i) *(f32x4*)(so + row * (HD + 4) + 16 * i + 4 * quad) = o[i];
+  if (quad == 0) ((float2*)(so + ROWS * (HD + 4)))[row] = make_float2(m, l);
+  __syncthreads();
+  for (int x = threadIdx.x; x < ROWS * HD / 4; x += 256) {
+    const int rr = x / (HD / 4), d = (x % (HD / 4)) * 4, ri = it.tile * ROWS + rr;
+    if (ri >= all_rows) break;
+    float2 ml[SPLIT_WAVES];
+    float mx = -INFINITY, sum = 0.f;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < SPLIT_WAVES; ++w) { ml[w] = ((const float2*)((const float*)(lds + w * C::OUT_LDS) + ROWS * (HD + 4)))[rr]; mx = fmaxf(mx, ml[w].x); }
+    const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+    for (int w = 0; w < SPLIT_WAVES; ++w) {
+      const float f = __builtin_amdgcn_exp2f(ml[w].x - ref);
+      sum = fmaf(f, ml[w].y, sum);
+      const f32x4 z = *(const f32x4*)((const float*)(lds + w * C::OUT_LDS) + rr * (HD + 4) + d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = fmaf(f, z[e], y[e]);
+    }
+    if (it.parts > 1) {
+      const int64_t at = ((int64_t)blockIdx.x * a.kv_heads + kvh) * ROWS + rr;
+      *(f32x4*)(a.part_o + at * HD + d) = y;
+      if (d == 0) a.part_ml[at] = make_float2(mx, sum);
+    } else {
+      const int t = ri / a.group, h = kvh * a.group + ri % a.group;
+      const bool none = mx == -INFINITY && sum == 0.f;    // nothing seen (a score that is no number leaves its mark on the sum)
+      const float inv = 1.0f / sum;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : y[e] * inv;
+      T* to = (T*)a.out + (int64_t)(it.rows0 + t) * a.o_tok + (int64_t)h * a.o_head + d;
+      *(typename Quad<T>::raw*)to = quad_out<T>(y);
+      if (a.lse && d == 0) a.lse[(int64_t)(it.rows0 + t) * a.heads + h] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718f;
+    }
+  }
+}
+
+// The parts of a row joined, in their order: HD / 4 lanes for a row.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
+  constexpr int LPR = HD / 4, RPW = 256 / LPR;
+  const int row = blockIdx.x, lane = threadIdx.x & 63;
   const int s = seq_of_row(a.b, row, lane);
   if (s < 0) return;
+  const int2 plan = a.plan[s];
+  const int parts = plan.y, h = blockIdx.y * RPW + threadIdx.x / LPR, d = (threadIdx.x % LPR) * 4;
+  if (parts <= 1 || h >= a.heads) return;
   const SeqRows sr = seq_rows(a.b, s);
-  const int pos = sr.pos0 + (row - sr.row0), first = a.window > 0 ? max(pos - a.window + 1, 0) : 0, kvh = h / (a.heads / a.kv_heads);
-  float q[E], o[E], m = -INFINITY, l = 0.f;
+  const int kvh = h / a.group, r = (row - sr.row0) * a.group + h % a.group;
+  const int64_t first = (int64_t)plan.x + (int64_t)(r / ROWS) * parts;
+  float mx = -INFINITY, sum = 0.f;
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < parts; ++p) mx = fmaxf(mx, a.part_ml[((first + p) * a.kv_heads + kvh) * ROWS + r % ROWS].x);
+  const float ref = mx == -INFINITY ? 0.f : mx;
+  for (int p = 0; p < parts; ++p) {
+    const int64_t at = ((first + p) * a.kv_heads + kvh) * ROWS + r % ROWS;
+    const float2 ml = a.part_ml[at];
+    const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+    sum = fmaf(f, ml.y, sum);
+    const f32x4 z = *(const f32x4*)(a.part_o + at * HD + d);
 #pragma unroll
-  for (int e = 0; e < E; ++e) { q[e] = elem<T>(a.q, row * a.q_tok + h * a.q_head + lane * E + e); o[e] = 0.f; }
-  const int end = min(pos, a.b.room - 1);      // (the table ends there, whatever the length says)
-  for (int p = first + wave; p <= end; p += 4) {
-    const int page = page_of(a.b, s, p);
-    if (page < 0) continue;
-    const int slot = (int)((unsigned)p % (unsigned)a.b.page_size);
-    float t = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) t = fmaf(q[e], elem<T>(a.kc, page * a.kc_page + slot * a.kc_pos + kvh * a.kc_head + lane * E + e), t);
-    t = wave_sum(t) * a.scale;
-    const float mn = fmaxf(m, t), safe = mn == -INFINITY ? 0.f : mn, keep = expf(m - safe), w = expf(t - safe);
-    l = l * keep + w; m = mn;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(w, elem<T>(a.vc, page * a.vc_page + slot * a.vc_pos + kvh * a.vc_head + lane * E + e), o[e] * keep);
+    for (int e = 0; e < 4; ++e) y[e] = fmaf(f, z[e], y[e]);
   }
-  if (lane == 0) { sm[wave] = m; sl[wave] = l; }
+  const bool none = mx == -INFINITY && sum == 0.f;
+  const float inv = 1.0f / sum;
 #pragma unroll
-  for (int e = 0; e < E; ++e) so[wave][lane * E + e] = o[e];
-  __syncthreads();
-  if (threadIdx.x >= HD) return;
-  m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-  const float safe = m == -INFINITY ? 0.f : m;
-  float y = 0.f;
-  l = 0.f;
-  for (int w = 0; w < 4; ++w) { const float f = expf(sm[w] - safe); l = fmaf(f, sl[w], l); y = fmaf(f, so[w][threadIdx.x], y); }
-  put((T*)a.out + row * a.o_tok + h * a.o_head + threadIdx.x, l == 0.f ? 0.f : y / l);
-  if (a.lse && threadIdx.x == 0) a.lse[(int64_t)row * a.heads + h] = l == 0.f ? -INFINITY : m + logf(l);
+  for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : y[e] * inv;
+  *(typename Quad<T>::raw*)((T*)a.out + (int64_t)row * a.o_tok + (int64_t)h * a.o_head + d) = quad_out<T>(y);
+  if (a.lse && d == 0) a.lse[(int64_t)row * a.heads + h] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718f;
 }
 
-template <typename T>
-hipError_t attn_go(const PagedAttnArgs& a, int head_dim, hipStream_t stream) {
-  const dim3 grid(a.b.n_tokens, a.heads);
-  if (head_dim == 64) hipLaunchKernelGGL((paged_attn_kernel<T, 64>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((paged_attn_kernel<T, 128>), grid, dim3(256), 0, stream, a);
-  return hipGetLastError();
-}
+// ---- host
+struct AttnPlan {
+  int want, least;          // see PagedAttnArgs
+  int64_t items;            // workgroups per key/value head: parts aimed at, and a part's end for every tile
+  uint64_t o_bytes, ml_bytes, plan_bytes;
+};
 
-int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, int n_heads) {
+int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, int n_heads, AttnPlan* p) {
   const int rc = check_paged(cache, batch);
   if (rc) return rc;
   if (n_heads < 1 || n_heads % cache->n_kv_heads) return PPD_EINVAL;
-  return n_heads > PPD_MAX_HEADS ? PPD_ELIMIT : PPD_OK;
+  if (n_heads > PPD_MAX_HEADS || (int64_t)batch->n_tokens * (n_heads / cache->n_kv_heads) > 1 << 26) return PPD_ELIMIT;
+  const int group = n_heads / cache->n_kv_heads;
+  const int64_t some = batch->n_tokens < batch->n_seqs ? batch->n_tokens : batch->n_seqs;
+  const int64_t tiles = (int64_t)batch->n_tokens * group / ROWS + some;
+  p->want = (1024 + cache->n_kv_heads - 1) / cache->n_kv_heads;
+  p->least = 2;
+  // tiles enough for the whole chip, or no position to cut at: one part each
+  if (tiles >= 2 * p->want || (int64_t)batch->max_pages * cache->page_size <= p->least * PLAN_BLOCK) p->least = 0;
+  p->items = tiles + (p->least ? p->want + 1 : 0);
+  const uint64_t rows = p->least ? (uint64_t)p->items * cache->n_kv_heads * ROWS : 0;
+  p->o_bytes = rows * cache->head_dim * 4;
+  p->ml_bytes = rows * 8;
+  p->plan_bytes = p->least ? ((uint64_t)batch->n_seqs * 8 + 15) & ~15ull : 0;
+  return PPD_OK;
+}
+
+template <typename T, int HD>
+hipError_t attn_go(const PagedAttnArgs& a, int items, hipStream_t stream) {
+  hipLaunchKernelGGL((paged_split_kernel<T, HD>), dim3(items, a.kv_heads), dim3(256), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.least == 0) return e;
+  constexpr int rpw = 256 / (HD / 4);
+  hipLaunchKernelGGL((paged_merge_kernel<T, HD>), dim3(a.b.n_tokens, (a.heads + rpw - 1) / rpw), dim3(256), 0, stream, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 extern "C" int ppd_paged_attention_workspace(const ppd_paged_cache* cache, const ppd_paged_batch* batch, int n_heads, uint64_t* bytes) {
-  const int rc = check_attention(cache, batch, n_heads);
+  AttnPlan p;
+  const int rc = check_attention(cache, batch, n_heads, &p);
   if (rc) return rc;
   if (!bytes) return PPD_EINVAL;
-  *bytes = 0;
+  *bytes = p.o_bytes + p.ml_bytes + p.plan_bytes;
   return PPD_OK;
 }
 
 extern "C" int ppd_paged_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, int n_heads, const ppd_rows* q,
                                    const ppd_rows* out, float* lse, float scale, int window, void* workspace,
                                    uint64_t workspace_bytes, void* hip_stream) {
-  uint64_t need = 0;
-  const int rc = ppd_paged_attention_workspace(cache, batch, n_heads, &need);
+  AttnPlan p;
+  const int rc = check_attention(cache, batch, n_heads, &p);
   if (rc) return rc;
   const int dt = cache->dtype, n = batch->n_tokens;
   if (!(scale > 0.f && isfinite(scale)) || window < 0) return PPD_EINVAL;
   if (n == 0) return PPD_OK;
   if (!good_rows(q, n, n_heads, dt, false) || !good_rows(out, n, n_heads, dt, true) || ((uintptr_t)lse & 3)) return PPD_EINVAL;
+  const uint64_t need = p.o_bytes + p.ml_bytes + p.plan_bytes;
   if (need && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need)) return PPD_EINVAL;
   PagedAttnArgs a;
   a.b = batch_of(*cache, *batch);
   a.q = q->p; a.out = out->p; a.lse = lse; a.kc = cache->k; a.vc = cache->v;
   a.q_tok = q->token; a.q_head = q->head; a.o_tok = out->token; a.o_head = out->head;
   a.kc_page = cache->k_page; a.kc_pos = cache->k_pos; a.kc_head = cache->k_head; a.vc_page = cache->v_page; a.vc_pos = cache->v_pos; a.vc_head = cache->v_head;
-  a.heads = n_heads; a.kv_heads = cache->n_kv_heads; a.window = window; a.scale = scale;
+  a.heads = n_heads; a.kv_heads = cache->n_kv_heads; a.group = n_heads / cache->n_kv_heads; a.window = window; a.to_log2 = scale * 1.44269504f;
+  a.want = p.want; a.least = p.least;
+  a.part_o = (float*)workspace; a.part_ml = (float2*)((char*)workspace + p.o_bytes); a.plan = (int2*)((char*)workspace + p.o_bytes + p.ml_bytes);
   hipStream_t st = (hipStream_t)hip_stream;
-  return launched(dt == PPD_FP32 ? attn_go<float>(a, cache->head_dim, st)
-                  : dt == PPD_BF16 ? attn_go<bf16_t>(a, cache->head_dim, st) : attn_go<f16_t>(a, cache->head_dim, st));
+  const int items = (int)p.items;
+  if (cache->head_dim == 64)
+    return launched(dt == PPD_FP32 ? attn_go<float, 64>(a, items, st) : dt == PPD_BF16 ? attn_go<bf16_t, 64>(a, items, st) : attn_go<f16_t, 64>(a, items, st));
+  return launched(dt == PPD_FP32 ? attn_go<float, 128>(a, items, st) : dt == PPD_BF16 ? attn_go<bf16_t, 128>(a, items, st) : attn_go<f16_t, 128>(a, items, st));
 }

@@ -117,7 +117,8 @@ int ppd_paged_attention_workspace(const ppd_paged_cache *cache, const ppd_paged_
  * [0, vocab) are not taken.  uniform: DEVICE float [n_rows][2] in [0, 1).
  * Out, DEVICE: tokens int32 [n_rows]: at a sequence's rows the drafts taken, then the drawn token, then -1; accepted
  * int32 [n_seqs]: the number of drafts taken (the sequence gained that many tokens and one more; 0 for one without
- * rows).  Rows of no sequence are not touched.  vocab 1 .. 2^24, n_rows 0 .. PPD_MAX_TOKENS, n_seqs 1 .. PPD_MAX_SEQS.
+ * rows).  Rows of no sequence are not touched.  vocab 1 .. 2^24, n_rows 0 .. PPD_MAX_TOKENS, n_seqs 1 .. PPD_MAX_SEQS,
+ * n_rows * ceil(vocab / 4096) at most 2^23.
  * target_logits and draft_logits of type dtype, aligned to it (any stride of at least vocab).  workspace as above, from
  * ppd_verify_drafts_workspace. */
 int ppd_verify_drafts(int n_seqs, int n_rows, int vocab, int dtype, const int32_t *row_start, const int32_t *ids,

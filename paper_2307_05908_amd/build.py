@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(HERE, "libppd.so")
 PROBE_PATH = os.path.join(HERE, "ppd_pmc_probe")
 N_INST = 8
 DEPS = [os.path.join(CSRC, f) for f in ("ppd_engine.hip", "ppd_ops.hip", "ppd_pmc_probe.cpp", "ppd_prefill.hip", "ppd_prefill.h", "ppd_fused.hip", "ppd_fused.h", "ppd_inst.hip", "ppd_kernels.h", "ppd_launch.h",
-                                         "ppd_layers_common.h", "ppd_append.hip", "ppd_paged_attn.hip", "ppd_verify.hip")] + \
+                                         "ppd_layers_common.h", "ppd_append.hip", "ppd_paged_attn.h", "ppd_paged_attn.hip", "ppd_paged_tiles.hip", "ppd_verify.hip")] + \
        [os.path.join(os.path.dirname(HERE), "include", f) for f in ("ppd.h", "ppd_measure.h", "ppd_layers.h")]
 # -ffp-contract=off: every fused multiply-add in the kernels is an explicit fmaf, so a row's arithmetic
 # does not depend on which template instance it runs in.  Packed-fp32 code generation is switched off.
@@ -51,6 +51,7 @@ def build(force: bool = True, verbose: bool = False, jobs: int = 0) -> str:
                  (os.path.join(CSRC, "ppd_fused.hip"), os.path.join(tmp, "fused.o"), [], verbose),
                  (os.path.join(CSRC, "ppd_append.hip"), os.path.join(tmp, "append.o"), [], verbose),
                  (os.path.join(CSRC, "ppd_paged_attn.hip"), os.path.join(tmp, "paged_attn.o"), [], verbose),
+                 (os.path.join(CSRC, "ppd_paged_tiles.hip"), os.path.join(tmp, "paged_tiles.o"), [], verbose),
                  (os.path.join(CSRC, "ppd_verify.hip"), os.path.join(tmp, "verify.o"), [], verbose)]
         for i in range(N_INST):
             units.append((os.path.join(CSRC, "ppd_inst.hip"), os.path.join(tmp, f"inst{i}.o"), [f"-DPPD_INST={i}"], verbose))

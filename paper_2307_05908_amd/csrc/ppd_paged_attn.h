@@ -1,0 +1,140 @@
+// What the kernels of ppd_paged_attention share: arguments, the plan of parts, element types as operands of the matrix units.
+//
+// For a key/value head its group of query heads is as many rows for each new token: row r of a sequence is token r / group, head
+// r % group of the group, and a tile is a number of rows that read the same keys and values.  Scores are computed transposed, S^T = K Q^T:
+// in a matrix product's result a lane then has one row (a column of S^T) and four positions in turn, so a row's maximum and sum stay in a
+// lane but for an exchange of two or four lanes, and the weights are, as they lie in the registers, the right operand of O^T = V^T P^T.
+#pragma once
+#include "ppd_layers_common.h"
+
+#include <type_traits>
+
+namespace ppd {
+
+constexpr int SPLIT_ROWS = 16, TILE_ROWS = 128;   // rows of a tile of paged_split_kernel and of paged_tile_kernel
+constexpr int PLAN_BLOCK = 64;                    // positions that lengths are cut by
+
+struct PagedAttnArgs {
+  Batch b;
+  const void* q; void* out; float* lse; const void *kc, *vc;
+  int64_t q_tok, q_head, o_tok, o_head;
+  int64_t kc_page, kc_pos, kc_head, vc_page, vc_pos, vc_head;
+  int heads, kv_heads, group, window;
+  int tile_rows;
+  int last_first;                     // tiles of a sequence from its end: the longest ones first
+  float to_log2;                      // scale * log2(e): a score's exponent of two
+  int want, least;                    // parts per key/value head to aim at; blocks of a part at least (0: one part each)
+  float* part_o; float2* part_ml;     // [item][kv_heads][rows of a tile][head_dim], [item][kv_heads][rows of a tile]
+  int2* plan;                         // [n_seqs]: first item of a sequence, parts of its tiles
+};
+
+// ---- element types as matrix operands
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+
+__device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c, bf16_t) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c, f16_t) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// two numbers rounded to the type, side by side, and what the rounding left of them
+__device__ __forceinline__ uint32_t pair(float a, float b, bf16_t) { const bf16x2 v = {(__bf16)a, (__bf16)b}; return __builtin_bit_cast(uint32_t, v); }
+__device__ __forceinline__ void rest(uint32_t p, float& a, float& b, bf16_t) { a -= __uint_as_float(p << 16); b -= __uint_as_float(p & 0xffff0000u); }
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pair(float a, float b, f16_t) { const f16x2 v = {(_Float16)a, (_Float16)b}; return __builtin_bit_cast(uint32_t, v); }
+__device__ __forceinline__ void rest(uint32_t p, float& a, float& b, f16_t) { const f16x2 v = __builtin_bit_cast(f16x2, p); a -= (float)v.x; b -= (float)v.y; }
+// the largest of the numbers' magnitudes, as bits, and whether it is infinite or no number
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+template <typename T> __device__ __forceinline__ uint32_t largest(uint32_t m, u32x4 v, T) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if constexpr (sizeof(T) == 4) m = max(m, v[e] & 0x7fffffffu);
+    else m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), __builtin_bit_cast(u16x2, v[e] & 0x7fff7fffu)));
+  return m;
+}
+__device__ __forceinline__ bool endless(uint32_t m, bf16_t) { return m >= 0x7f800000u || (m & 0xffffu) >= 0x7f80u; }
+__device__ __forceinline__ bool endless(uint32_t m, f16_t) { return m >= 0x7c000000u || (m & 0xffffu) >= 0x7c00u; }
+__device__ __forceinline__ bool endless(uint32_t m, float) { return m >= 0x7f800000u; }
+template <typename T> __device__ __forceinline__ typename Quad<T>::raw quad_out(f32x4 v) {
+  if constexpr (sizeof(T) == 4) return Quad<T>::narrow(v);
+  else return (u32x2){pair(v.x, v.y, T()), pair(v.z, v.w, T())};
+}
+
+// ---- what a workgroup does: a part of the positions of one tile of one sequence
+struct Item {
+  int s, rows0, n, pos0;   // the sequence, its first row of the tensors, its tokens, the first one's position
+  int tile, part, parts;
+  int slot;                // where its partial results go
+  int lo, hi;              // positions of the part, lo a multiple of PLAN_BLOCK
+};
+
+struct SeqPlan { int tiles, blocks, parts; SeqRows r; };
+__device__ __forceinline__ void seq_plan(const PagedAttnArgs& a, int s, SeqPlan& p) {
+  p.tiles = p.blocks = 0;
+  p.r = {0, 0, 0};
+  if (s >= a.b.n_seqs) return;
+  p.r = seq_rows(a.b, s);
+  if (p.r.rows == 0) return;
+  p.tiles = (int)(((int64_t)p.r.rows * a.group + a.tile_rows - 1) / a.tile_rows);
+  const int hi = min(p.r.pos0 + p.r.rows, a.b.room), lo = a.window > 0 ? max(p.r.pos0 - a.window + 1, 0) & -PLAN_BLOCK : 0;
+  p.blocks = max(1, (hi - lo + PLAN_BLOCK - 1) / PLAN_BLOCK);
+}
+__device__ __forceinline__ int scan_up(int v, int lane) {
+#pragma unroll
+  for (int o = 1; o < WAVE; o <<= 1) { const int u = __shfl_up(v, o, WAVE); if (lane >= o) v += u; }
+  return v;
+}
+// Every wave makes the plan for itself, from the lengths on the device: all tiles' blocks of positions together are cut into about
+// `want` parts of equal length, a tile at its own ends.  (The sum is in fp32, one order: every wave has the same; its error is far below
+// the one item that the grid has to spare.)  False: there is no such item.
+__device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, bool tell, int lane, Item& it) {
+  SeqPlan p;
+  int len = 1;
+  if (a.least > 0) {
+    float all = 0.f;
+    for (int s = 0; s < a.b.n_seqs; s += WAVE) {
+      seq_plan(a, s + lane, p);
+      all += wave_sum((float)p.tiles * (float)p.blocks);
+    }
+    len = max(a.least, (int)ceilf(all / (float)a.want));
+  }
+  int before = 0;
+  bool found = false;
+  for (int s = 0; s < a.b.n_seqs; s += WAVE) {
+    if (a.b.n_seqs > WAVE || a.least == 0) seq_plan(a, s + lane, p);
+    p.parts = a.least > 0 ? (p.blocks + len - 1) / len : p.blocks > 0;
+    const int items = p.tiles * p.parts, upto = before + scan_up(items, lane);
+    if (tell && s + lane < a.b.n_seqs) a.plan[s + lane] = make_int2(upto - items, p.parts);
+    const unsigned long long past = __ballot(upto > idx);
+    if (!found && past) {
+      const int w = __builtin_ctzll(past);
+      const int r = idx - __builtin_amdgcn_readlane(upto - items, w);
+      it.s = s + w;
+      it.parts = __builtin_amdgcn_readlane(p.parts, w);
+      it.rows0 = __builtin_amdgcn_readlane(p.r.row0, w);
+      it.n = __builtin_amdgcn_readlane(p.r.rows, w);
+      it.pos0 = __builtin_amdgcn_readlane(p.r.pos0, w);
+      it.tile = r / it.parts;
+      it.part = r % it.parts;
+      if (a.last_first) it.tile = __builtin_amdgcn_readlane(p.tiles, w) - 1 - it.tile;
+      it.slot = idx - r + it.tile * it.parts + it.part;
+      found = true;
+      if (!tell) break;
+    }
+    before = __builtin_amdgcn_readlane(upto, 63);
+  }
+  if (!found) return false;
+  const int first = (int)((int64_t)it.tile * a.tile_rows / a.group), last = min((int)(((int64_t)it.tile * a.tile_rows + a.tile_rows - 1) / a.group), it.n - 1);
+  const int hi = min(it.pos0 + last + 1, a.b.room), lo = a.window > 0 ? max(it.pos0 + first - a.window + 1, 0) & -PLAN_BLOCK : 0;
+  const int blocks = (max(hi - lo, 0) + PLAN_BLOCK - 1) / PLAN_BLOCK, per = (blocks + it.parts - 1) / it.parts;
+  it.lo = lo + min(it.part * per, blocks) * PLAN_BLOCK;
+  it.hi = min(hi, lo + min((it.part + 1) * per, blocks) * PLAN_BLOCK);
+  return true;
+}
+
+hipError_t launch_paged_tiles(const PagedAttnArgs& a, int dtype, int head_dim, int items, hipStream_t stream);
+
+}  // namespace ppd

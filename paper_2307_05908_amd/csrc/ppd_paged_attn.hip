@@ -1,138 +1,14 @@
-// ppd_paged_attention: attention of ragged runs of new tokens over paged keys and values.
-//
-// For a key/value head its group of query heads is as many rows for each new token: row r of a sequence is token r / group, head
-// r % group of the group, and a tile is 16 rows that read the same keys and values.  Scores are computed transposed, S^T = K Q^T: in a
-// matrix product's result a lane then has one row (column r of S^T) and four positions in turn, so a row's maximum and sum stay in a
-// lane but for one exchange of four lanes, and the weights are, as they lie in the registers, the right operand of O^T = V^T P^T.
-#include "ppd_layers_common.h"
+// ppd_paged_attention: attention of ragged runs of new tokens over paged keys and values.  Few rows over many positions, the join of parts,
+// and the host's side; many rows: ppd_paged_tiles.hip.
+#include "ppd_paged_attn.h"
 
 #include <math.h>
-
-#include <type_traits>
 
 using namespace ppd;
 
 namespace {
 
-constexpr int ROWS = 16;              // rows of a tile
-constexpr int PLAN_BLOCK = 64;        // positions that lengths are cut by
 constexpr int SPLIT_WAVES = 4;
-
-struct PagedAttnArgs {
-  Batch b;
-  const void* q; void* out; float* lse; const void *kc, *vc;
-  int64_t q_tok, q_head, o_tok, o_head;
-  int64_t kc_page, kc_pos, kc_head, vc_page, vc_pos, vc_head;
-  int heads, kv_heads, group, window;
-  float to_log2;                      // scale * log2(e): a score's exponent of two
-  int want, least;                    // parts per key/value head to aim at; blocks of a part at least (0: one part each)
-  float* part_o; float2* part_ml;     // [item][kv_heads][ROWS][head_dim], [item][kv_heads][ROWS]
-  int2* plan;                         // [n_seqs]: first item of a sequence, parts of its tiles
-};
-
-// ---- element types as matrix operands
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
-
-__device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c, bf16_t) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c, f16_t) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-// two numbers rounded to the type, side by side, and what the rounding left of them
-__device__ __forceinline__ uint32_t pair(float a, float b, bf16_t) { const bf16x2 v = {(__bf16)a, (__bf16)b}; return __builtin_bit_cast(uint32_t, v); }
-__device__ __forceinline__ void rest(uint32_t p, float& a, float& b, bf16_t) { a -= __uint_as_float(p << 16); b -= __uint_as_float(p & 0xffff0000u); }
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t pair(float a, float b, f16_t) { const f16x2 v = {(_Float16)a, (_Float16)b}; return __builtin_bit_cast(uint32_t, v); }
-__device__ __forceinline__ void rest(uint32_t p, float& a, float& b, f16_t) { const f16x2 v = __builtin_bit_cast(f16x2, p); a -= (float)v.x; b -= (float)v.y; }
-// the largest of the numbers' magnitudes, as bits, and whether it is infinite or no number
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-template <typename T> __device__ __forceinline__ uint32_t largest(uint32_t m, u32x4 v, T) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if constexpr (sizeof(T) == 4) m = max(m, v[e] & 0x7fffffffu);
-    else m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), __builtin_bit_cast(u16x2, v[e] & 0x7fff7fffu)));
-  return m;
-}
-__device__ __forceinline__ bool endless(uint32_t m, bf16_t) { return m >= 0x7f800000u || (m & 0xffffu) >= 0x7f80u; }
-__device__ __forceinline__ bool endless(uint32_t m, f16_t) { return m >= 0x7c000000u || (m & 0xffffu) >= 0x7c00u; }
-__device__ __forceinline__ bool endless(uint32_t m, float) { return m >= 0x7f800000u; }
-template <typename T> __device__ __forceinline__ typename Quad<T>::raw quad_out(f32x4 v) {
-  if constexpr (sizeof(T) == 4) return Quad<T>::narrow(v);
-  else return (u32x2){pair(v.x, v.y, T()), pair(v.z, v.w, T())};
-}
-
-// ---- what a workgroup does: a part of the positions of one tile of one sequence
-struct Item {
-  int s, rows0, n, pos0;   // the sequence, its first row of the tensors, its tokens, the first one's position
-  int tile, part, parts;
-  int lo, hi;              // positions of the part, lo a multiple of PLAN_BLOCK
-};
-
-struct SeqPlan { int tiles, blocks, parts; SeqRows r; };
-__device__ __forceinline__ void seq_plan(const PagedAttnArgs& a, int s, SeqPlan& p) {
-  p.tiles = p.blocks = 0;
-  p.r = {0, 0, 0};
-  if (s >= a.b.n_seqs) return;
-  p.r = seq_rows(a.b, s);
-  if (p.r.rows == 0) return;
-  p.tiles = (int)(((int64_t)p.r.rows * a.group + ROWS - 1) / ROWS);
-  const int hi = min(p.r.pos0 + p.r.rows, a.b.room), lo = a.window > 0 ? max(p.r.pos0 - a.window + 1, 0) & -PLAN_BLOCK : 0;
-  p.blocks = max(1, (hi - lo + PLAN_BLOCK - 1) / PLAN_BLOCK);
-}
-__device__ __forceinline__ int scan_up(int v, int lane) {
-#pragma unroll
-  for (int o = 1; o < WAVE; o <<= 1) { const int u = __shfl_up(v, o, WAVE); if (lane >= o) v += u; }
-  return v;
-}
-// Every wave makes the plan for itself, from the lengths on the device: all tiles' blocks of positions together are cut into about
-// `want` parts of equal length, a tile at its own ends.  (The sum is in fp32, one order: every wave has the same; its error is far below
-// the one item that the grid has to spare.)  False: there is no such item.
-__device__ bool find_item(const PagedAttnArgs& a, int idx, bool tell, int lane, Item& it) {
-  SeqPlan p;
-  int len = 1;
-  if (a.least > 0) {
-    float all = 0.f;
-    for (int s = 0; s < a.b.n_seqs; s += WAVE) {
-      seq_plan(a, s + lane, p);
-      all += wave_sum((float)p.tiles * (float)p.blocks);
-    }
-    len = max(a.least, (int)ceilf(all / (float)a.want));
-  }
-  int before = 0;
-  bool found = false;
-  for (int s = 0; s < a.b.n_seqs; s += WAVE) {
-    if (a.b.n_seqs > WAVE || a.least == 0) seq_plan(a, s + lane, p);
-    p.parts = a.least > 0 ? (p.blocks + len - 1) / len : p.blocks > 0;
-    const int items = p.tiles * p.parts, upto = before + scan_up(items, lane);
-    if (tell && s + lane < a.b.n_seqs) a.plan[s + lane] = make_int2(upto - items, p.parts);
-    const unsigned long long past = __ballot(upto > idx);
-    if (!found && past) {
-      const int w = __builtin_ctzll(past);
-      const int r = idx - __builtin_amdgcn_readlane(upto - items, w);
-      it.s = s + w;
-      it.parts = __builtin_amdgcn_readlane(p.parts, w);
-      it.rows0 = __builtin_amdgcn_readlane(p.r.row0, w);
-      it.n = __builtin_amdgcn_readlane(p.r.rows, w);
-      it.pos0 = __builtin_amdgcn_readlane(p.r.pos0, w);
-      it.tile = r / it.parts;
-      it.part = r % it.parts;
-      found = true;
-      if (!tell) break;
-    }
-    before = __builtin_amdgcn_readlane(upto, 63);
-  }
-  if (!found) return false;
-  const int first = (int)((int64_t)it.tile * ROWS / a.group), last = min((int)(((int64_t)it.tile * ROWS + ROWS - 1) / a.group), it.n - 1);
-  const int hi = min(it.pos0 + last + 1, a.b.room), lo = a.window > 0 ? max(it.pos0 + first - a.window + 1, 0) & -PLAN_BLOCK : 0;
-  const int blocks = (max(hi - lo, 0) + PLAN_BLOCK - 1) / PLAN_BLOCK, per = (blocks + it.parts - 1) / it.parts;
-  it.lo = lo + min(it.part * per, blocks) * PLAN_BLOCK;
-  it.hi = min(hi, lo + min((it.part + 1) * per, blocks) * PLAN_BLOCK);
-  return true;
-}
 
 // ---- few rows, many positions: bound by the stream of keys and values
 // A wave has every fourth step of BP positions of its part to itself: keys straight into registers as the left operand, values through
@@ -145,7 +21,7 @@ struct Split {
   static constexpr int LPR = HD * SZ / 16, RPI = WAVE / LPR, NV = BP / RPI;
   static constexpr int STRIDE = HD * SZ + (SZ == 4 ? 16 : 32);   // of a row of values in LDS: no two rows of an operand on the same banks
   static constexpr int WAVE_LDS = BP * STRIDE;
-  static constexpr int OUT_LDS = ROWS * (HD + 4) * 4 + ROWS * 8; // a wave's results: sums (rows 16 bytes longer than they are), maxima and totals
+  static constexpr int OUT_LDS = SPLIT_ROWS * (HD + 4) * 4 + SPLIT_ROWS * 8; // a wave's results: sums (rows 16 bytes longer than they are), maxima and totals
   static constexpr int LDS = SPLIT_WAVES * (WAVE_LDS > OUT_LDS ? WAVE_LDS : OUT_LDS);
 };
 
@@ -158,10 +34,10 @@ __global__ __launch_bounds__(256, 2) void paged_split_kernel(PagedAttnArgs a) {
   Item it;
   if (!find_item(a, blockIdx.x, blockIdx.x == 0 && kvh == 0 && wave == 0 && a.least > 0, lane, it)) return;
   const int all_rows = it.n * a.group;
-  const int r = it.tile * ROWS + row, rc = min(r, all_rows - 1), tok = rc / a.group, head = kvh * a.group + rc % a.group;
+  const int r = it.tile * SPLIT_ROWS + row, rc = min(r, all_rows - 1), tok = rc / a.group, head = kvh * a.group + rc % a.group;
   const int pos = r < all_rows ? it.pos0 + tok : -1;                          // what the lane's row sees ends there
   const int from = a.window > 0 ? pos - a.window + 1 : 0;
-  const int tok_first = it.tile * ROWS / a.group, tok_last = min((it.tile * ROWS + ROWS - 1) / a.group, it.n - 1);
+  const int tok_first = it.tile * SPLIT_ROWS / a.group, tok_last = min((it.tile * SPLIT_ROWS + SPLIT_ROWS - 1) / a.group, it.n - 1);
   const int all_see_to = it.pos0 + tok_first, all_see_from = a.window > 0 ? it.pos0 + tok_last - a.window + 1 : 0;
   u32x4 q[C::NK];
   {
@@ -329,16 +205,16 @@ __global__ __launch_bounds__(256, 2) void paged_split_kernel(PagedAttnArgs a) {
   float* const so = (float*)(lds + wave * C::OUT_LDS);
 #pragma unroll
   for (int i = 0; i < HD / 16; ++i) *(f32x4*)(so + row * (HD + 4) + 16 * i + 4 * quad) = o[i];
-  if (quad == 0) ((float2*)(so + ROWS * (HD + 4)))[row] = make_float2(m, l);
+  if (quad == 0) ((float2*)(so + SPLIT_ROWS * (HD + 4)))[row] = make_float2(m, l);
   __syncthreads();
-  for (int x = threadIdx.x; x < ROWS * HD / 4; x += 256) {
-    const int rr = x / (HD / 4), d = (x % (HD / 4)) * 4, ri = it.tile * ROWS + rr;
+  for (int x = threadIdx.x; x < SPLIT_ROWS * HD / 4; x += 256) {
+    const int rr = x / (HD / 4), d = (x % (HD / 4)) * 4, ri = it.tile * SPLIT_ROWS + rr;
     if (ri >= all_rows) break;
     float2 ml[SPLIT_WAVES];
     float mx = -INFINITY, sum = 0.f;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < SPLIT_WAVES; ++w) { ml[w] = ((const float2*)((const float*)(lds + w * C::OUT_LDS) + ROWS * (HD + 4)))[rr]; mx = fmaxf(mx, ml[w].x); }
+    for (int w = 0; w < SPLIT_WAVES; ++w) { ml[w] = ((const float2*)((const float*)(lds + w * C::OUT_LDS) + SPLIT_ROWS * (HD + 4)))[rr]; mx = fmaxf(mx, ml[w].x); }
     const float ref = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
     for (int w = 0; w < SPLIT_WAVES; ++w) {
@@ -349,7 +225,7 @@ __global__ __launch_bounds__(256, 2) void paged_split_kernel(PagedAttnArgs a) {
       for (int e = 0; e < 4; ++e) y[e] = fmaf(f, z[e], y[e]);
     }
     if (it.parts > 1) {
-      const int64_t at = ((int64_t)blockIdx.x * a.kv_heads + kvh) * ROWS + rr;
+      const int64_t at = ((int64_t)it.slot * a.kv_heads + kvh) * SPLIT_ROWS + rr;
       *(f32x4*)(a.part_o + at * HD + d) = y;
       if (d == 0) a.part_ml[at] = make_float2(mx, sum);
     } else {
@@ -377,13 +253,13 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   if (parts <= 1 || h >= a.heads) return;
   const SeqRows sr = seq_rows(a.b, s);
   const int kvh = h / a.group, r = (row - sr.row0) * a.group + h % a.group;
-  const int64_t first = (int64_t)plan.x + (int64_t)(r / ROWS) * parts;
+  const int64_t first = (int64_t)plan.x + (int64_t)(r / a.tile_rows) * parts;
   float mx = -INFINITY, sum = 0.f;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < parts; ++p) mx = fmaxf(mx, a.part_ml[((first + p) * a.kv_heads + kvh) * ROWS + r % ROWS].x);
+  for (int p = 0; p < parts; ++p) mx = fmaxf(mx, a.part_ml[((first + p) * a.kv_heads + kvh) * a.tile_rows + r % a.tile_rows].x);
   const float ref = mx == -INFINITY ? 0.f : mx;
   for (int p = 0; p < parts; ++p) {
-    const int64_t at = ((first + p) * a.kv_heads + kvh) * ROWS + r % ROWS;
+    const int64_t at = ((first + p) * a.kv_heads + kvh) * a.tile_rows + r % a.tile_rows;
     const float2 ml = a.part_ml[at];
     const float f = __builtin_amdgcn_exp2f(ml.x - ref);
     sum = fmaf(f, ml.y, sum);
@@ -401,6 +277,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
 
 // ---- host
 struct AttnPlan {
+  bool tiles;               // paged_tile_kernel, not paged_split_kernel
   int want, least;          // see PagedAttnArgs
   int64_t items;            // workgroups per key/value head: parts aimed at, and a part's end for every tile
   uint64_t o_bytes, ml_bytes, plan_bytes;
@@ -412,24 +289,30 @@ int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, 
   if (n_heads < 1 || n_heads % cache->n_kv_heads) return PPD_EINVAL;
   if (n_heads > PPD_MAX_HEADS || (int64_t)batch->n_tokens * (n_heads / cache->n_kv_heads) > 1 << 26) return PPD_ELIMIT;
   const int group = n_heads / cache->n_kv_heads;
-  const int64_t some = batch->n_tokens < batch->n_seqs ? batch->n_tokens : batch->n_seqs;
-  const int64_t tiles = (int64_t)batch->n_tokens * group / ROWS + some;
-  p->want = (1024 + cache->n_kv_heads - 1) / cache->n_kv_heads;
-  p->least = 2;
+  const int64_t rows = (int64_t)batch->n_tokens * group, some = batch->n_tokens < batch->n_seqs ? batch->n_tokens : batch->n_seqs;
+  p->tiles = cache->dtype != PPD_FP32 && rows > 32 * (int64_t)batch->n_seqs;
+  const int tile_rows = p->tiles ? TILE_ROWS : SPLIT_ROWS, slots = p->tiles ? 512 : 1024;
+  const int64_t tiles = rows / tile_rows + some;
+  p->want = (slots + cache->n_kv_heads - 1) / cache->n_kv_heads;
+  p->least = p->tiles ? 8 : 2;
   // tiles enough for the whole chip, or no position to cut at: one part each
   if (tiles >= 2 * p->want || (int64_t)batch->max_pages * cache->page_size <= p->least * PLAN_BLOCK) p->least = 0;
   p->items = tiles + (p->least ? p->want + 1 : 0);
-  const uint64_t rows = p->least ? (uint64_t)p->items * cache->n_kv_heads * ROWS : 0;
-  p->o_bytes = rows * cache->head_dim * 4;
-  p->ml_bytes = rows * 8;
+  const uint64_t kept = p->least ? (uint64_t)p->items * cache->n_kv_heads * tile_rows : 0;
+  p->o_bytes = kept * cache->head_dim * 4;
+  p->ml_bytes = kept * 8;
   p->plan_bytes = p->least ? ((uint64_t)batch->n_seqs * 8 + 15) & ~15ull : 0;
   return PPD_OK;
 }
 
 template <typename T, int HD>
-hipError_t attn_go(const PagedAttnArgs& a, int items, hipStream_t stream) {
-  hipLaunchKernelGGL((paged_split_kernel<T, HD>), dim3(items, a.kv_heads), dim3(256), 0, stream, a);
-  const hipError_t e = hipGetLastError();
+hipError_t attn_go(const PagedAttnArgs& a, int dtype, int items, hipStream_t stream) {
+  hipError_t e;
+  if (a.tile_rows == TILE_ROWS) e = launch_paged_tiles(a, dtype, HD, items, stream);
+  else {
+    hipLaunchKernelGGL((paged_split_kernel<T, HD>), dim3(items, a.kv_heads), dim3(256), 0, stream, a);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess || a.least == 0) return e;
   constexpr int rpw = 256 / (HD / 4);
   hipLaunchKernelGGL((paged_merge_kernel<T, HD>), dim3(a.b.n_tokens, (a.heads + rpw - 1) / rpw), dim3(256), 0, stream, a);
@@ -465,11 +348,11 @@ extern "C" int ppd_paged_attention(const ppd_paged_cache* cache, const ppd_paged
   a.q_tok = q->token; a.q_head = q->head; a.o_tok = out->token; a.o_head = out->head;
   a.kc_page = cache->k_page; a.kc_pos = cache->k_pos; a.kc_head = cache->k_head; a.vc_page = cache->v_page; a.vc_pos = cache->v_pos; a.vc_head = cache->v_head;
   a.heads = n_heads; a.kv_heads = cache->n_kv_heads; a.group = n_heads / cache->n_kv_heads; a.window = window; a.to_log2 = scale * 1.44269504f;
-  a.want = p.want; a.least = p.least;
+  a.tile_rows = p.tiles ? TILE_ROWS : SPLIT_ROWS; a.last_first = p.tiles; a.want = p.want; a.least = p.least;
   a.part_o = (float*)workspace; a.part_ml = (float2*)((char*)workspace + p.o_bytes); a.plan = (int2*)((char*)workspace + p.o_bytes + p.ml_bytes);
   hipStream_t st = (hipStream_t)hip_stream;
   const int items = (int)p.items;
   if (cache->head_dim == 64)
-    return launched(dt == PPD_FP32 ? attn_go<float, 64>(a, items, st) : dt == PPD_BF16 ? attn_go<bf16_t, 64>(a, items, st) : attn_go<f16_t, 64>(a, items, st));
-  return launched(dt == PPD_FP32 ? attn_go<float, 128>(a, items, st) : dt == PPD_BF16 ? attn_go<bf16_t, 128>(a, items, st) : attn_go<f16_t, 128>(a, items, st));
+    return launched(dt == PPD_FP32 ? attn_go<float, 64>(a, dt, items, st) : dt == PPD_BF16 ? attn_go<bf16_t, 64>(a, dt, items, st) : attn_go<f16_t, 64>(a, dt, items, st));
+  return launched(dt == PPD_FP32 ? attn_go<float, 128>(a, dt, items, st) : dt == PPD_BF16 ? attn_go<bf16_t, 128>(a, dt, items, st) : attn_go<f16_t, 128>(a, dt, items, st));
 }

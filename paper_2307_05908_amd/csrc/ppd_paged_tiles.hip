@@ -1,0 +1,224 @@
+// ppd_paged_attention, many rows: bound by the matrix units (two products of 2 head_dim operations for each row and position) and, right
+// beside them, by the exponentials of the softmax and the reads of LDS.
+#include "ppd_paged_attn.h"
+
+namespace ppd {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c, bf16_t) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c, f16_t) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// Four waves of 32 rows each; blocks of 64 positions in two LDS buffers, filled straight from the pages (a lane of a transfer names its own
+// source, so the rows of a block may lie anywhere, and 16-byte pieces change places within a row so that no operand's reads meet on a bank):
+// keys as they are, the left operand of S^T = K Q^T; values through the transposing reads, the left operand of O^T = V^T P^T.  The next
+// block is under way while one is worked on, with one barrier a block; two workgroups on a compute unit fill each other's gaps.
+template <typename T, int HD>
+__global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
+  constexpr int KV = PLAN_BLOCK, ROWB = HD * 2, UNITS = HD / 8, RPI = WAVE / UNITS, NI = 16 / RPI, SIDE = KV * ROWB;
+  __shared__ __align__(1024) char lds[4 * SIDE];           // [2 buffers][keys, values][64 positions][head_dim]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+  // workgroups go round the eight XCDs in turn: those of one key/value head to one XCD, whose L2 then has its keys and values
+  const int kvheads = a.kv_heads, items = gridDim.x / kvheads;
+  int idx, kvh;
+  if (kvheads % 8 == 0) {
+    const int per = items * 8, rem = blockIdx.x % per;
+    idx = rem / 8; kvh = blockIdx.x / per * 8 + rem % 8;
+  } else {
+    idx = blockIdx.x / kvheads; kvh = blockIdx.x % kvheads;
+  }
+  Item it;
+  if (!find_item(a, idx, idx == 0 && kvh == 0 && wave == 0 && a.least > 0, lane, it)) return;
+  const int all_rows = it.n * a.group;
+  const int r0 = it.tile * TILE_ROWS + 32 * wave, r = r0 + col, rc = min(r, all_rows - 1), tok = rc / a.group, head = kvh * a.group + rc % a.group;
+  const int pos = r < all_rows ? it.pos0 + tok : -1, from = a.window > 0 ? pos - a.window + 1 : 0;
+  const bool busy = r0 < all_rows;
+  const int wave_first = it.pos0 + min(r0, all_rows - 1) / a.group, wave_last = it.pos0 + min(r0 + 31, all_rows - 1) / a.group;    // positions of the wave's rows
+  u32x4 q[HD / 16];
+  {
+    const char* p = (const char*)a.q + ((int64_t)(it.rows0 + tok) * a.q_tok + (int64_t)head * a.q_head) * 2 + half * 16;
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) q[i] = *(const u32x4*)(p + i * 32);
+  }
+  const int blocks = (it.hi - it.lo + KV - 1) / KV;
+  // page (or -1) and slot of the block's position `lane`
+  int page, slot;
+  auto place = [&](int n) {
+    const int p = it.lo + n * KV + lane;
+    page = n < blocks && p < it.hi ? page_of(a.b, it.s, p) : -1;
+    slot = (int)((unsigned)p % (unsigned)a.b.page_size);
+  };
+  uint64_t have_next = 0;
+  const char* const kbase = (const char*)a.kc + (int64_t)kvh * a.kc_head * 2;
+  const char* const vbase = (const char*)a.vc + (int64_t)kvh * a.vc_head * 2;
+  auto request = [&](int n) {
+    have_next = __ballot(page >= 0);
+    const int pg = max(page, 0), sl = page >= 0 ? slot : 0;          // what has no page is read from where there is something, and not seen
+    char* const to = lds + (n & 1) * 2 * SIDE + 16 * wave * ROWB;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int row = 16 * wave + RPI * i + lane / UNITS, unit = lane % UNITS;
+      const int64_t rp = __shfl(pg, row, WAVE), rs = __shfl(sl, row, WAVE);
+      const int uk = unit ^ (HD == 128 ? row & 15 : (row >> 1) & 7), uv = unit ^ (HD == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3));
+      dma16(kbase + (rp * a.kc_page + rs * a.kc_pos) * 2 + uk * 16, to + i * RPI * ROWB);
+      dma16(vbase + (rp * a.vc_page + rs * a.vc_pos) * 2 + uv * 16, to + SIDE + i * RPI * ROWB);
+    }
+  };
+  f32x16 o[HD / 32];
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  // where a lane's operands begin: keys, row col of a half block, pieces 2 i + half; values, four positions of a step, 16 of 32 components
+  int kat[HD / 16], vat[HD / 32];
+#pragma unroll
+  for (int i = 0; i < HD / 16; ++i) kat[i] = col * ROWB + ((2 * i + half) ^ (HD == 128 ? col & 15 : (col >> 1) & 7)) * 16;
+  {
+    const int g = lane >> 4, i = lane & 15, row = 4 * half + (i >> 2);
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+      vat[d] = SIDE + row * ROWB + ((4 * d + 2 * (g & 1) + ((i & 3) >> 1)) ^ (HD == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3))) * 16 + 8 * (i & 1);
+  }
+  place(0);
+  if (blocks > 0) request(0);
+  place(1);
+  for (int n = 0; n < blocks; ++n) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const uint64_t have = have_next;
+    if (n + 1 < blocks) request(n + 1);
+    place(n + 2);
+    const int base = it.lo + n * KV;
+    if (!busy || base > wave_last || (a.window > 0 && base + KV - 1 < wave_first - a.window + 1)) continue;      // no row of the wave sees any of it
+    const bool whole = have == ~0ull && base + KV - 1 <= wave_first && (a.window == 0 || base >= wave_last - a.window + 1);
+    const char* const buf = lds + (n & 1) * 2 * SIDE;
+    f32x16 s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+#pragma unroll
+      for (int i = 0; i < HD / 16; ++i) s[t] = mma32(*(const u32x4*)(buf + kat[i] + t * 32 * ROWB), q[i], s[t], T());
+    }
+    if (!whole) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int at = 32 * t + 8 * (e / 4) + 4 * half + e % 4, p = base + at;
+          if (!((have >> at) & 1) || p > pos || p < from) s[t][e] = -INFINITY;
+        }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[t][e]), s[t][e + 1]);
+    top *= a.to_log2;
+    // the reference that weights are taken from follows the maximum only where that has left it by a factor of 2^8
+    if (__ballot(top > m + 8.f)) {
+      top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+      const float mn = fmaxf(m, top), keep = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= keep;
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] *= keep;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    // Weights go into the second product rounded to the type (their errors together are the size of the result's own rounding; a second term
+    // would cost half the products again), into the sum as they are.
+    u32x4 w[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[t / 2][8 * (t % 2) + 2 * e], a.to_log2, -ref)), y = __builtin_amdgcn_exp2f(fmaf(s[t / 2][8 * (t % 2) + 2 * e + 1], a.to_log2, -ref));
+        w[t][e] = pair(x, y, T());
+        l += x + y;
+      }
+    auto values = [&](int t, int d) {
+      const char* p = buf + vat[d] + t * 16 * ROWB;
+      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));
+      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 8 * ROWB)));
+      return (u32x4){x.x, x.y, y.x, y.y};
+    };
+    if (!whole) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d) most = largest(most, values(t, d), T());
+      if (__ballot(endless(most, T()))) {
+        // a value that is infinite, or no number, among positions that not every row sees: position by position, kept where it is seen
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          for (int p = 0; p < 16; ++p) {
+            const int e = (p & 3) + 4 * (p >> 3), at = base + 16 * t + p;
+            const bool seen = ((have >> (16 * t + p)) & 1) && at <= pos && at >= from;
+#pragma unroll
+            for (int d = 0; d < HD / 32; ++d) {
+              const u32x4 v = values(t, d);
+              u32x4 only = {0u, 0u, 0u, 0u};
+              if (((p >> 2) & 1) == half)
+#pragma unroll
+                for (int z = 0; z < 4; ++z) if (z == e / 2) only[z] = v[z] & (e & 1 ? 0xffff0000u : 0xffffu);
+              const f32x16 y = mma32(only, w[t], o[d], T());
+#pragma unroll
+              for (int z = 0; z < 16; ++z) o[d][z] = seen ? y[z] : o[d][z];
+            }
+          }
+        continue;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int d = 0; d < HD / 32; ++d) o[d] = mma32(values(t, d), w[t], o[d], T());
+  }
+  l += __shfl_xor(l, 32, WAVE);
+  if (r >= all_rows) return;
+  const bool none = m == -INFINITY && l == 0.f;
+  if (it.parts > 1) {
+    const int64_t at = ((int64_t)it.slot * kvheads + kvh) * TILE_ROWS + 32 * wave + col;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) *(f32x4*)(a.part_o + at * HD + 32 * d + 2 * e + 4 * half) = (f32x4){o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
+    if (half == 0) a.part_ml[at] = make_float2(m, l);
+    return;
+  }
+  const float inv = 1.0f / l;
+  T* const to = (T*)a.out + (int64_t)(it.rows0 + tok) * a.o_tok + (int64_t)head * a.o_head + 4 * half;
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      f32x4 y = {o[d][e] * inv, o[d][e + 1] * inv, o[d][e + 2] * inv, o[d][e + 3] * inv};
+      if (none) y = (f32x4){0.f, 0.f, 0.f, 0.f};
+      *(u32x2*)(to + 32 * d + 2 * e) = quad_out<T>(y);
+    }
+  if (a.lse && half == 0) a.lse[(int64_t)(it.rows0 + tok) * a.heads + head] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718f;
+}
+
+template <typename T>
+hipError_t tiles_go(const PagedAttnArgs& a, int head_dim, dim3 grid, hipStream_t stream) {
+  if (head_dim == 64) hipLaunchKernelGGL((paged_tile_kernel<T, 64>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((paged_tile_kernel<T, 128>), grid, dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_tiles(const PagedAttnArgs& a, int dtype, int head_dim, int items, hipStream_t stream) {
+  const dim3 grid((unsigned)items * a.kv_heads);
+  return dtype == PPD_BF16 ? tiles_go<bf16_t>(a, head_dim, grid, stream) : dtype == PPD_FP16 ? tiles_go<f16_t>(a, head_dim, grid, stream) : hipErrorInvalidValue;
+}
+
+}  // namespace ppd

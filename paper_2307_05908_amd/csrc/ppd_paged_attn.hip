@@ -167,6 +167,7 @@ __global__ __launch_bounds__(256, 2) void paged_split_kernel(PagedAttnArgs a) {
         if (odd && whole) o[i] = mma16(vt, hi, o[i], T());
         else if (odd) {
           // a value that is no number, or infinite, among positions that not every row sees: position by position, kept where it is seen
+#pragma unroll 1
           for (int p = 0; p < 32; ++p) {
             u32x4 only = {0u, 0u, 0u, 0u};
             const int e = (p >> 4) * 4 + (p & 3);

@@ -13,11 +13,19 @@ __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c, bf16_t) {
 __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c, f16_t) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
+// dma16 with the lanes' sources as 32-bit offsets from one address
+__device__ __forceinline__ void dma16_near(const void* base, int offset, void* lds_dst) {
+  const unsigned la = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds_dst;
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(la) : "memory", "m0");
+}
+
 // Four waves of 32 rows each; blocks of 64 positions in two LDS buffers, filled straight from the pages (a lane of a transfer names its own
 // source, so the rows of a block may lie anywhere, and 16-byte pieces change places within a row so that no operand's reads meet on a bank):
 // keys as they are, the left operand of S^T = K Q^T; values through the transposing reads, the left operand of O^T = V^T P^T.  The next
 // block is under way while one is worked on, with one barrier a block; two workgroups on a compute unit fill each other's gaps.
-template <typename T, int HD>
+// NEAR: 16 positions in a row that begin at a multiple of 16 lie in one page, within 2^31 bytes, so that a wave's share of a block has one
+// page and the lanes 32-bit offsets in it.
+template <typename T, int HD, bool NEAR>
 __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   constexpr int KV = PLAN_BLOCK, ROWB = HD * 2, UNITS = HD / 8, RPI = WAVE / UNITS, NI = 16 / RPI, SIDE = KV * ROWB;
   __shared__ __align__(1024) char lds[4 * SIDE];           // [2 buffers][keys, values][64 positions][head_dim]
@@ -55,17 +63,33 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   uint64_t have_next = 0;
   const char* const kbase = (const char*)a.kc + (int64_t)kvh * a.kc_head * 2;
   const char* const vbase = (const char*)a.vc + (int64_t)kvh * a.vc_head * 2;
+  // (lane / UNITS is the row of a transfer, and the piece that it brings is the one whose place the lane has: see kat, vat)
+  const int unit = lane % UNITS;
+  int piece_k = (unit ^ (lane >> 4)) * 16, piece_v = (unit ^ 2 * (lane >> 4)) * 16, trow = lane / UNITS;
   auto request = [&](int n) {
+    asm volatile("" : "+v"(piece_k), "+v"(piece_v), "+v"(trow));      // (worked out anew for every block: kept, the offsets would cost registers that there are not)
     have_next = __ballot(page >= 0);
-    const int pg = max(page, 0), sl = page >= 0 ? slot : 0;          // what has no page is read from where there is something, and not seen
     char* const to = lds + (n & 1) * 2 * SIDE + 16 * wave * ROWB;
+    if constexpr (NEAR) {
+      const int pg = __builtin_amdgcn_readlane(page, 16 * wave), sl = pg >= 0 ? __builtin_amdgcn_readlane(slot, 16 * wave) : 0;
+      // what has no page is read from where there is something, and not seen; so are positions behind the part in a page of its own
+      const char* const kp = kbase + ((int64_t)max(pg, 0) * a.kc_page + (int64_t)sl * a.kc_pos) * 2;
+      const char* const vp = vbase + ((int64_t)max(pg, 0) * a.vc_page + (int64_t)sl * a.vc_pos) * 2;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int row = 16 * wave + RPI * i + lane / UNITS, unit = lane % UNITS;
-      const int64_t rp = __shfl(pg, row, WAVE), rs = __shfl(sl, row, WAVE);
-      const int uk = unit ^ (HD == 128 ? row & 15 : (row >> 1) & 7), uv = unit ^ (HD == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3));
-      dma16(kbase + (rp * a.kc_page + rs * a.kc_pos) * 2 + uk * 16, to + i * RPI * ROWB);
-      dma16(vbase + (rp * a.vc_page + rs * a.vc_pos) * 2 + uv * 16, to + SIDE + i * RPI * ROWB);
+      for (int i = 0; i < NI; ++i) {
+        const int row = RPI * i + trow;
+        dma16_near(kp, row * (int)a.kc_pos * 2 + (piece_k ^ 64 * i), to + i * RPI * ROWB);
+        dma16_near(vp, row * (int)a.vc_pos * 2 + (HD == 128 ? piece_v ^ 128 * (i & 1) : piece_v), to + SIDE + i * RPI * ROWB);
+      }
+    } else {
+      const int pg = max(page, 0), sl = page >= 0 ? slot : 0;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int row = 16 * wave + RPI * i + trow;
+        const int64_t rp = __shfl(pg, row, WAVE), rs = __shfl(sl, row, WAVE);
+        dma16(kbase + (rp * a.kc_page + rs * a.kc_pos) * 2 + (piece_k ^ 64 * i), to + i * RPI * ROWB);
+        dma16(vbase + (rp * a.vc_page + rs * a.vc_pos) * 2 + (HD == 128 ? piece_v ^ 128 * (i & 1) : piece_v), to + SIDE + i * RPI * ROWB);
+      }
     }
   };
   f32x16 o[HD / 32];
@@ -74,16 +98,14 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
   float m = -INFINITY, l = 0.f;
-  // where a lane's operands begin: keys, row col of a half block, pieces 2 i + half; values, four positions of a step, 16 of 32 components
-  int kat[HD / 16], vat[HD / 32];
-#pragma unroll
-  for (int i = 0; i < HD / 16; ++i) kat[i] = col * ROWB + ((2 * i + half) ^ (HD == 128 ? col & 15 : (col >> 1) & 7)) * 16;
-  {
-    const int g = lane >> 4, i = lane & 15, row = 4 * half + (i >> 2);
-#pragma unroll
-    for (int d = 0; d < HD / 32; ++d)
-      vat[d] = SIDE + row * ROWB + ((4 * d + 2 * (g & 1) + ((i & 3) >> 1)) ^ (HD == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3))) * 16 + 8 * (i & 1);
-  }
+  int odd_first = 0x7fffffff, odd_last = -1;              // blocks with a value that is infinite or no number where not every row sees it
+  // Where a lane's operands begin.  A row's 16-byte pieces have changed places by an exclusive or: keys with the row (head_dim 64: half of it),
+  // so that eight rows in turn have a piece on eight places; values two pieces at a time, so that the four rows of a transposing read and
+  // the four of the other half lie on different banks.  Keys: row col of half a block, piece 2 i + half at kat ^ 32 i.  Values: position
+  // 4 half + i / 4 of 16, components 32 d + 16 (g % 2) + 4 (i % 4) at vat ^ 64 d, g = lane / 16, i = lane % 16.
+  int kat = col * ROWB + (half ^ (HD == 128 ? col & 15 : (col >> 1) & 7)) * 16;
+  const int vrow = 4 * half + ((lane & 15) >> 2);
+  int vat = SIDE + vrow * ROWB + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (HD == 128 ? 2 * (vrow & 7) : 2 * ((vrow >> 1) & 3))) * 16 + 8 * (lane & 1);
   place(0);
   if (blocks > 0) request(0);
   place(1);
@@ -97,21 +119,25 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
     if (!busy || base > wave_last || (a.window > 0 && base + KV - 1 < wave_first - a.window + 1)) continue;      // no row of the wave sees any of it
     const bool whole = have == ~0ull && base + KV - 1 <= wave_first && (a.window == 0 || base >= wave_last - a.window + 1);
     const char* const buf = lds + (n & 1) * 2 * SIDE;
+    asm volatile("" : "+v"(kat), "+v"(vat));
     f32x16 s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
 #pragma unroll
-      for (int i = 0; i < HD / 16; ++i) s[t] = mma32(*(const u32x4*)(buf + kat[i] + t * 32 * ROWB), q[i], s[t], T());
+      for (int i = 0; i < HD / 16; ++i) s[t] = mma32(*(const u32x4*)(buf + (kat ^ 32 * i) + t * 32 * ROWB), q[i], s[t], T());
     }
     if (!whole) {
+      const int to = pos - base - 4 * half, since = from - base - 4 * half;
+      const uint32_t have_lo = (uint32_t)(have >> (4 * half)), have_hi = (uint32_t)(have >> (32 + 4 * half));
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int at = 32 * t + 8 * (e / 4) + 4 * half + e % 4, p = base + at;
-          if (!((have >> at) & 1) || p > pos || p < from) s[t][e] = -INFINITY;
+          const int at = 8 * (e / 4) + e % 4;
+          const bool seen = (((t ? have_hi : have_lo) >> at & 1) != 0) & (32 * t + at <= to) & (32 * t + at >= since);
+          s[t][e] = seen ? s[t][e] : -INFINITY;
         }
     }
     float top = -INFINITY;
@@ -144,43 +170,69 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
         l += x + y;
       }
     auto values = [&](int t, int d) {
-      const char* p = buf + vat[d] + t * 16 * ROWB;
+      const char* p = buf + (vat ^ 64 * d) + t * 16 * ROWB;
       const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));
       const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 8 * ROWB)));
       return (u32x4){x.x, x.y, y.x, y.y};
     };
-    if (!whole) {
+    if (whole) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d) o[d] = mma32(values(t, d), w[t], o[d], T());
+    } else {
+      // Positions that not every row sees.  Values of those that none sees are cleared; what is infinite among the others, or no number, is
+      // left out, and put in behind the loop where it is seen.
+      uint64_t vis = have & ~0ull >> max(base + KV - 1 - wave_last, 0);
+      if (a.window > 0) vis &= ~0ull << max(wave_first - a.window + 1 - base, 0);
+      u32x4 keep[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t two = (uint32_t)(vis >> (16 * t + 8 * (e / 2) + 2 * (e % 2) + 4 * half)) & 3;
+          keep[t][e] = (two & 1) * 0xffffu | (two >> 1) * 0xffff0000u;
+        }
       uint32_t most = 0;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int d = 0; d < HD / 32; ++d) most = largest(most, values(t, d), T());
-      if (__ballot(endless(most, T()))) {
-        // a value that is infinite, or no number, among positions that not every row sees: position by position, kept where it is seen
+        for (int d = 0; d < HD / 32; ++d) most = largest(most, values(t, d) & keep[t], T());
+      const bool odd = __ballot(endless(most, T())) != 0;
+      if (odd) { odd_first = min(odd_first, n); odd_last = n; }
+      asm volatile("" : "+v"(vat));                       // (read again: there are no registers to keep them in)
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-          for (int p = 0; p < 16; ++p) {
-            const int e = (p & 3) + 4 * (p >> 3), at = base + 16 * t + p;
-            const bool seen = ((have >> (16 * t + p)) & 1) && at <= pos && at >= from;
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int d = 0; d < HD / 32; ++d) {
-              const u32x4 v = values(t, d);
-              u32x4 only = {0u, 0u, 0u, 0u};
-              if (((p >> 2) & 1) == half)
+        for (int d = 0; d < HD / 32; ++d) {
+          u32x4 v = values(t, d) & keep[t];
+          if (odd)
 #pragma unroll
-                for (int z = 0; z < 4; ++z) if (z == e / 2) only[z] = v[z] & (e & 1 ? 0xffff0000u : 0xffffu);
-              const f32x16 y = mma32(only, w[t], o[d], T());
-#pragma unroll
-              for (int z = 0; z < 16; ++z) o[d][z] = seen ? y[z] : o[d][z];
-            }
-          }
-        continue;
-      }
+            for (int e = 0; e < 4; ++e) { if (endless(v[e] & 0x7fffu, T())) v[e] &= 0xffff0000u; if (endless(v[e] & 0x7fff0000u, T())) v[e] &= 0xffffu; }
+          o[d] = mma32(v, w[t], o[d], T());
+        }
     }
+  }
+#pragma unroll 1
+  for (int n = odd_first; n <= odd_last; ++n) {
+    // such a block once more, position by position, from the pages: a row that sees an infinite value, or no number, takes it up
+    const int base = it.lo + n * KV, x = base + lane;
+    const bool there = __ballot(x < it.hi && page_of(a.b, it.s, x) >= 0) == ~0ull;
+    if (there && base + KV - 1 <= wave_first && (a.window == 0 || base >= wave_last - a.window + 1)) continue;
+#pragma unroll 1
+    for (int p = base; p < min(base + KV, it.hi); ++p) {
+      const int pg = page_of(a.b, it.s, p);
+      if (pg < 0 || p > pos || p < from) continue;
+      const T* const row = (const T*)vbase + (int64_t)pg * a.vc_page + (int64_t)((unsigned)p % (unsigned)a.b.page_size) * a.vc_pos + 4 * half;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+      for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
-      for (int d = 0; d < HD / 32; ++d) o[d] = mma32(values(t, d), w[t], o[d], T());
+        for (int e = 0; e < 16; e += 4) {
+          const f32x4 v = Quad<T>::wide(*(const u32x2*)(row + 32 * d + 2 * e));
+#pragma unroll
+          for (int z = 0; z < 4; ++z) o[d][e + z] += fabsf(v[z]) < INFINITY ? 0.f : v[z];
+        }
+    }
   }
   l += __shfl_xor(l, 32, WAVE);
   if (r >= all_rows) return;
@@ -207,10 +259,10 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   if (a.lse && half == 0) a.lse[(int64_t)(it.rows0 + tok) * a.heads + head] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718f;
 }
 
-template <typename T>
+template <typename T, bool NEAR>
 hipError_t tiles_go(const PagedAttnArgs& a, int head_dim, dim3 grid, hipStream_t stream) {
-  if (head_dim == 64) hipLaunchKernelGGL((paged_tile_kernel<T, 64>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((paged_tile_kernel<T, 128>), grid, dim3(256), 0, stream, a);
+  if (head_dim == 64) hipLaunchKernelGGL((paged_tile_kernel<T, 64, NEAR>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((paged_tile_kernel<T, 128, NEAR>), grid, dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -218,7 +270,11 @@ hipError_t tiles_go(const PagedAttnArgs& a, int head_dim, dim3 grid, hipStream_t
 
 hipError_t launch_paged_tiles(const PagedAttnArgs& a, int dtype, int head_dim, int items, hipStream_t stream) {
   const dim3 grid((unsigned)items * a.kv_heads);
-  return dtype == PPD_BF16 ? tiles_go<bf16_t>(a, head_dim, grid, stream) : dtype == PPD_FP16 ? tiles_go<f16_t>(a, head_dim, grid, stream) : hipErrorInvalidValue;
+  const int64_t far = (1 << 26) - 1;
+  const bool near = a.b.page_size % 16 == 0 && a.kc_pos <= far && a.vc_pos <= far;
+  if (dtype == PPD_BF16) return near ? tiles_go<bf16_t, true>(a, head_dim, grid, stream) : tiles_go<bf16_t, false>(a, head_dim, grid, stream);
+  if (dtype == PPD_FP16) return near ? tiles_go<f16_t, true>(a, head_dim, grid, stream) : tiles_go<f16_t, false>(a, head_dim, grid, stream);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace ppd

@@ -53,12 +53,14 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
     for (int i = 0; i < HD / 16; ++i) q[i] = *(const u32x4*)(p + i * 32);
   }
   const int blocks = (it.hi - it.lo + KV - 1) / KV;
-  // page (or -1) and slot of the block's position `lane`
-  int page, slot;
+  // The table's entry for, and the slot of, the block's position `lane`: asked for here, looked at when the block is requested, a whole block
+  // later.  (Looked at here it would wait for the transfers that are under way.)
+  int entry, slot;
+  const int32_t* const table = a.b.pages + (int64_t)it.s * a.b.pages_stride;
   auto place = [&](int n) {
-    const int p = it.lo + n * KV + lane;
-    page = n < blocks && p < it.hi ? page_of(a.b, it.s, p) : -1;
-    slot = (int)((unsigned)p % (unsigned)a.b.page_size);
+    const int p = it.lo + n * KV + lane, i = (int)((unsigned)p / (unsigned)a.b.page_size);
+    slot = p - i * a.b.page_size;
+    entry = table[min(i, a.b.max_pages - 1)];
   };
   uint64_t have_next = 0;
   const char* const kbase = (const char*)a.kc + (int64_t)kvh * a.kc_head * 2;
@@ -68,6 +70,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   int piece_k = (unit ^ (lane >> 4)) * 16, piece_v = (unit ^ 2 * (lane >> 4)) * 16, trow = lane / UNITS;
   auto request = [&](int n) {
     asm volatile("" : "+v"(piece_k), "+v"(piece_v), "+v"(trow));      // (worked out anew for every block: kept, the offsets would cost registers that there are not)
+    const int page = it.lo + n * KV + lane < it.hi && (unsigned)entry < (unsigned)a.b.n_pages ? entry : -1;      // (hi is within the table)
     have_next = __ballot(page >= 0);
     char* const to = lds + (n & 1) * 2 * SIDE + 16 * wave * ROWB;
     if constexpr (NEAR) {
@@ -106,18 +109,8 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   int kat = col * ROWB + (half ^ (HD == 128 ? col & 15 : (col >> 1) & 7)) * 16;
   const int vrow = 4 * half + ((lane & 15) >> 2);
   int vat = SIDE + vrow * ROWB + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (HD == 128 ? 2 * (vrow & 7) : 2 * ((vrow >> 1) & 3))) * 16 + 8 * (lane & 1);
-  place(0);
-  if (blocks > 0) request(0);
-  place(1);
-  for (int n = 0; n < blocks; ++n) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    const uint64_t have = have_next;
-    if (n + 1 < blocks) request(n + 1);
-    place(n + 2);
-    const int base = it.lo + n * KV;
-    if (!busy || base > wave_last || (a.window > 0 && base + KV - 1 < wave_first - a.window + 1)) continue;      // no row of the wave sees any of it
-    const bool whole = have == ~0ull && base + KV - 1 <= wave_first && (a.window == 0 || base >= wave_last - a.window + 1);
+  auto step = [&](int n, int base, uint64_t have, auto whole) {
+    constexpr bool WHOLE = decltype(whole)::value;         // every row of the wave sees every position
     const char* const buf = lds + (n & 1) * 2 * SIDE;
     asm volatile("" : "+v"(kat), "+v"(vat));
     f32x16 s[2];
@@ -128,7 +121,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
 #pragma unroll
       for (int i = 0; i < HD / 16; ++i) s[t] = mma32(*(const u32x4*)(buf + (kat ^ 32 * i) + t * 32 * ROWB), q[i], s[t], T());
     }
-    if (!whole) {
+    if constexpr (!WHOLE) {
       const int to = pos - base - 4 * half, since = from - base - 4 * half;
       const uint32_t have_lo = (uint32_t)(have >> (4 * half)), have_hi = (uint32_t)(have >> (32 + 4 * half));
 #pragma unroll
@@ -175,7 +168,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 8 * ROWB)));
       return (u32x4){x.x, x.y, y.x, y.y};
     };
-    if (whole) {
+    if constexpr (WHOLE) {
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -185,33 +178,53 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       // left out, and put in behind the loop where it is seen.
       uint64_t vis = have & ~0ull >> max(base + KV - 1 - wave_last, 0);
       if (a.window > 0) vis &= ~0ull << max(wave_first - a.window + 1 - base, 0);
-      u32x4 keep[4];
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
+      uint32_t vis_lo = (uint32_t)(vis >> (4 * half)), vis_hi = (uint32_t)(vis >> (32 + 4 * half));
+      auto cleared = [&](int t, int d) {
+        u32x4 v = values(t, d);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint32_t two = (uint32_t)(vis >> (16 * t + 8 * (e / 2) + 2 * (e % 2) + 4 * half)) & 3;
-          keep[t][e] = (two & 1) * 0xffffu | (two >> 1) * 0xffff0000u;
+          const uint32_t two = (t < 2 ? vis_lo : vis_hi) >> (16 * (t % 2) + 8 * (e / 2) + 2 * (e % 2));
+          v[e] &= (two & 1 ? 0xffffu : 0u) | (two & 2 ? 0xffff0000u : 0u);
         }
+        return v;
+      };
       uint32_t most = 0;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int d = 0; d < HD / 32; ++d) most = largest(most, values(t, d) & keep[t], T());
+        for (int d = 0; d < HD / 32; ++d) most = largest(most, cleared(t, d), T());
       const bool odd = __ballot(endless(most, T())) != 0;
       if (odd) { odd_first = min(odd_first, n); odd_last = n; }
-      asm volatile("" : "+v"(vat));                       // (read again: there are no registers to keep them in)
+      asm volatile("" : "+v"(vat), "+v"(vis_lo), "+v"(vis_hi));      // (read again: there are no registers to keep them in)
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int d = 0; d < HD / 32; ++d) {
-          u32x4 v = values(t, d) & keep[t];
+          u32x4 v = cleared(t, d);
           if (odd)
 #pragma unroll
             for (int e = 0; e < 4; ++e) { if (endless(v[e] & 0x7fffu, T())) v[e] &= 0xffff0000u; if (endless(v[e] & 0x7fff0000u, T())) v[e] &= 0xffffu; }
           o[d] = mma32(v, w[t], o[d], T());
         }
     }
+  };
+  place(0);
+  if (blocks > 0) request(0);
+  place(1);
+  // the queries are waited for here: a wait in the loop would be one for the transfers, of which the compiler knows nothing
+#pragma unroll
+  for (int i = 0; i < HD / 16; ++i) asm volatile("" : "+v"(q[i]));
+  for (int n = 0; n < blocks; ++n) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const uint64_t have = have_next;
+    if (n + 1 < blocks) request(n + 1);
+    place(n + 2);
+    const int base = it.lo + n * KV;
+    if (!busy || base > wave_last || (a.window > 0 && base + KV - 1 < wave_first - a.window + 1)) continue;      // no row of the wave sees any of it
+    const bool whole = have == ~0ull && base + KV - 1 <= wave_first && (a.window == 0 || base >= wave_last - a.window + 1);
+    if (whole) step(n, base, have, std::true_type());
+    else step(n, base, have, std::false_type());
   }
 #pragma unroll 1
   for (int n = odd_first; n <= odd_last; ++n) {

@@ -39,6 +39,8 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   } else {
     idx = blockIdx.x / kvheads; kvh = blockIdx.x % kvheads;
   }
+  __shared__ int s_odd[2];                                 // first and last block with a value that is infinite, or no number, where not every row sees it
+  if (threadIdx.x == 0) { s_odd[0] = 0x7fffffff; s_odd[1] = -1; }
   Item it;
   if (!find_item(a, idx, idx == 0 && kvh == 0 && wave == 0 && a.least > 0, lane, it)) return;
   const int all_rows = it.n * a.group;
@@ -46,6 +48,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   const int pos = r < all_rows ? it.pos0 + tok : -1, from = a.window > 0 ? pos - a.window + 1 : 0;
   const bool busy = r0 < all_rows;
   const int wave_first = it.pos0 + min(r0, all_rows - 1) / a.group, wave_last = it.pos0 + min(r0 + 31, all_rows - 1) / a.group;    // positions of the wave's rows
+  const int tile_first = it.pos0 + it.tile * TILE_ROWS / a.group, tile_last = it.pos0 + min((it.tile * TILE_ROWS + TILE_ROWS - 1) / a.group, it.n - 1);
   u32x4 q[HD / 16];
   {
     const char* p = (const char*)a.q + ((int64_t)(it.rows0 + tok) * a.q_tok + (int64_t)head * a.q_head) * 2 + half * 16;
@@ -101,7 +104,6 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
   float m = -INFINITY, l = 0.f;
-  int odd_first = 0x7fffffff, odd_last = -1;              // blocks with a value that is infinite or no number where not every row sees it
   // Where a lane's operands begin.  A row's 16-byte pieces have changed places by an exclusive or: keys with the row (head_dim 64: half of it),
   // so that eight rows in turn have a piece on eight places; values two pieces at a time, so that the four rows of a transposing read and
   // the four of the other half lie on different banks.  Keys: row col of half a block, piece 2 i + half at kat ^ 32 i.  Values: position
@@ -109,8 +111,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   int kat = col * ROWB + (half ^ (HD == 128 ? col & 15 : (col >> 1) & 7)) * 16;
   const int vrow = 4 * half + ((lane & 15) >> 2);
   int vat = SIDE + vrow * ROWB + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (HD == 128 ? 2 * (vrow & 7) : 2 * ((vrow >> 1) & 3))) * 16 + 8 * (lane & 1);
-  auto step = [&](int n, int base, uint64_t have, auto whole) {
-    constexpr bool WHOLE = decltype(whole)::value;         // every row of the wave sees every position
+  auto step = [&](int n, int base, uint64_t have, bool whole) {      // whole: every row of the wave sees every position
     const char* const buf = lds + (n & 1) * 2 * SIDE;
     asm volatile("" : "+v"(kat), "+v"(vat));
     f32x16 s[2];
@@ -121,7 +122,8 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
 #pragma unroll
       for (int i = 0; i < HD / 16; ++i) s[t] = mma32(*(const u32x4*)(buf + (kat ^ 32 * i) + t * 32 * ROWB), q[i], s[t], T());
     }
-    if constexpr (!WHOLE) {
+    if (!whole) {
+      asm volatile("");                                    // (a branch, not selections that every block goes through)
       const int to = pos - base - 4 * half, since = from - base - 4 * half;
       const uint32_t have_lo = (uint32_t)(have >> (4 * half)), have_hi = (uint32_t)(have >> (32 + 4 * half));
 #pragma unroll
@@ -168,44 +170,30 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 8 * ROWB)));
       return (u32x4){x.x, x.y, y.x, y.y};
     };
-    if constexpr (WHOLE) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int d = 0; d < HD / 32; ++d) o[d] = mma32(values(t, d), w[t], o[d], T());
-    } else {
-      // Positions that not every row sees.  Values of those that none sees are cleared; what is infinite among the others, or no number, is
-      // left out, and put in behind the loop where it is seen.
-      uint64_t vis = have & ~0ull >> max(base + KV - 1 - wave_last, 0);
-      if (a.window > 0) vis &= ~0ull << max(wave_first - a.window + 1 - base, 0);
-      uint32_t vis_lo = (uint32_t)(vis >> (4 * half)), vis_hi = (uint32_t)(vis >> (32 + 4 * half));
-      auto cleared = [&](int t, int d) {
-        u32x4 v = values(t, d);
+      for (int d = 0; d < HD / 32; ++d) o[d] = mma32(values(t, d), w[t], o[d], T());
+  };
+  // Where not every row of the tile sees all of a block: a weight of zero does not silence a value that is infinite or no number, so these
+  // are cleared in LDS (each wave its own 16 positions), and put in behind the loop where they are seen.
+  auto clean = [&](int n, int base, uint64_t have) {
+    char* const p = lds + (n & 1) * 2 * SIDE + SIDE + 16 * wave * ROWB + lane * 16;
+    uint32_t most = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t two = (t < 2 ? vis_lo : vis_hi) >> (16 * (t % 2) + 8 * (e / 2) + 2 * (e % 2));
-          v[e] &= (two & 1 ? 0xffffu : 0u) | (two & 2 ? 0xffff0000u : 0u);
-        }
-        return v;
-      };
-      uint32_t most = 0;
+    for (int i = 0; i < NI; ++i) most = largest(most, *(const u32x4*)(p + i * RPI * ROWB), T());
+    if (__ballot(endless(most, T()))) {
+      bool seen = false;
+#pragma unroll 1
+      for (int i = 0; i < NI; ++i) {
+        const int row = 16 * wave + RPI * i + lane / UNITS;
+        u32x4 v = *(const u32x4*)(p + i * RPI * ROWB);
+        seen |= endless(largest(0, v, T()), T()) && ((have >> row) & 1);
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int d = 0; d < HD / 32; ++d) most = largest(most, cleared(t, d), T());
-      const bool odd = __ballot(endless(most, T())) != 0;
-      if (odd) { odd_first = min(odd_first, n); odd_last = n; }
-      asm volatile("" : "+v"(vat), "+v"(vis_lo), "+v"(vis_hi));      // (read again: there are no registers to keep them in)
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int d = 0; d < HD / 32; ++d) {
-          u32x4 v = cleared(t, d);
-          if (odd)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { if (endless(v[e] & 0x7fffu, T())) v[e] &= 0xffff0000u; if (endless(v[e] & 0x7fff0000u, T())) v[e] &= 0xffffu; }
-          o[d] = mma32(v, w[t], o[d], T());
-        }
+        for (int e = 0; e < 4; ++e) { if (endless(v[e] & 0x7fffu, T())) v[e] &= 0xffff0000u; if (endless(v[e] & 0x7fff0000u, T())) v[e] &= 0xffffu; }
+        *(u32x4*)(p + i * RPI * ROWB) = v;
+      }
+      if (__ballot(seen) && lane == 0) { atomicMin(&s_odd[0], n); atomicMax(&s_odd[1], n); }
     }
   };
   place(0);
@@ -221,17 +209,22 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
     if (n + 1 < blocks) request(n + 1);
     place(n + 2);
     const int base = it.lo + n * KV;
+    if (!(have == ~0ull && base + KV - 1 <= tile_first && (a.window == 0 || base >= tile_last - a.window + 1))) {
+      clean(n, base, have);
+      __syncthreads();
+    }
     if (!busy || base > wave_last || (a.window > 0 && base + KV - 1 < wave_first - a.window + 1)) continue;      // no row of the wave sees any of it
     const bool whole = have == ~0ull && base + KV - 1 <= wave_first && (a.window == 0 || base >= wave_last - a.window + 1);
-    if (whole) step(n, base, have, std::true_type());
-    else step(n, base, have, std::false_type());
+    step(n, base, have, whole);
   }
+  __syncthreads();
+  const int odd_first = s_odd[0], odd_last = s_odd[1];
 #pragma unroll 1
   for (int n = odd_first; n <= odd_last; ++n) {
     // such a block once more, position by position, from the pages: a row that sees an infinite value, or no number, takes it up
     const int base = it.lo + n * KV, x = base + lane;
     const bool there = __ballot(x < it.hi && page_of(a.b, it.s, x) >= 0) == ~0ull;
-    if (there && base + KV - 1 <= wave_first && (a.window == 0 || base >= wave_last - a.window + 1)) continue;
+    if (there && base + KV - 1 <= tile_first && (a.window == 0 || base >= tile_last - a.window + 1)) continue;
 #pragma unroll 1
     for (int p = base; p < min(base + KV, it.hi); ++p) {
       const int pg = page_of(a.b, it.s, p);

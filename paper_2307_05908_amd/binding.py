@@ -8,7 +8,9 @@ if the library cannot be loaded, importing the symbols raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
+import struct
 from typing import Dict, List, Optional
 
 import numpy as np
@@ -186,62 +188,87 @@ def ppd_early_topk_noalloc(h, norm_g, norm_b, head, k, norm, norm_eps=1e-5, want
 
 
 # ---- operators on paged keys and values (include/ppd_layers.h)
-def _dtype_code(t) -> int:
-    import torch
-    codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-    if t.dtype not in codes:
-        raise ValueError(f"float32, bfloat16 or float16 expected, not {t.dtype}")
-    return codes[t.dtype]
+# A call's host side is most of its time where there is little to do, so the structs go over as packed bytes (the layouts of PagedCache,
+# PagedBatch and Rows) and each check is made once.
+_PACK_CACHE, _PACK_BATCH, _PACK_ROWS = struct.Struct("@QQ6q5i4x").pack, struct.Struct("@3Qq3i4x").pack, struct.Struct("@Q2q").pack
+_fast = None
 
 
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
+def _layers():
+    """torch, the type codes, and the library's functions as they are called here."""
+    global _fast
+    if _fast is None:
+        import torch
+        lib = load_library()
+        vp, ci, cl, cu, cf = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float
+
+        def fn(name, *argtypes):
+            f = lib._FuncPtr((name, lib))
+            f.argtypes = argtypes
+            return f
+
+        _fast = (torch, {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
+                 fn("ppd_paged_append", vp, vp, ci, vp, vp, vp, vp, vp, vp, cf, ci, cf, vp),
+                 fn("ppd_paged_attention", vp, vp, ci, vp, vp, vp, cf, ci, vp, cu, vp),
+                 fn("ppd_verify_drafts", ci, ci, ci, ci, vp, vp, vp, cl, vp, cl, vp, vp, vp, vp, vp, cu, vp))
+    return _fast
 
 
 def _on_device(first, others, stream, call):
-    """call(stream) with the tensors' device as the current one and what it allocates on the stream that it works on.  Tensors that
-    another stream than the current one reads or writes are not given away before that stream is done with them."""
-    import torch
+    """call() with the tensors' GPU as the current one, on `stream`, which is where it allocates too.  Tensors that another stream than the
+    current one reads or writes are not given away before that stream is done with them."""
+    torch = _layers()[0]
     dev = first.device
-    _need(dev.type == "cuda" and all(t is None or t.device == dev for t in others), "all tensors on one GPU")
-    if dev.index != torch.cuda.current_device():
-        with torch.cuda.device(dev):
-            return _on_device(first, others, stream, call)
-    cur = torch.cuda.current_stream()
-    if stream is None or stream == cur:
-        return call(ctypes.c_void_p(cur.cuda_stream))
-    _need(stream.device == dev, "the stream is another GPU's")
-    for t in (first, *others):
-        if t is not None:
-            t.record_stream(stream)
-    with torch.cuda.stream(stream):
-        return call(ctypes.c_void_p(stream.cuda_stream))
+    if dev.type != "cuda":
+        raise ValueError("tensors on a GPU")
+    with torch.cuda.device(dev):
+        if stream is None or stream == torch.cuda.current_stream():
+            return call()
+        if stream.device != dev:
+            raise ValueError("the stream is another GPU's")
+        for t in (first, *others):
+            if t is not None:
+                t.record_stream(stream)
+        with torch.cuda.stream(stream):
+            return call()
+
+
+def _same_gpu(dev, *tensors):
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("all tensors on one GPU")
 
 
 def _paged_args(k_cache, v_cache, pages, q_start, kv_len, n_tokens):
-    import torch
-    _need(k_cache.dim() == 4 and k_cache.shape == v_cache.shape and k_cache.dtype == v_cache.dtype,
-          "k_cache, v_cache: [n_pages, page_size, n_kv_heads, head_dim] of one type")
+    """(cache, batch) as bytes, and the sizes that a workspace depends on."""
+    torch, codes = _layers()[:2]
+    shape, dtype, i32 = k_cache.shape, k_cache.dtype, torch.int32
+    if len(shape) != 4 or v_cache.shape != shape or dtype not in codes or v_cache.dtype != dtype:
+        raise ValueError("k_cache, v_cache: [n_pages, page_size, n_kv_heads, head_dim], both float32, bfloat16 or float16")
     ks, vs = k_cache.stride(), v_cache.stride()
-    _need(ks[3] == 1 and vs[3] == 1, "head_dim must be contiguous")
-    i32 = torch.int32
-    _need(pages.dtype == i32 and q_start.dtype == i32 and kv_len.dtype == i32, "pages, q_start, kv_len: int32")
-    n = kv_len.numel()
-    _need(pages.dim() == 2 and pages.shape[0] == n and q_start.numel() == n + 1, "pages [n_seqs, max_pages], q_start [n_seqs + 1], kv_len [n_seqs]")
-    _need(q_start.is_contiguous() and kv_len.is_contiguous() and (pages.shape[1] < 2 or pages.stride(1) == 1), "contiguous index arrays")
-    shape = k_cache.shape
-    c = PagedCache(k_cache.data_ptr(), v_cache.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], shape[0], shape[1], shape[2], shape[3], _dtype_code(k_cache))
-    b = PagedBatch(q_start.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), pages.stride(0), pages.shape[1], n, n_tokens)
-    return c, b
+    if ks[3] != 1 or vs[3] != 1:
+        raise ValueError("k_cache, v_cache: head_dim must be contiguous")
+    if pages.dtype != i32 or q_start.dtype != i32 or kv_len.dtype != i32:
+        raise ValueError("pages, q_start, kv_len: int32")
+    n, table = kv_len.numel(), pages.shape
+    if len(table) != 2 or table[0] != n or q_start.numel() != n + 1:
+        raise ValueError("pages [n_seqs, max_pages], q_start [n_seqs + 1], kv_len [n_seqs]")
+    if not (q_start.is_contiguous() and kv_len.is_contiguous()) or (table[1] > 1 and pages.stride(1) != 1):
+        raise ValueError("q_start, kv_len and the rows of pages must be contiguous")
+    pages_, size, kv_heads, head_dim = shape
+    code = codes[dtype]
+    return (_PACK_CACHE(k_cache.data_ptr(), v_cache.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], pages_, size, kv_heads, head_dim, code),
+            _PACK_BATCH(q_start.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), pages.stride(0), table[1], n, n_tokens),
+            (pages_, size, kv_heads, head_dim, code, table[1], n, n_tokens))
 
 
-def _rows(t, like, what, n_tokens, heads=None) -> Rows:
-    _need(t.dim() == 3 and t.shape[0] == n_tokens and t.shape[2] == like.shape[3] and t.dtype == like.dtype and (heads is None or t.shape[1] == heads),
-          f"{what}: [n_tokens, heads, head_dim] of the cache's type")
-    s = t.stride()
-    _need(s[2] == 1, f"{what}: head_dim must be contiguous")
-    return Rows(t.data_ptr(), s[0], s[1])
+def _rows(t, like, what, n_tokens, heads=None):
+    shape, s = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != n_tokens or shape[2] != like.shape[3] or t.dtype != like.dtype or (heads is not None and shape[1] != heads):
+        raise ValueError(what + ": [n_tokens, heads, head_dim] of the cache's type")
+    if s[2] != 1:
+        raise ValueError(what + ": head_dim must be contiguous")
+    return _PACK_ROWS(t.data_ptr(), s[0], s[1])
 
 
 def ppd_paged_append(k_cache, v_cache, pages, q_start, kv_len, q, k, v, q_gain=None, k_gain=None, norm_eps=1e-5, rotary_dim=0,
@@ -249,58 +276,73 @@ def ppd_paged_append(k_cache, v_cache, pages, q_start, kv_len, q, k, v, q_gain=N
     """Queries and keys of a ragged batch normalised per head (where a gain is given) and rotated, keys and values written to their
     pages.  q [n_tokens, n_heads, head_dim] (None: keys and values only), k and v [n_tokens, n_kv_heads, head_dim].  Returns q_out
     (made here if not given, without contents where a row belongs to no sequence; may be q itself).  Asynchronous."""
-    import torch
-    lib = load_library()
+    torch, _, device, raw_stream, append, _, _ = _layers()
+    dev = k_cache.get_device()
+    if stream is not None or dev < 0 or dev != device():
+        return _on_device(k_cache, (v_cache, pages, q_start, kv_len, q, k, v, q_gain, k_gain, q_out), stream, lambda: ppd_paged_append(
+            k_cache, v_cache, pages, q_start, kv_len, q, k, v, q_gain, k_gain, norm_eps, rotary_dim, rope_theta, q_out))
+    _same_gpu(dev, v_cache, pages, q_start, kv_len, q, k, v, q_gain, k_gain, q_out)
+    n = k.shape[0]
+    cache, batch, sizes = _paged_args(k_cache, v_cache, pages, q_start, kv_len, n)
+    kr, vr = _rows(k, k_cache, "k", n, sizes[2]), _rows(v, k_cache, "v", n, sizes[2])
+    qr, outr, heads = None, None, 0
+    if q is not None:
+        qr, heads = _rows(q, k_cache, "q", n), q.shape[1]
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        outr = _rows(q_out, k_cache, "q_out", n, heads)
+    for g in (q_gain, k_gain):
+        if g is not None and (g.dtype != k_cache.dtype or g.numel() != sizes[3] or not g.is_contiguous()):
+            raise ValueError("gains: [head_dim] of the cache's type")
+    rc = append(cache, batch, heads, qr, outr, kr, vr, None if q_gain is None else q_gain.data_ptr(), None if k_gain is None else k_gain.data_ptr(),
+                norm_eps, rotary_dim, rope_theta, raw_stream(dev))
+    if rc != 0:
+        raise PPDError(rc, "ppd_paged_append", load_library().ppd_last_hip_error(None))
+    return q_out if q is not None else None
 
-    def call(st):
-        n = k.shape[0]
-        c, b = _paged_args(k_cache, v_cache, pages, q_start, kv_len, n)
-        kr, vr = _rows(k, k_cache, "k", n, c.n_kv_heads), _rows(v, k_cache, "v", n, c.n_kv_heads)
-        out, qr, outr, heads = q_out, None, None, 0
-        if q is not None:
-            qr, heads = _rows(q, k_cache, "q", n), q.shape[1]
-            if out is None:
-                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            outr = _rows(out, k_cache, "q_out", n, heads)
-        for g in (q_gain, k_gain):
-            _need(g is None or (g.dtype == k_cache.dtype and g.numel() == c.head_dim and g.is_contiguous()), "gains: [head_dim] of the cache's type")
-        rc = lib.ppd_paged_append(c, b, heads, qr, outr, kr, vr, None if q_gain is None else q_gain.data_ptr(),
-                                  None if k_gain is None else k_gain.data_ptr(), norm_eps, rotary_dim, rope_theta, st)
-        if rc != 0:
-            raise PPDError(rc, "ppd_paged_append", lib.ppd_last_hip_error(None))
-        return out
 
-    return _on_device(k_cache, (v_cache, pages, q_start, kv_len, q, k, v, q_gain, k_gain, q_out), stream, call)
+@functools.lru_cache(maxsize=4096)
+def _attention_workspace(sizes, heads):
+    """Bytes that ppd_paged_attention_workspace gives for these sizes (0 where it refuses: the call itself will)."""
+    pages, size, kv_heads, head_dim, code, max_pages, seqs, tokens = sizes
+    c = PagedCache(4096, 4096, 0, 0, 0, 0, 0, 0, pages, size, kv_heads, head_dim, code)
+    b = PagedBatch(4096, 4096, 4096, max_pages, max_pages, seqs, tokens)
+    need = ctypes.c_uint64()
+    return need.value if load_library().ppd_paged_attention_workspace(c, b, heads, need) == 0 else 0
 
 
 def ppd_paged_attention(q, k_cache, v_cache, pages, q_start, kv_len, scale=None, window=0, out=None, want_lse=False, workspace=None, stream=None):
     """Attention of a ragged batch's new tokens over their sequences' pages: (out [n_tokens, n_heads, head_dim], lse float32
     [n_tokens, n_heads] or None).  scale None: 1 / sqrt(head_dim).  out, and workspace (a uint8 tensor), are made here if not given; rows
     of no sequence keep what out holds (a new one holds nothing there).  Asynchronous."""
-    import torch
-    lib = load_library()
+    torch, _, device, raw_stream, _, attention, _ = _layers()
+    dev = k_cache.get_device()
+    if stream is not None or dev < 0 or dev != device():
+        return _on_device(k_cache, (q, v_cache, pages, q_start, kv_len, out, workspace), stream, lambda: ppd_paged_attention(
+            q, k_cache, v_cache, pages, q_start, kv_len, scale, window, out, want_lse, workspace))
+    _same_gpu(dev, q, v_cache, pages, q_start, kv_len, out, workspace)
+    n = q.shape[0]
+    cache, batch, sizes = _paged_args(k_cache, v_cache, pages, q_start, kv_len, n)
+    qr, heads = _rows(q, k_cache, "q", n), q.shape[1]
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    outr = _rows(out, k_cache, "out", n, heads)
+    lse = torch.empty((n, heads), dtype=torch.float32, device=q.device) if want_lse else None
+    if workspace is None:
+        need = _attention_workspace(sizes, heads)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    rc = attention(cache, batch, heads, qr, outr, None if lse is None else lse.data_ptr(), sizes[3] ** -0.5 if scale is None else scale, window,
+                   None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, raw_stream(dev))
+    if rc != 0:
+        raise PPDError(rc, "ppd_paged_attention", load_library().ppd_last_hip_error(None))
+    return out, lse
 
-    def call(st):
-        n = q.shape[0]
-        c, b = _paged_args(k_cache, v_cache, pages, q_start, kv_len, n)
-        qr, heads = _rows(q, k_cache, "q", n), q.shape[1]
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-        outr = _rows(o, k_cache, "out", n, heads)
-        lse = torch.empty((n, heads), dtype=torch.float32, device=q.device) if want_lse else None
-        need = ctypes.c_uint64()
-        rc = lib.ppd_paged_attention_workspace(c, b, heads, need)
-        w = workspace
-        if rc == 0 and w is None and need.value:
-            w = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-        if rc == 0:
-            rc = lib.ppd_paged_attention(c, b, heads, qr, outr, None if lse is None else lse.data_ptr(),
-                                         c.head_dim ** -0.5 if scale is None else scale, window, None if w is None else w.data_ptr(),
-                                         0 if w is None else w.numel() * w.element_size(), st)
-        if rc != 0:
-            raise PPDError(rc, "ppd_paged_attention", lib.ppd_last_hip_error(None))
-        return o, lse
 
-    return _on_device(q, (k_cache, v_cache, pages, q_start, kv_len, out, workspace), stream, call)
+@functools.lru_cache(maxsize=4096)
+def _verify_workspace(seqs, rows, vocab, code):
+    need = ctypes.c_uint64()
+    return need.value if load_library().ppd_verify_drafts_workspace(seqs, rows, vocab, code, need) == 0 else 0
 
 
 def ppd_verify_drafts(target_logits, ids, row_start, uniform, draft_logits=None, temperature=None, tokens=None, accepted=None, workspace=None,
@@ -308,39 +350,44 @@ def ppd_verify_drafts(target_logits, ids, row_start, uniform, draft_logits=None,
     """Drafted tokens against the target model's logits: (tokens int32 [n_rows], accepted int32 [n_seqs]).  target_logits and
     draft_logits [n_rows, vocab], ids int32 [n_rows], row_start int32 [n_seqs + 1], uniform float32 [n_rows, 2], temperature float32
     [n_seqs] (0: arg max).  tokens, accepted and workspace (a uint8 tensor) are made here if not given.  Asynchronous."""
-    import torch
-    lib = load_library()
-
-    def call(st):
-        i32, f32 = torch.int32, torch.float32
-        z, d = target_logits, draft_logits
-        _need(z.dim() == 2 and (z.shape[1] < 2 or z.stride(1) == 1), "target_logits: [n_rows, vocab], vocab contiguous")
-        n, vocab = z.shape
-        _need(d is None or (d.shape == z.shape and d.dtype == z.dtype and (vocab < 2 or d.stride(1) == 1)), "draft_logits: as target_logits")
-        seqs = row_start.numel() - 1
-        _need(ids.dtype == i32 and ids.numel() == n and row_start.dtype == i32 and seqs >= 1, "ids int32 [n_rows], row_start int32 [n_seqs + 1]")
-        _need(uniform.dtype == f32 and uniform.numel() == 2 * n, "uniform: float32 [n_rows, 2]")
-        _need(temperature is None or (temperature.dtype == f32 and temperature.numel() == seqs), "temperature: float32 [n_seqs]")
-        t = torch.empty(n, dtype=i32, device=z.device) if tokens is None else tokens
-        a = torch.empty(seqs, dtype=i32, device=z.device) if accepted is None else accepted
-        _need(t.dtype == i32 and t.numel() == n and a.dtype == i32 and a.numel() == seqs, "tokens int32 [n_rows], accepted int32 [n_seqs]")
-        _need(all(x is None or x.is_contiguous() for x in (ids, row_start, uniform, temperature, t, a)), "contiguous arrays")
-        need = ctypes.c_uint64()
-        code = _dtype_code(z)
-        rc = lib.ppd_verify_drafts_workspace(seqs, n, vocab, code, need)
-        w = workspace
-        if rc == 0 and w is None and need.value:
-            w = torch.empty(need.value, dtype=torch.uint8, device=z.device)
-        if rc == 0:
-            rc = lib.ppd_verify_drafts(seqs, n, vocab, code, row_start.data_ptr(), ids.data_ptr(), z.data_ptr(), z.stride(0) if n > 1 else vocab,
-                                       None if d is None else d.data_ptr(), 0 if d is None else d.stride(0) if n > 1 else vocab,
-                                       None if temperature is None else temperature.data_ptr(), uniform.data_ptr(), t.data_ptr(), a.data_ptr(),
-                                       None if w is None else w.data_ptr(), 0 if w is None else w.numel() * w.element_size(), st)
-        if rc != 0:
-            raise PPDError(rc, "ppd_verify_drafts", lib.ppd_last_hip_error(None))
-        return t, a
-
-    return _on_device(target_logits, (ids, row_start, uniform, draft_logits, temperature, tokens, accepted, workspace), stream, call)
+    torch, codes, device, raw_stream, _, _, verify = _layers()
+    z, d = target_logits, draft_logits
+    dev = z.get_device()
+    if stream is not None or dev < 0 or dev != device():
+        return _on_device(z, (ids, row_start, uniform, d, temperature, tokens, accepted, workspace), stream, lambda: ppd_verify_drafts(
+            z, ids, row_start, uniform, d, temperature, tokens, accepted, workspace))
+    _same_gpu(dev, ids, row_start, uniform, d, temperature, tokens, accepted, workspace)
+    i32, f32 = torch.int32, torch.float32
+    if z.dim() != 2 or z.dtype not in codes or (z.shape[1] > 1 and z.stride(1) != 1):
+        raise ValueError("target_logits: [n_rows, vocab], vocab contiguous, float32, bfloat16 or float16")
+    n, vocab = z.shape
+    if d is not None and (d.shape != z.shape or d.dtype != z.dtype or (vocab > 1 and d.stride(1) != 1)):
+        raise ValueError("draft_logits: as target_logits")
+    seqs = row_start.numel() - 1
+    if ids.dtype != i32 or ids.numel() != n or row_start.dtype != i32 or seqs < 1:
+        raise ValueError("ids int32 [n_rows], row_start int32 [n_seqs + 1]")
+    if uniform.dtype != f32 or uniform.numel() != 2 * n or (temperature is not None and (temperature.dtype != f32 or temperature.numel() != seqs)):
+        raise ValueError("uniform float32 [n_rows, 2], temperature float32 [n_seqs]")
+    if tokens is None:
+        tokens = torch.empty(n, dtype=i32, device=z.device)
+    if accepted is None:
+        accepted = torch.empty(seqs, dtype=i32, device=z.device)
+    if tokens.dtype != i32 or tokens.numel() != n or accepted.dtype != i32 or accepted.numel() != seqs:
+        raise ValueError("tokens int32 [n_rows], accepted int32 [n_seqs]")
+    if not all(x is None or x.is_contiguous() for x in (ids, row_start, uniform, temperature, tokens, accepted)):
+        raise ValueError("all but the logits must be contiguous")
+    code = codes[z.dtype]
+    if workspace is None:
+        need = _verify_workspace(seqs, n, vocab, code)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=z.device)
+    rc = verify(seqs, n, vocab, code, row_start.data_ptr(), ids.data_ptr(), z.data_ptr(), z.stride(0) if n > 1 else vocab,
+                None if d is None else d.data_ptr(), 0 if d is None else d.stride(0) if n > 1 else vocab,
+                None if temperature is None else temperature.data_ptr(), uniform.data_ptr(), tokens.data_ptr(), accepted.data_ptr(),
+                None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, raw_stream(dev))
+    if rc != 0:
+        raise PPDError(rc, "ppd_verify_drafts", load_library().ppd_last_hip_error(None))
+    return tokens, accepted
 
 
 class PPD:

@@ -320,7 +320,9 @@ def test_a_workspace_of_the_callers():
     import ctypes
     b = Batch([1, 2], [3000, 90], 4, 2, 128, BF16).cuda()
     ref, _ = call(b)
-    c, bb = binding._paged_args(b.k_cache, b.v_cache, b.pages, b.q_start, b.kv_len, b.n)
+    k = b.k_cache
+    c = binding.PagedCache(k.data_ptr(), b.v_cache.data_ptr(), *k.stride()[:3], *k.stride()[:3], *k.shape, 1)
+    bb = binding.PagedBatch(b.q_start.data_ptr(), b.kv_len.data_ptr(), b.pages.data_ptr(), b.pages.stride(0), b.pages.shape[1], 2, b.n)
     need = ctypes.c_uint64()
     assert binding.load_library().ppd_paged_attention_workspace(c, bb, 4, need) == 0
     if need.value:

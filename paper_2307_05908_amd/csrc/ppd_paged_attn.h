@@ -25,7 +25,8 @@ struct PagedAttnArgs {
   float to_log2;                      // scale * log2(e): a score's exponent of two
   int want, least;                    // parts per key/value head to aim at; blocks of a part at least (0: one part each)
   float* part_o; float2* part_ml;     // [item][kv_heads][rows of a tile][head_dim], [item][kv_heads][rows of a tile]
-  int2* plan;                         // [n_seqs]: first item of a sequence, parts of its tiles
+  uint64_t* stamps; uint64_t stamp;   // paged_split_kernel, [item][kv_heads]: this call's number, once the part is there (see join_parts)
+  int2* plan;                         // paged_tile_kernel, [n_seqs]: first item of a sequence, parts of its tiles
 };
 
 // ---- element types as matrix operands
@@ -78,7 +79,7 @@ __device__ __forceinline__ void seq_plan(const PagedAttnArgs& a, int s, SeqPlan&
   if (s >= a.b.n_seqs) return;
   p.r = seq_rows(a.b, s);
   if (p.r.rows == 0) return;
-  p.tiles = (int)(((int64_t)p.r.rows * a.group + a.tile_rows - 1) / a.tile_rows);
+  p.tiles = (p.r.rows * a.group + a.tile_rows - 1) / a.tile_rows;              // (2^26 rows at most)
   const int hi = min(p.r.pos0 + p.r.rows, a.b.room), lo = a.window > 0 ? max(p.r.pos0 - a.window + 1, 0) & -PLAN_BLOCK : 0;
   p.blocks = max(1, (hi - lo + PLAN_BLOCK - 1) / PLAN_BLOCK);
 }
@@ -101,33 +102,37 @@ __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, bool 
     }
     len = max(a.least, (int)ceilf(all / (float)a.want));
   }
+  // Tiles of several parts come first, the others fill up behind them.
+  auto items_of = [&](const SeqPlan& q, bool several) { return (q.parts > 1) == several ? q.tiles * q.parts : 0; };
+  auto parts_of = [&](const SeqPlan& q) { return a.least > 0 ? (q.blocks + len - 1) / len : q.blocks > 0 ? 1 : 0; };
   int before = 0;
   bool found = false;
-  for (int s = 0; s < a.b.n_seqs; s += WAVE) {
-    if (a.b.n_seqs > WAVE || a.least == 0) seq_plan(a, s + lane, p);
-    p.parts = a.least > 0 ? (p.blocks + len - 1) / len : p.blocks > 0;
-    const int items = p.tiles * p.parts, upto = before + scan_up(items, lane);
-    if (tell && s + lane < a.b.n_seqs) a.plan[s + lane] = make_int2(upto - items, p.parts);
-    const unsigned long long past = __ballot(upto > idx);
-    if (!found && past) {
-      const int w = __builtin_ctzll(past);
-      const int r = idx - __builtin_amdgcn_readlane(upto - items, w);
-      it.s = s + w;
-      it.parts = __builtin_amdgcn_readlane(p.parts, w);
-      it.rows0 = __builtin_amdgcn_readlane(p.r.row0, w);
-      it.n = __builtin_amdgcn_readlane(p.r.rows, w);
-      it.pos0 = __builtin_amdgcn_readlane(p.r.pos0, w);
-      it.tile = r / it.parts;
-      it.part = r % it.parts;
-      if (a.last_first) it.tile = __builtin_amdgcn_readlane(p.tiles, w) - 1 - it.tile;
-      it.slot = idx - r + it.tile * it.parts + it.part;
-      found = true;
-      if (!tell) break;
+  for (int turn = a.least > 0 ? 0 : 1; turn < 2 && (tell || !found); ++turn)
+    for (int s = 0; s < a.b.n_seqs; s += WAVE) {
+      if (a.b.n_seqs > WAVE || a.least == 0) seq_plan(a, s + lane, p);
+      p.parts = parts_of(p);
+      const int items = items_of(p, turn == 0), upto = before + scan_up(items, lane);
+      if (tell && s + lane < a.b.n_seqs && items > 0) a.plan[s + lane] = make_int2(upto - items, p.parts);
+      const unsigned long long past = __ballot(upto > idx);
+      if (!found && past) {
+        const int w = __builtin_ctzll(past);
+        const int r = idx - __builtin_amdgcn_readlane(upto - items, w);
+        it.s = s + w;
+        it.parts = __builtin_amdgcn_readlane(p.parts, w);
+        it.rows0 = __builtin_amdgcn_readlane(p.r.row0, w);
+        it.n = __builtin_amdgcn_readlane(p.r.rows, w);
+        it.pos0 = __builtin_amdgcn_readlane(p.r.pos0, w);
+        it.tile = r / it.parts;
+        it.part = r % it.parts;
+        if (a.last_first) it.tile = __builtin_amdgcn_readlane(p.tiles, w) - 1 - it.tile;
+        it.slot = idx - r + it.tile * it.parts + it.part;
+        found = true;
+        if (!tell) break;
+      }
+      before = __builtin_amdgcn_readlane(upto, 63);
     }
-    before = __builtin_amdgcn_readlane(upto, 63);
-  }
   if (!found) return false;
-  const int first = (int)((int64_t)it.tile * a.tile_rows / a.group), last = min((int)(((int64_t)it.tile * a.tile_rows + a.tile_rows - 1) / a.group), it.n - 1);
+  const int first = it.tile * a.tile_rows / a.group, last = min((it.tile * a.tile_rows + a.tile_rows - 1) / a.group, it.n - 1);
   const int hi = min(it.pos0 + last + 1, a.b.room), lo = a.window > 0 ? max(it.pos0 + first - a.window + 1, 0) & -PLAN_BLOCK : 0;
   const int blocks = (max(hi - lo, 0) + PLAN_BLOCK - 1) / PLAN_BLOCK, per = (blocks + it.parts - 1) / it.parts;
   it.lo = lo + min(it.part * per, blocks) * PLAN_BLOCK;
@@ -135,6 +140,8 @@ __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, bool 
   return true;
 }
 
+// Whether 16 positions in a row that begin at a multiple of 16 lie in one page, within 2^31 bytes
+inline bool near_pages(const PagedAttnArgs& a) { return a.b.page_size % 16 == 0 && a.kc_pos < 1 << 25 && a.vc_pos < 1 << 25; }
 hipError_t launch_paged_tiles(const PagedAttnArgs& a, int dtype, int head_dim, int items, hipStream_t stream);
 
 }  // namespace ppd

@@ -1,19 +1,86 @@
-// ppd_paged_attention: attention of ragged runs of new tokens over paged keys and values.  Few rows over many positions, the join of parts,
+// ppd_paged_attention: attention of ragged runs of new tokens over paged keys and values.  Few rows over many positions,
 // and the host's side; many rows: ppd_paged_tiles.hip.
 #include "ppd_paged_attn.h"
 
 #include <math.h>
 
+#include <atomic>
+
 using namespace ppd;
 
 namespace {
 
-constexpr int SPLIT_WAVES = 4;
+constexpr int SPLIT_WAVES = 4, SPLIT_THREADS = SPLIT_WAVES * WAVE;
+
+// A part's results: sums of a row's components, and its maximum and total, past the L2, for whoever joins them.
+__device__ __forceinline__ void leave(float* to, f32x4 v) {
+  typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+  const u64x2 u = __builtin_bit_cast(u64x2, v);
+  __hip_atomic_store((uint64_t*)to, u.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store((uint64_t*)to + 1, u.y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void leave(float2* to, float m, float l) {
+  const f32x2 v = {m, l};
+  __hip_atomic_store((uint64_t*)to, __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2 left(const void* from) {
+  return __builtin_bit_cast(f32x2, __hip_atomic_load((const uint64_t*)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+// The end of a workgroup that had one of several parts (all of its threads, its results left): it puts the call's number beside them and
+// looks at the other parts' places; who finds the number everywhere joins them, in their order, and clears the places.  Nobody waits.
+// The number goes out, past the L2, before the others are looked at, so the last one to leave it finds all; two may, and write the
+// same bits.  Scratch memory needs nothing in it beforehand (numbers are 64 bits wide and never come twice, but for a replayed
+// launch's, and that one's own places are clear again by then).
+template <typename T, int HD>
+__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const Item& it, int kvh, int tid, int* s_flag) {
+  const int lane = tid & 63;
+  const int first = it.slot - it.part;                    // (the parts' places lie side by side)
+  uint64_t* const stamps = a.stamps + (int64_t)first * a.kv_heads + kvh;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid < WAVE) {
+    if (lane == 0) __hip_atomic_store(stamps + (int64_t)it.part * a.kv_heads, a.stamp, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    bool missing = false;
+    for (int p = lane; p < it.parts; p += WAVE) missing |= __hip_atomic_load(stamps + (int64_t)p * a.kv_heads, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != a.stamp;
+    missing = __ballot(missing) != 0;
+    if (lane == 0) *s_flag = !missing;
+  }
+  __syncthreads();
+  if (!*s_flag) return;
+  const int rows = min(SPLIT_ROWS, it.n * a.group - it.tile * SPLIT_ROWS);
+  for (int x = tid; x < rows * (HD / 4); x += SPLIT_THREADS) {
+    const int rr = x / (HD / 4), d = x % (HD / 4) * 4, ri = it.tile * SPLIT_ROWS + rr;
+    auto at = [&](int p) { return ((int64_t)p * a.kv_heads + kvh) * SPLIT_ROWS + rr; };
+    float mx = -INFINITY, sum = 0.f;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int p = 0; p < it.parts; ++p) mx = fmaxf(mx, left(a.part_ml + at(p)).x);
+    const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll 4
+    for (int p = 0; p < it.parts; ++p) {
+      const float* const po = a.part_o + at(p) * HD + d;
+      const f32x2 one = left(a.part_ml + at(p)), u = left(po), w = left(po + 2);
+      const float f = __builtin_amdgcn_exp2f(one.x - ref);
+      sum = fmaf(f, one.y, sum);
+      y.x = fmaf(f, u.x, y.x); y.y = fmaf(f, u.y, y.y); y.z = fmaf(f, w.x, y.z); y.w = fmaf(f, w.y, y.w);
+    }
+    const bool none = mx == -INFINITY && sum == 0.f;      // nothing seen (a score that is no number leaves its mark on the sum)
+    const float inv = 1.0f / sum;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : y[e] * inv;
+    const int t = ri / a.group, h = kvh * a.group + ri % a.group;
+    *(typename Quad<T>::raw*)((T*)a.out + (int64_t)(it.rows0 + t) * a.o_tok + (int64_t)h * a.o_head + d) = quad_out<T>(y);
+    if (a.lse && d == 0) a.lse[(int64_t)(it.rows0 + t) * a.heads + h] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718f;
+  }
+  for (int p = tid; p < it.parts; p += SPLIT_THREADS) __hip_atomic_store(stamps + (int64_t)p * a.kv_heads, (uint64_t)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 
 // ---- few rows, many positions: bound by the stream of keys and values
 // A wave has every fourth step of BP positions of its part to itself: keys straight into registers as the left operand, values through
 // registers into LDS rows of its own, from where the transposing reads (fp32: plain ones) make them the left operand of the second product.
-// The next step's are requested before this one's arithmetic; nothing waits at a barrier until the four waves' results are joined.
+// The next step's are under way, in registers of their own, while one is worked on; nothing waits at a barrier until the waves' results are
+// joined.
 template <typename T, int HD>
 struct Split {
   static constexpr int SZ = sizeof(T) == 4 ? 4 : 2, BP = SZ == 4 ? 16 : 32, NT = BP / 16;
@@ -25,14 +92,17 @@ struct Split {
   static constexpr int LDS = SPLIT_WAVES * (WAVE_LDS > OUT_LDS ? WAVE_LDS : OUT_LDS);
 };
 
-template <typename T, int HD>
-__global__ __launch_bounds__(256, 2) void paged_split_kernel(PagedAttnArgs a) {
+// NEAR: 16 positions in a row that begin at a multiple of 16 lie in one page, within 2^31 bytes: addresses are the page's, one for the wave,
+// and 32-bit offsets.
+template <typename T, int HD, bool NEAR>
+__global__ __launch_bounds__(SPLIT_THREADS, 2) void paged_split_kernel(PagedAttnArgs a) {
   using C = Split<T, HD>;
   __shared__ __align__(16) char lds[C::LDS];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = blockIdx.y, row = lane & 15, quad = lane >> 4;
+  __shared__ int s_flag;
+  // the heads of one part side by side: a position's keys are one run of memory, and its pieces then come at the same time
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kvh = blockIdx.x % a.kv_heads, row = lane & 15, quad = lane >> 4;
   Item it;
-  if (!find_item(a, blockIdx.x, blockIdx.x == 0 && kvh == 0 && wave == 0 && a.least > 0, lane, it)) return;
+  if (!find_item(a, blockIdx.x / a.kv_heads, false, lane, it)) return;
   const int all_rows = it.n * a.group;
   const int r = it.tile * SPLIT_ROWS + row, rc = min(r, all_rows - 1), tok = rc / a.group, head = kvh * a.group + rc % a.group;
   const int pos = r < all_rows ? it.pos0 + tok : -1;                          // what the lane's row sees ends there
@@ -52,42 +122,61 @@ __global__ __launch_bounds__(256, 2) void paged_split_kernel(PagedAttnArgs a) {
   }
   const float to_log2 = C::SZ == 4 ? 1.0f : a.to_log2;
   char* const mine = lds + wave * C::WAVE_LDS;
-  const char* const kbase = (const char*)a.kc + (int64_t)kvh * a.kc_head * C::SZ + quad * 16;
-  const char* const vbase = (const char*)a.vc + (int64_t)kvh * a.vc_head * C::SZ + (lane % C::LPR) * 16;
+  const char* const kbase = (const char*)a.kc + (int64_t)kvh * a.kc_head * C::SZ;
+  const char* const vbase = (const char*)a.vc + (int64_t)kvh * a.vc_head * C::SZ;
   const int steps = (it.hi - it.lo + C::BP - 1) / C::BP;
-  // the page (or -1) and slot of position lo + step * BP + (lane % BP)
-  auto place = [&](int step, int& page, int& slot) {
-    const int p = it.lo + step * C::BP + (lane & (C::BP - 1));
-    page = step < steps && p < it.hi ? page_of(a.b, it.s, p) : -1;
-    slot = (int)((unsigned)p % (unsigned)a.b.page_size);
+  // The table's entry for, and the slot of, position lo + step * BP + (lane % BP): asked for here, looked at when the step is requested, a
+  // whole step later (looked at here it would wait for the keys and values that are under way).
+  const int32_t* const table = a.b.pages + (int64_t)it.s * a.b.pages_stride;
+  int entry, slot;
+  auto place = [&](int step) {
+    const int p = it.lo + step * C::BP + (lane & (C::BP - 1)), i = (int)((unsigned)p / (unsigned)a.b.page_size);
+    slot = p - i * a.b.page_size;
+    entry = table[min(i, a.b.max_pages - 1)];
   };
-  u32x4 k[C::NT][C::NK], v[C::NV];
-  uint32_t there = 0;                                     // a bit for each of the step's positions that has a page
-  auto request = [&](int page, int slot) {
-    there = (uint32_t)__ballot(page >= 0) & (uint32_t)((1ull << C::BP) - 1);
-    const int pg = max(page, 0), sl = page >= 0 ? slot : 0;      // what has no page is read from where there is something, and not used
-    const int64_t ko = ((int64_t)pg * a.kc_page + (int64_t)sl * a.kc_pos) * C::SZ, vo = ((int64_t)pg * a.vc_page + (int64_t)sl * a.vc_pos) * C::SZ;
+  u32x4 k[2][C::NT][C::NK], v[2][C::NV];
+  uint32_t there[2];                                      // a bit for each of a step's positions that has a page
+  const int vrow = lane / C::LPR, vpiece = lane % C::LPR * 16;
+  auto request = [&](int step, auto set) {
+    constexpr int S = decltype(set)::value;
+    const int page = it.lo + step * C::BP + (lane & (C::BP - 1)) < it.hi && (unsigned)entry < (unsigned)a.b.n_pages ? entry : -1;      // (hi is within the table)
+    there[S] = (uint32_t)__ballot(page >= 0) & (uint32_t)((1ull << C::BP) - 1);
+    // what has no page is read from where there is something, and not used
+    if constexpr (NEAR) {
 #pragma unroll
-    for (int t = 0; t < C::NT; ++t) {
-      const char* p = kbase + __shfl(ko, 16 * t + row, WAVE);
+      for (int t = 0; t < C::NT; ++t) {
+        const int pg = __builtin_amdgcn_readlane(page, 16 * t), sl = pg >= 0 ? __builtin_amdgcn_readlane(slot, 16 * t) : 0;
+        const char* const kp = kbase + ((int64_t)max(pg, 0) * a.kc_page + (int64_t)sl * a.kc_pos) * C::SZ;
+        const char* const vp = vbase + ((int64_t)max(pg, 0) * a.vc_page + (int64_t)sl * a.vc_pos) * C::SZ;
+        const unsigned ko = (unsigned)(row * (int)a.kc_pos * C::SZ + quad * 16);
 #pragma unroll
-      for (int i = 0; i < C::NK; ++i) k[t][i] = *(const u32x4*)(p + i * 64);
+        for (int i = 0; i < C::NK; ++i) k[S][t][i] = *(const u32x4*)(kp + ko + i * 64);
+        const unsigned vo = (unsigned)(vrow * (int)a.vc_pos * C::SZ + vpiece);
+#pragma unroll
+        for (int i = 0; i < C::NV / C::NT; ++i) v[S][t * (C::NV / C::NT) + i] = *(const u32x4*)(vp + (int64_t)i * C::RPI * a.vc_pos * C::SZ + vo);
+      }
+    } else {
+      const int pg = max(page, 0), sl = page >= 0 ? slot : 0;
+      const int64_t ko = ((int64_t)pg * a.kc_page + (int64_t)sl * a.kc_pos) * C::SZ, vo = ((int64_t)pg * a.vc_page + (int64_t)sl * a.vc_pos) * C::SZ;
+#pragma unroll
+      for (int t = 0; t < C::NT; ++t) {
+        const char* const p = kbase + quad * 16 + __shfl(ko, 16 * t + row, WAVE);
+#pragma unroll
+        for (int i = 0; i < C::NK; ++i) k[S][t][i] = *(const u32x4*)(p + i * 64);
+      }
+#pragma unroll
+      for (int i = 0; i < C::NV; ++i) v[S][i] = *(const u32x4*)(vbase + vpiece + __shfl(vo, i * C::RPI + vrow, WAVE));
     }
-#pragma unroll
-    for (int i = 0; i < C::NV; ++i) v[i] = *(const u32x4*)(vbase + __shfl(vo, i * C::RPI + lane / C::LPR, WAVE));
   };
   f32x4 o[HD / 16];
-#pragma unroll
-  for (int i = 0; i < HD / 16; ++i) o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;                           // the row's maximum (of scores times to_log2; the same in its four lanes) and the lane's part of the sum
-  int page, slot;
-  int step = wave;
-  place(step, page, slot);
-  if (step < steps) request(page, slot);
-  place(step + SPLIT_WAVES, page, slot);
-  for (; step < steps; step += SPLIT_WAVES) {
+  float m, l;                                             // the row's maximum (of scores times to_log2; the same in its four lanes) and the lane's part of the sum
+  // One step.  CAREFUL: with values that are infinite, or no numbers, among it (the first way through gives such a row no number where it
+  // should have one: 0 times infinity where the row does not see it, or for the second term of a weight).
+  auto work = [&](int step, auto set, auto careful) {
+    constexpr int S = decltype(set)::value;
+    constexpr bool CAREFUL = decltype(careful)::value;
     const int base = it.lo + step * C::BP;
-    const uint32_t have = there;
+    const uint32_t have = there[S];
     const bool whole = have == (uint32_t)((1ull << C::BP) - 1) && base + C::BP - 1 <= all_see_to && base >= all_see_from;
     f32x4 s[C::NT];
 #pragma unroll
@@ -95,33 +184,33 @@ __global__ __launch_bounds__(256, 2) void paged_split_kernel(PagedAttnArgs a) {
       s[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < C::NK; ++i) {
-        if constexpr (C::SZ == 2) s[t] = mma16(k[t][i], q[i], s[t], T());
+        if constexpr (C::SZ == 2) s[t] = mma16(k[S][t][i], q[i], s[t], T());
         else
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[t][i][e]), __uint_as_float(q[i][e]), s[t], 0, 0, 0);
+          for (int e = 0; e < 4; ++e) s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[S][t][i][e]), __uint_as_float(q[i][e]), s[t], 0, 0, 0);
       }
     }
-    uint32_t most = 0;
-#pragma unroll
-    for (int i = 0; i < C::NV; ++i) {
-      const int at = i * C::RPI + lane / C::LPR;
-      u32x4 w = v[i];
-      if (!whole && !((have >> at) & 1)) w = (u32x4){0u, 0u, 0u, 0u};
-      most = largest(most, w, T());
-      *(u32x4*)(mine + at * C::STRIDE + (lane % C::LPR) * 16) = w;
-    }
-    if (step + SPLIT_WAVES < steps) request(page, slot);
-    place(step + 2 * SPLIT_WAVES, page, slot);
-    const bool odd = __ballot(endless(most, T())) != 0;
     if (!whole) {
+      asm volatile("");                                   // (a branch, not selections that every step goes through)
+#pragma unroll
+      for (int i = 0; i < C::NV; ++i) if (!((have >> (i * C::RPI + vrow)) & 1)) v[S][i] = (u32x4){0u, 0u, 0u, 0u};
+      const int to = pos - base - 4 * quad, since = from - base - 4 * quad;
+      const uint32_t mapped = have >> (4 * quad);
 #pragma unroll
       for (int t = 0; t < C::NT; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int at = 16 * t + 4 * quad + e, p = base + at;
-          if (!((have >> at) & 1) || p > pos || p < from) s[t][e] = -INFINITY;
+          const bool seen = ((mapped >> (16 * t + e) & 1) != 0) & (16 * t + e <= to) & (16 * t + e >= since);
+          s[t][e] = seen ? s[t][e] : -INFINITY;
         }
     }
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < C::NV; ++i) {
+      if (CAREFUL) most = largest(most, v[S][i], T());
+      *(u32x4*)(mine + (i * C::RPI + vrow) * C::STRIDE + vpiece) = v[S][i];
+    }
+    const bool odd = CAREFUL && __ballot(endless(most, T())) != 0;
     // running maximum: joined and sums rescaled only where it grows for some row
     float top = -INFINITY;
 #pragma unroll
@@ -144,7 +233,7 @@ __global__ __launch_bounds__(256, 2) void paged_split_kernel(PagedAttnArgs a) {
     if constexpr (C::SZ == 2) {
       // Weights in two terms of the type: the rounding of one alone is as large as the output's own.  Beside infinite values one: what is left
       // of a weight may be zero or negative, and so that no weight above zero becomes one, half floats go no lower than their smallest number.
-      if (sizeof(T) == 2 && std::is_same<T, f16_t>::value && odd)
+      if (CAREFUL && std::is_same<T, f16_t>::value && odd)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -164,9 +253,8 @@ __global__ __launch_bounds__(256, 2) void paged_split_kernel(PagedAttnArgs a) {
         const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(src + 16 * C::STRIDE + i * 32));
         const u32x2 xu = __builtin_bit_cast(u32x2, x), yu = __builtin_bit_cast(u32x2, y);
         const u32x4 vt = {xu.x, xu.y, yu.x, yu.y};
-        if (odd && whole) o[i] = mma16(vt, hi, o[i], T());
-        else if (odd) {
-          // a value that is no number, or infinite, among positions that not every row sees: position by position, kept where it is seen
+        if (CAREFUL && odd) {
+          // position by position, kept where it is seen
 #pragma unroll 1
           for (int p = 0; p < 32; ++p) {
             u32x4 only = {0u, 0u, 0u, 0u};
@@ -189,7 +277,7 @@ __global__ __launch_bounds__(256, 2) void paged_split_kernel(PagedAttnArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float x = *(const float*)(mine + (4 * quad + e) * C::STRIDE + (16 * i + row) * 4);
-          if (!whole && odd) {
+          if (CAREFUL && odd) {
             for (int c = 0; c < 4; ++c) {
               const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x4f32(c == quad ? x : 0.f, s[0][e], o[i], 0, 0, 0);
               const int p = 4 * c + e;
@@ -198,17 +286,48 @@ __global__ __launch_bounds__(256, 2) void paged_split_kernel(PagedAttnArgs a) {
           } else o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, s[0][e], o[i], 0, 0, 0);
         }
     }
+  };
+  auto begin = [&]() {
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY; l = 0.f;
+  };
+  const std::integral_constant<int, 0> even;
+  const std::integral_constant<int, 1> uneven;
+  begin();
+  place(wave);
+  if (wave < steps) request(wave, even);
+  place(wave + SPLIT_WAVES);
+  for (int step = wave; step < steps; step += 2 * SPLIT_WAVES) {
+    const int next = step + SPLIT_WAVES, after = next + SPLIT_WAVES;
+    if (next < steps) request(next, uneven);
+    place(after);
+    work(step, even, std::false_type());
+    if (next >= steps) break;
+    if (after < steps) request(after, even);
+    place(after + SPLIT_WAVES);
+    work(next, uneven, std::false_type());
+  }
+  {
+    float sum = l;                                        // (no number, if one is)
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) sum += (o[i].x - o[i].x) + (o[i].y - o[i].y) + (o[i].z - o[i].z) + (o[i].w - o[i].w);
+    if (__ballot(!(fabsf(sum) < INFINITY))) {
+      begin();
+#pragma unroll 1
+      for (int step = wave; step < steps; step += SPLIT_WAVES) { place(step); request(step, even); work(step, even, std::true_type()); }
+    }
   }
   l += __shfl_xor(l, 16, WAVE);
   l += __shfl_xor(l, 32, WAVE);
-  // ---- the four waves' results
+  // ---- the waves' results
   __syncthreads();
   float* const so = (float*)(lds + wave * C::OUT_LDS);
 #pragma unroll
   for (int i = 0; i < HD / 16; ++i) *(f32x4*)(so + row * (HD + 4) + 16 * i + 4 * quad) = o[i];
   if (quad == 0) ((float2*)(so + SPLIT_ROWS * (HD + 4)))[row] = make_float2(m, l);
   __syncthreads();
-  for (int x = threadIdx.x; x < SPLIT_ROWS * HD / 4; x += 256) {
+  for (int x = tid; x < SPLIT_ROWS * HD / 4; x += SPLIT_THREADS) {
     const int rr = x / (HD / 4), d = (x % (HD / 4)) * 4, ri = it.tile * SPLIT_ROWS + rr;
     if (ri >= all_rows) break;
     float2 ml[SPLIT_WAVES];
@@ -227,8 +346,8 @@ __global__ __launch_bounds__(256, 2) void paged_split_kernel(PagedAttnArgs a) {
     }
     if (it.parts > 1) {
       const int64_t at = ((int64_t)it.slot * a.kv_heads + kvh) * SPLIT_ROWS + rr;
-      *(f32x4*)(a.part_o + at * HD + d) = y;
-      if (d == 0) a.part_ml[at] = make_float2(mx, sum);
+      leave(a.part_o + at * HD + d, y);
+      if (d == 0) leave(a.part_ml + at, mx, sum);
     } else {
       const int t = ri / a.group, h = kvh * a.group + ri % a.group;
       const bool none = mx == -INFINITY && sum == 0.f;    // nothing seen (a score that is no number leaves its mark on the sum)
@@ -240,40 +359,7 @@ __global__ __launch_bounds__(256, 2) void paged_split_kernel(PagedAttnArgs a) {
       if (a.lse && d == 0) a.lse[(int64_t)(it.rows0 + t) * a.heads + h] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718f;
     }
   }
-}
-
-// The parts of a row joined, in their order: HD / 4 lanes for a row.
-template <typename T, int HD>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
-  constexpr int LPR = HD / 4, RPW = 256 / LPR;
-  const int row = blockIdx.x, lane = threadIdx.x & 63;
-  const int s = seq_of_row(a.b, row, lane);
-  if (s < 0) return;
-  const int2 plan = a.plan[s];
-  const int parts = plan.y, h = blockIdx.y * RPW + threadIdx.x / LPR, d = (threadIdx.x % LPR) * 4;
-  if (parts <= 1 || h >= a.heads) return;
-  const SeqRows sr = seq_rows(a.b, s);
-  const int kvh = h / a.group, r = (row - sr.row0) * a.group + h % a.group;
-  const int64_t first = (int64_t)plan.x + (int64_t)(r / a.tile_rows) * parts;
-  float mx = -INFINITY, sum = 0.f;
-  f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < parts; ++p) mx = fmaxf(mx, a.part_ml[((first + p) * a.kv_heads + kvh) * a.tile_rows + r % a.tile_rows].x);
-  const float ref = mx == -INFINITY ? 0.f : mx;
-  for (int p = 0; p < parts; ++p) {
-    const int64_t at = ((first + p) * a.kv_heads + kvh) * a.tile_rows + r % a.tile_rows;
-    const float2 ml = a.part_ml[at];
-    const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-    sum = fmaf(f, ml.y, sum);
-    const f32x4 z = *(const f32x4*)(a.part_o + at * HD + d);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = fmaf(f, z[e], y[e]);
-  }
-  const bool none = mx == -INFINITY && sum == 0.f;
-  const float inv = 1.0f / sum;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : y[e] * inv;
-  *(typename Quad<T>::raw*)((T*)a.out + (int64_t)row * a.o_tok + (int64_t)h * a.o_head + d) = quad_out<T>(y);
-  if (a.lse && d == 0) a.lse[(int64_t)row * a.heads + h] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718f;
+  if (it.parts > 1) join_parts<T, HD>(a, it, kvh, tid, &s_flag);
 }
 
 // ---- host
@@ -281,7 +367,7 @@ struct AttnPlan {
   bool tiles;               // paged_tile_kernel, not paged_split_kernel
   int want, least;          // see PagedAttnArgs
   int64_t items;            // workgroups per key/value head: parts aimed at, and a part's end for every tile
-  uint64_t o_bytes, ml_bytes, plan_bytes;
+  uint64_t o_bytes, ml_bytes, more_bytes;      // more: stamps, or the plan
 };
 
 int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, int n_heads, AttnPlan* p) {
@@ -292,31 +378,32 @@ int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, 
   const int group = n_heads / cache->n_kv_heads;
   const int64_t rows = (int64_t)batch->n_tokens * group, some = batch->n_tokens < batch->n_seqs ? batch->n_tokens : batch->n_seqs;
   p->tiles = cache->dtype != PPD_FP32 && rows > 32 * (int64_t)batch->n_seqs;
-  const int tile_rows = p->tiles ? TILE_ROWS : SPLIT_ROWS, slots = p->tiles ? 512 : 1024;
+  const int tile_rows = p->tiles ? TILE_ROWS : SPLIT_ROWS;
   const int64_t tiles = rows / tile_rows + some;
+  const int slots = p->tiles ? 512 : 256;
   p->want = (slots + cache->n_kv_heads - 1) / cache->n_kv_heads;
-  p->least = p->tiles ? 8 : 2;
+  p->least = p->tiles ? 8 : 4;
   // tiles enough for the whole chip, or no position to cut at: one part each
-  if (tiles >= 2 * p->want || (int64_t)batch->max_pages * cache->page_size <= p->least * PLAN_BLOCK) p->least = 0;
+  if (tiles >= (p->tiles ? 2 : 8) * p->want || (int64_t)batch->max_pages * cache->page_size <= p->least * PLAN_BLOCK) p->least = 0;
   p->items = tiles + (p->least ? p->want + 1 : 0);
-  const uint64_t kept = p->least ? (uint64_t)p->items * cache->n_kv_heads * tile_rows : 0;
-  p->o_bytes = kept * cache->head_dim * 4;
-  p->ml_bytes = kept * 8;
-  p->plan_bytes = p->least ? ((uint64_t)batch->n_seqs * 8 + 15) & ~15ull : 0;
+  const uint64_t places = p->least ? (uint64_t)p->items * cache->n_kv_heads : 0;
+  p->o_bytes = places * tile_rows * cache->head_dim * 4;
+  p->ml_bytes = places * tile_rows * 8;
+  p->more_bytes = !p->least ? 0 : p->tiles ? (uint64_t)batch->n_seqs * 8 : places * 8;
   return PPD_OK;
+}
+
+// Numbers of calls: a product with an odd constant never comes twice in 2^64 calls, and looks like nothing that memory holds by chance.
+uint64_t next_stamp() {
+  static std::atomic<uint64_t> calls{0};
+  return (calls.fetch_add(1, std::memory_order_relaxed) + 1) * 0x9e3779b97f4a7c15ull;
 }
 
 template <typename T, int HD>
 hipError_t attn_go(const PagedAttnArgs& a, int dtype, int items, hipStream_t stream) {
-  hipError_t e;
-  if (a.tile_rows == TILE_ROWS) e = launch_paged_tiles(a, dtype, HD, items, stream);
-  else {
-    hipLaunchKernelGGL((paged_split_kernel<T, HD>), dim3(items, a.kv_heads), dim3(256), 0, stream, a);
-    e = hipGetLastError();
-  }
-  if (e != hipSuccess || a.least == 0) return e;
-  constexpr int rpw = 256 / (HD / 4);
-  hipLaunchKernelGGL((paged_merge_kernel<T, HD>), dim3(a.b.n_tokens, (a.heads + rpw - 1) / rpw), dim3(256), 0, stream, a);
+  if (a.tile_rows == TILE_ROWS) return launch_paged_tiles(a, dtype, HD, items, stream);
+  if (near_pages(a)) hipLaunchKernelGGL((paged_split_kernel<T, HD, true>), dim3(items * a.kv_heads), dim3(SPLIT_THREADS), 0, stream, a);
+  else hipLaunchKernelGGL((paged_split_kernel<T, HD, false>), dim3(items * a.kv_heads), dim3(SPLIT_THREADS), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -327,7 +414,7 @@ extern "C" int ppd_paged_attention_workspace(const ppd_paged_cache* cache, const
   const int rc = check_attention(cache, batch, n_heads, &p);
   if (rc) return rc;
   if (!bytes) return PPD_EINVAL;
-  *bytes = p.o_bytes + p.ml_bytes + p.plan_bytes;
+  *bytes = p.o_bytes + p.ml_bytes + p.more_bytes;
   return PPD_OK;
 }
 
@@ -341,7 +428,7 @@ extern "C" int ppd_paged_attention(const ppd_paged_cache* cache, const ppd_paged
   if (!(scale > 0.f && isfinite(scale)) || window < 0) return PPD_EINVAL;
   if (n == 0) return PPD_OK;
   if (!good_rows(q, n, n_heads, dt, false) || !good_rows(out, n, n_heads, dt, true) || ((uintptr_t)lse & 3)) return PPD_EINVAL;
-  const uint64_t need = p.o_bytes + p.ml_bytes + p.plan_bytes;
+  const uint64_t need = p.o_bytes + p.ml_bytes + p.more_bytes;
   if (need && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need)) return PPD_EINVAL;
   PagedAttnArgs a;
   a.b = batch_of(*cache, *batch);
@@ -350,7 +437,9 @@ extern "C" int ppd_paged_attention(const ppd_paged_cache* cache, const ppd_paged
   a.kc_page = cache->k_page; a.kc_pos = cache->k_pos; a.kc_head = cache->k_head; a.vc_page = cache->v_page; a.vc_pos = cache->v_pos; a.vc_head = cache->v_head;
   a.heads = n_heads; a.kv_heads = cache->n_kv_heads; a.group = n_heads / cache->n_kv_heads; a.window = window; a.to_log2 = scale * 1.44269504f;
   a.tile_rows = p.tiles ? TILE_ROWS : SPLIT_ROWS; a.last_first = p.tiles; a.want = p.want; a.least = p.least;
-  a.part_o = (float*)workspace; a.part_ml = (float2*)((char*)workspace + p.o_bytes); a.plan = (int2*)((char*)workspace + p.o_bytes + p.ml_bytes);
+  a.part_o = (float*)workspace; a.part_ml = (float2*)((char*)workspace + p.o_bytes); a.stamps = (uint64_t*)((char*)workspace + p.o_bytes + p.ml_bytes);
+  a.plan = (int2*)a.stamps;
+  a.stamp = next_stamp();
   hipStream_t st = (hipStream_t)hip_stream;
   const int items = (int)p.items;
   if (cache->head_dim == 64)

@@ -242,7 +242,6 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   }
   l += __shfl_xor(l, 32, WAVE);
   if (r >= all_rows) return;
-  const bool none = m == -INFINITY && l == 0.f;
   if (it.parts > 1) {
     const int64_t at = ((int64_t)it.slot * kvheads + kvh) * TILE_ROWS + 32 * wave + col;
 #pragma unroll
@@ -252,6 +251,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
     if (half == 0) a.part_ml[at] = make_float2(m, l);
     return;
   }
+  const bool none = m == -INFINITY && l == 0.f;
   const float inv = 1.0f / l;
   T* const to = (T*)a.out + (int64_t)(it.rows0 + tok) * a.o_tok + (int64_t)head * a.o_head + 4 * half;
 #pragma unroll
@@ -265,10 +265,50 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   if (a.lse && half == 0) a.lse[(int64_t)(it.rows0 + tok) * a.heads + head] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718f;
 }
 
+// The parts of a row joined, in their order: HD / 4 lanes for a row.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
+  constexpr int LPR = HD / 4, RPW = 256 / LPR;
+  const int row = blockIdx.x, lane = threadIdx.x & 63;
+  const int s = seq_of_row(a.b, row, lane);
+  if (s < 0) return;
+  const int2 plan = a.plan[s];
+  const int parts = plan.y, h = blockIdx.y * RPW + threadIdx.x / LPR, d = (threadIdx.x % LPR) * 4;
+  if (parts <= 1 || h >= a.heads) return;
+  const SeqRows sr = seq_rows(a.b, s);
+  const int kvh = h / a.group, r = (row - sr.row0) * a.group + h % a.group;
+  const int64_t first = (int64_t)plan.x + (int64_t)(r / a.tile_rows) * parts;
+  float mx = -INFINITY, sum = 0.f;
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < parts; ++p) mx = fmaxf(mx, a.part_ml[((first + p) * a.kv_heads + kvh) * a.tile_rows + r % a.tile_rows].x);
+  const float ref = mx == -INFINITY ? 0.f : mx;
+  for (int p = 0; p < parts; ++p) {
+    const int64_t at = ((first + p) * a.kv_heads + kvh) * a.tile_rows + r % a.tile_rows;
+    const float2 ml = a.part_ml[at];
+    const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+    sum = fmaf(f, ml.y, sum);
+    const f32x4 z = *(const f32x4*)(a.part_o + at * HD + d);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = fmaf(f, z[e], y[e]);
+  }
+  const bool none = mx == -INFINITY && sum == 0.f;
+  const float inv = 1.0f / sum;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : y[e] * inv;
+  *(typename Quad<T>::raw*)((T*)a.out + (int64_t)row * a.o_tok + (int64_t)h * a.o_head + d) = quad_out<T>(y);
+  if (a.lse && d == 0) a.lse[(int64_t)row * a.heads + h] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718f;
+}
+
 template <typename T, bool NEAR>
 hipError_t tiles_go(const PagedAttnArgs& a, int head_dim, dim3 grid, hipStream_t stream) {
   if (head_dim == 64) hipLaunchKernelGGL((paged_tile_kernel<T, 64, NEAR>), grid, dim3(256), 0, stream, a);
   else hipLaunchKernelGGL((paged_tile_kernel<T, 128, NEAR>), grid, dim3(256), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.least == 0) return e;
+  const int rpw = 256 / (head_dim / 4);
+  const dim3 rows(a.b.n_tokens, (a.heads + rpw - 1) / rpw);
+  if (head_dim == 64) hipLaunchKernelGGL((paged_merge_kernel<T, 64>), rows, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((paged_merge_kernel<T, 128>), rows, dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -276,8 +316,7 @@ hipError_t tiles_go(const PagedAttnArgs& a, int head_dim, dim3 grid, hipStream_t
 
 hipError_t launch_paged_tiles(const PagedAttnArgs& a, int dtype, int head_dim, int items, hipStream_t stream) {
   const dim3 grid((unsigned)items * a.kv_heads);
-  const int64_t far = (1 << 26) - 1;
-  const bool near = a.b.page_size % 16 == 0 && a.kc_pos <= far && a.vc_pos <= far;
+  const bool near = near_pages(a);
   if (dtype == PPD_BF16) return near ? tiles_go<bf16_t, true>(a, head_dim, grid, stream) : tiles_go<bf16_t, false>(a, head_dim, grid, stream);
   if (dtype == PPD_FP16) return near ? tiles_go<f16_t, true>(a, head_dim, grid, stream) : tiles_go<f16_t, false>(a, head_dim, grid, stream);
   return hipErrorInvalidValue;

@@ -51,7 +51,7 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const Item& i
   const int rows = min(SPLIT_ROWS, it.n * a.group - it.tile * SPLIT_ROWS);
   for (int x = tid; x < rows * (HD / 4); x += SPLIT_THREADS) {
     const int rr = x / (HD / 4), d = x % (HD / 4) * 4, ri = it.tile * SPLIT_ROWS + rr;
-    auto at = [&](int p) { return ((int64_t)p * a.kv_heads + kvh) * SPLIT_ROWS + rr; };
+    auto at = [&](int p) { return ((int64_t)(first + p) * a.kv_heads + kvh) * SPLIT_ROWS + rr; };
     float mx = -INFINITY, sum = 0.f;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8

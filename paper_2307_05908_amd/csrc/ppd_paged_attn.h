@@ -101,6 +101,13 @@ __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, bool 
       all += wave_sum((float)p.tiles * (float)p.blocks);
     }
     len = max(a.least, (int)ceilf(all / (float)a.want));
+    // few tiles: where their ends make it more parts than `want`, longer ones (a second round of workgroups for a few of them would cost more)
+    for (int again = 0; again < 3 && a.b.n_seqs <= WAVE; ++again) {
+      const int parts = (p.blocks + len - 1) / len;
+      const float items = wave_sum((float)(p.tiles * parts)), tiles = wave_sum((float)p.tiles);
+      if (items <= (float)a.want || 2.f * tiles > (float)a.want) break;
+      len = (int)ceilf((float)len * items / (float)a.want);
+    }
   }
   // Tiles of several parts come first, the others fill up behind them.
   auto items_of = [&](const SeqPlan& q, bool several) { return (q.parts > 1) == several ? q.tiles * q.parts : 0; };

@@ -381,7 +381,7 @@ int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, 
   const int tile_rows = p->tiles ? TILE_ROWS : SPLIT_ROWS;
   const int64_t tiles = rows / tile_rows + some;
   const int slots = p->tiles ? 512 : 256;
-  p->want = (slots + cache->n_kv_heads - 1) / cache->n_kv_heads;
+  p->want = slots / cache->n_kv_heads + (slots < cache->n_kv_heads);
   p->least = p->tiles ? 8 : 4;
   // tiles enough for the whole chip, or no position to cut at: one part each
   if (tiles >= (p->tiles ? 2 : 8) * p->want || (int64_t)batch->max_pages * cache->page_size <= p->least * PLAN_BLOCK) p->least = 0;

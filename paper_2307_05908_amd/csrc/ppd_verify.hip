@@ -57,9 +57,11 @@ template <> struct Logits<f16_t> {
     for (int e = 0; e < 4; ++e) { const uint32_t x = r[e]; const h2 h = __builtin_bit_cast(h2, x); f[2 * e] = (float)h.x; f[2 * e + 1] = (float)h.y; }
   }
 };
-template <typename T> __device__ __forceinline__ float logit(const void* p, int64_t i) { const float v = Logits<T>::one(p, i); return v == v ? v : -INFINITY; }
+// NaN counts as -inf, and +inf as the largest number: where there is one, nothing else has a weight
+__device__ __forceinline__ float usable(float z) { return fminf(fmaxf(z, -INFINITY), 3.40282347e38f); }
+template <typename T> __device__ __forceinline__ float logit(const void* p, int64_t i) { return usable(Logits<T>::one(p, i)); }
 
-// A thread's logits of a chunk: PER / VEC runs of VEC, run v of thread t at (v * VT + t) * VEC.  NaN and what lies behind the row: -inf.
+// A thread's logits of a chunk: PER / VEC runs of VEC, run v of thread t at (v * VT + t) * VEC.  What lies behind the row: -inf.
 // Rows begin at any multiple of the type's size.
 template <typename T>
 __device__ __forceinline__ void load_chunk(const void* p, int64_t row, int chunk, int vocab, float (&z)[PER]) {
@@ -75,38 +77,26 @@ __device__ __forceinline__ void load_chunk(const void* p, int64_t row, int chunk
       for (int e = 0; e < VEC; ++e) z[v * VEC + e] = j + e < vocab ? Logits<T>::one(base, j + e) : -INFINITY;
   }
 #pragma unroll
-  for (int e = 0; e < PER; ++e) z[e] = z[e] == z[e] ? z[e] : -INFINITY;
+  for (int e = 0; e < PER; ++e) z[e] = usable(z[e]);
 }
 __device__ __forceinline__ int id_of(int chunk, int e, int vec) { return chunk * CHUNK + (e / vec * VT + (int)threadIdx.x) * vec + e % vec; }
 
-// exp((z - top) / t), relative error below 2^-46: 2^(y / 32) with y = (z - top) * 32 log2(e) / t, its nearest whole number from a table
-// of 2^(i / 32) and the exponent, the rest (at most a half) by the exponential's series to the fifth power.
+// exp((z - top) / t), relative error below 2^-43: 2^(y / 64) with y = (z - top) * 64 log2(e) / t, its nearest whole number k from a table
+// of 2^(i / 64) and the exponent, the rest (at most a half) by the exponential's series to the fourth power.  -inf, and what is 64000
+// and more below (2^-1000): exactly 0.  (Where all of a row is -inf the difference is no number, and that is less than anything, too.)
 struct Weigh {
-  double scale, top; float cut, top_f;      // below cut: exactly 0 (under 2^-1000, and -inf)
-  bool endless;                             // the largest is +inf: 1 for those, 0 for the others
-  __device__ __forceinline__ Weigh(float top_, double t) {
-    top_f = top_ == -INFINITY ? INFINITY : top_;      // (nothing is the largest of nothing)
-    top = top_; scale = 46.166241308446828 / t;
-    endless = top_ == INFINITY;
-    cut = top_ == -INFINITY ? INFINITY : (float)((double)top_ - 690.0 * t);
-  }
-  __device__ __forceinline__ double operator()(float z, const double* table) const {
-    if (endless) return z == top_f ? 1.0 : 0.0;
-    const double y = ((double)z - top) * scale, magic = 6755399441055744.0;
-    const double shifted = y + magic, r = y - (shifted - magic);
+  double scale, top;
+  const double* table;
+  __device__ __forceinline__ Weigh(float top_, double t, const double* table_) : scale(92.332482616893657 / t), top(top_), table(table_) {}
+  __device__ __forceinline__ double operator()(float z) const {
+    constexpr double L = 0.010830424696249145, magic = 6755399441055744.0;      // ln 2 / 64; 1.5 * 2^52
+    const double y = fmax(((double)z - top) * scale, -128000.0), shifted = y + magic, r = y - (shifted - magic);
     const int k = __double2loint(shifted);
-    const double a = r * 0.021660849392498290;             // ln 2 / 32
-    double p = fma(a, fma(a, fma(a, fma(a, fma(a, 1.0 / 120, 1.0 / 24), 1.0 / 6), 0.5), 1.0), 1.0) * table[k & 31];
-    p = __hiloint2double(__double2hiint(p) + ((k >> 5) << 20), __double2loint(p));
-    return z > cut || z == top_f ? p : 0.0;
+    const double p = fma(r, fma(r, fma(r, fma(r, L * L * L * L / 24, L * L * L / 6), L * L / 2), L), 1.0) * table[k & 63];
+    return ldexp(p, k >> 6);
   }
 };
-__device__ __forceinline__ void fill_table(double* table) { if (threadIdx.x < 32) table[threadIdx.x] = exp2(threadIdx.x * 0.03125); }
-
-// what a chunk's sum is worth beside the row's largest logit
-__device__ __forceinline__ double in_row(const RowPart& p, float top, double inv_t) {
-  return p.sum == 0.0 ? 0.0 : p.top == top ? p.sum : p.sum * exp(((double)p.top - (double)top) * inv_t);
-}
+__device__ __forceinline__ void fill_table(double* table) { if (threadIdx.x < 64) table[threadIdx.x] = exp2(threadIdx.x * 0.015625); }
 
 __device__ __forceinline__ double wave_sum_f64(double v) {
 #pragma unroll
@@ -119,25 +109,35 @@ __device__ __forceinline__ double temperature_of(const VerifyArgs& a, int s) { r
 template <typename T>
 __global__ __launch_bounds__(VT) void verify_rows_kernel(VerifyArgs a) {
   constexpr int VEC = Logits<T>::VEC;
-  __shared__ double table[32], ds[4];
+  __shared__ double table[64], ds[4];
   __shared__ float fs[4]; __shared__ int is[4];
   const int chunk = blockIdx.x % a.chunks, row = blockIdx.x / a.chunks, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool draft = blockIdx.y == 1;
   if (chunk == 0 && row == 0 && !draft) for (int i = tid; i < a.n_seqs; i += VT) a.done[i] = 0;
+  float z[PER];
+  if (!draft) load_chunk<T>(a.target, row * a.target_stride, chunk, a.vocab, z);         // (under way while the row's sequence is looked for)
   Batch b = {};
   b.q_start = a.row_start; b.n_seqs = a.n_seqs;
   const int s = seq_of_row(b, row, lane);
   if (s < 0) return;
   const double t = temperature_of(a, s);
   const bool by_max = !(t > 0.0);
-  if (draft && (by_max || row + 1 >= min(a.row_start[s + 1], a.n_rows))) return;        // rows that nothing asks for
-  float z[PER];
-  load_chunk<T>(draft ? a.draft : a.target, row * (draft ? a.draft_stride : a.target_stride), chunk, a.vocab, z);
+  if (draft) {
+    if (by_max || row + 1 >= min(a.row_start[s + 1], a.n_rows)) return;                  // rows that nothing asks for
+    load_chunk<T>(a.draft, row * a.draft_stride, chunk, a.vocab, z);
+  }
   fill_table(table);
   float top = -INFINITY; int arg = 0x7fffffff;
+  if (by_max) {
 #pragma unroll
-  for (int e = 0; e < PER; ++e) if (z[e] > top) { top = z[e]; arg = id_of(chunk, e, VEC); }
-  wave_best(top, arg);
+    for (int e = 0; e < PER; ++e) if (z[e] > top) { top = z[e]; arg = id_of(chunk, e, VEC); }
+    wave_best(top, arg);
+  } else {
+#pragma unroll
+    for (int e = 0; e < PER; ++e) top = fmaxf(top, z[e]);
+    top = wave_max(top);
+    arg = top > -INFINITY ? chunk * CHUNK : 0x7fffffff;                                  // (only whether there is one is asked)
+  }
   if (lane == 0) { fs[wave] = top; is[wave] = arg; }
   __syncthreads();
   top = fs[0]; arg = is[0];
@@ -145,9 +145,9 @@ __global__ __launch_bounds__(VT) void verify_rows_kernel(VerifyArgs a) {
   for (int w = 1; w < 4; ++w) if (better(fs[w], is[w], top, arg)) { top = fs[w]; arg = is[w]; }
   double sum = 0.0;
   if (!by_max) {
-    const Weigh weigh(top, t);
+    const Weigh weigh(top, t, table);
 #pragma unroll
-    for (int e = 0; e < PER; ++e) sum += weigh(z[e], table);
+    for (int e = 0; e < PER; ++e) sum += weigh(z[e]);
     sum = wave_sum_f64(sum);
     if (lane == 0) ds[wave] = sum;
     __syncthreads();
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(VT) void verify_rows_kernel(VerifyArgs a) {
 // ---- which drafts are taken, and the draw.  grid: (chunks, n_seqs)
 struct Row { float top; int arg; double sum; };
 // a row's parts joined by 16 lanes, in all of them
-__device__ __forceinline__ Row join_row(const RowPart* p, int chunks, double inv_t, bool by_max) {
+__device__ __forceinline__ Row join_row(const RowPart* p, int chunks, double t, bool by_max, const double* table) {
   const int l = threadIdx.x & 15;
   Row r = {-INFINITY, 0x7fffffff, 0.0};
   for (int c = l; c < chunks; c += 16) { const float v = p[c].top; const int i = p[c].arg; if (better(v, i, r.top, r.arg)) { r.top = v; r.arg = i; } }
@@ -169,7 +169,8 @@ __device__ __forceinline__ Row join_row(const RowPart* p, int chunks, double inv
     if (better(v, i, r.top, r.arg)) { r.top = v; r.arg = i; }
   }
   if (!by_max) {
-    for (int c = l; c < chunks; c += 16) r.sum += in_row(p[c], r.top, inv_t);
+    const Weigh weigh(r.top, t, table);
+    for (int c = l; c < chunks; c += 16) r.sum += p[c].sum * weigh(p[c].top);
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) r.sum += __shfl_xor(r.sum, o, WAVE);
   }
@@ -179,7 +180,7 @@ __device__ __forceinline__ Row join_row(const RowPart* p, int chunks, double inv
 template <typename T>
 __global__ __launch_bounds__(VT) void verify_draw_kernel(VerifyArgs a) {
   constexpr int VEC = Logits<T>::VEC, RUNS = PER / VEC;
-  __shared__ double table[32], seg[RUNS * 4], ds[4], chunk_sum[VT];
+  __shared__ double table[64], seg[RUNS * 4], ds[4], chunk_sum[VT];
   __shared__ int s_end, s_last, s_token;
   __shared__ Row s_p, s_q;
   const int chunk = blockIdx.x, s = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -188,7 +189,7 @@ __global__ __launch_bounds__(VT) void verify_draw_kernel(VerifyArgs a) {
     if (chunk == 0 && tid == 0) a.accepted[s] = 0;
     return;
   }
-  const double t = temperature_of(a, s), inv_t = 1.0 / t;
+  const double t = temperature_of(a, s);
   const bool by_max = !(t > 0.0);
   fill_table(table);
   if (tid == 0) s_end = hi;
@@ -198,17 +199,17 @@ __global__ __launch_bounds__(VT) void verify_draw_kernel(VerifyArgs a) {
     const int r = r0 + (tid >> 4);
     const bool in = r < hi, last = r + 1 >= hi;
     const int rc = in ? r : hi - 1;
-    const Row p = join_row(a.parts + (int64_t)rc * a.chunks, a.chunks, inv_t, by_max);
+    const Row p = join_row(a.parts + (int64_t)rc * a.chunks, a.chunks, t, by_max, table);
     const int d = last ? -1 : a.ids[rc + 1];
     const bool real = (unsigned)d < (unsigned)a.vocab;
     Row q = {0.f, 0, 0.0};
     bool take = false;
     if (by_max) take = real && d == p.arg && p.top > -INFINITY;
     else {
-      if (!last && a.draft) q = join_row(a.parts + ((int64_t)a.n_rows + rc) * a.chunks, a.chunks, inv_t, false);
+      if (!last && a.draft) q = join_row(a.parts + ((int64_t)a.n_rows + rc) * a.chunks, a.chunks, t, false, table);
       if (real) {
-        const double pd = p.sum > 0.0 ? Weigh(p.top, t)(logit<T>(a.target, rc * a.target_stride + d), table) / p.sum : 0.0;
-        const double qd = !a.draft ? 1.0 : q.sum > 0.0 ? Weigh(q.top, t)(logit<T>(a.draft, rc * a.draft_stride + d), table) / q.sum : 0.0;
+        const double pd = p.sum > 0.0 ? Weigh(p.top, t, table)(logit<T>(a.target, rc * a.target_stride + d)) / p.sum : 0.0;
+        const double qd = !a.draft ? 1.0 : q.sum > 0.0 ? Weigh(q.top, t, table)(logit<T>(a.draft, rc * a.draft_stride + d)) / q.sum : 0.0;
         take = (double)a.uniform[2 * (int64_t)rc] * qd < pd;
       }
     }
@@ -232,19 +233,19 @@ __global__ __launch_bounds__(VT) void verify_draw_kernel(VerifyArgs a) {
     return;
   }
   const bool residual = !last && (a.draft ? q.sum > 0.0 : (unsigned)d < (unsigned)a.vocab);
-  const Weigh wp(p.top, t), wq(q.top, t);
+  const Weigh wp(p.top, t, table), wq(q.top, t, table);
   const double ip = 1.0 / p.sum, iq = q.sum > 0.0 ? 1.0 / q.sum : 0.0;
   // the weights that the draw goes by, of a thread's logits of chunk c
   auto weights = [&](int c, bool rest, double (&w)[PER]) {
-    float z[PER];
+    float z[PER], y[PER];
     load_chunk<T>(a.target, end * a.target_stride, c, a.vocab, z);
+    if (rest && a.draft) load_chunk<T>(a.draft, end * a.draft_stride, c, a.vocab, y);
 #pragma unroll
-    for (int e = 0; e < PER; ++e) w[e] = wp(z[e], table) * ip;
+    for (int e = 0; e < PER; ++e) w[e] = wp(z[e]) * ip;
     if (!rest) return;
     if (a.draft) {
-      load_chunk<T>(a.draft, end * a.draft_stride, c, a.vocab, z);
 #pragma unroll
-      for (int e = 0; e < PER; ++e) w[e] = fmax(w[e] - wq(z[e], table) * iq, 0.0);
+      for (int e = 0; e < PER; ++e) w[e] = fmax(w[e] - wq(y[e]) * iq, 0.0);
     } else {
 #pragma unroll
       for (int e = 0; e < PER; ++e) if (id_of(c, e, VEC) == d) w[e] = fmax(w[e] - 1.0, 0.0);
@@ -272,7 +273,7 @@ __global__ __launch_bounds__(VT) void verify_draw_kernel(VerifyArgs a) {
   bool rest = residual;
   auto part = [&](int c) {
     return rest ? __hip_atomic_load(a.left + (int64_t)s * a.chunks + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)
-                : in_row(a.parts[(int64_t)end * a.chunks + c], p.top, inv_t) * ip;
+                : a.parts[(int64_t)end * a.chunks + c].sum * wp(a.parts[(int64_t)end * a.chunks + c].top) * ip;
   };
   // (all chunks' parts by all threads, 256 at a time, and then in their order; chunks of more than 2^20 tokens come in several turns)
   auto walk = [&](auto&& each) {

@@ -15,15 +15,17 @@ namespace {
 constexpr int VERIFY_MAX_VOCAB = 1 << 24;
 constexpr int VT = 256;                       // threads of a workgroup
 constexpr int PER = 16;                       // logits of a thread
+constexpr int PIECE = WAVE * PER;             // of a wave
 constexpr int CHUNK = VT * PER;               // of a workgroup
 
-struct RowPart { double sum; float top; int arg; };      // of a chunk: the weights' sum relative to top, the largest logit, its lowest id
+struct RowPart { double sum; float top; int arg; };      // of a piece: the weights' sum relative to top, the largest logit, its lowest id
 
 struct VerifyArgs {
   const int32_t *row_start, *ids; const void *target, *draft; int64_t target_stride, draft_stride;
   const float *temperature, *uniform; int32_t *tokens, *accepted;
-  int n_seqs, n_rows, vocab, chunks;
-  RowPart* parts;          // [2 (target, draft)][n_rows][chunks]
+  int n_seqs, n_rows, vocab, chunks, pieces;
+  int run;                 // pieces that a wave of the first launch takes in turn
+  RowPart* parts;          // [2 (target, draft)][n_rows][pieces]
   double* left;            // [n_seqs][chunks]: sums of the residual
   unsigned* done;          // [n_seqs]: workgroups of a sequence that have left theirs (set to zero by the first launch)
 };
@@ -61,61 +63,100 @@ template <> struct Logits<f16_t> {
 __device__ __forceinline__ float usable(float z) { return fminf(fmaxf(z, -INFINITY), 3.40282347e38f); }
 template <typename T> __device__ __forceinline__ float logit(const void* p, int64_t i) { return usable(Logits<T>::one(p, i)); }
 
-// A thread's logits of a chunk: PER / VEC runs of VEC, run v of thread t at (v * VT + t) * VEC.  What lies behind the row: -inf.
-// Rows begin at any multiple of the type's size.
+// A lane's logits of a piece: PER / VEC runs of VEC, run v of lane l at (v * 64 + l) * VEC.  What lies behind the row: -inf.  Rows begin at
+// any multiple of the type's size.
 template <typename T>
-__device__ __forceinline__ void load_chunk(const void* p, int64_t row, int chunk, int vocab, float (&z)[PER]) {
+__device__ __forceinline__ void load_piece(const void* p, int64_t row, int piece, int vocab, int lane, float (&z)[PER]) {
   constexpr int VEC = Logits<T>::VEC;
   typedef typename Logits<T>::loose loose;
   const char* base = (const char*)p + row * (16 / VEC);
+  if ((piece + 1) * PIECE <= vocab) {
 #pragma unroll
-  for (int v = 0; v < PER / VEC; ++v) {
-    const int j = chunk * CHUNK + (v * VT + (int)threadIdx.x) * VEC;
-    if (j + VEC <= vocab) Logits<T>::wide(*(const loose*)(base + (int64_t)j * (16 / VEC)), z + v * VEC);
-    else
+    for (int v = 0; v < PER / VEC; ++v) Logits<T>::wide(*(const loose*)(base + (int64_t)(piece * PIECE + (v * WAVE + lane) * VEC) * (16 / VEC)), z + v * VEC);
+  } else {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) z[v * VEC + e] = j + e < vocab ? Logits<T>::one(base, j + e) : -INFINITY;
+    for (int e = 0; e < PER; ++e) {
+      const int j = piece * PIECE + (e / VEC * WAVE + lane) * VEC + e % VEC;
+      z[e] = j < vocab ? Logits<T>::one(base, j) : -INFINITY;
+    }
   }
-#pragma unroll
-  for (int e = 0; e < PER; ++e) z[e] = usable(z[e]);
 }
-__device__ __forceinline__ int id_of(int chunk, int e, int vec) { return chunk * CHUNK + (e / vec * VT + (int)threadIdx.x) * vec + e % vec; }
+__device__ __forceinline__ int id_of(int piece, int e, int vec, int lane) { return piece * PIECE + (e / vec * WAVE + lane) * vec + e % vec; }
 
-// exp((z - top) / t), relative error below 2^-43: 2^(y / 64) with y = (z - top) * 64 log2(e) / t, its nearest whole number k from a table
-// of 2^(i / 64) and the exponent, the rest (at most a half) by the exponential's series to the fourth power.  -inf, and what is 64000
-// and more below (2^-1000): exactly 0.  (Where all of a row is -inf the difference is no number, and that is less than anything, too.)
+// exp((z - top) / t), relative error below 2^-42: 2^(y / 256) with y = (z - top) * 256 log2(e) / t, its nearest whole number k from a table
+// of 2^(i / 256) and the exponent, the rest (at most a half) by the exponential's series to the third power.  -inf, and all that is further
+// down, comes as 2^-1000, which counts as nothing wherever a weight is looked at by itself (some), and is nothing in a sum beside the
+// largest logit's 1.  The table's entries have i << 12 taken off their upper words, so that k << 12 puts the exponent there and leaves the
+// rest.  Twelve instructions: these weights, not the reading of the logits, are what the launch takes its time for.
+constexpr double SOME = 0x1p-900;
+constexpr int STEPS = 256;
 struct Weigh {
-  double scale, top;
+  double scale, top, least;
   const double* table;
-  __device__ __forceinline__ Weigh(float top_, double t, const double* table_) : scale(92.332482616893657 / t), top(top_), table(table_) {}
-  __device__ __forceinline__ double operator()(float z) const {
-    constexpr double L = 0.010830424696249145, magic = 6755399441055744.0;      // ln 2 / 64; 1.5 * 2^52
-    const double y = fmax(((double)z - top) * scale, -128000.0), shifted = y + magic, r = y - (shifted - magic);
+  __device__ __forceinline__ Weigh(float top_, double t, const double* table_) : scale(369.32993046757463 / t), top(top_), least(-693.0 * t), table(table_) {}
+  __device__ __forceinline__ double series(float z, double& power) const {
+    constexpr double L = 0.0027076061740622863, magic = 6755399441055744.0;      // ln 2 / 256; 1.5 * 2^52
+    const double d = fmax((double)z - top, least), shifted = fma(d, scale, magic), r = fma(d, scale, magic - shifted);
     const int k = __double2loint(shifted);
-    const double p = fma(r, fma(r, fma(r, fma(r, L * L * L * L / 24, L * L * L / 6), L * L / 2), L), 1.0) * table[k & 63];
-    return ldexp(p, k >> 6);
+    const double entry = table[k & (STEPS - 1)];
+    power = __hiloint2double(__double2hiint(entry) + (k << 12), __double2loint(entry));
+    return fma(r, fma(r, fma(r, L * L * L / 6, L * L / 2), L), 1.0);
   }
+  __device__ __forceinline__ double operator()(float z) const { double power; const double p = series(z, power); return p * power; }
+  __device__ __forceinline__ void add(float z, double& sum) const { double power; const double p = series(z, power); sum = fma(p, power, sum); }
+  __device__ __forceinline__ double some(float z) const { const double p = (*this)(z); return p > SOME ? p : 0.0; }
 };
-__device__ __forceinline__ void fill_table(double* table) { if (threadIdx.x < 64) table[threadIdx.x] = exp2(threadIdx.x * 0.015625); }
-
-__device__ __forceinline__ double wave_sum_f64(double v) {
+// 2^(i / 256) by the bits of i
+__device__ __forceinline__ void fill_table(double* table) {
+  static_assert(STEPS == VT, "an entry a thread");
+  const int i = threadIdx.x;
+  const double f[8] = {1.0027112750502025, 1.0054299011128027, 1.0108892860517005, 1.0218971486541166, 1.0442737824274138, 1.0905077326652577, 1.189207115002721, 1.4142135623730951};
+  double p = 1.0;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, WAVE);
+  for (int b = 0; b < 8; ++b) p *= i >> b & 1 ? f[b] : 1.0;
+  table[i] = __hiloint2double(__double2hiint(p) - (i << 12), __double2loint(p));
+}
+
+template <int CTRL> __device__ __forceinline__ double dpp_f64(double v) {
+  return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xf, 0xf, false), __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ double lane_f64(double v, int l) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), l), __builtin_amdgcn_readlane(__double2loint(v), l));
+}
+__device__ __forceinline__ double row_sum_f64(double v) {      // over 16 lanes, the same in all of them
+  v += dpp_f64<0xB1>(v);
+  v += dpp_f64<0x4E>(v);
+  v += dpp_f64<0x141>(v);
+  return v + dpp_f64<0x140>(v);
+}
+__device__ __forceinline__ double wave_sum_f64(double v) {
+  v = row_sum_f64(v);
+  return ((lane_f64(v, 0) + lane_f64(v, 16)) + lane_f64(v, 32)) + lane_f64(v, 48);
+}
+__device__ __forceinline__ double scan_f64(double v, int lane) {
+#pragma unroll
+  for (int o = 1; o < WAVE; o <<= 1) { const double y = __shfl_up(v, o, WAVE); if (lane >= o) v += y; }
   return v;
 }
 __device__ __forceinline__ double temperature_of(const VerifyArgs& a, int s) { return a.temperature ? (double)a.temperature[s] : 1.0; }
 
-// ---- all rows: the largest logit and the weights' sum, chunk by chunk.  grid: (n_rows * chunks, 1 or 2: target, draft)
+// ---- all rows: the largest logit and the weights' sum, piece by piece.  A wave has `run` pieces of a row, and the next one's logits under way
+// while it works on one; nothing waits for another wave but for the table.  grid: (runs of all rows / 4, 1 or 2: target, draft)
 template <typename T>
-__global__ __launch_bounds__(VT) void verify_rows_kernel(VerifyArgs a) {
+__global__ __launch_bounds__(VT, 6) void verify_rows_kernel(VerifyArgs a) {
   constexpr int VEC = Logits<T>::VEC;
-  __shared__ double table[64], ds[4];
-  __shared__ float fs[4]; __shared__ int is[4];
-  const int chunk = blockIdx.x % a.chunks, row = blockIdx.x / a.chunks, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ double table[STEPS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const bool draft = blockIdx.y == 1;
-  if (chunk == 0 && row == 0 && !draft) for (int i = tid; i < a.n_seqs; i += VT) a.done[i] = 0;
-  float z[PER];
-  if (!draft) load_chunk<T>(a.target, row * a.target_stride, chunk, a.vocab, z);         // (under way while the row's sequence is looked for)
+  if (blockIdx.x == 0 && !draft) for (int i = tid; i < a.n_seqs; i += VT) a.done[i] = 0;
+  fill_table(table);
+  __syncthreads();
+  const int runs = (a.pieces + a.run - 1) / a.run, at = blockIdx.x * 4 + wave, row = at / runs, first = at % runs * a.run, end = min(first + a.run, a.pieces);
+  if (row >= a.n_rows) return;
+  const void* const src = draft ? a.draft : a.target;
+  const int64_t from = row * (draft ? a.draft_stride : a.target_stride);
+  float z[PER], next[PER];
+  if (!draft) load_piece<T>(src, from, first, a.vocab, lane, z);         // (under way while the row's sequence is looked for)
   Batch b = {};
   b.q_start = a.row_start; b.n_seqs = a.n_seqs;
   const int s = seq_of_row(b, row, lane);
@@ -124,45 +165,48 @@ __global__ __launch_bounds__(VT) void verify_rows_kernel(VerifyArgs a) {
   const bool by_max = !(t > 0.0);
   if (draft) {
     if (by_max || row + 1 >= min(a.row_start[s + 1], a.n_rows)) return;                  // rows that nothing asks for
-    load_chunk<T>(a.draft, row * a.draft_stride, chunk, a.vocab, z);
+    load_piece<T>(src, from, first, a.vocab, lane, z);
   }
-  fill_table(table);
-  float top = -INFINITY; int arg = 0x7fffffff;
-  if (by_max) {
+  RowPart* const out = a.parts + ((int64_t)(draft ? a.n_rows : 0) + row) * a.pieces;
+  for (int piece = first; piece < end; ++piece) {
+    if (piece + 1 < end) load_piece<T>(src, from, piece + 1, a.vocab, lane, next);
+    float top = -INFINITY; int arg = 0x7fffffff;
+    double sum = 0.0;
+    if (by_max) {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) if (z[e] > top) { top = z[e]; arg = id_of(chunk, e, VEC); }
-    wave_best(top, arg);
-  } else {
+      for (int e = 0; e < PER; ++e) { const float x = usable(z[e]); if (x > top) { top = x; arg = id_of(piece, e, VEC, lane); } }
+      wave_best(top, arg);
+    } else {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) top = fmaxf(top, z[e]);
-    top = wave_max(top);
-    arg = top > -INFINITY ? chunk * CHUNK : 0x7fffffff;                                  // (only whether there is one is asked)
+      for (int e = 0; e < PER; ++e) top = fmaxf(top, z[e]);              // (no NaN comes out)
+      top = wave_max(top);
+      if (top == INFINITY) {
+        top = usable(top);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) z[e] = usable(z[e]);
+      }
+      arg = top > -INFINITY ? piece * PIECE : 0x7fffffff;                // (only whether there is one is asked)
+      const Weigh weigh(top, t, table);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        weigh.add(z[e], sum);
+        if (e % 4 == 3) { asm volatile("" : "+v"(sum)); __builtin_amdgcn_sched_barrier(0); }      // (four at a time: sixteen take 144 registers)
+      }
+      sum = top > -INFINITY ? wave_sum_f64(sum) : 0.0;
+    }
+    if (lane == 0) out[piece] = {sum, top, arg};
+#pragma unroll
+    for (int e = 0; e < PER; ++e) z[e] = next[e];
   }
-  if (lane == 0) { fs[wave] = top; is[wave] = arg; }
-  __syncthreads();
-  top = fs[0]; arg = is[0];
-#pragma unroll
-  for (int w = 1; w < 4; ++w) if (better(fs[w], is[w], top, arg)) { top = fs[w]; arg = is[w]; }
-  double sum = 0.0;
-  if (!by_max) {
-    const Weigh weigh(top, t, table);
-#pragma unroll
-    for (int e = 0; e < PER; ++e) sum += weigh(z[e]);
-    sum = wave_sum_f64(sum);
-    if (lane == 0) ds[wave] = sum;
-    __syncthreads();
-    sum = ((ds[0] + ds[1]) + ds[2]) + ds[3];
-  }
-  if (tid == 0) a.parts[((int64_t)(draft ? a.n_rows : 0) + row) * a.chunks + chunk] = {sum, top, arg};
 }
 
 // ---- which drafts are taken, and the draw.  grid: (chunks, n_seqs)
 struct Row { float top; int arg; double sum; };
-// a row's parts joined by 16 lanes, in all of them
-__device__ __forceinline__ Row join_row(const RowPart* p, int chunks, double t, bool by_max, const double* table) {
+// a row's pieces joined by 16 lanes, in all of them
+__device__ __forceinline__ Row join_row(const RowPart* p, int pieces, double t, bool by_max, const double* table) {
   const int l = threadIdx.x & 15;
   Row r = {-INFINITY, 0x7fffffff, 0.0};
-  for (int c = l; c < chunks; c += 16) { const float v = p[c].top; const int i = p[c].arg; if (better(v, i, r.top, r.arg)) { r.top = v; r.arg = i; } }
+  for (int c = l; c < pieces; c += 16) { const float v = p[c].top; const int i = p[c].arg; if (better(v, i, r.top, r.arg)) { r.top = v; r.arg = i; } }
 #pragma unroll
   for (int o = 1; o < 16; o <<= 1) {
     const float v = __shfl_xor(r.top, o, WAVE); const int i = __shfl_xor(r.arg, o, WAVE);
@@ -170,9 +214,8 @@ __device__ __forceinline__ Row join_row(const RowPart* p, int chunks, double t, 
   }
   if (!by_max) {
     const Weigh weigh(r.top, t, table);
-    for (int c = l; c < chunks; c += 16) r.sum += p[c].sum * weigh(p[c].top);
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) r.sum += __shfl_xor(r.sum, o, WAVE);
+    for (int c = l; c < pieces; c += 16) r.sum += p[c].sum * weigh(p[c].top);
+    r.sum = row_sum_f64(r.sum);
   }
   return r;
 }
@@ -180,10 +223,10 @@ __device__ __forceinline__ Row join_row(const RowPart* p, int chunks, double t, 
 template <typename T>
 __global__ __launch_bounds__(VT) void verify_draw_kernel(VerifyArgs a) {
   constexpr int VEC = Logits<T>::VEC, RUNS = PER / VEC;
-  __shared__ double table[64], seg[RUNS * 4], ds[4], chunk_sum[VT];
-  __shared__ int s_end, s_last, s_token;
+  __shared__ double table[STEPS], ds[4];
+  __shared__ int s_end, s_last;
   __shared__ Row s_p, s_q;
-  const int chunk = blockIdx.x, s = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int chunk = blockIdx.x, s = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lo = min(max(a.row_start[s], 0), a.n_rows), hi = min(max(a.row_start[s + 1], lo), a.n_rows);
   if (lo == hi) {
     if (chunk == 0 && tid == 0) a.accepted[s] = 0;
@@ -199,19 +242,23 @@ __global__ __launch_bounds__(VT) void verify_draw_kernel(VerifyArgs a) {
     const int r = r0 + (tid >> 4);
     const bool in = r < hi, last = r + 1 >= hi;
     const int rc = in ? r : hi - 1;
-    const Row p = join_row(a.parts + (int64_t)rc * a.chunks, a.chunks, t, by_max, table);
     const int d = last ? -1 : a.ids[rc + 1];
     const bool real = (unsigned)d < (unsigned)a.vocab;
+    float zd = -INFINITY, yd = -INFINITY, u = 0.f;
+    if (real && !by_max) {
+      zd = logit<T>(a.target, rc * a.target_stride + d);
+      if (a.draft) yd = logit<T>(a.draft, rc * a.draft_stride + d);
+      u = a.uniform[2 * (int64_t)rc];
+    }
+    const Row p = join_row(a.parts + (int64_t)rc * a.pieces, a.pieces, t, by_max, table);
     Row q = {0.f, 0, 0.0};
+    if (!by_max && a.draft && !last) q = join_row(a.parts + ((int64_t)a.n_rows + rc) * a.pieces, a.pieces, t, false, table);
     bool take = false;
     if (by_max) take = real && d == p.arg && p.top > -INFINITY;
-    else {
-      if (!last && a.draft) q = join_row(a.parts + ((int64_t)a.n_rows + rc) * a.chunks, a.chunks, t, false, table);
-      if (real) {
-        const double pd = p.sum > 0.0 ? Weigh(p.top, t, table)(logit<T>(a.target, rc * a.target_stride + d)) / p.sum : 0.0;
-        const double qd = !a.draft ? 1.0 : q.sum > 0.0 ? Weigh(q.top, t, table)(logit<T>(a.draft, rc * a.draft_stride + d)) / q.sum : 0.0;
-        take = (double)a.uniform[2 * (int64_t)rc] * qd < pd;
-      }
+    else if (real) {
+      const double pd = p.sum > 0.0 ? Weigh(p.top, t, table).some(zd) / p.sum : 0.0;
+      const double qd = !a.draft ? 1.0 : q.sum > 0.0 ? Weigh(q.top, t, table).some(yd) / q.sum : 0.0;
+      take = (double)u * qd < pd;
     }
     if (in && !take && (tid & 15) == 0) atomicMin(&s_end, r);
     __syncthreads();
@@ -224,147 +271,135 @@ __global__ __launch_bounds__(VT) void verify_draw_kernel(VerifyArgs a) {
   const Row p = s_p, q = s_q;
   const bool last = end + 1 >= hi;
   const int d = last ? -1 : a.ids[end + 1];
-  auto finish = [&](int token) {
-    for (int i = lo + tid; i < hi; i += VT) a.tokens[i] = i < end ? a.ids[i + 1] : i == end ? token : -1;
-    if (tid == 0) a.accepted[s] = end - lo;
+  auto finish = [&](int token) {               // by one thread: its sequence has few rows as a rule
+    a.accepted[s] = end - lo;
+    a.tokens[end] = token;
   };
+  if (chunk == 0) for (int i = lo + tid; i < hi; i += VT) if (i != end) a.tokens[i] = i < end ? a.ids[i + 1] : -1;
   if (by_max || !(p.sum > 0.0)) {
-    if (chunk == 0) finish(p.arg != 0x7fffffff ? p.arg : 0);
+    if (chunk == 0 && tid == 0) finish(p.arg != 0x7fffffff ? p.arg : 0);
     return;
   }
   const bool residual = !last && (a.draft ? q.sum > 0.0 : (unsigned)d < (unsigned)a.vocab);
   const Weigh wp(p.top, t, table), wq(q.top, t, table);
   const double ip = 1.0 / p.sum, iq = q.sum > 0.0 ? 1.0 / q.sum : 0.0;
-  // the weights that the draw goes by, of a thread's logits of chunk c
-  auto weights = [&](int c, bool rest, double (&w)[PER]) {
+  // the weights that the draw goes by, of a lane's logits of a piece
+  auto weights = [&](int piece, bool rest, double (&w)[PER]) {
     float z[PER], y[PER];
-    load_chunk<T>(a.target, end * a.target_stride, c, a.vocab, z);
-    if (rest && a.draft) load_chunk<T>(a.draft, end * a.draft_stride, c, a.vocab, y);
+    load_piece<T>(a.target, end * a.target_stride, piece, a.vocab, lane, z);
+    if (rest && a.draft) load_piece<T>(a.draft, end * a.draft_stride, piece, a.vocab, lane, y);
 #pragma unroll
-    for (int e = 0; e < PER; ++e) w[e] = wp(z[e]) * ip;
+    for (int e = 0; e < PER; ++e) w[e] = wp(usable(z[e])) * ip;
     if (!rest) return;
     if (a.draft) {
 #pragma unroll
-      for (int e = 0; e < PER; ++e) w[e] = fmax(w[e] - wq(y[e]) * iq, 0.0);
+      for (int e = 0; e < PER; ++e) w[e] = fmax(w[e] - wq(usable(y[e])) * iq, 0.0);
     } else {
 #pragma unroll
-      for (int e = 0; e < PER; ++e) if (id_of(c, e, VEC) == d) w[e] = fmax(w[e] - 1.0, 0.0);
+      for (int e = 0; e < PER; ++e) if (id_of(piece, e, VEC, lane) == d) w[e] = fmax(w[e] - 1.0, 0.0);
     }
   };
   double w[PER];
   if (residual) {
-    weights(chunk, true, w);
+    weights(chunk * 4 + wave, true, w);
     double sum = 0.0;
 #pragma unroll
     for (int e = 0; e < PER; ++e) sum += w[e];
     sum = wave_sum_f64(sum);
-    if (lane == 0) ds[wave] = sum;
+    double* const mine = a.left + (int64_t)s * 4 * a.chunks + chunk * 4 + wave;
+    if (lane == 0) __hip_atomic_store(mine, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the sums are where every XCD finds them
     __syncthreads();
-    if (tid == 0) {
-      __hip_atomic_store(a.left + (int64_t)s * a.chunks + chunk, ((ds[0] + ds[1]) + ds[2]) + ds[3], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      s_last = __hip_atomic_fetch_add(a.done + s, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
-    }
+    if (tid == 0) s_last = __hip_atomic_fetch_add(a.done + s, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
     __syncthreads();
     if (!s_last) return;
   } else if (chunk != 0) return;
-  // one workgroup is left of the sequence's: the chunk that the number falls into, then the run of a wave's logits in it, the lane, the logit
+  if (wave != 0) return;
+  // One wave is left of the sequence's: the piece that the number falls into, then the run of 64 lanes' logits in it, the lane, the logit.
+  // (Sums in another order may fall short of the aim: then the last one that holds anything.)
   const double u = a.uniform[2 * (int64_t)end + 1];
-  double total = 0.0;
   bool rest = residual;
   auto part = [&](int c) {
-    return rest ? __hip_atomic_load(a.left + (int64_t)s * a.chunks + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)
-                : a.parts[(int64_t)end * a.chunks + c].sum * wp(a.parts[(int64_t)end * a.chunks + c].top) * ip;
+    if (c >= a.pieces) return 0.0;
+    if (rest) return __hip_atomic_load(a.left + (int64_t)s * 4 * a.chunks + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const RowPart x = a.parts[(int64_t)end * a.pieces + c];
+    return x.sum * wp(x.top) * ip;
   };
-  // (all chunks' parts by all threads, 256 at a time, and then in their order; chunks of more than 2^20 tokens come in several turns)
-  auto walk = [&](auto&& each) {
-    for (int c0 = 0; c0 < a.chunks; c0 += VT) {
-      __syncthreads();
-      if (c0 + tid < a.chunks) chunk_sum[tid] = part(c0 + tid);
-      __syncthreads();
-      const int n = min(VT, a.chunks - c0);
-      for (int i = 0; i < n; ++i) if (each(c0 + i, chunk_sum[i])) return;
-    }
+  auto all = [&]() {
+    double x = 0.0;
+    for (int c = lane; c < a.pieces; c += WAVE) x += part(c);
+    return wave_sum_f64(x);
   };
-  auto add = [&](int, double x) { total += x; return false; };
-  walk(add);
-  if (rest && !(total > 0.0)) {                 // p and q are the same: from p
-    rest = false;
-    total = 0.0;
-    walk(add);
-  }
+  double total = all();
+  if (rest && !(total > SOME)) { rest = false; total = all(); }      // p and q are the same: from p
   const double aim = u * total;
   double before = 0.0, upto = 0.0;
   int pick = 0;
-  walk([&](int c, double x) {
-    if (x > 0.0) { pick = c; before = upto; }
-    upto += x;
-    return x > 0.0 && upto > aim;               // (else the last one that holds anything: sums in another order may fall short of the aim)
-  });
+  for (int c0 = 0; c0 < a.pieces; c0 += WAVE) {
+    const double x = part(c0 + lane), up = scan_f64(x, lane);
+    const unsigned long long some = __ballot(x > SOME), past = __ballot(x > SOME && upto + up > aim);
+    if (past || some) {
+      const int l = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
+      pick = c0 + l;
+      before = upto + lane_f64(up - x, l);
+    }
+    if (past) break;
+    upto += lane_f64(up, 63);
+  }
   weights(pick, rest, w);
-  double mine[RUNS];
+  int token = 0;
+  bool found = false;
 #pragma unroll
   for (int v = 0; v < RUNS; ++v) {
-    mine[v] = 0.0;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) mine[v] += w[v * VEC + e];
-    const double x = wave_sum_f64(mine[v]);
-    if (lane == 0) seg[v * 4 + wave] = x;
-  }
-  if (tid == 0) s_token = 0;
-  __syncthreads();
-  upto = before;
-  int at = -1;
-#pragma unroll
-  for (int i = 0; i < RUNS * 4; ++i) {
-    const double x = seg[i];
-    if (x > 0.0 && (at < 0 || !(upto > aim))) { at = i; before = upto; }
-    if (at < 0 || !(upto > aim)) upto += x;
-  }
-  if (at >= 0 && (at & 3) == wave) {
     double x = 0.0;
 #pragma unroll
-    for (int v = 0; v < RUNS; ++v) if (v == at >> 2) x = mine[v];
-    double up = x;
-#pragma unroll
-    for (int o = 1; o < WAVE; o <<= 1) { const double y = __shfl_up(up, o, WAVE); if (lane >= o) up += y; }
-    const unsigned long long some = __ballot(x > 0.0), past = __ballot(x > 0.0 && before + up > aim);
-    const int who = past ? __builtin_ctzll(past) : some ? 63 - __builtin_clzll(some) : -1;
-    if (lane == who) {
+    for (int e = 0; e < VEC; ++e) x += w[v * VEC + e];
+    const double up = scan_f64(x, lane);
+    const unsigned long long some = __ballot(x > SOME), past = __ballot(x > SOME && before + up > aim);
+    if (!found && (past || some)) {
+      const int l = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
       double run = before + (up - x);
-      int token = 0;
-      bool found = false;
+      int mine = 0;
+      bool over = false;
 #pragma unroll
-      for (int v = 0; v < RUNS; ++v)
-        if (v == at >> 2)
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            const double y = w[v * VEC + e];
-            if (!found && y > 0.0) { token = id_of(pick, v * VEC + e, VEC); run += y; found = run > aim; }
-          }
-      s_token = token;
+      for (int e = 0; e < VEC; ++e) {
+        const double y = w[v * VEC + e];
+        if (!over && y > SOME) { mine = id_of(pick, v * VEC + e, VEC, lane); run += y; over = run > aim; }
+      }
+      token = __builtin_amdgcn_readlane(mine, l);
+      found = past != 0;
     }
+    before += lane_f64(up, 63);
   }
-  __syncthreads();
-  finish(s_token);
+  if (lane == 0) finish(token);
 }
 
-struct VerifyPlan { int chunks; uint64_t part_bytes, left_bytes, done_bytes; };
+struct VerifyPlan { int chunks, pieces; uint64_t part_bytes, left_bytes, done_bytes; };
 
 int check_verify(int n_seqs, int n_rows, int vocab, int dtype, VerifyPlan* p) {
   if (n_seqs < 1 || n_rows < 0 || vocab < 1 || dtype < PPD_FP32 || dtype > PPD_FP16) return PPD_EINVAL;
   if (n_seqs > PPD_MAX_SEQS || n_rows > PPD_MAX_TOKENS || vocab > VERIFY_MAX_VOCAB) return PPD_ELIMIT;
   p->chunks = (vocab + CHUNK - 1) / CHUNK;
   if ((int64_t)n_rows * p->chunks > 1 << 23) return PPD_ELIMIT;
-  p->part_bytes = (uint64_t)2 * n_rows * p->chunks * sizeof(RowPart);
-  p->left_bytes = (uint64_t)n_seqs * p->chunks * sizeof(double);
+  p->pieces = (vocab + PIECE - 1) / PIECE;
+  p->part_bytes = (uint64_t)2 * n_rows * p->pieces * sizeof(RowPart);
+  p->left_bytes = (uint64_t)n_seqs * p->chunks * 4 * sizeof(double);
   p->done_bytes = (uint64_t)n_seqs * sizeof(unsigned);
   return PPD_OK;
+}
+
+// Pieces that a wave takes in turn: as many as leave every unit two dozen waves (its places at the kernel's registers), eight at most.  bf16, a
+// target and drafts' logits, us of the launch: 901 rows of 32000 at 4 / 8 pieces 42.2 / 41.4, 163 of 50272 at 1 / 3 pieces 12.7 / 13.4.
+int run_of(int pieces, int n_rows, bool draft) {
+  const int64_t run = (int64_t)n_rows * (draft ? 2 : 1) * pieces / (256 * 24);
+  return run < 1 ? 1 : run > 8 ? 8 : (int)run;
 }
 
 template <typename T>
 hipError_t verify_go(const VerifyArgs& a, hipStream_t st) {
   if (a.n_rows > 0) {
-    hipLaunchKernelGGL(verify_rows_kernel<T>, dim3(a.n_rows * a.chunks, a.draft ? 2 : 1), dim3(VT), 0, st, a);
+    const int64_t waves = (int64_t)a.n_rows * ((a.pieces + a.run - 1) / a.run);
+    hipLaunchKernelGGL(verify_rows_kernel<T>, dim3((unsigned)((waves + 3) / 4), a.draft ? 2 : 1), dim3(VT), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -395,7 +430,8 @@ extern "C" int ppd_verify_drafts(int n_seqs, int n_rows, int vocab, int dtype, c
   const uintptr_t words = (uintptr_t)row_start | (uintptr_t)ids | (uintptr_t)temperature | (uintptr_t)uniform | (uintptr_t)tokens | (uintptr_t)accepted;
   if ((words & 3) || (((uintptr_t)target_logits | (uintptr_t)draft_logits) & (elem_size(dtype) - 1))) return PPD_EINVAL;
   if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < p.part_bytes + p.left_bytes + p.done_bytes) return PPD_EINVAL;
-  VerifyArgs a = {row_start, ids, target_logits, draft_logits, target_stride, draft_stride, temperature, uniform, tokens, accepted, n_seqs, n_rows, vocab, p.chunks,
+  VerifyArgs a = {row_start, ids, target_logits, draft_logits, target_stride, draft_stride, temperature, uniform, tokens, accepted,
+                  n_seqs, n_rows, vocab, p.chunks, p.pieces, run_of(p.pieces, n_rows, draft_logits != nullptr),
                   (RowPart*)workspace, (double*)((char*)workspace + p.part_bytes), (unsigned*)((char*)workspace + p.part_bytes + p.left_bytes)};
   hipStream_t st = (hipStream_t)hip_stream;
   return launched(dtype == PPD_FP32 ? verify_go<float>(a, st) : dtype == PPD_BF16 ? verify_go<bf16_t>(a, st) : verify_go<f16_t>(a, st));

@@ -13,10 +13,15 @@ struct AppendArgs {
   int64_t q_tok, q_head, o_tok, o_head, k_tok, k_head, v_tok, v_head;
   int64_t kc_page, kc_pos, kc_head, vc_page, vc_pos, vc_head;
   const void *q_gain, *k_gain;
-  int heads, kv_heads, rotary, iters;
+  int heads, kv_heads, rotary;
   float eps;
   double turns[64];      // angle of pair i per position, in whole turns
 };
+
+// Four sets of heads' rows a workgroup from this many sets on: the lookups and the angles are then found once for them all, and a wave's loads
+// cover more of their wait; below, more workgroups are quicker.  us at one / four: 107 bf16 tokens of 48 rows 5.2 / 5.9, 777 fp32 ones of 36
+// half-rows 6.2 / 6.1, 4915 bf16 ones of 120 rows 104 / 59 (302 MB: 5.1 TB/s, and a large copy reaches 4.6).
+constexpr int MANY = 2048;
 
 // sin and cos of 2 pi t, t a whole number of turns and a rest: in 64 bits to the nearest quarter turn, the rest (at most an eighth, so
 // at most pi / 4) by the Taylor series, whose next terms are below 2^-29.
@@ -34,19 +39,32 @@ __device__ __forceinline__ void sincos_turns(double t, float& sn, float& cs) {
 }
 
 // A row of head_dim elements is HD / 8 lanes' work: lane l has two runs of four elements that are turned together (or, behind the rotated
-// part, copied), so that nothing crosses lanes but the norm's sum.  A workgroup has one token and `iters` times 16 (32) of its heads' rows.
-template <typename T, int HD>
+// part, copied), so that nothing crosses lanes but the norm's sum.  A workgroup has one token and ITERS times 16 (32) of its heads' rows, all
+// under way while the token's sequence, page and angles are found.
+template <typename T, int HD, int ITERS>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
   typedef typename Quad<T>::raw raw;
   constexpr int LPR = HD / 8, RPW = WAVE / LPR;
   const int tok = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l = lane % LPR, half = a.rotary / 2, turning = a.rotary / 8;
+  const int lo = l < turning ? 4 * l : a.rotary + 8 * (l - turning), hi = l < turning ? half + 4 * l : lo + 4;
+  const int rows = a.heads + 2 * a.kv_heads, first = blockIdx.y * ITERS * 4 * RPW + wave * RPW + lane / LPR;
+  raw ra[ITERS], rb[ITERS], gains[4] = {};
+#pragma unroll
+  for (int it = 0; it < ITERS; ++it) {
+    const int r = first + it * 4 * RPW;
+    const T* const src = r < a.heads ? (const T*)a.q + tok * a.q_tok + r * a.q_head
+                       : r < a.heads + a.kv_heads ? (const T*)a.k + tok * a.k_tok + (r - a.heads) * a.k_head
+                       : (const T*)a.v + tok * a.v_tok + (r - a.heads - a.kv_heads) * a.v_head;
+    if (r < rows) { ra[it] = *(const raw*)(src + lo); rb[it] = *(const raw*)(src + hi); } else { ra[it] = {}; rb[it] = {}; }
+  }
+  if (a.q_gain) { gains[0] = *(const raw*)((const T*)a.q_gain + lo); gains[1] = *(const raw*)((const T*)a.q_gain + hi); }
+  if (a.k_gain) { gains[2] = *(const raw*)((const T*)a.k_gain + lo); gains[3] = *(const raw*)((const T*)a.k_gain + hi); }
   const int s = seq_of_row(a.b, tok, lane);
   if (s < 0) return;
   const SeqRows sr = seq_rows(a.b, s);
   const int pos = sr.pos0 + (tok - sr.row0), page = page_of(a.b, s, pos);
   const int slot = page < 0 ? 0 : (int)((unsigned)pos % (unsigned)a.b.page_size);
-  const int lo = l < turning ? 4 * l : a.rotary + 8 * (l - turning), hi = l < turning ? half + 4 * l : lo + 4;
   f32x4 sn = {0.f, 0.f, 0.f, 0.f}, cs = {1.f, 1.f, 1.f, 1.f};
   if (l < turning) {
 #pragma unroll
@@ -56,24 +74,17 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
       sn[e] = u; cs[e] = w;
     }
   }
-  const int rows = a.heads + 2 * a.kv_heads;
-  for (int it = 0; it < a.iters; ++it) {
-    const int r = ((blockIdx.y * a.iters + it) * 4 + wave) * RPW + lane / LPR;
+#pragma unroll
+  for (int it = 0; it < ITERS; ++it) {
+    const int r = first + it * 4 * RPW;
     const bool is_q = r < a.heads, is_k = !is_q && r < a.heads + a.kv_heads;
-    const int h = is_q ? r : is_k ? r - a.heads : r - a.heads - a.kv_heads;
-    const bool there = r < rows && (is_q || page >= 0);
-    const T* src = nullptr; T* dst = nullptr; const T* gain = nullptr;
-    if (is_q) {
-      src = (const T*)a.q + tok * a.q_tok + h * a.q_head; dst = (T*)a.q_out + tok * a.o_tok + h * a.o_head; gain = (const T*)a.q_gain;
-    } else if (is_k) {
-      src = (const T*)a.k + tok * a.k_tok + h * a.k_head; dst = (T*)a.kc + page * a.kc_page + slot * a.kc_pos + h * a.kc_head; gain = (const T*)a.k_gain;
-    } else {
-      src = (const T*)a.v + tok * a.v_tok + h * a.v_head; dst = (T*)a.vc + page * a.vc_page + slot * a.vc_pos + h * a.vc_head;
-    }
-    raw ra = {}, rb = {};
-    if (there) { ra = *(const raw*)(src + lo); rb = *(const raw*)(src + hi); }
+    T* dst;
+    if (is_q) dst = (T*)a.q_out + tok * a.o_tok + r * a.o_head;
+    else if (is_k) dst = (T*)a.kc + page * a.kc_page + slot * a.kc_pos + (r - a.heads) * a.kc_head;
+    else dst = (T*)a.vc + page * a.vc_page + slot * a.vc_pos + (r - a.heads - a.kv_heads) * a.vc_head;
     if (is_q || is_k) {
-      f32x4 x = Quad<T>::wide(ra), y = Quad<T>::wide(rb);
+      f32x4 x = Quad<T>::wide(ra[it]), y = Quad<T>::wide(rb[it]);
+      const bool gain = is_q ? a.q_gain != nullptr : a.k_gain != nullptr;
       if (gain) {
         float t = 0.f;
 #pragma unroll
@@ -83,23 +94,24 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
         t += dpp_f32<0x141>(t);
         if (LPR == 16) t += dpp_f32<0x140>(t);
         const float rs = 1.0f / sqrtf(t * (1.0f / HD) + a.eps);
-        const f32x4 ga = Quad<T>::wide(*(const raw*)(gain + lo)), gb = Quad<T>::wide(*(const raw*)(gain + hi));
+        const f32x4 ga = Quad<T>::wide(is_q ? gains[0] : gains[2]), gb = Quad<T>::wide(is_q ? gains[1] : gains[3]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) { x[e] = x[e] * rs * ga[e]; y[e] = y[e] * rs * gb[e]; }
       }
       f32x4 u, w;
 #pragma unroll
       for (int e = 0; e < 4; ++e) { u[e] = fmaf(x[e], cs[e], -(y[e] * sn[e])); w[e] = fmaf(y[e], cs[e], x[e] * sn[e]); }
-      if (l < turning || gain) { ra = Quad<T>::narrow(l < turning ? u : x); rb = Quad<T>::narrow(l < turning ? w : y); }
+      if (l < turning || gain) { ra[it] = Quad<T>::narrow(l < turning ? u : x); rb[it] = Quad<T>::narrow(l < turning ? w : y); }
     }
-    if (there) { *(raw*)(dst + lo) = ra; *(raw*)(dst + hi) = rb; }
+    if (r < rows && (is_q || page >= 0)) { *(raw*)(dst + lo) = ra[it]; *(raw*)(dst + hi) = rb[it]; }
   }
 }
 
-template <typename T>
-hipError_t append_go(const AppendArgs& a, int head_dim, dim3 grid, hipStream_t stream) {
-  if (head_dim == 64) hipLaunchKernelGGL((append_kernel<T, 64>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((append_kernel<T, 128>), grid, dim3(256), 0, stream, a);
+template <typename T, int HD>
+hipError_t append_go(const AppendArgs& a, hipStream_t stream) {
+  const int rows = a.heads + 2 * a.kv_heads, per = 4 * (WAVE / (HD / 8)), sets = (rows + per - 1) / per;
+  if ((int64_t)a.b.n_tokens * sets <= MANY) hipLaunchKernelGGL((append_kernel<T, HD, 1>), dim3(a.b.n_tokens, sets), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((append_kernel<T, HD, 4>), dim3(a.b.n_tokens, (sets + 3) / 4), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -132,10 +144,7 @@ extern "C" int ppd_paged_append(const ppd_paged_cache* cache, const ppd_paged_ba
   const double step = rotary_dim ? pow((double)rope_theta, -2.0 / rotary_dim) : 0.0;
   double turn = 1.0 / 6.283185307179586476925286766559;
   for (int i = 0; i < 64; ++i) { a.turns[i] = turn; turn *= step; }
-  const int rows = n_heads + 2 * cache->n_kv_heads, per = 4 * (WAVE / (cache->head_dim / 8)), sets = (rows + per - 1) / per;
-  a.iters = 1;
-  const dim3 grid(batch->n_tokens, sets);
   hipStream_t st = (hipStream_t)hip_stream;
-  return launched(dt == PPD_FP32 ? append_go<float>(a, cache->head_dim, grid, st)
-                  : dt == PPD_BF16 ? append_go<bf16_t>(a, cache->head_dim, grid, st) : append_go<f16_t>(a, cache->head_dim, grid, st));
+  if (cache->head_dim == 64) return launched(dt == PPD_FP32 ? append_go<float, 64>(a, st) : dt == PPD_BF16 ? append_go<bf16_t, 64>(a, st) : append_go<f16_t, 64>(a, st));
+  return launched(dt == PPD_FP32 ? append_go<float, 128>(a, st) : dt == PPD_BF16 ? append_go<bf16_t, 128>(a, st) : append_go<f16_t, 128>(a, st));
 }

@@ -82,6 +82,13 @@ def test_many_rows_and_a_padded_batch():
     check(Batch([700], [900], 2, 2, 64, F32, pad=130), (True, True), rotary=32)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_several_sets_of_rows_a_workgroup(dtype):
+    check(Batch([600, 0, 1], [610, 5, 40], 33, 11, 64, dtype, pad=4), (True, True), rotary=64)
+    check(Batch([500, 300], [500, 300], 21, 7, 128, dtype, page=20), (False, True), rotary=64)
+    check(Batch([1300, 900], [1300, 1000], 3, 1, 64, dtype), (True, False), in_place=True)
+
+
 def test_many_sequences():
     rng = np.random.default_rng(3)
     new = rng.integers(0, 3, 200)

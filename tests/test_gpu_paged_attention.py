@@ -79,6 +79,19 @@ def test_pages(page, dtype):
     check(Batch([1, 40, 3], [90, 130, 200], 4, 2, 128, dtype, page=page, seed=page))
 
 
+@pytest.mark.parametrize("page", [1, 3, 8, 16, 20, 48, 64, 100, 256])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_pages_of_long_runs(page, dtype):
+    check(Batch([100, 1, 70], [260, 5, 90], 4, 2, 128, dtype, page=page, seed=page))
+    check(Batch([100, 1, 70], [260, 5, 90], 3, 1, 64, dtype, page=page, seed=page), window=77)
+
+
+@pytest.mark.parametrize("layout", ["pkhd", "hpkd", "khpd"])
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (9, 1), (14, 2), (40, 8)])
+def test_orders_and_shared_heads_of_long_runs(layout, heads, kv_heads):
+    check(Batch([150, 67], [170, 267], heads, kv_heads, 64, F16, layout=layout, seed=heads))
+
+
 @pytest.mark.parametrize("layout", ["phkd", "pkhd", "hpkd", "khpd"])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_orders_of_the_cache(layout, dtype):
@@ -213,6 +226,24 @@ def test_one_infinite_value_is_one_infinite_component(dtype):
     hit[0, 0, 5] = True
     hit[1 + 30:, 0, 5] = True                                                 # positions 20 .. 59: from 50 on
     assert torch.isinf(o[hit]).all() and torch.isfinite(o[~hit]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_infinite_values_in_long_runs(dtype, hd):
+    """They stay in their component, and in the rows that see them."""
+    b = Batch([200, 90], [200, 300], 2, 2, hd, dtype)
+    d = b.cuda()
+    for s, p in ((0, 17), (0, 130), (1, 250)):
+        d.v_cache[b.slot(s, p)][0, 5] = -math.inf
+    out, _ = call(d)
+    clean = attention64(b)
+    tol, _ = limits(b, *clean)
+    o = out.cpu().double()
+    hit = torch.zeros_like(o, dtype=torch.bool)
+    hit[17:200, 0, 5] = True
+    hit[200 + 40:, 0, 5] = True                                               # positions 210 .. 299: from 250 on
+    assert (o[hit] == -math.inf).all() and ((o - clean[0]).abs() <= tol)[~hit].all()
 
 
 @pytest.mark.parametrize("dtype", TYPES)

@@ -259,6 +259,11 @@ def test_long_and_many():
     check(make(np.random.default_rng(0).integers(0, 4, 700).tolist(), 100, torch.bfloat16, 2))
 
 
+@pytest.mark.parametrize("vocab,with_draft,dtype", [(20013, True, torch.bfloat16), (30001, False, torch.float32), (126000, True, torch.float16)])
+def test_waves_that_take_several_pieces_of_a_row(vocab, with_draft, dtype):
+    check(make([3, 2, 4] * 33, vocab, dtype, 21, with_draft, temp=[0.8, 1.0, 0.0] * 33))
+
+
 def test_the_emitted_tokens_have_the_targets_distribution():
     """The rule's point.  40000 sequences of one draft over 12 tokens: the first emitted token's counts against p, within 5 standard
     deviations of a binomial count each (a correct rule fails one of the 12 in about 10^5 runs; the numbers are fixed)."""

@@ -289,7 +289,7 @@ def ppd_paged_append(k_cache, v_cache, pages, q_start, kv_len, q, k, v, q_gain=N
     if q is not None:
         qr, heads = _rows(q, k_cache, "q", n), q.shape[1]
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         outr = _rows(q_out, k_cache, "q_out", n, heads)
     for g in (q_gain, k_gain):
         if g is not None and (g.dtype != k_cache.dtype or g.numel() != sizes[3] or not g.is_contiguous()):
@@ -325,7 +325,7 @@ def ppd_paged_attention(q, k_cache, v_cache, pages, q_start, kv_len, scale=None,
     cache, batch, sizes = _paged_args(k_cache, v_cache, pages, q_start, kv_len, n)
     qr, heads = _rows(q, k_cache, "q", n), q.shape[1]
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     outr = _rows(out, k_cache, "out", n, heads)
     lse = torch.empty((n, heads), dtype=torch.float32, device=q.device) if want_lse else None
     if workspace is None:

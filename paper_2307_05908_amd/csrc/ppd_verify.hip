@@ -202,19 +202,32 @@ __global__ __launch_bounds__(VT, 6) void verify_rows_kernel(VerifyArgs a) {
 
 // ---- which drafts are taken, and the draw.  grid: (chunks, n_seqs)
 struct Row { float top; int arg; double sum; };
-// a row's pieces joined by 16 lanes, in all of them
-__device__ __forceinline__ Row join_row(const RowPart* p, int pieces, double t, bool by_max, const double* table) {
+// A row's pieces joined by 16 lanes, in all of them.  The first 64 pieces come in one go (before anything waits for them), the others in turn.
+struct First { RowPart x[4]; };
+__device__ __forceinline__ First first_parts(const RowPart* p, int pieces) {
+  First f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int c = (threadIdx.x & 15) + 16 * i;
+    f.x[i] = {0.0, -INFINITY, 0x7fffffff};
+    if (c < pieces) f.x[i] = p[c];
+  }
+  return f;
+}
+__device__ __forceinline__ Row join_row(const First& f, const RowPart* p, int pieces, double t, bool by_max, const double* table) {
   const int l = threadIdx.x & 15;
   Row r = {-INFINITY, 0x7fffffff, 0.0};
-  for (int c = l; c < pieces; c += 16) { const float v = p[c].top; const int i = p[c].arg; if (better(v, i, r.top, r.arg)) { r.top = v; r.arg = i; } }
+  auto larger = [&](float v, int i) { if (better(v, i, r.top, r.arg)) { r.top = v; r.arg = i; } };
 #pragma unroll
-  for (int o = 1; o < 16; o <<= 1) {
-    const float v = __shfl_xor(r.top, o, WAVE); const int i = __shfl_xor(r.arg, o, WAVE);
-    if (better(v, i, r.top, r.arg)) { r.top = v; r.arg = i; }
-  }
+  for (int i = 0; i < 4; ++i) larger(f.x[i].top, f.x[i].arg);
+  for (int c = l + 64; c < pieces; c += 16) larger(p[c].top, p[c].arg);
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) larger(__shfl_xor(r.top, o, WAVE), __shfl_xor(r.arg, o, WAVE));
   if (!by_max) {
     const Weigh weigh(r.top, t, table);
-    for (int c = l; c < pieces; c += 16) r.sum += p[c].sum * weigh(p[c].top);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.sum += f.x[i].sum * weigh(f.x[i].top);
+    for (int c = l + 64; c < pieces; c += 16) r.sum += p[c].sum * weigh(p[c].top);
     r.sum = row_sum_f64(r.sum);
   }
   return r;
@@ -250,9 +263,12 @@ __global__ __launch_bounds__(VT) void verify_draw_kernel(VerifyArgs a) {
       if (a.draft) yd = logit<T>(a.draft, rc * a.draft_stride + d);
       u = a.uniform[2 * (int64_t)rc];
     }
-    const Row p = join_row(a.parts + (int64_t)rc * a.pieces, a.pieces, t, by_max, table);
+    const RowPart *const pp = a.parts + (int64_t)rc * a.pieces, *const qp = pp + (int64_t)a.n_rows * a.pieces;
+    const bool drawn = !by_max && a.draft && !last;
+    const First fp = first_parts(pp, a.pieces), fq = first_parts(qp, drawn ? a.pieces : 0);
+    const Row p = join_row(fp, pp, a.pieces, t, by_max, table);
     Row q = {0.f, 0, 0.0};
-    if (!by_max && a.draft && !last) q = join_row(a.parts + ((int64_t)a.n_rows + rc) * a.pieces, a.pieces, t, false, table);
+    if (drawn) q = join_row(fq, qp, a.pieces, t, false, table);
     bool take = false;
     if (by_max) take = real && d == p.arg && p.top > -INFINITY;
     else if (real) {
@@ -325,9 +341,10 @@ __global__ __launch_bounds__(VT) void verify_draw_kernel(VerifyArgs a) {
     const RowPart x = a.parts[(int64_t)end * a.pieces + c];
     return x.sum * wp(x.top) * ip;
   };
+  double near;                                 // this lane's of the first 64 pieces
   auto all = [&]() {
-    double x = 0.0;
-    for (int c = lane; c < a.pieces; c += WAVE) x += part(c);
+    double x = near = part(lane);
+    for (int c = lane + WAVE; c < a.pieces; c += WAVE) x += part(c);
     return wave_sum_f64(x);
   };
   double total = all();
@@ -336,7 +353,7 @@ __global__ __launch_bounds__(VT) void verify_draw_kernel(VerifyArgs a) {
   double before = 0.0, upto = 0.0;
   int pick = 0;
   for (int c0 = 0; c0 < a.pieces; c0 += WAVE) {
-    const double x = part(c0 + lane), up = scan_f64(x, lane);
+    const double x = c0 ? part(c0 + lane) : near, up = scan_f64(x, lane);
     const unsigned long long some = __ballot(x > SOME), past = __ballot(x > SOME && upto + up > aim);
     if (past || some) {
       const int l = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);

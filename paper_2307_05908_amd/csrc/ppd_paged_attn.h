@@ -23,7 +23,8 @@ struct PagedAttnArgs {
   int tile_rows;
   int last_first;                     // tiles of a sequence from its end: the longest ones first
   float to_log2;                      // scale * log2(e): a score's exponent of two
-  int want, least;                    // parts per key/value head to aim at; blocks of a part at least (0: one part each)
+  int want, fine, least;              // parts per key/value head to aim at, and among sequences of unlike lengths; blocks of a part at least (0:
+                                      // one part each)
   float* part_o; float2* part_ml;     // [item][kv_heads][rows of a tile][head_dim], [item][kv_heads][rows of a tile]
   uint64_t* stamps; uint64_t stamp;   // paged_split_kernel, [item][kv_heads]: this call's number, once the part is there (see join_parts)
   int2* plan;                         // paged_tile_kernel, [n_seqs]: first item of a sequence, parts of its tiles
@@ -95,30 +96,41 @@ __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, bool 
   SeqPlan p;
   int len = 1;
   if (a.least > 0) {
-    float all = 0.f;
+    float all = 0.f, tiles = 0.f, longest = 0.f;
     for (int s = 0; s < a.b.n_seqs; s += WAVE) {
       seq_plan(a, s + lane, p);
       all += wave_sum((float)p.tiles * (float)p.blocks);
+      tiles += wave_sum((float)p.tiles);
+      longest = fmaxf(longest, wave_max((float)p.blocks));
     }
-    len = max(a.least, (int)ceilf(all / (float)a.want));
+    // Two workgroups run on a unit, and where lengths differ and two long parts meet on one it is the last to end: then shorter parts, if they
+    // are not too short for that.  bf16, us at `want` / `fine`: 64 sequences of 60 to 8000 positions 97 / 88, 32 of them 39.2 / 37.2, 64 of 60 to
+    // 2000 32.1 / 34.2; of like lengths, 48 of 1000 38.6 / 45.1, 16 of 2000 29.3 / 32.9.
+    const float want = longest * tiles > 2.f * all && all >= 12.f * (float)a.fine ? (float)a.fine : (float)a.want;
+    len = max(a.least, (int)ceilf(all / want));
     // few tiles: where their ends make it more parts than `want`, longer ones (a second round of workgroups for a few of them would cost more)
     for (int again = 0; again < 3 && a.b.n_seqs <= WAVE; ++again) {
       const int parts = (p.blocks + len - 1) / len;
-      const float items = wave_sum((float)(p.tiles * parts)), tiles = wave_sum((float)p.tiles);
-      if (items <= (float)a.want || 2.f * tiles > (float)a.want) break;
-      len = (int)ceilf((float)len * items / (float)a.want);
+      const float items = wave_sum((float)(p.tiles * parts));
+      if (items <= want || 2.f * tiles > want) break;
+      len = (int)ceilf((float)len * items / want);
     }
   }
-  // Tiles of several parts come first, the others fill up behind them.
-  auto items_of = [&](const SeqPlan& q, bool several) { return (q.parts > 1) == several ? q.tiles * q.parts : 0; };
+  // Tiles of several parts come first, then those of more than half a part's length, more than a quarter, and the rest: what is begun late is
+  // short.  (For up to 64 sequences, which are looked at once; more of them are gone through for each turn: two turns.)
+  auto turn_of = [&](const SeqPlan& q) {
+    if (a.least == 0) return 3;
+    if (q.parts > 1) return 0;
+    return a.b.n_seqs > WAVE || 4 * q.blocks <= len ? 3 : 2 * q.blocks <= len ? 2 : 1;
+  };
   auto parts_of = [&](const SeqPlan& q) { return a.least > 0 ? (q.blocks + len - 1) / len : q.blocks > 0 ? 1 : 0; };
   int before = 0;
   bool found = false;
-  for (int turn = a.least > 0 ? 0 : 1; turn < 2 && (tell || !found); ++turn)
+  for (int turn = a.least > 0 ? 0 : 3; turn < 4 && (tell || !found); turn += a.b.n_seqs > WAVE ? 3 : 1)
     for (int s = 0; s < a.b.n_seqs; s += WAVE) {
       if (a.b.n_seqs > WAVE || a.least == 0) seq_plan(a, s + lane, p);
       p.parts = parts_of(p);
-      const int items = items_of(p, turn == 0), upto = before + scan_up(items, lane);
+      const int items = turn_of(p) == turn ? p.tiles * p.parts : 0, upto = before + scan_up(items, lane);
       if (tell && s + lane < a.b.n_seqs && items > 0) a.plan[s + lane] = make_int2(upto - items, p.parts);
       const unsigned long long past = __ballot(upto > idx);
       if (!found && past) {

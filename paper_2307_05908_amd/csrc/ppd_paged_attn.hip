@@ -365,7 +365,7 @@ __global__ __launch_bounds__(SPLIT_THREADS, 2) void paged_split_kernel(PagedAttn
 // ---- host
 struct AttnPlan {
   bool tiles;               // paged_tile_kernel, not paged_split_kernel
-  int want, least;          // see PagedAttnArgs
+  int want, fine, least;    // see PagedAttnArgs
   int64_t items;            // workgroups per key/value head: parts aimed at, and a part's end for every tile
   uint64_t o_bytes, ml_bytes, more_bytes;      // more: stamps, or the plan
 };
@@ -382,10 +382,11 @@ int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, 
   const int64_t tiles = rows / tile_rows + some;
   const int slots = p->tiles ? 512 : 256;
   p->want = slots / cache->n_kv_heads + (slots < cache->n_kv_heads);
+  p->fine = p->tiles || tiles * cache->n_kv_heads < 160 ? p->want : p->want * 7 / 4;
   p->least = p->tiles ? 8 : 4;
   // tiles enough for the whole chip, or no position to cut at: one part each
   if (tiles >= (p->tiles ? 2 : 8) * p->want || (int64_t)batch->max_pages * cache->page_size <= p->least * PLAN_BLOCK) p->least = 0;
-  p->items = tiles + (p->least ? p->want + 1 : 0);
+  p->items = tiles + (p->least ? p->fine + 1 : 0);
   const uint64_t places = p->least ? (uint64_t)p->items * cache->n_kv_heads : 0;
   p->o_bytes = places * tile_rows * cache->head_dim * 4;
   p->ml_bytes = places * tile_rows * 8;
@@ -436,7 +437,7 @@ extern "C" int ppd_paged_attention(const ppd_paged_cache* cache, const ppd_paged
   a.q_tok = q->token; a.q_head = q->head; a.o_tok = out->token; a.o_head = out->head;
   a.kc_page = cache->k_page; a.kc_pos = cache->k_pos; a.kc_head = cache->k_head; a.vc_page = cache->v_page; a.vc_pos = cache->v_pos; a.vc_head = cache->v_head;
   a.heads = n_heads; a.kv_heads = cache->n_kv_heads; a.group = n_heads / cache->n_kv_heads; a.window = window; a.to_log2 = scale * 1.44269504f;
-  a.tile_rows = p.tiles ? TILE_ROWS : SPLIT_ROWS; a.last_first = p.tiles; a.want = p.want; a.least = p.least;
+  a.tile_rows = p.tiles ? TILE_ROWS : SPLIT_ROWS; a.last_first = p.tiles; a.want = p.want; a.fine = p.fine; a.least = p.least;
   a.part_o = (float*)workspace; a.part_ml = (float2*)((char*)workspace + p.o_bytes); a.stamps = (uint64_t*)((char*)workspace + p.o_bytes + p.ml_bytes);
   a.plan = (int2*)a.stamps;
   a.stamp = next_stamp();

@@ -254,6 +254,12 @@ def test_long_and_split(dtype):
     check(Batch([20, 1], [2500, 2000], 4, 4, 128, dtype, page=16), window=1500)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_lengths_that_differ_a_hundredfold(dtype):
+    """Cut into shorter parts than like lengths are, the longest of them first."""
+    check(Batch([1, 1, 2, 1, 1, 1, 1], [60, 6000, 1500, 300, 3000, 100, 40], 32, 32, 64, dtype))
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_many_sequences(dtype):
     rng = np.random.default_rng(5)

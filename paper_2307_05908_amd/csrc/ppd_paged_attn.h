@@ -84,10 +84,14 @@ __device__ __forceinline__ void seq_plan(const PagedAttnArgs& a, int s, SeqPlan&
   const int hi = min(p.r.pos0 + p.r.rows, a.b.room), lo = a.window > 0 ? max(p.r.pos0 - a.window + 1, 0) & -PLAN_BLOCK : 0;
   p.blocks = max(1, (hi - lo + PLAN_BLOCK - 1) / PLAN_BLOCK);
 }
-__device__ __forceinline__ int scan_up(int v, int lane) {
-#pragma unroll
-  for (int o = 1; o < WAVE; o <<= 1) { const int u = __shfl_up(v, o, WAVE); if (lane >= o) v += u; }
-  return v;
+template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_add(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int scan_up(int v) {          // sums up to the lane's: within rows of 16, then of the rows before
+  v = dpp_add<0x111, 0xf>(v);
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  v = dpp_add<0x118, 0xf>(v);
+  v = dpp_add<0x142, 0xa>(v);
+  return dpp_add<0x143, 0xc>(v);
 }
 // Every wave makes the plan for itself, from the lengths on the device: all tiles' blocks of positions together are cut into about
 // `want` parts of equal length, a tile at its own ends.  (The sum is in fp32, one order: every wave has the same; its error is far below
@@ -130,7 +134,9 @@ __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, bool 
     for (int s = 0; s < a.b.n_seqs; s += WAVE) {
       if (a.b.n_seqs > WAVE || a.least == 0) seq_plan(a, s + lane, p);
       p.parts = parts_of(p);
-      const int items = turn_of(p) == turn ? p.tiles * p.parts : 0, upto = before + scan_up(items, lane);
+      const int items = turn_of(p) == turn ? p.tiles * p.parts : 0;
+      if (!__ballot(items > 0)) continue;
+      const int upto = before + scan_up(items);
       if (tell && s + lane < a.b.n_seqs && items > 0) a.plan[s + lane] = make_int2(upto - items, p.parts);
       const unsigned long long past = __ballot(upto > idx);
       if (!found && past) {

@@ -54,16 +54,29 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const Item& i
     auto at = [&](int p) { return ((int64_t)(first + p) * a.kv_heads + kvh) * SPLIT_ROWS + rr; };
     float mx = -INFINITY, sum = 0.f;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int p = 0; p < it.parts; ++p) mx = fmaxf(mx, left(a.part_ml + at(p)).x);
-    const float ref = mx == -INFINITY ? 0.f : mx;
-#pragma unroll 4
-    for (int p = 0; p < it.parts; ++p) {
-      const float* const po = a.part_o + at(p) * HD + d;
-      const f32x2 one = left(a.part_ml + at(p)), u = left(po), w = left(po + 2);
-      const float f = __builtin_amdgcn_exp2f(one.x - ref);
-      sum = fmaf(f, one.y, sum);
-      y.x = fmaf(f, u.x, y.x); y.y = fmaf(f, u.y, y.y); y.z = fmaf(f, w.x, y.z); y.w = fmaf(f, w.y, y.w);
+    for (int p0 = 0; p0 < it.parts; p0 += 4) {            // four parts at a time, their sums and totals in one go
+      f32x2 ml[4], u[4], w[4];
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const int64_t from = at(min(p0 + p, it.parts - 1));
+        ml[p] = left(a.part_ml + from); u[p] = left(a.part_o + from * HD + d); w[p] = left(a.part_o + from * HD + d + 2);
+      }
+      const float before = mx;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) mx = fmaxf(mx, ml[p].x);
+      const float ref = mx == -INFINITY ? 0.f : mx, keep = __builtin_amdgcn_exp2f(before - ref);
+      if (p0 > 0) {
+        sum *= keep;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] *= keep;
+      }
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        if (p0 + p >= it.parts) break;
+        const float f = __builtin_amdgcn_exp2f(ml[p].x - ref);
+        sum = fmaf(f, ml[p].y, sum);
+        y.x = fmaf(f, u[p].x, y.x); y.y = fmaf(f, u[p].y, y.y); y.z = fmaf(f, w[p].x, y.z); y.w = fmaf(f, w[p].y, y.w);
+      }
     }
     const bool none = mx == -INFINITY && sum == 0.f;      // nothing seen (a score that is no number leaves its mark on the sum)
     const float inv = 1.0f / sum;

@@ -280,16 +280,28 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   const int64_t first = (int64_t)plan.x + (int64_t)(r / a.tile_rows) * parts;
   float mx = -INFINITY, sum = 0.f;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < parts; ++p) mx = fmaxf(mx, a.part_ml[((first + p) * a.kv_heads + kvh) * a.tile_rows + r % a.tile_rows].x);
-  const float ref = mx == -INFINITY ? 0.f : mx;
-  for (int p = 0; p < parts; ++p) {
-    const int64_t at = ((first + p) * a.kv_heads + kvh) * a.tile_rows + r % a.tile_rows;
-    const float2 ml = a.part_ml[at];
-    const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-    sum = fmaf(f, ml.y, sum);
-    const f32x4 z = *(const f32x4*)(a.part_o + at * HD + d);
+  for (int p0 = 0; p0 < parts; p0 += 4) {                  // four parts at a time, their sums and totals in one go
+    float2 ml[4];
+    f32x4 z[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = fmaf(f, z[e], y[e]);
+    for (int p = 0; p < 4; ++p) {
+      const int64_t at = ((first + min(p0 + p, parts - 1)) * a.kv_heads + kvh) * a.tile_rows + r % a.tile_rows;
+      ml[p] = a.part_ml[at];
+      z[p] = *(const f32x4*)(a.part_o + at * HD + d);
+    }
+    const float before = mx;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) mx = fmaxf(mx, ml[p].x);
+    const float ref = mx == -INFINITY ? 0.f : mx, keep = __builtin_amdgcn_exp2f(before - ref);
+    if (p0 > 0) { sum *= keep; y *= keep; }
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      if (p0 + p >= parts) break;
+      const float f = __builtin_amdgcn_exp2f(ml[p].x - ref);
+      sum = fmaf(f, ml[p].y, sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = fmaf(f, z[p][e], y[e]);
+    }
   }
   const bool none = mx == -INFINITY && sum == 0.f;
   const float inv = 1.0f / sum;

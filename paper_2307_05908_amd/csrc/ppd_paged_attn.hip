@@ -390,7 +390,12 @@ int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, 
   if (n_heads > PPD_MAX_HEADS || (int64_t)batch->n_tokens * (n_heads / cache->n_kv_heads) > 1 << 26) return PPD_ELIMIT;
   const int group = n_heads / cache->n_kv_heads;
   const int64_t rows = (int64_t)batch->n_tokens * group, some = batch->n_tokens < batch->n_seqs ? batch->n_tokens : batch->n_seqs;
-  p->tiles = cache->dtype != PPD_FP32 && rows > 32 * (int64_t)batch->n_seqs;
+  const int64_t capacity = (int64_t)batch->max_pages * cache->page_size;
+  // Which kernel: paged_tile_kernel for 16-bit types and more than 32 rows a sequence (bf16, 8 key/value heads, 2000 positions, us of the split /
+  // the tile kernel: 8 sequences of 16 rows 21.2 / 21.9, of 32 25.4 / 22.5, of 48 32.2 / 23.8; 32 of 32 54.7 / 52.2), but not where these are
+  // few in all, over no great lengths: the split kernel then has more workgroups to fill the chip with (one sequence of 128 rows over 200 positions
+  // 9.1 / 12.5, over 2000 17.3 / 21.6, over 20000 66 / 44).
+  p->tiles = cache->dtype != PPD_FP32 && rows > 32 * (int64_t)batch->n_seqs && (rows * cache->n_kv_heads > 1024 || capacity > 8192);
   const int tile_rows = p->tiles ? TILE_ROWS : SPLIT_ROWS;
   const int64_t tiles = rows / tile_rows + some;
   const int slots = p->tiles ? 512 : 256;
@@ -398,7 +403,7 @@ int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, 
   p->fine = p->tiles || tiles * cache->n_kv_heads < 160 ? p->want : p->want * 7 / 4;
   p->least = p->tiles ? 8 : 4;
   // tiles enough for the whole chip, or no position to cut at: one part each
-  if (tiles >= (p->tiles ? 2 : 8) * p->want || (int64_t)batch->max_pages * cache->page_size <= p->least * PLAN_BLOCK) p->least = 0;
+  if (tiles >= (p->tiles ? 2 : 8) * p->want || capacity <= p->least * PLAN_BLOCK) p->least = 0;
   p->items = tiles + (p->least ? p->fine + 1 : 0);
   const uint64_t places = p->least ? (uint64_t)p->items * cache->n_kv_heads : 0;
   p->o_bytes = places * tile_rows * cache->head_dim * 4;

@@ -55,6 +55,7 @@ SHAPES = {
     "runs": ([16, 17, 0, 33, 2], [16, 80, 5, 33, 300]),
     "chunk": ([130, 1], [257, 90]),
     "prompt": ([200], [200]),
+    "prompts": ([300, 250], [300, 400]),
 }
 
 
@@ -82,14 +83,14 @@ def test_pages(page, dtype):
 @pytest.mark.parametrize("page", [1, 3, 8, 16, 20, 48, 64, 100, 256])
 @pytest.mark.parametrize("dtype", [BF16, F16])
 def test_pages_of_long_runs(page, dtype):
-    check(Batch([100, 1, 70], [260, 5, 90], 4, 2, 128, dtype, page=page, seed=page))
-    check(Batch([100, 1, 70], [260, 5, 90], 3, 1, 64, dtype, page=page, seed=page), window=77)
+    check(Batch([100, 1, 70], [260, 5, 90], 8, 2, 128, dtype, page=page, seed=page))
+    check(Batch([100, 1, 70], [260, 5, 90], 9, 1, 64, dtype, page=page, seed=page), window=77)
 
 
 @pytest.mark.parametrize("layout", ["pkhd", "hpkd", "khpd"])
 @pytest.mark.parametrize("heads,kv_heads", [(1, 1), (9, 1), (14, 2), (40, 8)])
 def test_orders_and_shared_heads_of_long_runs(layout, heads, kv_heads):
-    check(Batch([150, 67], [170, 267], heads, kv_heads, 64, F16, layout=layout, seed=heads))
+    check(Batch([550, 500], [570, 700], heads, kv_heads, 64, F16, layout=layout, seed=heads))
 
 
 @pytest.mark.parametrize("layout", ["phkd", "pkhd", "hpkd", "khpd"])
@@ -100,8 +101,9 @@ def test_orders_of_the_cache(layout, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("window", [1, 2, 16, 63, 64, 65, 100, 1000])
-def test_windows(dtype, window):
-    b = Batch([1, 40, 3, 150], [190, 130, 200, 333], 4, 2, 64, dtype, seed=window)
+@pytest.mark.parametrize("heads", [4, 8])
+def test_windows(dtype, window, heads):
+    b = Batch([1, 40, 3, 150], [190, 130, 200, 333], heads, 2, 64, dtype, seed=window)
     check(b, window=window)
     # pages that no row's window reaches any more are given back
     for s, (m, x) in enumerate(zip(b.new, b.kv)):
@@ -157,14 +159,16 @@ def test_rows_that_see_nothing(dtype):
     b = Batch([5, 3, 70, 2], [2, 0, 60, 40], 4, 2, 64, dtype, spare=8)        # kv below the rows: the first ones have no position
     b.pages[3, :] = -1                                                        # a sequence without any page
     check(b)
+    check(Batch([5, 3, 300, 2], [2, 0, 260, 40], 8, 2, 64, dtype))
     b = Batch([1, 1], [0, 33], 4, 2, 64, dtype)
     check(b)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-def test_pages_that_are_not_there(dtype):
+@pytest.mark.parametrize("heads", [4, 16])
+def test_pages_that_are_not_there(dtype, heads):
     """Holes, numbers that are no page's, lengths behind the table."""
-    b = Batch([3, 70, 1, 2], [200, 170, 300, 90], 4, 2, 128, dtype, spare=4)
+    b = Batch([3, 70, 1, 2], [200, 170, 300, 90], heads, 2, 128, dtype, spare=4)
     b.pages[0, 3], b.pages[0, 11], b.pages[1, 0], b.pages[1, 5] = -1, b.n_pages, 2 ** 31 - 1, -2 ** 31
     b.pages = b.pages[:, :15].contiguous()
     check(b)
@@ -178,9 +182,10 @@ def test_pages_that_are_not_there(dtype):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-def test_what_is_not_seen_has_no_part(dtype, hd, bad):
+@pytest.mark.parametrize("heads", [4, 8])
+def test_what_is_not_seen_has_no_part(dtype, hd, bad, heads):
     """NaN and infinities in free slots, in other sequences' pages, outside the window and in later tokens."""
-    b = Batch([1, 60, 4, 140], [90, 77, 30, 140], 4, 2, hd, dtype)
+    b = Batch([1, 60, 4, 140], [90, 77, 30, 140], heads, 2, hd, dtype)
     ref = attention64(b)
     d = b.cuda()
     used = torch.zeros(b.n_pages, b.page, dtype=torch.bool)
@@ -202,7 +207,7 @@ def test_what_is_not_seen_has_no_part(dtype, hd, bad):
     late = out[first + 60 - 40:first + 60].cpu()
     assert late.isnan().any(-1).all() if math.isnan(bad) else True
     # outside the window
-    b = Batch([1, 60, 4, 140], [90, 77, 30, 140], 4, 2, hd, dtype)
+    b = Batch([1, 60, 4, 140], [90, 77, 30, 140], heads, 2, hd, dtype)
     ref = attention64(b, window=20)
     d = b.cuda()
     slot = b.slot(3, 50)
@@ -232,7 +237,7 @@ def test_one_infinite_value_is_one_infinite_component(dtype):
 @pytest.mark.parametrize("hd", [64, 128])
 def test_infinite_values_in_long_runs(dtype, hd):
     """They stay in their component, and in the rows that see them."""
-    b = Batch([200, 90], [200, 300], 2, 2, hd, dtype)
+    b = Batch([200, 90], [200, 300], 4, 4, hd, dtype)
     d = b.cuda()
     for s, p in ((0, 17), (0, 130), (1, 250)):
         d.v_cache[b.slot(s, p)][0, 5] = -math.inf
@@ -351,6 +356,24 @@ def test_streams_replays_and_growing_lengths():
             torch.cuda.synchronize()
             want, wz = call(x)
             assert torch.equal(o, want) and torch.equal(z, wz)
+
+
+def test_replays_of_long_runs_in_parts():
+    """Their plan is made anew by every replay; the scratch memory's contents do not matter."""
+    b = Batch([200, 1, 90], [2900, 5, 700], 8, 2, 128, F16, extra_pages=8).cuda()
+    for s in range(3):
+        b.pages[s] = torch.randint(0, b.n_pages, (b.pages.shape[1],), dtype=torch.int32)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = call(b)
+    for i in range(4):
+        b.kv_len += torch.tensor([7, 100, -40], dtype=torch.int32, device="cuda")
+        b.q.copy_(torch.randn_like(b.q))
+        graph.replay()
+        o, z = out.clone(), lse.clone()
+        torch.cuda.synchronize()
+        want, wz = call(b)
+        assert torch.equal(o, want) and torch.equal(z, wz)
 
 
 def test_a_workspace_of_the_callers():

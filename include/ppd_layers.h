@@ -82,10 +82,12 @@ int ppd_paged_append(const ppd_paged_cache *cache, const ppd_paged_batch *batch,
                      const void *k_gain, float norm_eps, int rotary_dim, float rope_theta, void *hip_stream);
 
 /* Attention of the new tokens over their sequences' pages: query head h reads key/value head h / (n_heads / n_kv_heads)
- * (n_heads a multiple of n_kv_heads; PPD_ELIMIT where n_tokens * n_heads / n_kv_heads passes 2^26), out = sum_j softmax_j(scale * q . k_j) v_j over the sequence's positions j up to
- * the row's own (the new tokens' keys and values are in the pages already) and, with window > 0, the last `window` of
- * them only, its own included.  scale > 0, finite.  A row that sees no position gives zeros.  What a row does not see
- * has no part in its result, whatever its bits (infinities, NaN, pages of other sequences).
+ * (n_heads a multiple of n_kv_heads; PPD_ELIMIT where n_tokens * n_heads / n_kv_heads passes 2^26),
+ *   out = sum_j softmax_j(scale * q . k_j) v_j
+ * over the sequence's positions j up to the row's own (the new tokens' keys and values are in the pages already) and, with
+ * window > 0, the last `window` of them only, its own included.  scale > 0, finite.  A row that sees no position gives
+ * zeros.  What a row does not see has no part in its result, whatever its bits (infinities, NaN, pages of other
+ * sequences).
  * lse: DEVICE float [n_tokens][n_heads] or NULL: log of the sum of exp(scale * q . k_j), -inf where nothing is seen (for
  * a merge with attention over other positions).
  * Scores, softmax and sums are fp32; results do not depend on what else is in the batch beyond the order of additions
@@ -111,10 +113,11 @@ int ppd_paged_attention_workspace(const ppd_paged_cache *cache, const ppd_paged_
  *   and behind the last draft, all being taken, from p: the lowest id whose cumulative mass, in id order, exceeds
  *   uniform[r][1] times the whole.
  * temperature: DEVICE float [n_seqs], or NULL: 1 for all.  t <= 0 (or NaN): arg max, ties to the lowest id; a draft is
- * taken if it is the arg max, and neither draft_logits nor uniform have a say.  Probabilities and their sums are fp64.
- * Logits of -inf and NaN have probability 0 (tokens that top-k or top-p filtering took out); a row of nothing else
- * takes no draft and gives token 0, as an arg max of it does; where a row has +inf, only those count, equally.  Drafts outside
- * [0, vocab) are not taken.  uniform: DEVICE float [n_rows][2] in [0, 1).
+ * taken if it is the arg max, and neither draft_logits nor uniform have a say.  Probabilities and their sums are fp64;
+ * those below 2^-900 of the largest count as 0.  Logits of -inf and NaN have probability 0 (tokens that top-k or top-p
+ * filtering took out); a row of nothing else takes no draft and gives token 0, as an arg max of it does; +inf counts as
+ * the type's largest finite number would in fp32 (tokens that have it share the row).  Drafts outside [0, vocab) are not
+ * taken.  uniform: DEVICE float [n_rows][2] in [0, 1).
  * Out, DEVICE: tokens int32 [n_rows]: at a sequence's rows the drafts taken, then the drawn token, then -1; accepted
  * int32 [n_seqs]: the number of drafts taken (the sequence gained that many tokens and one more; 0 for one without
  * rows).  Rows of no sequence are not touched.  vocab 1 .. 2^24, n_rows 0 .. PPD_MAX_TOKENS, n_seqs 1 .. PPD_MAX_SEQS,

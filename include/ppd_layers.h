@@ -85,14 +85,15 @@ int ppd_paged_append(const ppd_paged_cache *cache, const ppd_paged_batch *batch,
  * (n_heads a multiple of n_kv_heads; PPD_ELIMIT where n_tokens * n_heads / n_kv_heads passes 2^26),
  *   out = sum_j softmax_j(scale * q . k_j) v_j
  * over the sequence's positions j up to the row's own (the new tokens' keys and values are in the pages already) and, with
- * window > 0, the last `window` of them only, its own included.  scale > 0, finite.  A row that sees no position gives
+ * window > 0, the last `window` of them only, its own included.  scale > 0, at most 2^127.  A row that sees no position gives
  * zeros.  What a row does not see has no part in its result, whatever its bits (infinities, NaN, pages of other
  * sequences).
  * lse: DEVICE float [n_tokens][n_heads] or NULL: log of the sum of exp(scale * q . k_j), -inf where nothing is seen (for
  * a merge with attention over other positions).
- * Scores, softmax and sums are fp32; results do not depend on what else is in the batch beyond the order of additions
- * (a sequence's positions are cut into as many parts as the batch leaves compute units for), and two calls with the same
- * arguments give the same bits.
+ * Scores, softmax and sums are fp32.  A 16-bit type's softmax weights go into their product with the values as two terms
+ * of the type, or, where the batch has more than 32 rows a sequence, rounded to it.  Beyond that and the order of additions
+ * (a sequence's positions are cut into as many parts as the batch leaves compute units for) results do not depend on what
+ * else is in the batch, and two calls with the same arguments give the same bits.
  * workspace: DEVICE scratch of at least the bytes that ppd_paged_attention_workspace gives for the same arguments (it
  * depends on sizes only, not on lengths), 16-byte aligned; NULL where those are 0.  PPD_EINVAL if workspace_bytes is less. */
 int ppd_paged_attention(const ppd_paged_cache *cache, const ppd_paged_batch *batch, int n_heads, const ppd_rows *q,

@@ -450,7 +450,7 @@ extern "C" int ppd_paged_attention(const ppd_paged_cache* cache, const ppd_paged
   const int rc = check_attention(cache, batch, n_heads, &p);
   if (rc) return rc;
   const int dt = cache->dtype, n = batch->n_tokens;
-  if (!(scale > 0.f && isfinite(scale)) || window < 0) return PPD_EINVAL;
+  if (!(scale > 0.f && isfinite(scale * 1.44269504f)) || window < 0) return PPD_EINVAL;
   if (n == 0) return PPD_OK;
   if (!good_rows(q, n, n_heads, dt, false) || !good_rows(out, n, n_heads, dt, true) || ((uintptr_t)lse & 3)) return PPD_EINVAL;
   const uint64_t need = p.o_bytes + p.ml_bytes + p.more_bytes;

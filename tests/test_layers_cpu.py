@@ -73,6 +73,7 @@ def test_bad_rows(kw):
 def test_bad_attention_arguments():
     assert attention(heads=0) == EINVAL and attention(heads=12) == EINVAL and attention(heads=1032, c=cache(n_kv_heads=8)) == ELIMIT
     assert attention(scale=0.0) == EINVAL and attention(scale=-1.0) == EINVAL and attention(scale=float("nan")) == EINVAL and attention(scale=float("inf")) == EINVAL
+    assert attention(scale=3e38) == EINVAL                                                            # (its product with log2 e is not finite)
     assert attention(window=-1) == EINVAL and attention(lse=ctypes.c_void_p(4098)) == EINVAL
     assert attention(out=rows(token=0)) == EINVAL and attention(out=rows(head=0)) == EINVAL          # rows written onto each other
 

@@ -1,9 +1,10 @@
 // ppd_paged_attention, many rows: bound by the issue of instructions: a 32 x 32 x 16 product keeps its SIMD's vector units from the other wave
 // for two thirds of its 32 cycles, and a block of 64 positions is 32 products of a wave, 32 exponentials and 160 other vector instructions.
-// Two bf16 prompts of 3700 to 4096 tokens (32 heads, 8 of keys and values, 259 GFLOP): 283 us, 915 TFLOP/s; a large matrix product of the
+// Two bf16 prompts of 3700 to 4096 tokens (32 heads, 8 of keys and values, 259 GFLOP): 277 us, 935 TFLOP/s; a large matrix product of the
 // library's reaches 1200.  Products 46 % of the cycles, vector instructions 46 %, LDS 31 %.
-// (Tried and not kept: the next block's scores between this one's exponentials, 286 to 292 us; a higher priority for the waves in products or
-// in exponentials, 284 to 292; offsets kept in registers from block to block, 281 to 287.)
+// (Tried and not kept, beside 283 us at the time: the next block's scores between this one's exponentials, 286 to 292; a higher priority for
+// the waves in products or in exponentials, 284 to 292; offsets kept in registers from block to block, 281 to 287.  Blocks of 32 positions and three
+// workgroups a unit: 278 beside 279, 500 tokens over 4000 positions 81 beside 77, head_dim 64 113 beside 100.)
 #include "ppd_paged_attn.h"
 
 namespace ppd {
@@ -55,14 +56,17 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
     for (int i = 0; i < HD / 16; ++i) q[i] = *(const u32x4*)(p + i * 32);
   }
   const int blocks = (it.hi - it.lo + KV - 1) / KV;
-  // The table's entry for, and the slot of, the block's position `lane`: asked for here, looked at when the block is requested, a whole block
-  // later.  (Looked at here it would wait for the transfers that are under way.)
-  int entry, slot;
+  // The table's entry for, and the slot of, a block's position `lane`: asked for a block before it is looked at, when the block is requested.
+  // (Looked at at once it would wait for the transfers that are under way.)  From block to block both move on by the same step.
   const int32_t* const table = a.b.pages + (int64_t)it.s * a.b.pages_stride;
-  auto place = [&](int n) {
-    const int p = it.lo + n * KV + lane, i = (int)((unsigned)p / (unsigned)a.b.page_size);
-    slot = p - i * a.b.page_size;
-    entry = table[min(i, a.b.max_pages - 1)];
+  int index = (int)((unsigned)(it.lo + lane) / (unsigned)a.b.page_size), slot = it.lo + lane - index * a.b.page_size;
+  const int more_index = KV / a.b.page_size, more_slot = KV - more_index * a.b.page_size;
+  int entry = table[min(index, a.b.max_pages - 1)];
+  auto place = [&]() {
+    slot += more_slot;
+    index += more_index;
+    if (slot >= a.b.page_size) { slot -= a.b.page_size; ++index; }
+    entry = table[min(index, a.b.max_pages - 1)];
   };
   uint64_t have_next = 0;
   const char* const kbase = (const char*)a.kc + (int64_t)kvh * a.kc_head * 2;
@@ -195,9 +199,8 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       if (__ballot(seen) && lane == 0) { atomicMin(&s_odd[0], n); atomicMax(&s_odd[1], n); }
     }
   };
-  place(0);
   if (blocks > 0) request(0);
-  place(1);
+  place();
   // the queries are waited for here: a wait in the loop would be one for the transfers, of which the compiler knows nothing
 #pragma unroll
   for (int i = 0; i < HD / 16; ++i) asm volatile("" : "+v"(q[i]));
@@ -206,7 +209,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
     __syncthreads();
     const uint64_t have = have_next;
     if (n + 1 < blocks) request(n + 1);
-    place(n + 2);
+    place();
     const int base = it.lo + n * KV;
     if (!(have == ~0ull && base + KV - 1 <= tile_first && (a.window == 0 || base >= tile_last - a.window + 1))) {
       clean(n, base, have);

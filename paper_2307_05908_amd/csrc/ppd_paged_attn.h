@@ -21,7 +21,6 @@ struct PagedAttnArgs {
   int64_t kc_page, kc_pos, kc_head, vc_page, vc_pos, vc_head;
   int heads, kv_heads, group, window;
   int tile_rows;
-  int last_first;                     // tiles of a sequence from its end: the longest ones first
   float to_log2;                      // scale * log2(e): a score's exponent of two
   int want, fine, least;              // parts per key/value head to aim at, and among sequences of unlike lengths; blocks of a part at least (0:
                                       // one part each)
@@ -73,14 +72,15 @@ struct Item {
   int lo, hi;              // positions of the part, lo a multiple of PLAN_BLOCK
 };
 
-struct SeqPlan { int tiles, blocks, parts; SeqRows r; };
+struct SeqPlan { int tiles, blocks; SeqRows r; };
+template <int TILE>
 __device__ __forceinline__ void seq_plan(const PagedAttnArgs& a, int s, SeqPlan& p) {
   p.tiles = p.blocks = 0;
   p.r = {0, 0, 0};
   if (s >= a.b.n_seqs) return;
   p.r = seq_rows(a.b, s);
   if (p.r.rows == 0) return;
-  p.tiles = (p.r.rows * a.group + a.tile_rows - 1) / a.tile_rows;              // (2^26 rows at most)
+  p.tiles = (p.r.rows * a.group + TILE - 1) / TILE;                            // (2^26 rows at most)
   const int hi = min(p.r.pos0 + p.r.rows, a.b.room), lo = a.window > 0 ? max(p.r.pos0 - a.window + 1, 0) & -PLAN_BLOCK : 0;
   p.blocks = max(1, (hi - lo + PLAN_BLOCK - 1) / PLAN_BLOCK);
 }
@@ -93,71 +93,130 @@ __device__ __forceinline__ int scan_up(int v) {          // sums up to the lane'
   v = dpp_add<0x142, 0xa>(v);
   return dpp_add<0x143, 0xc>(v);
 }
+// One part for each tile: sequence s has items from q_start[s] * group / TILE + min(s, q_start[s]) on.  That leaves room for its tiles (and sometimes
+// for one more), is known without the lengths before it, and never decreases: the last sequence that begins at or before the item has it.
+template <int TILE>
+__device__ __forceinline__ bool find_whole(const PagedAttnArgs& a, int idx, int lane, Item& it) {
+  static_assert(PPD_MAX_SEQS <= WAVE * WAVE, "two rounds of loads");
+  auto first_of = [&](int s, int row) { return row * a.group / TILE + min(s, row); };
+  int from = 0;
+  if (a.b.n_seqs > WAVE) {                                  // which 64 sequences
+    const int s = lane * WAVE;
+    const bool begun = s < a.b.n_seqs && first_of(s, min(max(a.b.q_start[min(s, a.b.n_seqs)], 0), a.b.n_tokens)) <= idx;
+    from = max(__popcll(__ballot(begun)) - 1, 0) * WAVE;
+  }
+  SeqPlan p;
+  seq_plan<TILE>(a, from + lane, p);
+  const bool begun = from + lane < a.b.n_seqs && first_of(from + lane, p.r.row0) <= idx;
+  const int w = __popcll(__ballot(begun)) - 1;
+  if (w < 0) return false;
+  it.s = from + w;
+  it.rows0 = __builtin_amdgcn_readlane(p.r.row0, w);
+  it.n = __builtin_amdgcn_readlane(p.r.rows, w);
+  it.pos0 = __builtin_amdgcn_readlane(p.r.pos0, w);
+  const int tiles = __builtin_amdgcn_readlane(p.tiles, w), r = idx - first_of(it.s, it.rows0);
+  it.tile = TILE == TILE_ROWS ? tiles - 1 - r : r;
+  it.part = 0; it.parts = 1; it.slot = idx;
+  return r >= 0 && r < tiles;
+}
+
 // Every wave makes the plan for itself, from the lengths on the device: all tiles' blocks of positions together are cut into about
 // `want` parts of equal length, a tile at its own ends.  (The sum is in fp32, one order: every wave has the same; its error is far below
-// the one item that the grid has to spare.)  False: there is no such item.
-__device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, bool tell, int lane, Item& it) {
-  SeqPlan p;
-  int len = 1;
-  if (a.least > 0) {
-    float all = 0.f, tiles = 0.f, longest = 0.f;
-    for (int s = 0; s < a.b.n_seqs; s += WAVE) {
-      seq_plan(a, s + lane, p);
-      all += wave_sum((float)p.tiles * (float)p.blocks);
-      tiles += wave_sum((float)p.tiles);
-      longest = fmaxf(longest, wave_max((float)p.blocks));
+// the one item that the grid has to spare.)  A lane looks at J sequences in turn, all lanes at once: up to 64 J sequences need one look.
+// False: there is no such item.
+template <int TILE, int J>
+__device__ __forceinline__ bool find_part(const PagedAttnArgs& a, int idx, bool tell, int lane, Item& it) {
+  int tiles[J], blocks[J];
+  SeqRows r1;                                               // (J 1: the lane's sequence)
+  const bool few = a.b.n_seqs <= WAVE * J;
+  auto look = [&](int s) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      SeqPlan p;
+      seq_plan<TILE>(a, s + lane * J + j, p);
+      tiles[j] = p.tiles; blocks[j] = p.blocks;
+      if (J == 1) r1 = p.r;
     }
-    // Two workgroups run on a unit, and where lengths differ and two long parts meet on one it is the last to end: then shorter parts, if they
-    // are not too short for that.  bf16, us at `want` / `fine`: 64 sequences of 60 to 8000 positions 97 / 88, 32 of them 39.2 / 37.2, 64 of 60 to
-    // 2000 32.1 / 34.2; of like lengths, 48 of 1000 38.6 / 45.1, 16 of 2000 29.3 / 32.9.
-    const float want = longest * tiles > 2.f * all && all >= 12.f * (float)a.fine ? (float)a.fine : (float)a.want;
-    len = max(a.least, (int)ceilf(all / want));
-    // few tiles: where their ends make it more parts than `want`, longer ones (a second round of workgroups for a few of them would cost more)
-    for (int again = 0; again < 3 && a.b.n_seqs <= WAVE; ++again) {
-      const int parts = (p.blocks + len - 1) / len;
-      const float items = wave_sum((float)(p.tiles * parts));
-      if (items <= want || 2.f * tiles > want) break;
-      len = (int)ceilf((float)len * items / want);
-    }
+  };
+  float all = 0.f, count = 0.f, longest = 0.f;
+  for (int s = 0; s < a.b.n_seqs; s += WAVE * J) {
+    look(s);
+    float x = 0.f, y = 0.f, z = 0.f;
+#pragma unroll
+    for (int j = 0; j < J; ++j) { x += (float)tiles[j] * (float)blocks[j]; y += (float)tiles[j]; z = fmaxf(z, (float)blocks[j]); }
+    all += wave_sum(x);
+    count += wave_sum(y);
+    longest = fmaxf(longest, wave_max(z));
+  }
+  // Two workgroups run on a unit, and where lengths differ and two long parts meet on one it is the last to end: then shorter parts, if they
+  // are not too short for that.  bf16, us at `want` / `fine`: 64 sequences of 60 to 8000 positions 97 / 88, 32 of them 39.2 / 37.2, 64 of 60 to
+  // 2000 32.1 / 34.2; of like lengths, 48 of 1000 38.6 / 45.1, 16 of 2000 29.3 / 32.9.
+  const float want = longest * count > 2.f * all && all >= 12.f * (float)a.fine ? (float)a.fine : (float)a.want;
+  int len = max(a.least, (int)ceilf(all / want));
+  // few tiles: where their ends make it more parts than `want`, longer ones (a second round of workgroups for a few of them would cost more)
+  for (int again = 0; again < 3 && few; ++again) {
+    float x = 0.f;
+#pragma unroll
+    for (int j = 0; j < J; ++j) x += (float)(tiles[j] * ((blocks[j] + len - 1) / len));
+    const float items = wave_sum(x);
+    if (items <= want || 2.f * count > want) break;
+    len = (int)ceilf((float)len * items / want);
   }
   // Tiles of several parts come first, then those of more than half a part's length, more than a quarter, and the rest: what is begun late is
-  // short.  (For up to 64 sequences, which are looked at once; more of them are gone through for each turn: two turns.)
-  auto turn_of = [&](const SeqPlan& q) {
-    if (a.least == 0) return 3;
-    if (q.parts > 1) return 0;
-    return a.b.n_seqs > WAVE || 4 * q.blocks <= len ? 3 : 2 * q.blocks <= len ? 2 : 1;
-  };
-  auto parts_of = [&](const SeqPlan& q) { return a.least > 0 ? (q.blocks + len - 1) / len : q.blocks > 0 ? 1 : 0; };
+  // short.  (Two turns for sequences that take more than one look.)
+  auto parts_of = [&](int j) { return (blocks[j] + len - 1) / len; };
+  auto turn_of = [&](int j) { return parts_of(j) > 1 ? 0 : !few || 4 * blocks[j] <= len ? 3 : 2 * blocks[j] <= len ? 2 : 1; };
   int before = 0;
   bool found = false;
-  for (int turn = a.least > 0 ? 0 : 3; turn < 4 && (tell || !found); turn += a.b.n_seqs > WAVE ? 3 : 1)
-    for (int s = 0; s < a.b.n_seqs; s += WAVE) {
-      if (a.b.n_seqs > WAVE || a.least == 0) seq_plan(a, s + lane, p);
-      p.parts = parts_of(p);
-      const int items = turn_of(p) == turn ? p.tiles * p.parts : 0;
-      if (!__ballot(items > 0)) continue;
-      const int upto = before + scan_up(items);
-      if (tell && s + lane < a.b.n_seqs && items > 0) a.plan[s + lane] = make_int2(upto - items, p.parts);
+  for (int turn = 0; turn < 4 && (tell || !found); turn += few ? 1 : 3)
+    for (int s = 0; s < a.b.n_seqs; s += WAVE * J) {
+      if (!few) look(s);
+      int items[J], mine = 0;
+#pragma unroll
+      for (int j = 0; j < J; ++j) { items[j] = turn_of(j) == turn ? tiles[j] * parts_of(j) : 0; mine += items[j]; }
+      if (!__ballot(mine > 0)) continue;
+      const int upto = before + scan_up(mine);
+      if (tell) {
+        int at = upto - mine;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          if (items[j] > 0) a.plan[s + lane * J + j] = make_int2(at, parts_of(j));     // (no items behind the last sequence)
+          at += items[j];
+        }
+      }
       const unsigned long long past = __ballot(upto > idx);
       if (!found && past) {
         const int w = __builtin_ctzll(past);
-        const int r = idx - __builtin_amdgcn_readlane(upto - items, w);
-        it.s = s + w;
-        it.parts = __builtin_amdgcn_readlane(p.parts, w);
-        it.rows0 = __builtin_amdgcn_readlane(p.r.row0, w);
-        it.n = __builtin_amdgcn_readlane(p.r.rows, w);
-        it.pos0 = __builtin_amdgcn_readlane(p.r.pos0, w);
+        int r = idx - (upto - mine), j0 = 0, parts = 0, its = 0;                       // (of lane w's sequences, the one that has the item)
+        bool there = false;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          if (there) continue;
+          if (r < items[j]) { there = true; j0 = j; parts = parts_of(j); its = tiles[j]; } else r -= items[j];
+        }
+        r = __builtin_amdgcn_readlane(r, w);
+        it.s = s + w * J + __builtin_amdgcn_readlane(j0, w);
+        it.parts = __builtin_amdgcn_readlane(parts, w);
+        SeqRows q;
+        if (J == 1) q = {__builtin_amdgcn_readlane(r1.row0, w), __builtin_amdgcn_readlane(r1.rows, w), __builtin_amdgcn_readlane(r1.pos0, w)};
+        else q = seq_rows(a.b, it.s);
+        it.rows0 = q.row0; it.n = q.rows; it.pos0 = q.pos0;
         it.tile = r / it.parts;
         it.part = r % it.parts;
-        if (a.last_first) it.tile = __builtin_amdgcn_readlane(p.tiles, w) - 1 - it.tile;
+        if (TILE == TILE_ROWS) it.tile = __builtin_amdgcn_readlane(its, w) - 1 - it.tile;   // (the longest ones first)
         it.slot = idx - r + it.tile * it.parts + it.part;
         found = true;
         if (!tell) break;
       }
       before = __builtin_amdgcn_readlane(upto, 63);
     }
-  if (!found) return false;
-  const int first = it.tile * a.tile_rows / a.group, last = min((it.tile * a.tile_rows + a.tile_rows - 1) / a.group, it.n - 1);
+  return found;
+}
+
+template <int TILE>
+__device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, bool tell, int lane, Item& it) {
+  if (!(a.least == 0 ? find_whole<TILE>(a, idx, lane, it) : a.b.n_seqs <= WAVE ? find_part<TILE, 1>(a, idx, tell, lane, it) : find_part<TILE, 8>(a, idx, tell, lane, it))) return false;
+  const int first = it.tile * TILE / a.group, last = min((it.tile * TILE + TILE - 1) / a.group, it.n - 1);
   const int hi = min(it.pos0 + last + 1, a.b.room), lo = a.window > 0 ? max(it.pos0 + first - a.window + 1, 0) & -PLAN_BLOCK : 0;
   const int blocks = (max(hi - lo, 0) + PLAN_BLOCK - 1) / PLAN_BLOCK, per = (blocks + it.parts - 1) / it.parts;
   it.lo = lo + min(it.part * per, blocks) * PLAN_BLOCK;

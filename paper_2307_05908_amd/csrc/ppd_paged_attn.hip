@@ -118,7 +118,7 @@ __global__ __launch_bounds__(SPLIT_THREADS, 2) void paged_split_kernel(PagedAttn
   // the heads of one part side by side: a position's keys are one run of memory, and its pieces then come at the same time
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kvh = blockIdx.x % a.kv_heads, row = lane & 15, quad = lane >> 4;
   Item it;
-  if (!find_item(a, blockIdx.x / a.kv_heads, false, lane, it)) return;
+  if (!find_item<SPLIT_ROWS>(a, blockIdx.x / a.kv_heads, false, lane, it)) return;
   const int all_rows = it.n * a.group;
   const int r = it.tile * SPLIT_ROWS + row, rc = min(r, all_rows - 1), tok = rc / a.group, head = kvh * a.group + rc % a.group;
   const int pos = r < all_rows ? it.pos0 + tok : -1;                          // what the lane's row sees ends there
@@ -461,7 +461,7 @@ extern "C" int ppd_paged_attention(const ppd_paged_cache* cache, const ppd_paged
   a.q_tok = q->token; a.q_head = q->head; a.o_tok = out->token; a.o_head = out->head;
   a.kc_page = cache->k_page; a.kc_pos = cache->k_pos; a.kc_head = cache->k_head; a.vc_page = cache->v_page; a.vc_pos = cache->v_pos; a.vc_head = cache->v_head;
   a.heads = n_heads; a.kv_heads = cache->n_kv_heads; a.group = n_heads / cache->n_kv_heads; a.window = window; a.to_log2 = scale * 1.44269504f;
-  a.tile_rows = p.tiles ? TILE_ROWS : SPLIT_ROWS; a.last_first = p.tiles; a.want = p.want; a.fine = p.fine; a.least = p.least;
+  a.tile_rows = p.tiles ? TILE_ROWS : SPLIT_ROWS; a.want = p.want; a.fine = p.fine; a.least = p.least;
   a.part_o = (float*)workspace; a.part_ml = (float2*)((char*)workspace + p.o_bytes); a.stamps = (uint64_t*)((char*)workspace + p.o_bytes + p.ml_bytes);
   a.plan = (int2*)a.stamps;
   a.stamp = next_stamp();

@@ -42,7 +42,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   __shared__ int s_odd[2];                                 // first and last block with a value that is infinite, or no number, where not every row sees it
   if (threadIdx.x == 0) { s_odd[0] = 0x7fffffff; s_odd[1] = -1; }
   Item it;
-  if (!find_item(a, idx, idx == 0 && kvh == 0 && wave == 0 && a.least > 0, lane, it)) return;
+  if (!find_item<TILE_ROWS>(a, idx, idx == 0 && kvh == 0 && wave == 0 && a.least > 0, lane, it)) return;
   const int all_rows = it.n * a.group;
   const int r0 = it.tile * TILE_ROWS + 32 * wave, r = r0 + col, rc = min(r, all_rows - 1), tok = rc / a.group, head = kvh * a.group + rc % a.group;
   const int pos = r < all_rows ? it.pos0 + tok : -1, from = a.window > 0 ? pos - a.window + 1 : 0;
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   if (parts <= 1 || h >= a.heads) return;
   const SeqRows sr = seq_rows(a.b, s);
   const int kvh = h / a.group, r = (row - sr.row0) * a.group + h % a.group;
-  const int64_t first = (int64_t)plan.x + (int64_t)(r / a.tile_rows) * parts;
+  const int64_t first = (int64_t)plan.x + (int64_t)(r / TILE_ROWS) * parts;
   float mx = -INFINITY, sum = 0.f;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
   for (int p0 = 0; p0 < parts; p0 += 4) {                  // four parts at a time, their sums and totals in one go
@@ -288,7 +288,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
     f32x4 z[4];
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-      const int64_t at = ((first + min(p0 + p, parts - 1)) * a.kv_heads + kvh) * a.tile_rows + r % a.tile_rows;
+      const int64_t at = ((first + min(p0 + p, parts - 1)) * a.kv_heads + kvh) * TILE_ROWS + r % TILE_ROWS;
       ml[p] = a.part_ml[at];
       z[p] = *(const f32x4*)(a.part_o + at * HD + d);
     }

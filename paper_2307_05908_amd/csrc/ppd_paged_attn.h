@@ -154,7 +154,7 @@ __device__ __forceinline__ bool find_part(const PagedAttnArgs& a, int idx, bool 
   const float want = longest * count > 2.f * all && all >= 12.f * (float)a.fine ? (float)a.fine : (float)a.want;
   int len = max(a.least, (int)ceilf(all / want));
   // few tiles: where their ends make it more parts than `want`, longer ones (a second round of workgroups for a few of them would cost more)
-  for (int again = 0; again < 3 && few; ++again) {
+  for (int again = 0; again < 3 && few && J == 1; ++again) {
     float x = 0.f;
 #pragma unroll
     for (int j = 0; j < J; ++j) x += (float)(tiles[j] * ((blocks[j] + len - 1) / len));
@@ -164,39 +164,46 @@ __device__ __forceinline__ bool find_part(const PagedAttnArgs& a, int idx, bool 
   }
   // Tiles of several parts come first, then those of more than half a part's length, more than a quarter, and the rest: what is begun late is
   // short.  (Two turns for sequences that take more than one look.)
-  auto parts_of = [&](int j) { return (blocks[j] + len - 1) / len; };
-  auto turn_of = [&](int j) { return parts_of(j) > 1 ? 0 : !few || 4 * blocks[j] <= len ? 3 : 2 * blocks[j] <= len ? 2 : 1; };
+  int parts[J], turns[J];
+  auto cut = [&]() {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      parts[j] = (int)((unsigned)(blocks[j] + len - 1) / (unsigned)len);
+      turns[j] = parts[j] > 1 ? 0 : !few || 4 * blocks[j] <= len ? 3 : 2 * blocks[j] <= len ? 2 : 1;
+    }
+  };
+  cut();
   int before = 0;
   bool found = false;
   for (int turn = 0; turn < 4 && (tell || !found); turn += few ? 1 : 3)
     for (int s = 0; s < a.b.n_seqs; s += WAVE * J) {
-      if (!few) look(s);
+      if (!few) { look(s); cut(); }
       int items[J], mine = 0;
 #pragma unroll
-      for (int j = 0; j < J; ++j) { items[j] = turn_of(j) == turn ? tiles[j] * parts_of(j) : 0; mine += items[j]; }
+      for (int j = 0; j < J; ++j) { items[j] = turns[j] == turn ? tiles[j] * parts[j] : 0; mine += items[j]; }
       if (!__ballot(mine > 0)) continue;
       const int upto = before + scan_up(mine);
       if (tell) {
         int at = upto - mine;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-          if (items[j] > 0) a.plan[s + lane * J + j] = make_int2(at, parts_of(j));     // (no items behind the last sequence)
+          if (items[j] > 0) a.plan[s + lane * J + j] = make_int2(at, parts[j]);     // (no items behind the last sequence)
           at += items[j];
         }
       }
       const unsigned long long past = __ballot(upto > idx);
       if (!found && past) {
         const int w = __builtin_ctzll(past);
-        int r = idx - (upto - mine), j0 = 0, parts = 0, its = 0;                       // (of lane w's sequences, the one that has the item)
+        int r = idx - (upto - mine), j0 = 0, many = 0, its = 0;                       // (of lane w's sequences, the one that has the item)
         bool there = false;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           if (there) continue;
-          if (r < items[j]) { there = true; j0 = j; parts = parts_of(j); its = tiles[j]; } else r -= items[j];
+          if (r < items[j]) { there = true; j0 = j; many = parts[j]; its = tiles[j]; } else r -= items[j];
         }
         r = __builtin_amdgcn_readlane(r, w);
         it.s = s + w * J + __builtin_amdgcn_readlane(j0, w);
-        it.parts = __builtin_amdgcn_readlane(parts, w);
+        it.parts = __builtin_amdgcn_readlane(many, w);
         SeqRows q;
         if (J == 1) q = {__builtin_amdgcn_readlane(r1.row0, w), __builtin_amdgcn_readlane(r1.rows, w), __builtin_amdgcn_readlane(r1.pos0, w)};
         else q = seq_rows(a.b, it.s);

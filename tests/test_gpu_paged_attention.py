@@ -273,6 +273,19 @@ def test_many_sequences(dtype):
     check(Batch([1] * 300, rng.integers(1, 50, 300).tolist(), 2, 2, 64, dtype))
 
 
+@pytest.mark.parametrize("seqs,kv_heads,most", [(65, 2, 900), (130, 2, 600), (530, 1, 400)])
+def test_many_sequences_in_parts(seqs, kv_heads, most):
+    rng = np.random.default_rng(seqs)
+    new = rng.integers(0, 3, seqs)
+    check(Batch(new.tolist(), (new + rng.integers(0, most, seqs)).tolist(), 3 * kv_heads, kv_heads, 64, BF16, pad=3))
+
+
+def test_many_long_runs_in_parts():
+    rng = np.random.default_rng(1)
+    new = np.where(rng.random(70) < 0.2, 0, rng.integers(30, 60, 70))
+    check(Batch(new.tolist(), (new + rng.integers(0, 700, 70)).tolist(), 2, 1, 64, F16, pad=3))
+
+
 def test_prompts_beside_tokens():
     check(Batch([1, 300, 1, 0, 64, 1, 5], [400, 300, 20, 7, 200, 1, 90], 8, 2, 128, BF16, pad=3))
     check(Batch([1, 300, 1, 0, 64, 1, 5], [400, 300, 20, 7, 200, 1, 90], 8, 8, 64, F16, pad=3), window=50)

@@ -56,12 +56,18 @@ __device__ __forceinline__ SeqRows seq_rows(const Batch& b, int s) {
   const int lo = min(max(b.q_start[s], 0), b.n_tokens), hi = min(max(b.q_start[s + 1], lo), b.n_tokens);
   return {lo, hi - lo, max(b.kv_len[s], 0) - (hi - lo)};
 }
-// The sequence of a row, or -1, by a whole wave: the last one that begins at or before it.  One round of loads for 64 sequences (a
-// binary search is a chain of as many as it has steps).
+// The sequence of a row, or -1, by a whole wave: the last one that begins at or before it.  One round of loads for 64 sequences, two for
+// more (a binary search is a chain of as many as it has steps).
 __device__ __forceinline__ int seq_of_row(const Batch& b, int row, int lane) {
-  int n = 0;
-  for (int s = lane; s - lane <= b.n_seqs; s += WAVE) n += __popcll(__ballot(s <= b.n_seqs && b.q_start[min(s, b.n_seqs)] <= row));
-  return n >= 1 && n <= b.n_seqs ? n - 1 : -1;
+  static_assert(PPD_MAX_SEQS <= WAVE * WAVE, "two rounds of loads");
+  const int end = b.q_start[b.n_seqs];
+  int from = 0;
+  if (b.n_seqs > WAVE) {
+    const int s = lane * WAVE;
+    from = max(__popcll(__ballot(s < b.n_seqs && b.q_start[min(s, b.n_seqs)] <= row)) - 1, 0) * WAVE;
+  }
+  const int s = from + lane, n = __popcll(__ballot(s < b.n_seqs && b.q_start[min(s, b.n_seqs)] <= row));
+  return n >= 1 && row < end ? from + n - 1 : -1;
 }
 // The page that holds a position of sequence s, or -1.
 __device__ __forceinline__ int page_of(const Batch& b, int s, int pos) {

@@ -243,32 +243,38 @@ def _paged_args(k_cache, v_cache, pages, q_start, kv_len, n_tokens):
     """(cache, batch) as bytes, and the sizes that a workspace depends on."""
     torch, codes = _layers()[:2]
     shape, dtype, i32 = k_cache.shape, k_cache.dtype, torch.int32
-    if len(shape) != 4 or v_cache.shape != shape or dtype not in codes or v_cache.dtype != dtype:
+    if len(shape) != 4 or v_cache.shape != shape or dtype not in codes or v_cache.dtype is not dtype:
         raise ValueError("k_cache, v_cache: [n_pages, page_size, n_kv_heads, head_dim], both float32, bfloat16 or float16")
-    ks, vs = k_cache.stride(), v_cache.stride()
-    if ks[3] != 1 or vs[3] != 1:
+    n_pages, size, kv_heads, head_dim = shape
+    k0, k1, k2, k3 = k_cache.stride()
+    v0, v1, v2, v3 = v_cache.stride()
+    if k3 != 1 or v3 != 1:
         raise ValueError("k_cache, v_cache: head_dim must be contiguous")
-    if pages.dtype != i32 or q_start.dtype != i32 or kv_len.dtype != i32:
+    if pages.dtype is not i32 or q_start.dtype is not i32 or kv_len.dtype is not i32:
         raise ValueError("pages, q_start, kv_len: int32")
     n, table = kv_len.numel(), pages.shape
     if len(table) != 2 or table[0] != n or q_start.numel() != n + 1:
         raise ValueError("pages [n_seqs, max_pages], q_start [n_seqs + 1], kv_len [n_seqs]")
-    if not (q_start.is_contiguous() and kv_len.is_contiguous()) or (table[1] > 1 and pages.stride(1) != 1):
+    most, (p0, p1) = table[1], pages.stride()
+    if not (q_start.is_contiguous() and kv_len.is_contiguous()) or (p1 != 1 and most > 1):
         raise ValueError("q_start, kv_len and the rows of pages must be contiguous")
-    pages_, size, kv_heads, head_dim = shape
     code = codes[dtype]
-    return (_PACK_CACHE(k_cache.data_ptr(), v_cache.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], pages_, size, kv_heads, head_dim, code),
-            _PACK_BATCH(q_start.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), pages.stride(0), table[1], n, n_tokens),
-            (pages_, size, kv_heads, head_dim, code, table[1], n, n_tokens))
+    return (_PACK_CACHE(k_cache.data_ptr(), v_cache.data_ptr(), k0, k1, k2, v0, v1, v2, n_pages, size, kv_heads, head_dim, code),
+            _PACK_BATCH(q_start.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), p0, most, n, n_tokens),
+            (n_pages, size, kv_heads, head_dim, code, most, n, n_tokens))
 
 
-def _rows(t, like, what, n_tokens, heads=None):
-    shape, s = t.shape, t.stride()
-    if len(shape) != 3 or shape[0] != n_tokens or shape[2] != like.shape[3] or t.dtype != like.dtype or (heads is not None and shape[1] != heads):
-        raise ValueError(what + ": [n_tokens, heads, head_dim] of the cache's type")
-    if s[2] != 1:
-        raise ValueError(what + ": head_dim must be contiguous")
-    return _PACK_ROWS(t.data_ptr(), s[0], s[1])
+def _rows(t, dtype, head_dim, what, n_tokens, heads=None):
+    """The rows as bytes, and their heads."""
+    shape = t.shape
+    if len(shape) == 3:
+        n, h, d = shape
+        if n == n_tokens and d == head_dim and t.dtype is dtype and (heads is None or h == heads):
+            s0, s1, s2 = t.stride()
+            if s2 != 1:
+                raise ValueError(what + ": head_dim must be contiguous")
+            return _PACK_ROWS(t.data_ptr(), s0, s1), h
+    raise ValueError(what + ": [n_tokens, heads, head_dim] of the cache's type")
 
 
 def ppd_paged_append(k_cache, v_cache, pages, q_start, kv_len, q, k, v, q_gain=None, k_gain=None, norm_eps=1e-5, rotary_dim=0,
@@ -284,15 +290,16 @@ def ppd_paged_append(k_cache, v_cache, pages, q_start, kv_len, q, k, v, q_gain=N
     _same_gpu(dev, v_cache, pages, q_start, kv_len, q, k, v, q_gain, k_gain, q_out)
     n = k.shape[0]
     cache, batch, sizes = _paged_args(k_cache, v_cache, pages, q_start, kv_len, n)
-    kr, vr = _rows(k, k_cache, "k", n, sizes[2]), _rows(v, k_cache, "v", n, sizes[2])
+    dtype, kv_heads, head_dim = k_cache.dtype, sizes[2], sizes[3]
+    kr, vr = _rows(k, dtype, head_dim, "k", n, kv_heads)[0], _rows(v, dtype, head_dim, "v", n, kv_heads)[0]
     qr, outr, heads = None, None, 0
     if q is not None:
-        qr, heads = _rows(q, k_cache, "q", n), q.shape[1]
+        qr, heads = _rows(q, dtype, head_dim, "q", n)
         if q_out is None:
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        outr = _rows(q_out, k_cache, "q_out", n, heads)
+        outr = _rows(q_out, dtype, head_dim, "q_out", n, heads)[0]
     for g in (q_gain, k_gain):
-        if g is not None and (g.dtype != k_cache.dtype or g.numel() != sizes[3] or not g.is_contiguous()):
+        if g is not None and (g.dtype is not dtype or g.numel() != head_dim or not g.is_contiguous()):
             raise ValueError("gains: [head_dim] of the cache's type")
     rc = append(cache, batch, heads, qr, outr, kr, vr, None if q_gain is None else q_gain.data_ptr(), None if k_gain is None else k_gain.data_ptr(),
                 norm_eps, rotary_dim, rope_theta, raw_stream(dev))
@@ -323,16 +330,17 @@ def ppd_paged_attention(q, k_cache, v_cache, pages, q_start, kv_len, scale=None,
     _same_gpu(dev, q, v_cache, pages, q_start, kv_len, out, workspace)
     n = q.shape[0]
     cache, batch, sizes = _paged_args(k_cache, v_cache, pages, q_start, kv_len, n)
-    qr, heads = _rows(q, k_cache, "q", n), q.shape[1]
+    dtype, head_dim = k_cache.dtype, sizes[3]
+    qr, heads = _rows(q, dtype, head_dim, "q", n)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    outr = _rows(out, k_cache, "out", n, heads)
+    outr = _rows(out, dtype, head_dim, "out", n, heads)[0]
     lse = torch.empty((n, heads), dtype=torch.float32, device=q.device) if want_lse else None
     if workspace is None:
         need = _attention_workspace(sizes, heads)
         if need:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    rc = attention(cache, batch, heads, qr, outr, None if lse is None else lse.data_ptr(), sizes[3] ** -0.5 if scale is None else scale, window,
+    rc = attention(cache, batch, heads, qr, outr, None if lse is None else lse.data_ptr(), head_dim ** -0.5 if scale is None else scale, window,
                    None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, raw_stream(dev))
     if rc != 0:
         raise PPDError(rc, "ppd_paged_attention", load_library().ppd_last_hip_error(None))

@@ -144,4 +144,4 @@ def test_binding_refuses_what_the_library_cannot_see():
             binding._paged_args(*bad, 2)
     for q in (t(2, 4, 32), t(3, 4, 64), t(2, 4, 64).half(), t(2, 64, 4).transpose(1, 2), t(2, 64)):
         with pytest.raises(ValueError):
-            binding._rows(q, k, "q", 2)
+            binding._rows(q, k.dtype, 64, "q", 2)

@@ -95,6 +95,13 @@ def test_many_sequences():
     check(Batch(new.tolist(), (new + rng.integers(0, 30, 200)).tolist(), 2, 1, 64, BF16), rotary=64)
 
 
+@pytest.mark.parametrize("seqs", [64, 65, 128, 1000, 4095, 4096])
+def test_as_many_sequences_as_there_may_be(seqs):
+    rng = np.random.default_rng(seqs)
+    new = rng.choice([0, 1, 3], seqs, p=[0.6, 0.3, 0.1])
+    check(Batch(new.tolist(), (new + rng.integers(0, 20, seqs)).tolist(), 1, 1, 64, F16, pad=2), rotary=64)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_far_positions(dtype):
     """Angles of a million radians, to the last digits of fp32."""

@@ -280,10 +280,19 @@ def test_many_sequences_in_parts(seqs, kv_heads, most):
     check(Batch(new.tolist(), (new + rng.integers(0, most, seqs)).tolist(), 3 * kv_heads, kv_heads, 64, BF16, pad=3))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("seqs", [1025, 4095, 4096])
+def test_as_many_sequences_as_there_may_be(seqs, dtype):
+    rng = np.random.default_rng(seqs)
+    new = rng.choice([0, 1, 3], seqs, p=[0.6, 0.3, 0.1])
+    check(Batch(new.tolist(), (new + rng.integers(0, 40, seqs)).tolist(), 2, 1, 64, dtype, pad=2))
+
+
 def test_many_long_runs_in_parts():
     rng = np.random.default_rng(1)
     new = np.where(rng.random(70) < 0.2, 0, rng.integers(30, 60, 70))
     check(Batch(new.tolist(), (new + rng.integers(0, 700, 70)).tolist(), 2, 1, 64, F16, pad=3))
+    check(Batch(new.tolist(), (new + rng.integers(0, 60, 70)).tolist(), 4, 2, 128, BF16, pad=3))           # (one part each)
 
 
 def test_prompts_beside_tokens():

@@ -276,6 +276,12 @@ def test_waves_that_take_several_pieces_of_a_row(vocab, with_draft, dtype):
     check(make([3, 2, 4] * 33, vocab, dtype, 21, with_draft, temp=[0.8, 1.0, 0.0] * 33))
 
 
+def test_as_many_sequences_as_there_may_be():
+    drafts = np.random.default_rng(4).integers(0, 3, 4096).tolist()
+    check(make(drafts, 70, torch.float16, 5))
+    check(make(drafts[:65], 3000, torch.bfloat16, 6))
+
+
 def test_the_emitted_tokens_have_the_targets_distribution():
     """The rule's point.  40000 sequences of one draft over 12 tokens: the first emitted token's counts against p, within 5 standard
     deviations of a binomial count each (a correct rule fails one of the 12 in about 10^5 runs; the numbers are fixed)."""

@@ -295,6 +295,35 @@ def test_many_long_runs_in_parts():
     check(Batch(new.tolist(), (new + rng.integers(0, 60, 70)).tolist(), 4, 2, 128, BF16, pad=3))           # (one part each)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("page,window", [(16, 0), (20, 0), (64, 100)])
+@pytest.mark.parametrize("heads,kv_heads", [(8, 8), (14, 2)])
+def test_long_runs_in_fp32(hd, page, window, heads, kv_heads):
+    check(Batch([700, 0, 1, 600], [900, 30, 40, 600], heads, kv_heads, hd, F32, page=page, pad=3, seed=hd), window=window)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_what_long_runs_in_fp32_do_not_see(bad):
+    b = Batch([700, 500], [700, 560], 8, 8, 64, F32, page=16)
+    ref = attention64(b)
+    d = b.cuda()
+    used = torch.zeros(b.n_pages, b.page, dtype=torch.bool)
+    for s in range(2):
+        for p in range(b.kv[s]):
+            used[b.slot(s, p)] = True
+    d.k_cache[~used.cuda()], d.v_cache[~used.cuda()] = bad, bad
+    check(b, d=d, ref=ref)
+    for s, p in ((0, 300), (1, 400)):
+        d.v_cache[b.slot(s, p)][3, 7] = bad
+    out, _ = call(d)
+    tol, _ = limits(b, *ref)
+    o = out.cpu().double()
+    hit = torch.zeros_like(o, dtype=torch.bool)
+    hit[300:700, 3, 7] = True
+    hit[700 + 340:1200, 3, 7] = True
+    assert not torch.isfinite(o[hit]).any() and ((o - ref[0]).abs() <= tol)[~hit].all()
+
+
 def test_prompts_beside_tokens():
     check(Batch([1, 300, 1, 0, 64, 1, 5], [400, 300, 20, 7, 200, 1, 90], 8, 2, 128, BF16, pad=3))
     check(Batch([1, 300, 1, 0, 64, 1, 5], [400, 300, 20, 7, 200, 1, 90], 8, 8, 64, F16, pad=3), window=50)

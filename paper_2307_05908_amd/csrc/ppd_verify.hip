@@ -144,7 +144,7 @@ __device__ __forceinline__ double temperature_of(const VerifyArgs& a, int s) {
 }
 
 // ---- all rows: the largest logit and the weights' sum, piece by piece.  A wave has `run` pieces of a row, and the next one's logits under way
-// while it works on one; nothing waits for another wave but for the table.  Bound by the vector units: 20 instructions a logit, 14 of them for
+// while it works on one; nothing waits for another wave but for the table.  Bound by the vector units: 20 instructions a logit, 12 of them for
 // its weight (901 bf16 rows of 32000 logits and 773 of drafts', 107 MB: 41 us, 65 % of the cycles with such an instruction under way; reading
 // alone would take 15).  Neither fewer instructions (one maximum for eight pieces: 17 a logit), nor more waves, nor four weights side by side in
 // each changed that time by more than 5 %.  grid: (runs of all rows / 4, 1 or 2: target, draft)

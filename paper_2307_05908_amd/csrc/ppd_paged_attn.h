@@ -22,8 +22,8 @@ struct PagedAttnArgs {
   int heads, kv_heads, group, window;
   int tile_rows;
   float to_log2;                      // scale * log2(e): a score's exponent of two
-  int want, fine, least;              // parts per key/value head to aim at, and among sequences of unlike lengths; blocks of a part at least (0:
-                                      // one part each)
+  int want, fine, least, whole;       // parts per key/value head to aim at, and among sequences of unlike lengths; blocks of a part at least (0:
+                                      // one part each), and up to which a tile is not cut
   float* part_o; float2* part_ml;     // [item][kv_heads][rows of a tile][head_dim], [item][kv_heads][rows of a tile]
   uint64_t* stamps; uint64_t stamp;   // paged_split_kernel, [item][kv_heads]: this call's number, once the part is there (see join_parts)
   int2* plan;                         // paged_tile_kernel, [n_seqs]: first item of a sequence, parts of its tiles
@@ -157,7 +157,7 @@ __device__ __forceinline__ bool find_part(const PagedAttnArgs& a, int idx, bool 
   for (int again = 0; again < 3 && few && J == 1; ++again) {
     float x = 0.f;
 #pragma unroll
-    for (int j = 0; j < J; ++j) x += (float)(tiles[j] * ((blocks[j] + len - 1) / len));
+    for (int j = 0; j < J; ++j) x += (float)(tiles[j] * (blocks[j] <= a.whole ? 1 : (blocks[j] + len - 1) / len));
     const float items = wave_sum(x);
     if (items <= want || 2.f * count > want) break;
     len = (int)ceilf((float)len * items / want);
@@ -168,7 +168,7 @@ __device__ __forceinline__ bool find_part(const PagedAttnArgs& a, int idx, bool 
   auto cut = [&]() {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      parts[j] = (int)((unsigned)(blocks[j] + len - 1) / (unsigned)len);
+      parts[j] = blocks[j] <= a.whole ? 1 : (int)((unsigned)(blocks[j] + len - 1) / (unsigned)len);
       turns[j] = parts[j] > 1 ? 0 : !few || 4 * blocks[j] <= len ? 3 : 2 * blocks[j] <= len ? 2 : 1;
     }
   };

@@ -383,7 +383,7 @@ __global__ __launch_bounds__(SPLIT_THREADS, 2) void paged_split_kernel(PagedAttn
 // ---- host
 struct AttnPlan {
   bool tiles;               // paged_tile_kernel, not paged_split_kernel
-  int want, fine, least;    // see PagedAttnArgs
+  int want, fine, least, whole;      // see PagedAttnArgs
   int64_t items;            // workgroups per key/value head: parts aimed at, and a part's end for every tile
   uint64_t o_bytes, ml_bytes, more_bytes;      // more: stamps, or the plan
 };
@@ -406,12 +406,14 @@ int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, 
   const int slots = p->tiles ? 512 : 256;
   p->want = slots / cache->n_kv_heads + (slots < cache->n_kv_heads);
   p->fine = p->tiles || tiles * cache->n_kv_heads < 160 ? p->want : p->want * 7 / 4;
-  p->least = p->tiles ? 8 : 4;
+  p->whole = p->tiles ? 8 : 4;
+  p->least = p->tiles ? 8 : 2;
   // (slots, one sequence of 60000 positions, 8 key/value heads, bf16, at 256 / 512 / 1024 / 2048: 48 / 55 / 67 / 97 us; fine: find_item.
-  // least, at 4 / 8: one token over 700 positions 13.0 / 13.8, over 2000 14.3 / 16.9, fp32 drafts over 100 to 1900 14.5 / 18.)
+  // least, at 2 / 4 / 6: one token over 700 positions 10.8 / 11.4 / 12.6, four of 500 9.3 / 10.8 / 10.8, two fp32 ones of 1000 14.2 / 17.1 / 21.0.  whole: one
+  // token over 200 positions in one part / two 7.5 / 8.6, over 300 9.7 / 9.3.)
   // Tiles enough for the whole chip, or no position to cut at: one part each.  (At whole / in parts: 300 sequences of 500 positions 128 / 156, of 60 to
   // 8000 462 / 476, but 128 of these 250 / 198; long runs, two prompts of 3700 to 4096 tokens 285 / 298, six chunks of 700 over 500 86 / 96.)
-  if (tiles >= (p->tiles ? 2 : 8) * p->want || capacity <= p->least * PLAN_BLOCK) p->least = 0;
+  if (tiles >= (p->tiles ? 2 : 8) * p->want || capacity <= p->whole * PLAN_BLOCK) p->least = 0;
   p->items = tiles + (p->least ? p->fine + 1 : 0);
   const uint64_t places = p->least ? (uint64_t)p->items * cache->n_kv_heads : 0;
   p->o_bytes = places * tile_rows * cache->head_dim * 4;
@@ -463,7 +465,7 @@ extern "C" int ppd_paged_attention(const ppd_paged_cache* cache, const ppd_paged
   a.q_tok = q->token; a.q_head = q->head; a.o_tok = out->token; a.o_head = out->head;
   a.kc_page = cache->k_page; a.kc_pos = cache->k_pos; a.kc_head = cache->k_head; a.vc_page = cache->v_page; a.vc_pos = cache->v_pos; a.vc_head = cache->v_head;
   a.heads = n_heads; a.kv_heads = cache->n_kv_heads; a.group = n_heads / cache->n_kv_heads; a.window = window; a.to_log2 = scale * 1.44269504f;
-  a.tile_rows = p.tiles ? TILE_ROWS : SPLIT_ROWS; a.want = p.want; a.fine = p.fine; a.least = p.least;
+  a.tile_rows = p.tiles ? TILE_ROWS : SPLIT_ROWS; a.want = p.want; a.fine = p.fine; a.least = p.least; a.whole = p.whole;
   a.part_o = (float*)workspace; a.part_ml = (float2*)((char*)workspace + p.o_bytes); a.stamps = (uint64_t*)((char*)workspace + p.o_bytes + p.ml_bytes);
   a.plan = (int2*)a.stamps;
   a.stamp = next_stamp();

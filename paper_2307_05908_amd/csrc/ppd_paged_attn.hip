@@ -93,8 +93,8 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const Item& i
 // numbers, keys and values, the join).  64 bf16 tokens over 60 to 8000 positions each (411 MB) take 90 us: 4.6 TB/s, and with the products
 // taken out no less; 64 of 4000 (1 GB) 197, 5.3 TB/s; a large copy reaches 4.6, a plain stream of reads 7.1.  Long runs of fp32 come here, too: four
 // prompts of 3000, 8 heads, 926 us, 80 of the 154 TFLOP/s that a large fp32 product reaches (32 rows a wave, for half the reads: 997, one wave on a
-// SIMD instead of two).  One token over 700 positions: 11 us,
-// 1.5 of them for the plan, 5 for two steps of each wave, 1 for the waves' results and 3 for the join.
+// SIMD instead of two).  One token over 700 positions: 11 us, of
+// which 1.5 for the plan, 1 for the waves' results and 3 for the join.
 // A wave has every fourth step of BP positions of its part to itself: keys straight into registers as the left operand, values through
 // registers into LDS rows of its own, from where the transposing reads (fp32: plain ones) make them the left operand of the second product.
 // The next step's are under way, in registers of their own, while one is worked on; nothing waits at a barrier until the waves' results are

@@ -408,7 +408,8 @@ int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, 
   p->fine = p->tiles || tiles * cache->n_kv_heads < 160 ? p->want : p->want * 7 / 4;
   p->whole = p->tiles ? 8 : 4;
   p->least = p->tiles ? 8 : 2;
-  // (slots, one sequence of 60000 positions, 8 key/value heads, bf16, at 256 / 512 / 1024 / 2048: 48 / 55 / 67 / 97 us; fine: find_item.
+  // (slots, one sequence of 60000 positions, 8 key/value heads, bf16, at 256 / 512 / 1024 / 2048: 48 / 55 / 67 / 97 us; fine: find_part.
+  // Long runs, at 384 / 512 / 640 / 1024: three chunks of 140 over 15000 219 / 173 / 203 / 175, a chunk of 500 over 4000 86 / 80 / 88 / 90.
   // least, at 2 / 4 / 6: one token over 700 positions 10.8 / 11.4 / 12.6, four of 500 9.3 / 10.8 / 10.8, two fp32 ones of 1000 14.2 / 17.1 / 21.0.  whole: one
   // token over 200 positions in one part / two 7.5 / 8.6, over 300 9.7 / 9.3.)
   // Tiles enough for the whole chip, or no position to cut at: one part each.  (At whole / in parts: 300 sequences of 500 positions 128 / 156, of 60 to

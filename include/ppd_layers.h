@@ -90,8 +90,8 @@ int ppd_paged_append(const ppd_paged_cache *cache, const ppd_paged_batch *batch,
  * sequences).
  * lse: DEVICE float [n_tokens][n_heads] or NULL: log of the sum of exp(scale * q . k_j), -inf where nothing is seen (for
  * a merge with attention over other positions).
- * Scores, softmax and sums are fp32.  A 16-bit type's softmax weights go into their product with the values as two terms
- * of the type, or, where the batch has more than 32 rows a sequence, rounded to it.  Beyond that and the order of additions
+ * Scores, softmax and sums are fp32; a 16-bit type's softmax weights go into their product with the values as two terms
+ * of the type, so that the result's own rounding is what counts.  Beyond the order of additions
  * (a sequence's positions are cut into as many parts as the batch leaves compute units for) results do not depend on what
  * else is in the batch, and two calls with the same arguments give the same bits.
  * workspace: DEVICE scratch of at least the bytes that ppd_paged_attention_workspace gives for the same arguments (it

@@ -1,8 +1,10 @@
-// ppd_paged_attention, many rows: bound by the issue of instructions: a 32 x 32 x 16 product keeps its SIMD's vector units from the other wave
-// for two thirds of its 32 cycles, and a block of 64 positions is 32 products of a wave, 32 exponentials and 160 other vector instructions.
-// Two bf16 prompts of 3700 to 4096 tokens (32 heads, 8 of keys and values, 259 GFLOP): 277 us, 935 TFLOP/s; a large matrix product of the
-// library's reaches 1200.  Products 46 % of the cycles, vector instructions 46 %, LDS 31 %.
-// (Tried and not kept, beside 283 us at the time: the next block's scores between this one's exponentials, 286 to 292; a higher priority for
+// ppd_paged_attention, many rows: bound by the matrix units and the issue of instructions beside them: a 32 x 32 x 16 product keeps its SIMD's
+// vector units from the other wave for two thirds of its 32 cycles, and a block of 64 positions is 48 products of a wave (16 of them for the
+// weights' second term), 32 exponentials and some 240 other vector instructions.  Two bf16 prompts of 3800 and 4000 tokens (32 heads, 8 of keys
+// and values, 249 GFLOP, 374 with the second term): 351 us, 1070 TFLOP/s of products; a large matrix product of the library's reaches 1200.
+// With weights of one term, rounded to the type: 267 us, and an error of 2.1e-3 of bf16 outputs where their own rounding is 1.6e-3.
+// (Tried and not kept: the first terms' products before the second terms', 351; the weights' rests by a dot instruction, one a weight less, 350.
+// With one term, beside 283 us at the time: the next block's scores between this one's exponentials, 286 to 292; a higher priority for
 // the waves in products or in exponentials, 284 to 292; offsets kept in registers from block to block, 281 to 287.  Blocks of 32 positions and three
 // workgroups a unit: 278 beside 279, 500 tokens over 4000 positions 81 beside 77, head_dim 64 113 beside 100.)
 #include "ppd_paged_attn.h"
@@ -39,7 +41,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   // a multiple of eight heads, and its L2 has the head's keys and values; and the longest parts of all heads come first.  (All of a head's
   // tiles before the next head's: 3000 fp16 rows of 40 heads 256 us, not 231.)
   const int kvheads = a.kv_heads, idx = blockIdx.x / kvheads, kvh = blockIdx.x % kvheads;
-  __shared__ int s_odd[2];                                 // first and last block with a value that is infinite, or no number, where not every row sees it
+  __shared__ int s_odd[2];                                 // first and last block from which a value that is infinite, or no number, was cleared
   if (threadIdx.x == 0) { s_odd[0] = 0x7fffffff; s_odd[1] = -1; }
   Item it;
   if (!find_item<TILE_ROWS>(a, idx, idx == 0 && kvh == 0 && wave == 0 && a.least > 0, lane, it)) return;
@@ -59,9 +61,13 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   // The table's entry for, and the slot of, a block's position `lane`: asked for a block before it is looked at, when the block is requested.
   // (Looked at at once it would wait for the transfers that are under way.)  From block to block both move on by the same step.
   const int32_t* const table = a.b.pages + (int64_t)it.s * a.b.pages_stride;
-  int index = (int)((unsigned)(it.lo + lane) / (unsigned)a.b.page_size), slot = it.lo + lane - index * a.b.page_size;
+  int index, slot, entry;
   const int more_index = KV / a.b.page_size, more_slot = KV - more_index * a.b.page_size;
-  int entry = table[min(index, a.b.max_pages - 1)];
+  auto first_place = [&]() {
+    index = (int)((unsigned)(it.lo + lane) / (unsigned)a.b.page_size);
+    slot = it.lo + lane - index * a.b.page_size;
+    entry = table[min(index, a.b.max_pages - 1)];
+  };
   auto place = [&]() {
     slot += more_slot;
     index += more_index;
@@ -102,11 +108,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
     }
   };
   f32x16 o[HD / 32];
-#pragma unroll
-  for (int i = 0; i < HD / 32; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-  float m = -INFINITY, l = 0.f;
+  float m, l;
   // Where a lane's operands begin.  A row's 16-byte pieces have changed places by an exclusive or: keys with the row (head_dim 64: half of it),
   // so that eight rows in turn have a piece on eight places; values two pieces at a time, so that the four rows of a transposing read and
   // the four of the other half lie on different banks.  Keys: row col of half a block, piece 2 i + half at kat ^ 32 i.  Values: position
@@ -156,16 +158,13 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
         for (int e = 0; e < 16; ++e) o[i][e] *= keep;
     }
     const float ref = m == -INFINITY ? 0.f : m;
-    // Weights go into the second product rounded to the type (their errors together are the size of the result's own rounding; a second term
-    // would cost half the products again), into the sum as they are.
-    u32x4 w[4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[t / 2][8 * (t % 2) + 2 * e], a.to_log2, -ref)), y = __builtin_amdgcn_exp2f(fmaf(s[t / 2][8 * (t % 2) + 2 * e + 1], a.to_log2, -ref));
-        w[t][e] = pair(x, y, T());
-        l += x + y;
+      for (int e = 0; e < 16; e += 2) {
+        s[t][e] = __builtin_amdgcn_exp2f(fmaf(s[t][e], a.to_log2, -ref));
+        s[t][e + 1] = __builtin_amdgcn_exp2f(fmaf(s[t][e + 1], a.to_log2, -ref));
+        l += s[t][e] + s[t][e + 1];
       }
     auto values = [&](int t, int d) {
       const char* p = buf + (vat ^ 64 * d) + t * 16 * ROWB;
@@ -173,13 +172,29 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 8 * ROWB)));
       return (u32x4){x.x, x.y, y.x, y.y};
     };
+    // Weights go into the second product in two terms of the type: the rounding of one alone is as large as the result's own.
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 4; ++t) {
+      u32x4 hi, lo;
 #pragma unroll
-      for (int d = 0; d < HD / 32; ++d) o[d] = mma32(values(t, d), w[t], o[d], T());
+      for (int e = 0; e < 4; ++e) {
+        float x = s[t / 2][8 * (t % 2) + 2 * e], y = s[t / 2][8 * (t % 2) + 2 * e + 1];
+        hi[e] = pair(x, y, T());
+        rest(hi[e], x, y, T());
+        lo[e] = pair(x, y, T());
+      }
+#pragma unroll
+      for (int d = 0; d < HD / 32; ++d) {
+        const u32x4 v = values(t, d);
+        o[d] = mma32(v, hi, o[d], T());
+        o[d] = mma32(v, lo, o[d], T());
+      }
+    }
   };
-  // Where not every row of the tile sees all of a block: a weight of zero does not silence a value that is infinite or no number, so these
-  // are cleared in LDS (each wave its own 16 positions), and put in behind the loop where they are seen.
+  // A weight of zero, or the second term of one, does not silence a value that is infinite or no number, so where not every row of the tile
+  // sees all of a block these are cleared in LDS (each wave its own 16 positions), and put in behind the loop where they are seen.  Blocks that
+  // all rows see are taken as they come, and if that has left something that is not finite the part is gone through once more, with every block
+  // cleaned.
   auto clean = [&](int n, int base, uint64_t have) {
     char* const p = lds + (n & 1) * 2 * SIDE + SIDE + 16 * wave * ROWB + lane * 16;
     uint32_t most = 0;
@@ -199,25 +214,42 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       if (__ballot(seen) && lane == 0) { atomicMin(&s_odd[0], n); atomicMax(&s_odd[1], n); }
     }
   };
-  if (blocks > 0) request(0);
-  place();
-  // the queries are waited for here: a wait in the loop would be one for the transfers, of which the compiler knows nothing
+  bool careful = false;
+  for (;;) {
 #pragma unroll
-  for (int i = 0; i < HD / 16; ++i) asm volatile("" : "+v"(q[i]));
-  for (int n = 0; n < blocks; ++n) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    const uint64_t have = have_next;
-    if (n + 1 < blocks) request(n + 1);
+    for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+    m = -INFINITY; l = 0.f;
+    first_place();
+    if (blocks > 0) request(0);
     place();
-    const int base = it.lo + n * KV;
-    if (!(have == ~0ull && base + KV - 1 <= tile_first && (a.window == 0 || base >= tile_last - a.window + 1))) {
-      clean(n, base, have);
+    // the queries are waited for here: a wait in the loop would be one for the transfers, of which the compiler knows nothing
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) asm volatile("" : "+v"(q[i]));
+    for (int n = 0; n < blocks; ++n) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
+      const uint64_t have = have_next;
+      if (n + 1 < blocks) request(n + 1);
+      place();
+      const int base = it.lo + n * KV;
+      if (careful || !(have == ~0ull && base + KV - 1 <= tile_first && (a.window == 0 || base >= tile_last - a.window + 1))) {
+        clean(n, base, have);
+        __syncthreads();
+      }
+      if (!busy || base > wave_last || (a.window > 0 && base + KV - 1 < wave_first - a.window + 1)) continue;      // no row of the wave sees any of it
+      const bool whole = have == ~0ull && base + KV - 1 <= wave_first && (a.window == 0 || base >= wave_last - a.window + 1);
+      step(n, base, have, whole);
     }
-    if (!busy || base > wave_last || (a.window > 0 && base + KV - 1 < wave_first - a.window + 1)) continue;      // no row of the wave sees any of it
-    const bool whole = have == ~0ull && base + KV - 1 <= wave_first && (a.window == 0 || base >= wave_last - a.window + 1);
-    step(n, base, have, whole);
+    if (careful) break;
+    float sum = l;                                         // (no number, if one is)
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sum += o[i][e] - o[i][e];
+    if (!__syncthreads_or(!(fabsf(sum) < INFINITY))) break;      // (every wave is behind its reads of LDS, too)
+    careful = true;
   }
   __syncthreads();
   const int odd_first = s_odd[0], odd_last = s_odd[1];
@@ -226,7 +258,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
     // such a block once more, position by position, from the pages: a row that sees an infinite value, or no number, takes it up
     const int base = it.lo + n * KV, x = base + lane;
     const bool there = __ballot(x < it.hi && page_of(a.b, it.s, x) >= 0) == ~0ull;
-    if (there && base + KV - 1 <= tile_first && (a.window == 0 || base >= tile_last - a.window + 1)) continue;
+    if (!careful && there && base + KV - 1 <= tile_first && (a.window == 0 || base >= tile_last - a.window + 1)) continue;
 #pragma unroll 1
     for (int p = base; p < min(base + KV, it.hi); ++p) {
       const int pg = page_of(a.b, it.s, p);

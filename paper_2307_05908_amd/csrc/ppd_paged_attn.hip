@@ -244,10 +244,12 @@ __global__ __launch_bounds__(SPLIT_THREADS, 2) void paged_split_kernel(PagedAttn
       for (int i = 0; i < HD / 16; ++i) o[i] *= keep;
     }
     const float ref = m == -INFINITY ? 0.f : m;
+    float total = 0.f;                                    // (a step's weights among themselves first: one by one, those below half a step of the row's sum would leave no trace in it)
 #pragma unroll
     for (int t = 0; t < C::NT; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { s[t][e] = __builtin_amdgcn_exp2f(fmaf(s[t][e], to_log2, -ref)); l += s[t][e]; }
+      for (int e = 0; e < 4; ++e) { s[t][e] = __builtin_amdgcn_exp2f(fmaf(s[t][e], to_log2, -ref)); total += s[t][e]; }
+    l += total;
     if constexpr (C::SZ == 2) {
       // Weights in two terms of the type: the rounding of one alone is as large as the output's own.  Beside infinite values one: what is left
       // of a weight may be zero or negative, and so that no weight above zero becomes one, half floats go no lower than their smallest number.

@@ -1,9 +1,9 @@
 // ppd_paged_attention, many rows: bound by the matrix units and the issue of instructions beside them: a 32 x 32 x 16 product keeps its SIMD's
 // vector units from the other wave for two thirds of its 32 cycles, and a block of 64 positions is 48 products of a wave (16 of them for the
 // weights' second term), 32 exponentials and some 240 other vector instructions.  Two bf16 prompts of 3800 and 4000 tokens (32 heads, 8 of keys
-// and values, 249 GFLOP, 374 with the second term): 351 us, 1070 TFLOP/s of products; a large matrix product of the library's reaches 1200.
+// and values, 249 GFLOP, 374 with the second term): 344 us, 1090 TFLOP/s of products; a large matrix product of the library's reaches 1200.
 // With weights of one term, rounded to the type: 267 us, and an error of 2.1e-3 of bf16 outputs where their own rounding is 1.6e-3.
-// (Tried and not kept: the first terms' products before the second terms', 351; the weights' rests by a dot instruction, one a weight less, 350.
+// (Tried and not kept: the first terms' products before the second terms' and weights' rests by a dot instruction, one a weight less: the same time.
 // With one term, beside 283 us at the time: the next block's scores between this one's exponentials, 286 to 292; a higher priority for
 // the waves in products or in exponentials, 284 to 292; offsets kept in registers from block to block, 281 to 287.  Blocks of 32 positions and three
 // workgroups a unit: 278 beside 279, 500 tokens over 4000 positions 81 beside 77, head_dim 64 113 beside 100.)
@@ -158,14 +158,16 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
         for (int e = 0; e < 16; ++e) o[i][e] *= keep;
     }
     const float ref = m == -INFINITY ? 0.f : m;
+    // (a block's weights among themselves first: one by one, those below half a step of the row's sum would leave no trace in it)
+    float total[2] = {0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int e = 0; e < 16; e += 2) {
+      for (int e = 0; e < 16; ++e) {
         s[t][e] = __builtin_amdgcn_exp2f(fmaf(s[t][e], a.to_log2, -ref));
-        s[t][e + 1] = __builtin_amdgcn_exp2f(fmaf(s[t][e + 1], a.to_log2, -ref));
-        l += s[t][e] + s[t][e + 1];
+        total[t] += s[t][e];
       }
+    l += total[0] + total[1];
     auto values = [&](int t, int d) {
       const char* p = buf + (vat ^ 64 * d) + t * 16 * ROWB;
       const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));

@@ -1,5 +1,7 @@
 """ppd_paged_attention's softmax weights: what their rounding may cost.  Scores are small here, so that the bound of their own errors leaves
 that of the weights to be seen; a row's outputs are sums of both signs, many of them near zero, which the result's rounding does not cover."""
+import math
+
 import pytest
 import torch
 
@@ -66,3 +68,34 @@ def test_infinite_values_that_all_rows_see(dtype, hd, new, kv):
         seen = o[rows, 2, c]
         assert seen.isnan().all() if x != x else (seen == x).all()
     assert ((o - ref).abs() <= limits(b, ref, size, reach))[~hit].all()
+
+
+def sink(seqs, rows, heads, n, dtype, hd, below):
+    """All sequences over the same pages: one position whose weight is 2^below times that of each of the other n - 1, every value 1."""
+    k = torch.zeros((n // 64, 64, heads, hd), dtype=dtype, device="cuda")
+    v = torch.ones((n // 64, 64, heads, hd), dtype=dtype, device="cuda")
+    q = torch.zeros((seqs * rows, heads, hd), dtype=dtype, device="cuda")
+    k[0, 0, :, 0], q[:, :, 0] = 4.0, 4.0
+    pages = torch.arange(n // 64, dtype=torch.int32, device="cuda").repeat(seqs, 1)
+    start = torch.arange(0, seqs * rows + 1, rows, dtype=torch.int32, device="cuda")
+    # (the rows' own positions are the last ones: row r of a sequence sees n - rows + r + 1)
+    out, lse = binding.ppd_paged_attention(q, k, v, pages, start, torch.full((seqs,), n, dtype=torch.int32, device="cuda"), scale=below * math.log(2) / 16, want_lse=True)
+    seen = torch.arange(n - rows + 1, n + 1, dtype=torch.float64).repeat(seqs)[:, None]
+    return out.cpu().double(), lse.cpu().double(), below * math.log(2) + torch.log1p((seen - 1) * 2.0 ** -below)
+
+
+# Sequences enough that each row's positions are one part: long runs (a lane's sum has half of the positions, 32 at a time), and single tokens
+# (a wave has a quarter of the positions, a lane's sum a quarter of these, 4 or 8 at a time).
+SINKS = [(32, 40, 32, 65536), (64, 1, 32, 131072)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("seqs,rows,heads,n", SINKS)
+@pytest.mark.parametrize("below", [24.1, 25.1])
+def test_many_small_weights_count_in_the_sum(seqs, rows, heads, n, dtype, below):
+    """Each is below half a step of the sum that the large one alone is; together they are a thousandth of it, or several.  A lane adds to its
+    sum n / 64 times at most, each addition off by half a step (2^-24) of a sum near 1.  The score, 17.4 at most, is rounded eight times on its
+    way (the scale, its product with log2 e, that constant, the product with the score twice, the log sum's product and constant, its end)."""
+    _, lse, want = sink(seqs, rows, heads, n, dtype, 64, below)
+    tol = (n / 64 + 8 * 17.4 + 4) * 2.0 ** -24
+    assert ((lse - want).abs() <= tol).all(), (float((lse - want).abs().max()), tol)

@@ -47,6 +47,11 @@ __device__ __forceinline__ void rest(uint32_t p, float& a, float& b, bf16_t) { a
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t pair(float a, float b, f16_t) { const f16x2 v = {(_Float16)a, (_Float16)b}; return __builtin_bit_cast(uint32_t, v); }
 __device__ __forceinline__ void rest(uint32_t p, float& a, float& b, f16_t) { const f16x2 v = __builtin_bit_cast(f16x2, p); a -= (float)v.x; b -= (float)v.y; }
+// What weights are taken from, as an exponent of two.  For half floats so far below the row's maximum that the largest weight is 2^15, near their
+// largest number (2^(15 - slack) where the maximum may leave the reference by slack before that follows): they end at 2^-24, and of many
+// weights far below one of 1 the sum has what the products with the values lose (65536 positions at 2^-25.1 beside one: 1.8e-3 of
+// the result).  bf16 and fp32 go down to 2^-126 and lower.
+template <typename T> __device__ __forceinline__ float reference(float top, int slack) { return std::is_same<T, f16_t>::value ? top - (float)(15 - slack) : top; }
 // the largest of the numbers' magnitudes, as bits, and whether it is infinite or no number
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 template <typename T> __device__ __forceinline__ uint32_t largest(uint32_t m, u32x4 v, T) {

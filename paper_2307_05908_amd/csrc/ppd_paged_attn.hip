@@ -12,7 +12,7 @@ namespace {
 
 constexpr int SPLIT_WAVES = 4, SPLIT_THREADS = SPLIT_WAVES * WAVE;
 
-// A part's results: sums of a row's components, and its maximum and total, past the L2, for whoever joins them.
+// A part's results: sums of a row's components, and its reference and total, past the L2, for whoever joins them.
 __device__ __forceinline__ void leave(float* to, f32x4 v) {
   typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
   const u64x2 u = __builtin_bit_cast(u64x2, v);
@@ -106,7 +106,7 @@ struct Split {
   static constexpr int LPR = HD * SZ / 16, RPI = WAVE / LPR, NV = BP / RPI;
   static constexpr int STRIDE = HD * SZ + (SZ == 4 ? 16 : 32);   // of a row of values in LDS: no two rows of an operand on the same banks
   static constexpr int WAVE_LDS = BP * STRIDE;
-  static constexpr int OUT_LDS = SPLIT_ROWS * (HD + 4) * 4 + SPLIT_ROWS * 8; // a wave's results: sums (rows 16 bytes longer than they are), maxima and totals
+  static constexpr int OUT_LDS = SPLIT_ROWS * (HD + 4) * 4 + SPLIT_ROWS * 8; // a wave's results: sums (rows 16 bytes longer than they are), references and totals
   static constexpr int LDS = SPLIT_WAVES * (WAVE_LDS > OUT_LDS ? WAVE_LDS : OUT_LDS);
 };
 
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(SPLIT_THREADS, 2) void paged_split_kernel(PagedAttn
     }
   };
   f32x4 o[HD / 16];
-  float m, l;                                             // the row's maximum (of scores times to_log2; the same in its four lanes) and the lane's part of the sum
+  float m, l;                                             // the row's reference (from its maximum of scores times to_log2; the same in its four lanes) and the lane's part of the sum
   // One step.  CAREFUL: with values that are infinite, or no numbers, among it (the first way through gives such a row no number where it
   // should have one: 0 times infinity where the row does not see it, or for the second term of a weight).
   auto work = [&](int step, auto set, auto careful) {
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(SPLIT_THREADS, 2) void paged_split_kernel(PagedAttn
     float top = -INFINITY;
 #pragma unroll
     for (int t = 0; t < C::NT; ++t) top = fmaxf(top, fmaxf(fmaxf(s[t].x, s[t].y), fmaxf(s[t].z, s[t].w)));
-    top *= to_log2;
+    top = reference<T>(top * to_log2, 0);
     if (__ballot(top > m)) {
       top = fmaxf(top, __shfl_xor(top, 16, WAVE));
       top = fmaxf(top, __shfl_xor(top, 32, WAVE));

@@ -145,9 +145,10 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[t][e]), s[t][e + 1]);
-    top *= a.to_log2;
     // the reference that weights are taken from follows the maximum only where that has left it by a factor of 2^8
-    if (__ballot(top > m + 8.f)) {
+    constexpr int SLACK = 8;
+    top = reference<T>(top * a.to_log2, SLACK);
+    if (__ballot(top > m + SLACK)) {
       top = fmaxf(top, __shfl_xor(top, 32, WAVE));
       const float mn = fmaxf(m, top), keep = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
       m = mn;

@@ -99,3 +99,13 @@ def test_many_small_weights_count_in_the_sum(seqs, rows, heads, n, dtype, below)
     _, lse, want = sink(seqs, rows, heads, n, dtype, 64, below)
     tol = (n / 64 + 8 * 17.4 + 4) * 2.0 ** -24
     assert ((lse - want).abs() <= tol).all(), (float((lse - want).abs().max()), tol)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("seqs,rows,heads,n", SINKS)
+def test_many_small_weights_count_in_the_outputs(seqs, rows, heads, n, dtype):
+    """All values are 1, and so are the outputs, whatever the weights.  The products add n / 16 times (long runs), or n / 128 (a wave's quarter, 32
+    at a time), for two terms each, and the sum as above."""
+    out, _, _ = sink(seqs, rows, heads, n, dtype, 64, 25.1)
+    tol = HALF_STEP[dtype] + ((2 * n / 16 if rows > 1 else 2 * n / 128) + n / 64 + 16) * 2.0 ** -24
+    assert ((out - 1).abs() <= tol).all(), (float((out - 1).abs().max()), tol)

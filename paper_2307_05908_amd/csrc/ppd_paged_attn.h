@@ -77,6 +77,9 @@ struct Item {
   int lo, hi;              // positions of the part, lo a multiple of PLAN_BLOCK
 };
 
+// The first position that a row at `pos` sees.  Positions are negative where kv_len is below the rows, and windows go up to 2^31 - 1.
+__host__ __device__ __forceinline__ int first_seen(int pos, int window) { return window > 0 && pos >= window ? pos - window + 1 : 0; }
+
 struct SeqPlan { int tiles, blocks; SeqRows r; };
 template <int TILE>
 __device__ __forceinline__ void seq_plan(const PagedAttnArgs& a, int s, SeqPlan& p) {
@@ -86,7 +89,7 @@ __device__ __forceinline__ void seq_plan(const PagedAttnArgs& a, int s, SeqPlan&
   p.r = seq_rows(a.b, s);
   if (p.r.rows == 0) return;
   p.tiles = (p.r.rows * a.group + TILE - 1) / TILE;                            // (2^26 rows at most)
-  const int hi = min(p.r.pos0 + p.r.rows, a.b.room), lo = a.window > 0 ? max(p.r.pos0 - a.window + 1, 0) & -PLAN_BLOCK : 0;
+  const int hi = min(p.r.pos0 + p.r.rows, a.b.room), lo = first_seen(p.r.pos0, a.window) & -PLAN_BLOCK;
   p.blocks = max(1, (hi - lo + PLAN_BLOCK - 1) / PLAN_BLOCK);
 }
 template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_add(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
@@ -229,7 +232,7 @@ template <int TILE>
 __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, bool tell, int lane, Item& it) {
   if (!(a.least == 0 ? find_whole<TILE>(a, idx, lane, it) : a.b.n_seqs <= WAVE ? find_part<TILE, 1>(a, idx, tell, lane, it) : find_part<TILE, 8>(a, idx, tell, lane, it))) return false;
   const int first = it.tile * TILE / a.group, last = min((it.tile * TILE + TILE - 1) / a.group, it.n - 1);
-  const int hi = min(it.pos0 + last + 1, a.b.room), lo = a.window > 0 ? max(it.pos0 + first - a.window + 1, 0) & -PLAN_BLOCK : 0;
+  const int hi = min(it.pos0 + last + 1, a.b.room), lo = first_seen(it.pos0 + first, a.window) & -PLAN_BLOCK;
   const int blocks = (max(hi - lo, 0) + PLAN_BLOCK - 1) / PLAN_BLOCK, per = (blocks + it.parts - 1) / it.parts;
   it.lo = lo + min(it.part * per, blocks) * PLAN_BLOCK;
   it.hi = min(hi, lo + min((it.part + 1) * per, blocks) * PLAN_BLOCK);

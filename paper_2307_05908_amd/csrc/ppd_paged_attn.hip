@@ -124,9 +124,9 @@ __global__ __launch_bounds__(SPLIT_THREADS, 2) void paged_split_kernel(PagedAttn
   const int all_rows = it.n * a.group;
   const int r = it.tile * SPLIT_ROWS + row, rc = min(r, all_rows - 1), tok = rc / a.group, head = kvh * a.group + rc % a.group;
   const int pos = r < all_rows ? it.pos0 + tok : -1;                          // what the lane's row sees ends there
-  const int from = a.window > 0 ? pos - a.window + 1 : 0;
+  const int from = first_seen(pos, a.window);
   const int tok_first = it.tile * SPLIT_ROWS / a.group, tok_last = min((it.tile * SPLIT_ROWS + SPLIT_ROWS - 1) / a.group, it.n - 1);
-  const int all_see_to = it.pos0 + tok_first, all_see_from = a.window > 0 ? it.pos0 + tok_last - a.window + 1 : 0;
+  const int all_see_to = it.pos0 + tok_first, all_see_from = first_seen(it.pos0 + tok_last, a.window);
   u32x4 q[C::NK];
   {
     const char* p = (const char*)a.q + ((int64_t)(it.rows0 + tok) * a.q_tok + (int64_t)head * a.q_head) * C::SZ + quad * 16;

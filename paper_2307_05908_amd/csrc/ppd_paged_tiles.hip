@@ -47,10 +47,11 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   if (!find_item<TILE_ROWS>(a, idx, idx == 0 && kvh == 0 && wave == 0 && a.least > 0, lane, it)) return;
   const int all_rows = it.n * a.group;
   const int r0 = it.tile * TILE_ROWS + 32 * wave, r = r0 + col, rc = min(r, all_rows - 1), tok = rc / a.group, head = kvh * a.group + rc % a.group;
-  const int pos = r < all_rows ? it.pos0 + tok : -1, from = a.window > 0 ? pos - a.window + 1 : 0;
+  const int pos = r < all_rows ? it.pos0 + tok : -1, from = first_seen(pos, a.window);
   const bool busy = r0 < all_rows;
   const int wave_first = it.pos0 + min(r0, all_rows - 1) / a.group, wave_last = it.pos0 + min(r0 + 31, all_rows - 1) / a.group;    // positions of the wave's rows
   const int tile_first = it.pos0 + it.tile * TILE_ROWS / a.group, tile_last = it.pos0 + min((it.tile * TILE_ROWS + TILE_ROWS - 1) / a.group, it.n - 1);
+  const int wave_from = first_seen(wave_first, a.window), wave_all = first_seen(wave_last, a.window), tile_all = first_seen(tile_last, a.window);   // from where some row of the wave sees, all of its, all of the tile's
   u32x4 q[HD / 16];
   {
     const char* p = (const char*)a.q + ((int64_t)(it.rows0 + tok) * a.q_tok + (int64_t)head * a.q_head) * 2 + half * 16;
@@ -237,12 +238,12 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       if (n + 1 < blocks) request(n + 1);
       place();
       const int base = it.lo + n * KV;
-      if (careful || !(have == ~0ull && base + KV - 1 <= tile_first && (a.window == 0 || base >= tile_last - a.window + 1))) {
+      if (careful || !(have == ~0ull && base + KV - 1 <= tile_first && base >= tile_all)) {
         clean(n, base, have);
         __syncthreads();
       }
-      if (!busy || base > wave_last || (a.window > 0 && base + KV - 1 < wave_first - a.window + 1)) continue;      // no row of the wave sees any of it
-      const bool whole = have == ~0ull && base + KV - 1 <= wave_first && (a.window == 0 || base >= wave_last - a.window + 1);
+      if (!busy || base > wave_last || base + KV - 1 < wave_from) continue;      // no row of the wave sees any of it
+      const bool whole = have == ~0ull && base + KV - 1 <= wave_first && base >= wave_all;
       step(n, base, have, whole);
     }
     if (careful) break;
@@ -261,7 +262,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
     // such a block once more, position by position, from the pages: a row that sees an infinite value, or no number, takes it up
     const int base = it.lo + n * KV, x = base + lane;
     const bool there = __ballot(x < it.hi && page_of(a.b, it.s, x) >= 0) == ~0ull;
-    if (!careful && there && base + KV - 1 <= tile_first && (a.window == 0 || base >= tile_last - a.window + 1)) continue;
+    if (!careful && there && base + KV - 1 <= tile_first && base >= tile_all) continue;
 #pragma unroll 1
     for (int p = base; p < min(base + KV, it.hi); ++p) {
       const int pg = page_of(a.b, it.s, p);

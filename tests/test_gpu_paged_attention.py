@@ -452,3 +452,27 @@ def test_nothing_to_do():
     assert out.shape == (0, 4, 64) and lse.shape == (0, 4)
     b = Batch([0, 0], [5, 0], 4, 2, 64, BF16, pad=3)
     check(b)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("window", [2 ** 30, 2 ** 31 - 64, 2 ** 31 - 2, 2 ** 31 - 1])
+def test_windows_of_all_positions_and_rows_before_the_first(dtype, window):
+    """A window that no position is behind is none, also where kv_len is below the rows."""
+    for new, kv in (([5, 1, 4], [2, 300, 4]), ([70, 60], [60, 200])):
+        b = Batch(new, kv, 8, 2, 64, dtype)
+        out, lse = check(b, window=window)
+        whole, wlse = call(b.cuda())
+        assert torch.equal(out[:b.rows], whole[:b.rows]) and torch.equal(lse[:b.rows], wlse[:b.rows])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_windows_of_rows_far_behind_the_table(dtype):
+    """The last position there may be, and a window that begins in the table: as a row at the table's end whose window begins there."""
+    b = Batch([1, 1], [200, 300], 4, 2, 64, dtype)
+    room = b.pages.shape[1] * b.page
+    for first in (0, 1, 100, 150):
+        b.kv_len[1] = room
+        near, nlse = call(b.cuda(), window=room - first)
+        b.kv_len[1] = 2 ** 31 - 1
+        far, flse = call(b.cuda(), window=2 ** 31 - 1 - first)
+        assert torch.equal(near[1], far[1]) and torch.equal(nlse[1], flse[1])

@@ -74,11 +74,23 @@ struct Item {
   int s, rows0, n, pos0;   // the sequence, its first row of the tensors, its tokens, the first one's position
   int tile, part, parts;
   int slot;                // where its partial results go
-  int lo, hi;              // positions of the part, lo a multiple of PLAN_BLOCK
+  int lo, hi;              // positions of the part, see span_of
 };
 
 // The first position that a row at `pos` sees.  Positions are negative where kv_len is below the rows, and windows go up to 2^31 - 1.
 __host__ __device__ __forceinline__ int first_seen(int pos, int window) { return window > 0 && pos >= window ? pos - window + 1 : 0; }
+
+// Positions of a part of a tile, lo a multiple of PLAN_BLOCK; both 0 where there are none, so that what is looked up ahead of a loop over them is
+// no further off than a few steps behind the table's room (2^30 at most), whatever kv_len is.
+struct Span { int lo, hi; };
+__host__ __device__ __forceinline__ Span span_of(int pos0, int n, int tile, int tile_rows, int group, int part, int parts, int room, int window) {
+  const int first = tile * tile_rows / group, end = (tile * tile_rows + tile_rows - 1) / group, last = end < n - 1 ? end : n - 1;
+  const int to = pos0 + last + 1, hi = to < room ? to : room, lo = first_seen(pos0 + first, window) & -PLAN_BLOCK;
+  if (lo >= hi) return {0, 0};
+  const int blocks = (hi - lo + PLAN_BLOCK - 1) / PLAN_BLOCK, per = (blocks + parts - 1) / parts, b0 = part * per, b1 = b0 + per;
+  if (b0 >= blocks) return {0, 0};
+  return {lo + b0 * PLAN_BLOCK, b1 < blocks ? lo + b1 * PLAN_BLOCK : hi};
+}
 
 struct SeqPlan { int tiles, blocks; SeqRows r; };
 template <int TILE>
@@ -231,11 +243,8 @@ __device__ __forceinline__ bool find_part(const PagedAttnArgs& a, int idx, bool 
 template <int TILE>
 __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, bool tell, int lane, Item& it) {
   if (!(a.least == 0 ? find_whole<TILE>(a, idx, lane, it) : a.b.n_seqs <= WAVE ? find_part<TILE, 1>(a, idx, tell, lane, it) : find_part<TILE, 8>(a, idx, tell, lane, it))) return false;
-  const int first = it.tile * TILE / a.group, last = min((it.tile * TILE + TILE - 1) / a.group, it.n - 1);
-  const int hi = min(it.pos0 + last + 1, a.b.room), lo = first_seen(it.pos0 + first, a.window) & -PLAN_BLOCK;
-  const int blocks = (max(hi - lo, 0) + PLAN_BLOCK - 1) / PLAN_BLOCK, per = (blocks + it.parts - 1) / it.parts;
-  it.lo = lo + min(it.part * per, blocks) * PLAN_BLOCK;
-  it.hi = min(hi, lo + min((it.part + 1) * per, blocks) * PLAN_BLOCK);
+  const Span span = span_of(it.pos0, it.n, it.tile, TILE, a.group, it.part, it.parts, a.b.room, a.window);
+  it.lo = span.lo; it.hi = span.hi;
   return true;
 }
 

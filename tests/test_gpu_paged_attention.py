@@ -476,3 +476,17 @@ def test_windows_of_rows_far_behind_the_table(dtype):
         b.kv_len[1] = 2 ** 31 - 1
         far, flse = call(b.cuda(), window=2 ** 31 - 1 - first)
         assert torch.equal(near[1], far[1]) and torch.equal(nlse[1], flse[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("page", [1, 16])
+@pytest.mark.parametrize("new", [1, 70])
+def test_windows_wholly_behind_the_table(dtype, page, new):
+    """Rows at the last positions there may be, whose window ends before the table begins: they see nothing, and the others are as they were."""
+    b = Batch([new, new], [200, 300], 8, 2, 64, dtype, page=page)
+    ref, rlse = call(b.cuda(), window=50)
+    for length in (2 ** 31 - 1, 2 ** 31 - 64, 2 ** 31 - 129):
+        b.kv_len[1] = length
+        out, lse = call(b.cuda(), window=50)
+        assert torch.equal(out[:new], ref[:new]) and torch.equal(lse[:new], rlse[:new])
+        assert (out[new:] == 0).all() and (lse[new:] == -math.inf).all()

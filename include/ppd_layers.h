@@ -48,7 +48,8 @@ typedef struct {
  * pages[s * pages_stride + p / page_size].  A page number outside [0, n_pages) (-1, say) and a place behind max_pages
  * mean that there is no page: such positions are not written by ppd_paged_append and not seen by ppd_paged_attention.
  * Rows behind the last sequence (q_start[n_seqs] < n_tokens, a padded batch) and before the first are not touched.
- * q_start must not decrease (if it does, which rows are computed is undefined).  All three arrays: DEVICE. */
+ * q_start must not decrease (if it does, which rows of the outputs are written, and what to them, is undefined).  All three
+ * arrays: DEVICE. */
 typedef struct {
   const int32_t *q_start; /* [n_seqs + 1] */
   const int32_t *kv_len;  /* [n_seqs] */

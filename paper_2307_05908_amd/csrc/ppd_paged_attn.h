@@ -20,7 +20,7 @@ struct PagedAttnArgs {
   int64_t q_tok, q_head, o_tok, o_head;
   int64_t kc_page, kc_pos, kc_head, vc_page, vc_pos, vc_head;
   int heads, kv_heads, group, window;
-  int tile_rows;
+  int tile_rows, items;               // items: parts of a key/value head that there are workgroups and places for
   float to_log2;                      // scale * log2(e): a score's exponent of two
   int want, fine, least, whole;       // parts per key/value head to aim at, and among sequences of unlike lengths; blocks of a part at least (0:
                                       // one part each), and up to which a tile is not cut
@@ -239,10 +239,14 @@ __device__ __forceinline__ bool find_part(const PagedAttnArgs& a, int idx, bool 
     }
   return found;
 }
+// Whether parts from place `first` on have places: always, but where q_start decreases and sequences share rows, so that there are more parts than
+// the host has counted.
+__host__ __device__ __forceinline__ bool have_places(int first, int parts, int items) { return first >= 0 && parts <= items - first; }
 
 template <int TILE>
 __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, bool tell, int lane, Item& it) {
   if (!(a.least == 0 ? find_whole<TILE>(a, idx, lane, it) : a.b.n_seqs <= WAVE ? find_part<TILE, 1>(a, idx, tell, lane, it) : find_part<TILE, 8>(a, idx, tell, lane, it))) return false;
+  if (!have_places(it.slot - it.part, it.parts, a.items)) return false;
   const Span span = span_of(it.pos0, it.n, it.tile, TILE, a.group, it.part, it.parts, a.b.room, a.window);
   it.lo = span.lo; it.hi = span.hi;
   return true;
@@ -250,6 +254,6 @@ __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, bool 
 
 // Whether 16 positions in a row that begin at a multiple of 16 lie in one page, within 2^31 bytes
 inline bool near_pages(const PagedAttnArgs& a) { return a.b.page_size % 16 == 0 && a.kc_pos < 1 << 25 && a.vc_pos < 1 << 25; }
-hipError_t launch_paged_tiles(const PagedAttnArgs& a, int dtype, int head_dim, int items, hipStream_t stream);
+hipError_t launch_paged_tiles(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t stream);
 
 }  // namespace ppd

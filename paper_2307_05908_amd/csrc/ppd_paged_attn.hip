@@ -432,10 +432,10 @@ uint64_t next_stamp() {
 }
 
 template <typename T, int HD>
-hipError_t attn_go(const PagedAttnArgs& a, int dtype, int items, hipStream_t stream) {
-  if (a.tile_rows == TILE_ROWS) return launch_paged_tiles(a, dtype, HD, items, stream);
-  if (near_pages(a)) hipLaunchKernelGGL((paged_split_kernel<T, HD, true>), dim3(items * a.kv_heads), dim3(SPLIT_THREADS), 0, stream, a);
-  else hipLaunchKernelGGL((paged_split_kernel<T, HD, false>), dim3(items * a.kv_heads), dim3(SPLIT_THREADS), 0, stream, a);
+hipError_t attn_go(const PagedAttnArgs& a, int dtype, hipStream_t stream) {
+  if (a.tile_rows == TILE_ROWS) return launch_paged_tiles(a, dtype, HD, stream);
+  if (near_pages(a)) hipLaunchKernelGGL((paged_split_kernel<T, HD, true>), dim3(a.items * a.kv_heads), dim3(SPLIT_THREADS), 0, stream, a);
+  else hipLaunchKernelGGL((paged_split_kernel<T, HD, false>), dim3(a.items * a.kv_heads), dim3(SPLIT_THREADS), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -468,13 +468,12 @@ extern "C" int ppd_paged_attention(const ppd_paged_cache* cache, const ppd_paged
   a.q_tok = q->token; a.q_head = q->head; a.o_tok = out->token; a.o_head = out->head;
   a.kc_page = cache->k_page; a.kc_pos = cache->k_pos; a.kc_head = cache->k_head; a.vc_page = cache->v_page; a.vc_pos = cache->v_pos; a.vc_head = cache->v_head;
   a.heads = n_heads; a.kv_heads = cache->n_kv_heads; a.group = n_heads / cache->n_kv_heads; a.window = window; a.to_log2 = scale * 1.44269504f;
-  a.tile_rows = p.tiles ? TILE_ROWS : SPLIT_ROWS; a.want = p.want; a.fine = p.fine; a.least = p.least; a.whole = p.whole;
+  a.tile_rows = p.tiles ? TILE_ROWS : SPLIT_ROWS; a.items = (int)p.items; a.want = p.want; a.fine = p.fine; a.least = p.least; a.whole = p.whole;
   a.part_o = (float*)workspace; a.part_ml = (float2*)((char*)workspace + p.o_bytes); a.stamps = (uint64_t*)((char*)workspace + p.o_bytes + p.ml_bytes);
   a.plan = (int2*)a.stamps;
   a.stamp = next_stamp();
   hipStream_t st = (hipStream_t)hip_stream;
-  const int items = (int)p.items;
   if (cache->head_dim == 64)
-    return launched(dt == PPD_FP32 ? attn_go<float, 64>(a, dt, items, st) : dt == PPD_BF16 ? attn_go<bf16_t, 64>(a, dt, items, st) : attn_go<f16_t, 64>(a, dt, items, st));
-  return launched(dt == PPD_FP32 ? attn_go<float, 128>(a, dt, items, st) : dt == PPD_BF16 ? attn_go<bf16_t, 128>(a, dt, items, st) : attn_go<f16_t, 128>(a, dt, items, st));
+    return launched(dt == PPD_FP32 ? attn_go<float, 64>(a, dt, st) : dt == PPD_BF16 ? attn_go<bf16_t, 64>(a, dt, st) : attn_go<f16_t, 64>(a, dt, st));
+  return launched(dt == PPD_FP32 ? attn_go<float, 128>(a, dt, st) : dt == PPD_BF16 ? attn_go<bf16_t, 128>(a, dt, st) : attn_go<f16_t, 128>(a, dt, st));
 }

@@ -311,12 +311,13 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   const int row = blockIdx.x, lane = threadIdx.x & 63;
   const int s = seq_of_row(a.b, row, lane);
   if (s < 0) return;
+  const SeqRows sr = seq_rows(a.b, s);
+  if ((unsigned)(row - sr.row0) >= (unsigned)sr.rows) return;      // (q_start decreases: the sequence has other rows, or none and no plan)
   const int2 plan = a.plan[s];
   const int parts = plan.y, h = blockIdx.y * RPW + threadIdx.x / LPR, d = (threadIdx.x % LPR) * 4;
   if (parts <= 1 || h >= a.heads) return;
-  const SeqRows sr = seq_rows(a.b, s);
-  const int kvh = h / a.group, r = (row - sr.row0) * a.group + h % a.group;
-  const int64_t first = (int64_t)plan.x + (int64_t)(r / TILE_ROWS) * parts;
+  const int kvh = h / a.group, r = (row - sr.row0) * a.group + h % a.group, first = plan.x + r / TILE_ROWS * parts;
+  if (!have_places(first, parts, a.items)) return;
   float mx = -INFINITY, sum = 0.f;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
   for (int p0 = 0; p0 < parts; p0 += 4) {                  // four parts at a time, their sums and totals in one go
@@ -324,7 +325,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
     f32x4 z[4];
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-      const int64_t at = ((first + min(p0 + p, parts - 1)) * a.kv_heads + kvh) * TILE_ROWS + r % TILE_ROWS;
+      const int64_t at = ((int64_t)(first + min(p0 + p, parts - 1)) * a.kv_heads + kvh) * TILE_ROWS + r % TILE_ROWS;
       ml[p] = a.part_ml[at];
       z[p] = *(const f32x4*)(a.part_o + at * HD + d);
     }
@@ -365,8 +366,8 @@ hipError_t tiles_go(const PagedAttnArgs& a, int head_dim, dim3 grid, hipStream_t
 
 }  // namespace
 
-hipError_t launch_paged_tiles(const PagedAttnArgs& a, int dtype, int head_dim, int items, hipStream_t stream) {
-  const dim3 grid((unsigned)items * a.kv_heads);
+hipError_t launch_paged_tiles(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t stream) {
+  const dim3 grid((unsigned)a.items * a.kv_heads);
   const bool near = near_pages(a);
   if (dtype == PPD_BF16) return near ? tiles_go<bf16_t, true>(a, head_dim, grid, stream) : tiles_go<bf16_t, false>(a, head_dim, grid, stream);
   if (dtype == PPD_FP16) return near ? tiles_go<f16_t, true>(a, head_dim, grid, stream) : tiles_go<f16_t, false>(a, head_dim, grid, stream);

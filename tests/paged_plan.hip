@@ -7,3 +7,5 @@ extern "C" void t_span(int pos0, int n, int tile, int tile_rows, int group, int 
   const ppd::Span s = ppd::span_of(pos0, n, tile, tile_rows, group, part, parts, room, window);
   *lo = s.lo; *hi = s.hi;
 }
+
+extern "C" int t_have_places(int first, int parts, int items) { return ppd::have_places(first, parts, items); }

@@ -490,3 +490,29 @@ def test_windows_wholly_behind_the_table(dtype, page, new):
         out, lse = call(b.cuda(), window=50)
         assert torch.equal(out[:new], ref[:new]) and torch.equal(lse[:new], rlse[:new])
         assert (out[new:] == 0).all() and (lse[new:] == -math.inf).all()
+
+
+STARTS = [[0, 150, 100, 200], [0, 10, 5, 200], [0, 200, 0, 200], [200, 100, 50, 0], [0, 200, -7, 2 ** 31 - 1], [-2 ** 31, 2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1],
+          [0, 200] * 30, [3, 200, 3] * 40]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("starts", STARTS)
+@pytest.mark.parametrize("heads,kv_heads,length", [(8, 8, 3000), (4, 1, 3000), (8, 2, 300), (1, 1, 2000)])
+def test_rows_that_are_no_runs(dtype, starts, heads, kv_heads, length):
+    """Where q_start decreases it is undefined which rows are computed, but the scratch memory and the outputs end where they end, whatever the
+    scratch memory holds."""
+    b = Batch([200], [length], heads, kv_heads, 64, dtype).cuda()
+    seqs = len(starts) - 1
+    start = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    pages, kv_len = b.pages.repeat(seqs, 1).contiguous(), torch.full((seqs,), length, dtype=torch.int32, device="cuda")
+    n_pages, page = b.k_cache.shape[:2]
+    need = binding._attention_workspace((n_pages, page, kv_heads, 64, TYPES.index(dtype), pages.shape[1], seqs, b.n), heads)
+    for fill in (0x00, 0x7f, 0xff):
+        scratch = torch.full((need + 8192,), fill, dtype=torch.uint8, device="cuda")
+        outs = torch.full((b.n + 20, heads, 64), 3.0, dtype=dtype, device="cuda")
+        binding.ppd_paged_attention(b.q, b.k_cache, b.v_cache, pages, start, kv_len, out=outs[10:-10], workspace=scratch[4096:4096 + need])
+        torch.cuda.synchronize()
+        assert (scratch[:4096] == fill).all() and (scratch[4096 + need:] == fill).all()
+        assert (outs[:10] == 3.0).all() and (outs[-10:] == 3.0).all()
+    check(Batch([200], [length], heads, kv_heads, 64, dtype))                # (and what is well-formed is as it was)

@@ -53,3 +53,9 @@ def test_a_tiles_parts(plan, tile_rows, n, group, parts, room):
                     else:
                         assert a == b == 0
                 assert at == (hi if hi > lo else lo)
+
+
+def test_parts_without_places(plan):
+    have = plan.t_have_places
+    assert have(0, 1, 1) and have(5, 3, 8) and have(0, MOST, MOST)
+    assert not have(5, 4, 8) and not have(8, 1, 8) and not have(-1, 1, 8) and not have(MOST, 1, 8) and not have(0, MOST, 8) and not have(7, MOST, 8)

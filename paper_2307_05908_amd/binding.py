@@ -239,6 +239,15 @@ def _same_gpu(dev, *tensors):
             raise ValueError("all tensors on one GPU")
 
 
+def _scratch(workspace):
+    """(address, bytes): those that lie in a row."""
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return workspace.data_ptr(), workspace.nbytes
+
+
 def _paged_args(k_cache, v_cache, pages, q_start, kv_len, n_tokens):
     """(cache, batch) as bytes, and the sizes that a workspace depends on."""
     torch, codes = _layers()[:2]
@@ -341,7 +350,7 @@ def ppd_paged_attention(q, k_cache, v_cache, pages, q_start, kv_len, scale=None,
         if need:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     rc = attention(cache, batch, heads, qr, outr, None if lse is None else lse.data_ptr(), head_dim ** -0.5 if scale is None else scale, window,
-                   None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, raw_stream(dev))
+                   *_scratch(workspace), raw_stream(dev))
     if rc != 0:
         raise PPDError(rc, "ppd_paged_attention", load_library().ppd_last_hip_error(None))
     return out, lse
@@ -392,7 +401,7 @@ def ppd_verify_drafts(target_logits, ids, row_start, uniform, draft_logits=None,
     rc = verify(seqs, n, vocab, code, row_start.data_ptr(), ids.data_ptr(), z.data_ptr(), z.stride(0) if n > 1 else vocab,
                 None if d is None else d.data_ptr(), 0 if d is None else d.stride(0) if n > 1 else vocab,
                 None if temperature is None else temperature.data_ptr(), uniform.data_ptr(), tokens.data_ptr(), accepted.data_ptr(),
-                None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, raw_stream(dev))
+                *_scratch(workspace), raw_stream(dev))
     if rc != 0:
         raise PPDError(rc, "ppd_verify_drafts", load_library().ppd_last_hip_error(None))
     return tokens, accepted

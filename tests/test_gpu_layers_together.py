@@ -6,6 +6,7 @@ import functools
 import pytest
 import torch
 
+from paged_common import Batch
 from paper_2307_05908_amd import binding
 
 pytestmark = pytest.mark.gpu
@@ -222,3 +223,13 @@ def test_sampled_tokens_are_the_same_on_two_streams_at_once():
             with torch.cuda.stream(side):
                 g.append(next(r))
     assert got == alone
+
+
+def test_scratch_memory_that_is_not_in_a_row_is_refused():
+    b = Batch([1, 2], [3000, 90], 4, 2, 128, torch.bfloat16).cuda()
+    thin = torch.zeros(1, dtype=torch.uint8, device="cuda").expand(1 << 26)
+    with pytest.raises(ValueError, match="workspace"):
+        binding.ppd_paged_attention(b.q, b.k_cache, b.v_cache, b.pages, b.q_start, b.kv_len, workspace=thin)
+    with pytest.raises(ValueError, match="workspace"):
+        binding.ppd_verify_drafts(torch.zeros(3, 100, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda"),
+                                  torch.tensor([0, 3], dtype=torch.int32, device="cuda"), torch.zeros(3, 2, device="cuda"), workspace=thin)

@@ -145,3 +145,12 @@ def test_binding_refuses_what_the_library_cannot_see():
     for q in (t(2, 4, 32), t(3, 4, 64), t(2, 4, 64).half(), t(2, 64, 4).transpose(1, 2), t(2, 64)):
         with pytest.raises(ValueError):
             binding._rows(q, k.dtype, 64, "q", 2)
+
+
+def test_binding_refuses_scratch_memory_that_is_not_in_a_row():
+    """An expanded tensor's bytes are those of its shape, not of its memory."""
+    w = torch.zeros(64, dtype=torch.uint8)
+    assert binding._scratch(w) == (w.data_ptr(), 64) and binding._scratch(None) == (None, 0) and binding._scratch(w[16:32]) == (w.data_ptr() + 16, 16)
+    for bad in (torch.zeros(1, dtype=torch.uint8).expand(1 << 20), w[::2], torch.zeros(8, 8, dtype=torch.uint8).t()[:, :4]):
+        with pytest.raises(ValueError):
+            binding._scratch(bad)

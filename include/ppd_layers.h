@@ -83,7 +83,8 @@ int ppd_paged_append(const ppd_paged_cache *cache, const ppd_paged_batch *batch,
                      const void *k_gain, float norm_eps, int rotary_dim, float rope_theta, void *hip_stream);
 
 /* Attention of the new tokens over their sequences' pages: query head h reads key/value head h / (n_heads / n_kv_heads)
- * (n_heads a multiple of n_kv_heads; PPD_ELIMIT where n_tokens * n_heads / n_kv_heads passes 2^26),
+ * (n_heads a multiple of n_kv_heads; PPD_ELIMIT where n_tokens * n_heads / n_kv_heads passes 2^26, or a launch would have 2^24
+ * workgroups: from about n_tokens * n_heads = 2^28 on, 2^31 for long runs of 16-bit types),
  *   out = sum_j softmax_j(scale * q . k_j) v_j
  * over the sequence's positions j up to the row's own (the new tokens' keys and values are in the pages already) and, with
  * window > 0, the last `window` of them only, its own included.  scale > 0, at most 2^127.  A row that sees no position gives

@@ -418,6 +418,7 @@ int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, 
   // 8000 462 / 476, but 128 of these 250 / 198; long runs, two prompts of 3700 to 4096 tokens 285 / 298, six chunks of 700 over 500 86 / 96.)
   if (tiles >= (p->tiles ? 2 : 8) * p->want || capacity <= p->whole * PLAN_BLOCK) p->least = 0;
   p->items = tiles + (p->least ? p->fine + 1 : 0);
+  if (p->items * cache->n_kv_heads >= (int64_t)1 << 24) return PPD_ELIMIT;      // (a launch has fewer than 2^32 threads, 256 to a workgroup)
   const uint64_t places = p->least ? (uint64_t)p->items * cache->n_kv_heads : 0;
   p->o_bytes = places * tile_rows * cache->head_dim * 4;
   p->ml_bytes = places * tile_rows * 8;

@@ -90,6 +90,16 @@ def test_workspace_of_attention_is_checked():
     assert lib.ppd_paged_attention_workspace(cache(), batch(), 16, None) == EINVAL
 
 
+@pytest.mark.parametrize("dtype,tokens,heads", [(0, 1 << 22, 64), (0, 1 << 19, 512), (1, 1 << 22, 512)])
+def test_more_workgroups_than_a_launch_may_have(dtype, tokens, heads):
+    """Refused, and by the size of its scratch memory already; half of it is not."""
+    lib, need = binding.load_library(), ctypes.c_uint64()
+    c, q = cache(dtype=dtype, n_kv_heads=heads // 2, k_head=64, v_head=64), rows(token=heads * 64)
+    for n, rc in ((tokens, ELIMIT), (tokens // 2, 0)):
+        assert lib.ppd_paged_attention_workspace(c, batch(n_tokens=n), heads, ctypes.byref(need)) == rc
+    assert attention(c=c, b=batch(n_tokens=tokens), heads=heads, q=q, out=q) == ELIMIT
+
+
 def test_bad_append_arguments():
     assert append(heads=-1) == EINVAL and append(heads=1025) == ELIMIT
     for r in (-8, 4, 60, 72):

@@ -29,7 +29,7 @@ extern "C" {
 #define PPD_MAX_HEADS 1024
 
 /* Keys and values in pages: k and v are [n_pages][page_size][n_kv_heads][head_dim], in any order of the first three
- * that the strides (in elements) express; head_dim is contiguous.  Every row of head_dim elements begins at a multiple
+ * that the strides (in elements) express; head_dim is contiguous (strides of 0: for ppd_paged_attention only).  Every row of head_dim elements begins at a multiple
  * of 16 bytes (so do the tensors, and so do all strides). */
 typedef struct {
   void *k, *v;

@@ -125,6 +125,10 @@ extern "C" int ppd_paged_append(const ppd_paged_cache* cache, const ppd_paged_ba
   if (rc) return rc;
   const int dt = cache->dtype, n = batch->n_tokens;
   if (n_heads < 0) return PPD_EINVAL;
+  const auto apart = [](int64_t stride, int count) { return count <= 1 || stride > 0; };      // (rows that are written must not lie on each other)
+  if (!apart(cache->k_page, cache->n_pages) || !apart(cache->v_page, cache->n_pages) || !apart(cache->k_pos, cache->page_size) || !apart(cache->v_pos, cache->page_size) ||
+      !apart(cache->k_head, cache->n_kv_heads) || !apart(cache->v_head, cache->n_kv_heads))
+    return PPD_EINVAL;
   if (rotary_dim < 0 || rotary_dim > cache->head_dim || rotary_dim % 8) return PPD_EINVAL;
   if (rotary_dim > 0 && !(rope_theta > 0.f && isfinite(rope_theta))) return PPD_EINVAL;
   if ((q_gain || k_gain) && !(norm_eps >= 0.f && isfinite(norm_eps))) return PPD_EINVAL;

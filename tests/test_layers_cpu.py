@@ -114,6 +114,12 @@ def test_bad_append_arguments():
     assert append(q_out=rows(p=1 << 20, token=0)) == EINVAL
 
 
+@pytest.mark.parametrize("name", ["k_page", "k_pos", "k_head", "v_page", "v_pos", "v_head"])
+def test_append_to_pages_that_lie_on_each_other(name):
+    assert append(c=cache(**{name: 0})) == EINVAL
+    assert append(c=cache(n_pages=1, page_size=1, n_kv_heads=1, **{name: 0}), b=batch(n_tokens=0)) == 0      # (nothing to lie on)
+
+
 def test_nothing_to_do_is_no_error():
     assert attention(b=batch(n_tokens=0)) == 0 and append(b=batch(n_tokens=0)) == 0
 

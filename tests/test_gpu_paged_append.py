@@ -203,3 +203,20 @@ def test_streams_and_replays():
         want = binding.ppd_paged_append(ref_k, ref_v, *args, b.q, b.k, b.v, rotary_dim=128)
         torch.cuda.synchronize()
         assert torch.equal(got, want) and torch.equal(gk, ref_k)
+
+
+@pytest.mark.parametrize("starts", [[0, 20, 10, 30], [30, 20, 10, 0], [0, 30, -7, 2 ** 31 - 1], [-2 ** 31, 2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1], [0, 30] * 30])
+def test_rows_that_are_no_runs(starts):
+    """Where q_start decreases it is undefined which rows are written; what is written lies in the outputs and in the pages of the table."""
+    b, seqs = Batch([30], [90], 4, 2, 64, torch.float32, spare=5).cuda(), len(starts) - 1
+    start, kv_len = torch.tensor(starts, dtype=torch.int32, device="cuda"), torch.full((seqs,), 90, dtype=torch.int32, device="cuda")
+    n = b.k_cache.shape[0]
+    ks, vs = (torch.full((n + 4, *b.k_cache.shape[1:]), 5.0, device="cuda") for _ in range(2))
+    outs = torch.full((40, 4, 64), 5.0, device="cuda")
+    binding.ppd_paged_append(ks[2:-2], vs[2:-2], b.pages.repeat(seqs, 1).contiguous(), start, kv_len, b.q, b.k, b.v, rotary_dim=64, q_out=outs[5:-5])
+    torch.cuda.synchronize()
+    mine = torch.zeros(n, dtype=torch.bool)
+    mine[b.pages.cpu().flatten().long()] = True
+    for t in (ks, vs):
+        assert (t[:2] == 5.0).all() and (t[-2:] == 5.0).all() and (t[2:-2].cpu()[~mine] == 5.0).all()
+    assert (outs[:5] == 5.0).all() and (outs[-5:] == 5.0).all()

@@ -344,3 +344,44 @@ def test_streams_and_replays():
             want = run(d)
             torch.cuda.synchronize()
             assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("with_draft", [True, False])
+def test_a_random_number_of_zero_takes_every_draft_that_is_left(with_draft):
+    """u = 0: a draft is taken if its probability is above 0, that is, wherever filtering has left it."""
+    c = make([3, 2, 4, 1, 6, 2], 1000, torch.float32, 8, with_draft, temp=[0.8, 1.0, 0.3, 2.0, 1.0, 0.8], kept=20)
+    c["u"][:] = 0.0
+    z, ids, start = c["z"].numpy(), c["ids"].numpy(), c["start"].numpy()
+    for s, i in ((0, 1), (4, 4)):                        # (a drafter may go by other logits than it says: two drafts that filtering has taken out)
+        ids[start[s] + i + 1] = np.nonzero(~np.isfinite(z[start[s] + i]))[0][7]
+    want = []
+    for s, m in enumerate(c["drafts"]):
+        gone = [i for i in range(m) if not np.isfinite(z[start[s] + i, ids[start[s] + i + 1]])]
+        want.append(gone[0] if gone else m)
+    assert 0 < sum(want) < sum(c["drafts"])              # (some are left, some are not)
+    t, a = call(c)
+    np.testing.assert_array_equal(a.cpu().numpy(), want)
+    t = t.cpu().numpy()
+    for s in range(len(want)):
+        r = start[s] + want[s]
+        left = np.isfinite(z[r])
+        if with_draft is False and want[s] < c["drafts"][s]:
+            left[ids[r + 1]] = False
+        assert left[t[r]] and (t[start[s]:r] == ids[start[s] + 1:r + 1]).all() and (t[r + 1:start[s + 1]] == -1).all()
+
+
+@pytest.mark.parametrize("starts", [[0, 6, 3, 9], [9, 6, 3, 0], [0, 9, -5, 2 ** 31 - 1], [-2 ** 31, 2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1], [0, 9] * 30])
+@pytest.mark.parametrize("vocab", [700, 9000])
+@pytest.mark.parametrize("fill", [0x00, 0x7f, 0xff])
+def test_rows_that_are_no_runs(starts, vocab, fill):
+    """Where row_start decreases it is undefined which rows are written, but scratch memory and outputs end where they end, whatever the former
+    holds."""
+    c, seqs = make([8], vocab, torch.float32, 3), len(starts) - 1
+    need = binding._verify_workspace(seqs, 9, vocab, 0)
+    scratch = torch.full((need + 8192,), fill, dtype=torch.uint8, device="cuda")
+    tokens, accepted = (torch.full((n + 64,), 77, dtype=torch.int32, device="cuda") for n in (9, seqs))
+    binding.ppd_verify_drafts(c["z"].cuda(), c["ids"].cuda(), torch.tensor(starts, dtype=torch.int32, device="cuda"), c["u"].cuda(), draft_logits=c["zd"].cuda(),
+                              temperature=torch.full((seqs,), 0.8, device="cuda"), tokens=tokens[32:41], accepted=accepted[32:32 + seqs], workspace=scratch[4096:4096 + need])
+    torch.cuda.synchronize()
+    assert (scratch[:4096] == fill).all() and (scratch[4096 + need:] == fill).all()
+    assert (tokens[:32] == 77).all() and (tokens[41:] == 77).all() and (accepted[:32] == 77).all() and (accepted[32 + seqs:] == 77).all()

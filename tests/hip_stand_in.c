@@ -1,6 +1,6 @@
 /* Stand-in for the HIP runtime, for tests of the library's host code without a GPU: device memory is host memory, kernels do not
  * run, and what the host asks for is written down.  A replayed round reports a token and a match index to the pinned memory as its
- * last kernel would.  Loaded with RTLD_GLOBAL before libppd.so, whose calls then come here.  One thread, one context at a time. */
+ * last kernel would; one that goes launch by launch reports once the host waits for the stream.  Loaded with RTLD_GLOBAL before libppd.so, whose calls then come here.  One thread, one context at a time. */
 #include <stdint.h>
 #include <stdio.h>
 #include <stdlib.h>
@@ -23,6 +23,10 @@ static size_t log_at;
 int si_destroyed_under_way;              /* executable graphs destroyed before the stream was waited for behind their last launch */
 int si_destroyed;
 int32_t si_token = 1, si_match = -1;     /* what the next rounds report */
+int si_lose;                             /* captures that are lost from now on, as by another thread's device synchronisation: launches fail in
+                                            one, and go on failing until another capture has come to a good end */
+int si_refused;                          /* launches that failed */
+static int broken, last_error, selected;
 void si_clear(void) { log_at = 0; si_log[0] = 0; }
 
 static void line(const char *kind, const char *what) {
@@ -49,13 +53,21 @@ err_t __hipPopCallConfiguration(dim3_t *g, dim3_t *b, size_t *lds, void **st) { 
 err_t hipLaunchKernel(const void *f, dim3_t g, dim3_t b, void **args, size_t lds, void *st) {
   (void)args; (void)st;
   if (!g.x || !g.y || !g.z || !b.x || lds > 160 * 1024) abort();
-  if (!capturing) { line("K", name_of(f)); return 0; }
+  if (broken || (capturing && si_lose)) { si_refused += 1; return last_error = 901; }
+  if (!capturing) { line("K", name_of(f)); selected |= strstr(name_of(f), "select_kernel") != NULL; return 0; }
   if (cap->n == MAX_NODES) abort();
   cap->node[cap->n++] = name_of(f);
   return 0;
 }
 err_t hipStreamBeginCapture(void *s, int mode) { (void)s; (void)mode; capturing = 1; cap = calloc(1, sizeof *cap); line("C", ""); return 0; }
-err_t hipStreamEndCapture(void *s, void **g) { (void)s; capturing = 0; *g = cap; cap = NULL; return 0; }
+err_t hipStreamEndCapture(void *s, void **g) {
+  (void)s;
+  capturing = 0; *g = cap; cap = NULL; broken = 0;
+  if (!si_lose) return 0;
+  si_lose -= 1; broken = 1;
+  free(*g); *g = NULL;
+  return last_error = 901;
+}
 err_t hipGraphInstantiate(void **e, void *g, void *a, char *b, size_t c) { (void)a; (void)b; (void)c; *e = malloc(sizeof(graph_t)); memcpy(*e, g, sizeof(graph_t)); return 0; }
 err_t hipGraphDestroy(void *g) { free(g); return 0; }
 err_t hipGraphLaunch(void *e, void *s) {
@@ -64,7 +76,7 @@ err_t hipGraphLaunch(void *e, void *s) {
   line("G", "");
   for (int i = 0; i < g->n; ++i) line("K", g->node[i]);
   if (last_launch) last_launch->under_way = 0;             /* (has ended before this round reports) */
-  g->under_way = 1; last_launch = g;
+  g->under_way = 1; last_launch = g; selected = 0;
   pinned[0] = si_token; pinned[1] = si_match; pinned[SEQ] += 1;
   return 0;
 }
@@ -76,7 +88,12 @@ err_t hipGraphExecDestroy(void *e) {
   free(g);
   return 0;
 }
-err_t hipStreamSynchronize(void *s) { if (s && last_launch) last_launch->under_way = 0; line("S", ""); return 0; }
+err_t hipStreamSynchronize(void *s) {
+  if (s && last_launch) last_launch->under_way = 0;
+  line("S", "");
+  if (selected) { pinned[0] = si_token; pinned[1] = si_match; pinned[SEQ] += 1; selected = 0; }
+  return 0;
+}
 
 err_t hipMalloc(void **p, size_t n) { *p = calloc(1, n ? n : 1); return *p ? 0 : 2; }
 err_t hipFree(void *p) { free(p); return 0; }
@@ -96,7 +113,7 @@ err_t hipEventDestroy(void *e) { free(e); return 0; }
 err_t hipEventRecord(void *e, void *s) { (void)e; (void)s; return 0; }
 err_t hipEventSynchronize(void *e) { (void)e; return 0; }
 err_t hipEventElapsedTime(float *f, void *a, void *b) { (void)a; (void)b; *f = 1.f; return 0; }
-err_t hipGetLastError(void) { return 0; }
+err_t hipGetLastError(void) { const int e = last_error; last_error = 0; return e; }
 err_t hipFuncSetAttribute(const void *f, int a, int v) { (void)f; (void)a; (void)v; return 0; }
 err_t hipGetDevice(int *d) { *d = 0; return 0; }
 err_t hipDeviceGetAttribute(int *v, int a, int d) { (void)a; (void)d; *v = 256; return 0; }

@@ -144,3 +144,30 @@ for plain in (False, True):
     assert counter("si_destroyed_under_way") == 0
     C.close()
 """, PPD_FUSED="2")
+
+
+@pytest.mark.parametrize("lost", [1, 2, 5])
+@pytest.mark.parametrize("plain", [False, True])
+def test_a_round_whose_capture_is_lost_goes_launch_by_launch(stand_in, plain, lost):
+    """Another thread's device synchronisation takes a capture with it (and empty ones behind it, maybe): the round then is the launches that its
+    capture would have held, none of them on a stream that still refuses them, and the next round is captured again."""
+    run(stand_in, f"""
+plain, lost = {plain}, {lost}
+C = Context()
+C.prefill(64)
+C.step(plain)
+_, whole = C.step(plain)
+C.close()
+D = Context()
+D.prefill(64)
+D.step(plain)
+refused = counter("si_refused")
+ctypes.c_int.in_dll(SI, "si_lose").value = lost
+before, inside = D.step(plain)                                 # (of the second round, whose shape is not captured yet)
+assert counter("si_lose") == 0 and not inside and before == whole, (before, whole)
+inside = counter("si_refused") - refused
+assert inside == 1 or inside <= len(whole), inside            # (in the lost capture alone)
+again, replayed = D.step(plain)
+assert not again and replayed == whole
+D.close()
+""", PPD_FUSED="2")

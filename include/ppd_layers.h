@@ -6,8 +6,9 @@
  * pages needs no undoing: the next step's tokens are written over it.
  *
  * All three only queue their work on hip_stream (a hipStream_t of the current device, NULL = its default stream): they
- * allocate nothing, wait for nothing, keep nothing from call to call, and may be captured into HIP graphs.  Tensors are
- * DEVICE memory, borrowed until the queued work has run; the structs are HOST and are read before the call returns.
+ * allocate nothing, wait for nothing, keep nothing from call to call but a count of attention's (the number that a call's
+ * workgroups mark their scratch memory with), and may be captured into HIP graphs.  Tensors are DEVICE memory, borrowed
+ * until the queued work has run; the structs are HOST and are read before the call returns.
  * Scratch memory is the caller's; calls whose work may overlap in time need scratch of their own each, and so do graphs
  * whose replays may overlap.
  * Return codes as in ppd.h: PPD_EINVAL before anything is queued, PPD_ELIMIT for sizes beyond a stated maximum,
@@ -87,15 +88,16 @@ int ppd_paged_append(const ppd_paged_cache *cache, const ppd_paged_batch *batch,
  * workgroups: from about n_tokens * n_heads = 2^28 on, 2^31 for long runs of 16-bit types),
  *   out = sum_j softmax_j(scale * q . k_j) v_j
  * over the sequence's positions j up to the row's own (the new tokens' keys and values are in the pages already) and, with
- * window > 0, the last `window` of them only, its own included.  scale > 0, at most 2^127.  A row that sees no position gives
- * zeros.  What a row does not see has no part in its result, whatever its bits (infinities, NaN, pages of other
- * sequences).
+ * window > 0, the last `window` of them only, its own included.  scale > 0, at most 2^127 (fp32: scale * log2 e times
+ * each component of a query has to be finite, too).  A row that sees no position gives zeros.  What a row does not see
+ * has no part in its result, whatever its bits (infinities, NaN, pages of other sequences).  out may be q itself (the
+ * same strides), and overlaps no other input.
  * lse: DEVICE float [n_tokens][n_heads] or NULL: log of the sum of exp(scale * q . k_j), -inf where nothing is seen (for
  * a merge with attention over other positions).
  * Scores, softmax and sums are fp32; a 16-bit type's softmax weights go into their product with the values as two terms
- * of the type, so that the result's own rounding is what counts.  Beyond the order of additions
- * (a sequence's positions are cut into as many parts as the batch leaves compute units for) results do not depend on what
- * else is in the batch, and two calls with the same arguments give the same bits.
+ * of the type, so that the result's own rounding is what counts.  Beyond the order of additions (a sequence's positions
+ * are cut into as many parts as the batch leaves compute units for) results do not depend on what else is in the batch,
+ * and two calls with the same arguments give the same bits.
  * workspace: DEVICE scratch of at least the bytes that ppd_paged_attention_workspace gives for the same arguments (it
  * depends on sizes only, not on lengths), 16-byte aligned; NULL where those are 0.  PPD_EINVAL if workspace_bytes is less. */
 int ppd_paged_attention(const ppd_paged_cache *cache, const ppd_paged_batch *batch, int n_heads, const ppd_rows *q,
@@ -123,8 +125,8 @@ int ppd_paged_attention_workspace(const ppd_paged_cache *cache, const ppd_paged_
  * taken.  uniform: DEVICE float [n_rows][2] in [0, 1).
  * Out, DEVICE: tokens int32 [n_rows]: at a sequence's rows the drafts taken, then the drawn token, then -1; accepted
  * int32 [n_seqs]: the number of drafts taken (the sequence gained that many tokens and one more; 0 for one without
- * rows).  Rows of no sequence are not touched.  vocab 1 .. 2^24, n_rows 0 .. PPD_MAX_TOKENS, n_seqs 1 .. PPD_MAX_SEQS,
- * n_rows * ceil(vocab / 4096) at most 2^23.
+ * rows).  Rows of no sequence are not touched; no output overlaps an input.  vocab 1 .. 2^24, n_rows 0 ..
+ * PPD_MAX_TOKENS, n_seqs 1 .. PPD_MAX_SEQS, n_rows * ceil(vocab / 4096) at most 2^23.
  * target_logits and draft_logits of type dtype, aligned to it (any stride of at least vocab).  workspace as above, from
  * ppd_verify_drafts_workspace. */
 int ppd_verify_drafts(int n_seqs, int n_rows, int vocab, int dtype, const int32_t *row_start, const int32_t *ids,

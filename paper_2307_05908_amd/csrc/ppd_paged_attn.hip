@@ -398,10 +398,12 @@ int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, 
   const int group = n_heads / cache->n_kv_heads;
   const int64_t rows = (int64_t)batch->n_tokens * group, some = batch->n_tokens < batch->n_seqs ? batch->n_tokens : batch->n_seqs;
   const int64_t capacity = (int64_t)batch->max_pages * cache->page_size;
-  // Which kernel: paged_tile_kernel for 16-bit types and more than 32 rows a sequence (bf16, 8 key/value heads, 2000 positions, us of the split /
-  // the tile kernel: 8 sequences of 16 rows 21.2 / 21.9, of 32 25.4 / 22.5, of 48 32.2 / 23.8; 32 of 32 54.7 / 52.2), but not where these are
-  // few in all, over no great lengths: the split kernel then has more workgroups to fill the chip with (one sequence of 128 rows over 200 positions
-  // 9.1 / 12.5, over 2000 17.3 / 21.6, over 20000 66 / 44).
+  // Which kernel: paged_tile_kernel for 16-bit types and more than 32 rows a sequence, where the split kernel reads keys and values a third time.
+  // bf16, 8 key/value heads, us of the split / the tile kernel: 8 sequences over 2000 positions of 16 rows each 20.8 / 23.6, of 40 30.7 / 24.6; 32
+  // sequences 45.3 / 49.8 and 81.5 / 56.7.  At 17 to 32 rows either may be the quicker one (32 rows: 8 sequences 24.3 / 23.7, 32 of them 53.8 / 51.7,
+  // over 8000 positions 60.5 / 51.4 and 239 / 194, but over 500 13.1 / 17.6 and 20.6 / 20.2, with heads of 64 16.8 / 20.9 and 28.3 / 34.3).  The split
+  // kernel, too, where rows are few in all, over no great lengths: it then has more workgroups to fill the chip with (one sequence of 128 rows over
+  // 200 positions 9.2 / 13.7, over 2000 16.9 / 25.0, over 8000 34.5 / 29.0, over 20000 65 / 46).
   p->tiles = cache->dtype != PPD_FP32 && rows > 32 * (int64_t)batch->n_seqs && (rows * cache->n_kv_heads > 1024 || capacity > 8192);
   const int tile_rows = p->tiles ? TILE_ROWS : SPLIT_ROWS;
   const int64_t tiles = rows / tile_rows + some;
@@ -411,11 +413,11 @@ int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, 
   p->whole = p->tiles ? 8 : 4;
   p->least = p->tiles ? 8 : 2;
   // (slots, one sequence of 60000 positions, 8 key/value heads, bf16, at 256 / 512 / 1024 / 2048: 48 / 55 / 67 / 97 us; fine: find_part.
-  // Long runs, at 384 / 512 / 640 / 1024: three chunks of 140 over 15000 219 / 173 / 203 / 175, a chunk of 500 over 4000 86 / 80 / 88 / 90.
+  // Long runs, at 384 / 512 / 640 / 1024: three chunks of 140 over 15000 203 / 171 / 203 / 179, a chunk of 500 over 4000 103 / 86 / 98 / 98.
   // least, at 2 / 4 / 6: one token over 700 positions 10.8 / 11.4 / 12.6, four of 500 9.3 / 10.8 / 10.8, two fp32 ones of 1000 14.2 / 17.1 / 21.0.  whole: one
   // token over 200 positions in one part / two 7.5 / 8.6, over 300 9.7 / 9.3.)
   // Tiles enough for the whole chip, or no position to cut at: one part each.  (At whole / in parts: 300 sequences of 500 positions 128 / 156, of 60 to
-  // 8000 462 / 476, but 128 of these 250 / 198; long runs, two prompts of 3700 to 4096 tokens 285 / 298, six chunks of 700 over 500 86 / 96.)
+  // 8000 462 / 476, but 128 of these 250 / 198; long runs, two prompts of 3800 and 4000 tokens 350 / 366, six chunks of 700 over 500 105 / 114.)
   if (tiles >= (p->tiles ? 2 : 8) * p->want || capacity <= p->whole * PLAN_BLOCK) p->least = 0;
   p->items = tiles + (p->least ? p->fine + 1 : 0);
   if (p->items * cache->n_kv_heads >= (int64_t)1 << 24) return PPD_ELIMIT;      // (a launch has fewer than 2^32 threads, 256 to a workgroup)

@@ -1,7 +1,7 @@
 // ppd_paged_attention, many rows: bound by the matrix units and the issue of instructions beside them: a 32 x 32 x 16 product keeps its SIMD's
 // vector units from the other wave for two thirds of its 32 cycles, and a block of 64 positions is 48 products of a wave (16 of them for the
 // weights' second term), 32 exponentials and some 240 other vector instructions.  Two bf16 prompts of 3800 and 4000 tokens (32 heads, 8 of keys
-// and values, 249 GFLOP, 374 with the second term): 344 us, 1090 TFLOP/s of products; a large matrix product of the library's reaches 1200.
+// and values, 249 GFLOP, 374 with the second term): 344 to 352 us from card to card, 1060 to 1090 TFLOP/s of products; a large matrix product of the library's reaches 1200.
 // With weights of one term, rounded to the type: 267 us, and an error of 2.1e-3 of bf16 outputs where their own rounding is 1.6e-3.
 // (Tried and not kept: the first terms' products before the second terms' and weights' rests by a dot instruction, one a weight less: the same time.
 // With one term, beside 283 us at the time: the next block's scores between this one's exponentials, 286 to 292; a higher priority for
@@ -31,7 +31,7 @@ __device__ __forceinline__ void dma16_near(const void* base, int offset, void* l
 // keys as they are, the left operand of S^T = K Q^T; values through the transposing reads, the left operand of O^T = V^T P^T.  The next
 // block is under way while one is worked on, with one barrier a block; two workgroups on a compute unit fill each other's gaps.
 // NEAR: 16 positions in a row that begin at a multiple of 16 lie in one page, within 2^31 bytes, so that a wave's share of a block has one
-// page and the lanes 32-bit offsets in it (the two prompts 286 us, not 312; 500 tokens over 4000 positions 76, not 83).
+// page and the lanes 32-bit offsets in it (the two prompts 350 us, not 377; 500 tokens over 4000 positions 86, not 91).
 template <typename T, int HD, bool NEAR>
 __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   constexpr int KV = PLAN_BLOCK, ROWB = HD * 2, UNITS = HD / 8, RPI = WAVE / UNITS, NI = 16 / RPI, SIDE = KV * ROWB;
@@ -39,7 +39,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   // Workgroups go round the eight XCDs in turn, so with the heads of a part side by side those of a key/value head meet on one XCD where there are
   // a multiple of eight heads, and its L2 has the head's keys and values; and the longest parts of all heads come first.  (All of a head's
-  // tiles before the next head's: 3000 fp16 rows of 40 heads 256 us, not 231.)
+  // tiles before the next head's: 3000 fp16 rows of 40 heads 215 us, not 161.)
   const int kvheads = a.kv_heads, idx = blockIdx.x / kvheads, kvh = blockIdx.x % kvheads;
   __shared__ int s_odd[2];                                 // first and last block from which a value that is infinite, or no number, was cleared
   if (threadIdx.x == 0) { s_odd[0] = 0x7fffffff; s_odd[1] = -1; }
@@ -304,7 +304,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
 }
 
 // The parts of a row joined, in their order: HD / 4 lanes for a row.  Bound by reading them (500 rows of 40 heads in 3 parts, 31 MB: 9 us).  A launch
-// of its own: joined by the workgroups that had the parts, as paged_split_kernel does, 500 tokens over 4000 positions took 143 us, not 86.
+// of its own: joined by the workgroups that had the parts, as paged_split_kernel does, 500 tokens over 4000 positions took 143 us beside 86 then.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   constexpr int LPR = HD / 4, RPW = 256 / LPR;

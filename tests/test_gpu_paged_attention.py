@@ -516,3 +516,12 @@ def test_rows_that_are_no_runs(dtype, starts, heads, kv_heads, length):
         assert (scratch[:4096] == fill).all() and (scratch[4096 + need:] == fill).all()
         assert (outs[:10] == 3.0).all() and (outs[-10:] == 3.0).all()
     check(Batch([200], [length], heads, kv_heads, 64, dtype))                # (and what is well-formed is as it was)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("new,kv", [([1], [3000]), ([3, 20, 1], [50, 60, 700]), ([300, 250], [300, 400]), ([130], [2500])])
+def test_in_place(dtype, new, kv):
+    d = Batch(new, kv, 8, 2, 64, dtype).cuda()
+    ref, _ = call(d)
+    got, _ = call(d, out=d.q)
+    assert got is d.q and torch.equal(got, ref)

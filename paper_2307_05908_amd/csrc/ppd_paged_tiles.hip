@@ -1,6 +1,6 @@
 // ppd_paged_attention, many rows: bound by the matrix units and the issue of instructions beside them: a 32 x 32 x 16 product keeps its SIMD's
 // vector units from the other wave for two thirds of its 32 cycles, and a block of 64 positions is 48 products of a wave (16 of them for the
-// weights' second term), 32 exponentials and some 240 other vector instructions.  Two bf16 prompts of 3800 and 4000 tokens (32 heads, 8 of keys
+// weights' second term), 32 exponentials and some 270 other vector instructions.  Two bf16 prompts of 3800 and 4000 tokens (32 heads, 8 of keys
 // and values, 249 GFLOP, 374 with the second term): 344 to 352 us from card to card, 1060 to 1090 TFLOP/s of products; a large matrix product of the library's reaches 1200.
 // With weights of one term, rounded to the type: 267 us, and an error of 2.1e-3 of bf16 outputs where their own rounding is 1.6e-3.
 // (Tried and not kept: the first terms' products before the second terms' and weights' rests by a dot instruction, one a weight less: the same time.
@@ -20,6 +20,20 @@ __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c, bf16_t) {
 __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c, f16_t) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
+// Two weights as two terms of the type, side by side.  The first is cut off, not rounded, and the second is not zero where the weight is not (the
+// type's smallest normal number, or half floats' smallest one, 2^-31 of the row's largest weight): a value that is infinite has its sign in both
+// products.  (The rests of rounded first terms need a second pass without such values, 9 ms, not 0.6, for the two prompts where no value is a number;
+// else the same time.)
+__device__ __forceinline__ u32x2 two_terms(float x, float y, bf16_t) {
+  const uint32_t u = __float_as_uint(x), v = __float_as_uint(y);
+  const float a = x - __uint_as_float(u & 0xffff0000u), b = y - __uint_as_float(v & 0xffff0000u);
+  return (u32x2){__builtin_amdgcn_perm(v, u, 0x07060302u), pair(__builtin_amdgcn_fmed3f(a, x, 0x1p-126f), __builtin_amdgcn_fmed3f(b, y, 0x1p-126f), bf16_t())};
+}
+__device__ __forceinline__ u32x2 two_terms(float x, float y, f16_t) {
+  const auto h = __builtin_amdgcn_cvt_pkrtz(x, y);
+  const float a = x - (float)h[0], b = y - (float)h[1];
+  return (u32x2){__builtin_bit_cast(uint32_t, h), pair(__builtin_amdgcn_fmed3f(a, x, 0x1p-24f), __builtin_amdgcn_fmed3f(b, y, 0x1p-24f), f16_t())};
+}
 // dma16 with the lanes' sources as 32-bit offsets from one address
 __device__ __forceinline__ void dma16_near(const void* base, int offset, void* lds_dst) {
   const unsigned la = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds_dst;
@@ -30,10 +44,11 @@ __device__ __forceinline__ void dma16_near(const void* base, int offset, void* l
 // source, so the rows of a block may lie anywhere, and 16-byte pieces change places within a row so that no operand's reads meet on a bank):
 // keys as they are, the left operand of S^T = K Q^T; values through the transposing reads, the left operand of O^T = V^T P^T.  The next
 // block is under way while one is worked on, with one barrier a block; two workgroups on a compute unit fill each other's gaps.
+// Heads of 64 leave registers for four workgroups a unit, if the compiler is asked (three: two prompts of 3000 151 us, not 143).
 // NEAR: 16 positions in a row that begin at a multiple of 16 lie in one page, within 2^31 bytes, so that a wave's share of a block has one
 // page and the lanes 32-bit offsets in it (the two prompts 350 us, not 377; 500 tokens over 4000 positions 86, not 91).
 template <typename T, int HD, bool NEAR>
-__global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(256, HD == 64 ? 4 : 2) void paged_tile_kernel(PagedAttnArgs a) {
   constexpr int KV = PLAN_BLOCK, ROWB = HD * 2, UNITS = HD / 8, RPI = WAVE / UNITS, NI = 16 / RPI, SIDE = KV * ROWB;
   __shared__ __align__(1024) char lds[4 * SIDE];           // [2 buffers][keys, values][64 positions][head_dim]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
@@ -41,7 +56,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   // a multiple of eight heads, and its L2 has the head's keys and values; and the longest parts of all heads come first.  (All of a head's
   // tiles before the next head's: 3000 fp16 rows of 40 heads 215 us, not 161.)
   const int kvheads = a.kv_heads, idx = blockIdx.x / kvheads, kvh = blockIdx.x % kvheads;
-  __shared__ int s_odd[2];                                 // first and last block from which a value that is infinite, or no number, was cleared
+  __shared__ int s_odd[2];                                 // first and last block with a value that is infinite, or no number, where not every row sees it
   if (threadIdx.x == 0) { s_odd[0] = 0x7fffffff; s_odd[1] = -1; }
   Item it;
   if (!find_item<TILE_ROWS>(a, idx, idx == 0 && kvh == 0 && wave == 0 && a.least > 0, lane, it)) return;
@@ -62,13 +77,9 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   // The table's entry for, and the slot of, a block's position `lane`: asked for a block before it is looked at, when the block is requested.
   // (Looked at at once it would wait for the transfers that are under way.)  From block to block both move on by the same step.
   const int32_t* const table = a.b.pages + (int64_t)it.s * a.b.pages_stride;
-  int index, slot, entry;
+  int index = (int)((unsigned)(it.lo + lane) / (unsigned)a.b.page_size), slot = it.lo + lane - index * a.b.page_size;
   const int more_index = KV / a.b.page_size, more_slot = KV - more_index * a.b.page_size;
-  auto first_place = [&]() {
-    index = (int)((unsigned)(it.lo + lane) / (unsigned)a.b.page_size);
-    slot = it.lo + lane - index * a.b.page_size;
-    entry = table[min(index, a.b.max_pages - 1)];
-  };
+  int entry = table[min(index, a.b.max_pages - 1)];
   auto place = [&]() {
     slot += more_slot;
     index += more_index;
@@ -109,7 +120,11 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
     }
   };
   f32x16 o[HD / 32];
-  float m, l;
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+  float m = -INFINITY, l = 0.f;
   // Where a lane's operands begin.  A row's 16-byte pieces have changed places by an exclusive or: keys with the row (head_dim 64: half of it),
   // so that eight rows in turn have a piece on eight places; values two pieces at a time, so that the four rows of a transposing read and
   // the four of the other half lie on different banks.  Keys: row col of half a block, piece 2 i + half at kat ^ 32 i.  Values: position
@@ -182,10 +197,8 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       u32x4 hi, lo;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float x = s[t / 2][8 * (t % 2) + 2 * e], y = s[t / 2][8 * (t % 2) + 2 * e + 1];
-        hi[e] = pair(x, y, T());
-        rest(hi[e], x, y, T());
-        lo[e] = pair(x, y, T());
+        const u32x2 w = two_terms(s[t / 2][8 * (t % 2) + 2 * e], s[t / 2][8 * (t % 2) + 2 * e + 1], T());
+        hi[e] = w.x; lo[e] = w.y;
       }
 #pragma unroll
       for (int d = 0; d < HD / 32; ++d) {
@@ -195,10 +208,8 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       }
     }
   };
-  // A weight of zero, or the second term of one, does not silence a value that is infinite or no number, so where not every row of the tile
-  // sees all of a block these are cleared in LDS (each wave its own 16 positions), and put in behind the loop where they are seen.  Blocks that
-  // all rows see are taken as they come, and if that has left something that is not finite the part is gone through once more, with every block
-  // cleaned.
+  // Where not every row of the tile sees all of a block: a weight of zero does not silence a value that is infinite or no number, so these
+  // are cleared in LDS (each wave its own 16 positions), and put in behind the loop where they are seen.
   auto clean = [&](int n, int base, uint64_t have) {
     char* const p = lds + (n & 1) * 2 * SIDE + SIDE + 16 * wave * ROWB + lane * 16;
     uint32_t most = 0;
@@ -218,42 +229,25 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       if (__ballot(seen) && lane == 0) { atomicMin(&s_odd[0], n); atomicMax(&s_odd[1], n); }
     }
   };
-  bool careful = false;
-  for (;;) {
+  if (blocks > 0) request(0);
+  place();
+  // the queries are waited for here: a wait in the loop would be one for the transfers, of which the compiler knows nothing
 #pragma unroll
-    for (int i = 0; i < HD / 32; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-    m = -INFINITY; l = 0.f;
-    first_place();
-    if (blocks > 0) request(0);
+  for (int i = 0; i < HD / 16; ++i) asm volatile("" : "+v"(q[i]));
+  for (int n = 0; n < blocks; ++n) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const uint64_t have = have_next;
+    if (n + 1 < blocks) request(n + 1);
     place();
-    // the queries are waited for here: a wait in the loop would be one for the transfers, of which the compiler knows nothing
-#pragma unroll
-    for (int i = 0; i < HD / 16; ++i) asm volatile("" : "+v"(q[i]));
-    for (int n = 0; n < blocks; ++n) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const int base = it.lo + n * KV;
+    if (!(have == ~0ull && base + KV - 1 <= tile_first && base >= tile_all)) {
+      clean(n, base, have);
       __syncthreads();
-      const uint64_t have = have_next;
-      if (n + 1 < blocks) request(n + 1);
-      place();
-      const int base = it.lo + n * KV;
-      if (careful || !(have == ~0ull && base + KV - 1 <= tile_first && base >= tile_all)) {
-        clean(n, base, have);
-        __syncthreads();
-      }
-      if (!busy || base > wave_last || base + KV - 1 < wave_from) continue;      // no row of the wave sees any of it
-      const bool whole = have == ~0ull && base + KV - 1 <= wave_first && base >= wave_all;
-      step(n, base, have, whole);
     }
-    if (careful) break;
-    float sum = l;                                         // (no number, if one is)
-#pragma unroll
-    for (int i = 0; i < HD / 32; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sum += o[i][e] - o[i][e];
-    if (!__syncthreads_or(!(fabsf(sum) < INFINITY))) break;      // (every wave is behind its reads of LDS, too)
-    careful = true;
+    if (!busy || base > wave_last || base + KV - 1 < wave_from) continue;      // no row of the wave sees any of it
+    const bool whole = have == ~0ull && base + KV - 1 <= wave_first && base >= wave_all;
+    step(n, base, have, whole);
   }
   __syncthreads();
   const int odd_first = s_odd[0], odd_last = s_odd[1];
@@ -262,7 +256,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
     // such a block once more, position by position, from the pages: a row that sees an infinite value, or no number, takes it up
     const int base = it.lo + n * KV, x = base + lane;
     const bool there = __ballot(x < it.hi && page_of(a.b, it.s, x) >= 0) == ~0ull;
-    if (!careful && there && base + KV - 1 <= tile_first && base >= tile_all) continue;
+    if (there && base + KV - 1 <= tile_first && base >= tile_all) continue;
 #pragma unroll 1
     for (int p = base; p < min(base + KV, it.hi); ++p) {
       const int pg = page_of(a.b, it.s, p);

@@ -17,12 +17,12 @@ def call(d, **kw):
 
 
 def limits(b, ref, size, reach):
-    """How far a result may be off: fp32's products and sums as in test_gpu_paged_attention.py; a weight in two terms of the type, each off
-    by half a step (of what the first left, for the second); the result's own rounding.  (Weights of at least an eighth, so that half floats'
-    smallest step, 2^-24, has no part: the second term's half step is 2^-22 of the weight or less.)"""
+    """How far a result may be off: fp32's products and sums as in test_gpu_paged_attention.py; a weight in two terms of the type, the first
+    off by a step at most (it may be cut off), the second by half a step of that; the result's own rounding.  (Weights of at least an eighth of
+    the largest, which is 2^7 or more for half floats: their smallest number, 2^-24, which the second term may be in place of zero, has no part.)"""
     n = max(b.kv)
     w = ((b.hd + 8) * reach + n + 16) * 2.0 ** -24
-    two = 0.0 if b.dtype == F32 else HALF_STEP[b.dtype] ** 2
+    two = 0.0 if b.dtype == F32 else 2 * HALF_STEP[b.dtype] ** 2
     return size * (2 * w[..., None] + two) + ref.abs() * HALF_STEP[b.dtype] * (1 + 2.0 ** -9) + TINY[b.dtype]
 
 

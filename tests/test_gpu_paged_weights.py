@@ -109,3 +109,20 @@ def test_many_small_weights_count_in_the_outputs(seqs, rows, heads, n, dtype):
     out, _, _ = sink(seqs, rows, heads, n, dtype, 64, 25.1)
     tol = HALF_STEP[dtype] + ((2 * n / 16 if rows > 1 else 2 * n / 128) + n / 64 + 16) * 2.0 ** -24
     assert ((out - 1).abs() <= tol).all(), (float((out - 1).abs().max()), tol)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("new,kv", [([300], [700]), ([130], [2000]), ([1, 8], [300, 200])])
+def test_infinite_values_under_weights_without_a_rest(dtype, new, kv):
+    """Equal scores: every weight is a power of two, and nothing is left for its second term."""
+    d = Batch(new, kv, 8, 8, 64, dtype).cuda()
+    d.q.zero_()
+    for c, (p, x) in enumerate(((3, float("inf")), (70, float("-inf")), (kv[0] - 1, float("inf")))):
+        d.v_cache[tuple(d.slot(0, p))][1, c] = x
+    out, lse = call(d)
+    pos = torch.arange(kv[0] - new[0], kv[0])
+    for c, (p, x) in enumerate(((3, float("inf")), (70, float("-inf")), (kv[0] - 1, float("inf")))):
+        got = out[:new[0], 1, c].cpu().double()
+        assert (got[pos >= p] == x).all() and got[pos < p].isfinite().all()
+    out[:new[0], 1, :3] = 0
+    assert out.isfinite().all() and lse.isfinite().all()

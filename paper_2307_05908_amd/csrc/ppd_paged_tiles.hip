@@ -1,10 +1,11 @@
 // ppd_paged_attention, many rows: bound by the matrix units and the issue of instructions beside them: a 32 x 32 x 16 product keeps its SIMD's
 // vector units from the other wave for two thirds of its 32 cycles, and a block of 64 positions is 48 products of a wave (16 of them for the
-// weights' second term), 32 exponentials and some 270 other vector instructions.  Two bf16 prompts of 3800 and 4000 tokens (32 heads, 8 of keys
-// and values, 249 GFLOP, 374 with the second term): 344 to 352 us from card to card, 1060 to 1090 TFLOP/s of products; a large matrix product of the library's reaches 1200.
-// With weights of one term, rounded to the type: 267 us, and an error of 2.1e-3 of bf16 outputs where their own rounding is 1.6e-3.
-// (Tried and not kept: the first terms' products before the second terms' and weights' rests by a dot instruction, one a weight less: the same time.
-// With one term, beside 283 us at the time: the next block's scores between this one's exponentials, 286 to 292; a higher priority for
+// weights' second term), 32 exponentials and some 290 other vector instructions (products 53 % of the cycles, vector instructions 55 %, LDS
+// 27 %).  Two bf16 prompts of 3800 and 4000 tokens (32 heads, 8 of keys and values, 249 GFLOP, 374 with the second term): 344 to 352 us from
+// card to card, 1060 to 1090 TFLOP/s of products; a large matrix product of the library's reaches 1200.  With weights of one term, rounded to
+// the type: 267 us, and an error of 2.1e-3 of bf16 outputs where their own rounding is 1.6e-3.
+// (Tried and not kept: the first terms' products before the second terms', and weights' rests by a dot instruction, one a weight less: the same
+// time.  With one term, beside 283 us at the time: the next block's scores between this one's exponentials, 286 to 292; a higher priority for
 // the waves in products or in exponentials, 284 to 292; offsets kept in registers from block to block, 281 to 287.  Blocks of 32 positions and three
 // workgroups a unit: 278 beside 279, 500 tokens over 4000 positions 81 beside 77, head_dim 64 113 beside 100.)
 #include "ppd_paged_attn.h"

@@ -11,7 +11,7 @@ import ctypes
 import functools
 import os
 import struct
-from typing import Dict, List, Optional
+from typing import Dict, List, NamedTuple, Optional
 
 import numpy as np
 
@@ -66,11 +66,30 @@ class Rows(ctypes.Structure):
     _fields_ = [("p", ctypes.c_void_p), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
 
 
+class PageTable(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("pages_stride", ctypes.c_int64), ("free_pages", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int32) for n in ("max_pages", "n_pages", "page_size", "n_seqs")]
+
+
+class PagedCacheFp4(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scales", "v_scales")] + \
+               [(n, ctypes.c_int64) for n in ("k_page", "k_pos", "k_head", "v_page", "v_pos", "v_head",
+                                              "ks_page", "ks_pos", "ks_head", "vs_page", "vs_pos", "vs_head")] + \
+               [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")]
+
+
+class LogitRules(ctypes.Structure):
+    _fields_ = [("history", ctypes.c_void_p), ("history_stride", ctypes.c_int64)] + \
+               [(n, ctypes.c_void_p) for n in ("history_len", "prompt_len", "repetition", "presence", "frequency", "bias_start", "bias_ids", "bias", "mask")] + \
+               [("mask_stride", ctypes.c_int64), ("mask_row", ctypes.c_void_p), ("n_bias", ctypes.c_int32), ("n_masks", ctypes.c_int32)]
+
+
 EXPORTS = ("ppd_create", "ppd_reset", "ppd_prefill", "ppd_step", "plain_greedy_step", "ppd_get_logits",
            "ppd_get_early_logits", "ppd_get_stats", "ppd_set_profiling", "ppd_set_graphs", "ppd_set_sampling", "ppd_get_kernel_time",
            "ppd_time_ffn_in", "ppd_get_chain_rounds", "ppd_set_chain_wait", "ppd_stream_read_probe", "ppd_early_topk", "ppd_early_topk_noalloc", "ppd_destroy",
            "ppd_strerror", "ppd_last_hip_error",
-           "ppd_paged_append", "ppd_paged_attention", "ppd_paged_attention_workspace", "ppd_verify_drafts", "ppd_verify_drafts_workspace")
+           "ppd_paged_append", "ppd_paged_attention", "ppd_paged_attention_workspace", "ppd_verify_drafts", "ppd_verify_drafts_workspace",
+           "ppd_paged_plan", "ppd_paged_append_fp4", "ppd_paged_attention_fp4", "ppd_paged_attention_fp4_workspace", "ppd_adjust_logits")
 
 _lib = None
 
@@ -113,6 +132,12 @@ def load_library() -> ctypes.CDLL:
     lib.ppd_paged_attention_workspace.argtypes = [cp, bp, ci, ctypes.POINTER(cu)]
     lib.ppd_verify_drafts.argtypes = [ci, ci, ci, ci, vp, vp, vp, cl, vp, cl, vp, vp, vp, vp, vp, cu, vp]
     lib.ppd_verify_drafts_workspace.argtypes = [ci, ci, ci, ci, ctypes.POINTER(cu)]
+    tp, fp, lp = ctypes.POINTER(PageTable), ctypes.POINTER(PagedCacheFp4), ctypes.POINTER(LogitRules)
+    lib.ppd_paged_plan.argtypes = [tp, vp, vp, vp, vp, vp, ci, vp, vp, vp, vp, vp, vp, vp]
+    lib.ppd_paged_append_fp4.argtypes = [fp, bp, ci, rp, rp, rp, rp, rp, rp, vp, vp, cf, ci, cf, vp]
+    lib.ppd_paged_attention_fp4.argtypes = [fp, bp, ci, rp, rp, vp, cf, ci, vp, cu, vp]
+    lib.ppd_paged_attention_fp4_workspace.argtypes = [fp, bp, ci, ctypes.POINTER(cu)]
+    lib.ppd_adjust_logits.argtypes = [ci, ci, ci, ci, vp, vp, vp, cl, vp, cl, lp, vp]
     lib.ppd_destroy.argtypes = [vp]
     lib.ppd_destroy.restype = None
     lib.ppd_strerror.argtypes = [ci]
@@ -248,6 +273,19 @@ def _scratch(workspace):
     return workspace.data_ptr(), workspace.nbytes
 
 
+def _paged_batch(i32, pages, q_start, kv_len, n_tokens):
+    """(batch as bytes, entries of a row of the table, sequences)."""
+    if pages.dtype is not i32 or q_start.dtype is not i32 or kv_len.dtype is not i32:
+        raise ValueError("pages, q_start, kv_len: int32")
+    n, table = kv_len.numel(), pages.shape
+    if len(table) != 2 or table[0] != n or q_start.numel() != n + 1:
+        raise ValueError("pages [n_seqs, max_pages], q_start [n_seqs + 1], kv_len [n_seqs]")
+    most, (p0, p1) = table[1], pages.stride()
+    if not (q_start.is_contiguous() and kv_len.is_contiguous()) or (p1 != 1 and most > 1):
+        raise ValueError("q_start, kv_len and the rows of pages must be contiguous")
+    return _PACK_BATCH(q_start.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), p0, most, n, n_tokens), most, n
+
+
 def _paged_args(k_cache, v_cache, pages, q_start, kv_len, n_tokens):
     """(cache, batch) as bytes, and the sizes that a workspace depends on."""
     torch, codes = _layers()[:2]
@@ -259,17 +297,9 @@ def _paged_args(k_cache, v_cache, pages, q_start, kv_len, n_tokens):
     v0, v1, v2, v3 = v_cache.stride()
     if k3 != 1 or v3 != 1:
         raise ValueError("k_cache, v_cache: head_dim must be contiguous")
-    if pages.dtype is not i32 or q_start.dtype is not i32 or kv_len.dtype is not i32:
-        raise ValueError("pages, q_start, kv_len: int32")
-    n, table = kv_len.numel(), pages.shape
-    if len(table) != 2 or table[0] != n or q_start.numel() != n + 1:
-        raise ValueError("pages [n_seqs, max_pages], q_start [n_seqs + 1], kv_len [n_seqs]")
-    most, (p0, p1) = table[1], pages.stride()
-    if not (q_start.is_contiguous() and kv_len.is_contiguous()) or (p1 != 1 and most > 1):
-        raise ValueError("q_start, kv_len and the rows of pages must be contiguous")
     code = codes[dtype]
-    return (_PACK_CACHE(k_cache.data_ptr(), v_cache.data_ptr(), k0, k1, k2, v0, v1, v2, n_pages, size, kv_heads, head_dim, code),
-            _PACK_BATCH(q_start.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), p0, most, n, n_tokens),
+    batch, most, n = _paged_batch(i32, pages, q_start, kv_len, n_tokens)
+    return (_PACK_CACHE(k_cache.data_ptr(), v_cache.data_ptr(), k0, k1, k2, v0, v1, v2, n_pages, size, kv_heads, head_dim, code), batch,
             (n_pages, size, kv_heads, head_dim, code, most, n, n_tokens))
 
 
@@ -405,6 +435,249 @@ def ppd_verify_drafts(target_logits, ids, row_start, uniform, draft_logits=None,
     if rc != 0:
         raise PPDError(rc, "ppd_verify_drafts", load_library().ppd_last_hip_error(None))
     return tokens, accepted
+
+
+# ---- a step's batch, pages of 4-bit numbers, logits as requests want them
+_PACK_TABLE, _PACK_CACHE_FP4 = struct.Struct("@QqQ4i").pack, struct.Struct("@4Q12q5i4x").pack
+_PACK_RULES = struct.Struct("@Qq9QqQ2i").pack
+_step_fns = None
+
+
+def _step():
+    """torch, the type codes, and the library's functions as they are called here."""
+    global _step_fns
+    if _step_fns is None:
+        torch, codes, device, raw_stream = _layers()[:4]
+        lib = load_library()
+        vp, ci, cl, cu, cf = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float
+
+        def fn(name, *argtypes):
+            f = lib._FuncPtr((name, lib))
+            f.argtypes = argtypes
+            return f
+
+        _step_fns = (torch, codes, device, raw_stream,
+                     fn("ppd_paged_plan", vp, vp, vp, vp, vp, vp, ci, vp, vp, vp, vp, vp, vp, vp),
+                     fn("ppd_paged_append_fp4", vp, vp, ci, vp, vp, vp, vp, vp, vp, vp, vp, cf, ci, cf, vp),
+                     fn("ppd_paged_attention_fp4", vp, vp, ci, vp, vp, vp, cf, ci, vp, cu, vp),
+                     fn("ppd_adjust_logits", ci, ci, ci, ci, vp, vp, vp, cl, vp, cl, vp, vp))
+    return _step_fns
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+class Plan(NamedTuple):
+    """What ppd_paged_plan gives: q_start, kv_len and granted are a batch for the operators on pages; row_seq, positions and slots are None
+    where they were not asked for."""
+    q_start: object
+    kv_len: object
+    granted: object
+    counters: object
+    row_seq: object
+    positions: object
+    slots: object
+
+
+def ppd_paged_plan(pages, free_pages, counters, held, wanted, page_size, n_rows, kept=None, want_rows=True, q_start=None, kv_len=None, granted=None,
+                   counters_out=None, row_seq=None, positions=None, slots=None, stream=None):
+    """A step's batch from what each sequence holds, keeps and wants: pages int32 [n_seqs, max_pages] and free_pages int32 [n_pages] are changed
+    in place, counters int64 [2], held, wanted and kept (None: all stays) int32 [n_seqs], n_rows the rows of the batch's tensors.  Returns
+    a Plan; its tensors are made here if not given (kv_len may be held, counters_out counters), row_seq, positions and slots only with want_rows.
+    Asynchronous."""
+    torch, _, device, raw_stream, plan, _, _, _ = _step()
+    dev = pages.get_device()
+    given = (q_start, kv_len, granted, counters_out, row_seq, positions, slots)
+    if stream is not None or dev < 0 or dev != device():
+        return _on_device(pages, (free_pages, counters, held, wanted, kept, *given), stream, lambda: ppd_paged_plan(
+            pages, free_pages, counters, held, wanted, page_size, n_rows, kept, want_rows, *given))
+    _same_gpu(dev, free_pages, counters, held, wanted, kept, *given)
+    i32, i64 = torch.int32, torch.int64
+    n = held.numel()
+    table = pages.shape
+    if pages.dtype is not i32 or len(table) != 2 or table[0] != n or (table[1] > 1 and pages.stride(1) != 1) or free_pages.dtype is not i32 or free_pages.dim() != 1:
+        raise ValueError("pages int32 [n_seqs, max_pages], its rows contiguous, free_pages int32 [n_pages]")
+    for t in (held, wanted, kept):
+        if t is not None and (t.dtype is not i32 or t.numel() != n):
+            raise ValueError("held, wanted, kept: int32 [n_seqs]")
+    if counters.dtype is not i64 or counters.numel() != 2:
+        raise ValueError("counters: int64 [2]")
+    made = []
+    for t, size, dtype, make, name in ((q_start, n + 1, i32, True, "q_start"), (kv_len, n, i32, True, "kv_len"), (granted, n, i32, True, "granted"),
+                                       (counters_out, 2, i64, True, "counters_out"), (row_seq, n_rows, i32, want_rows, "row_seq"),
+                                       (positions, n_rows, i32, want_rows, "positions"), (slots, n_rows, i64, want_rows, "slots")):
+        if t is None and make:
+            t = torch.empty(size, dtype=dtype, device=pages.device)
+        elif t is not None and (t.dtype is not dtype or t.numel() != size):
+            raise ValueError(f"{name}: {dtype}, {size} numbers")
+        made.append(t)
+    if not all(t is None or t.is_contiguous() for t in (free_pages, counters, held, wanted, kept, *made)):
+        raise ValueError("all but pages must be contiguous")
+    rc = plan(_PACK_TABLE(pages.data_ptr(), pages.stride(0), free_pages.data_ptr(), table[1], free_pages.numel(), page_size, n), counters.data_ptr(), _ptr(made[3]),
+              held.data_ptr(), _ptr(kept), wanted.data_ptr(), n_rows, _ptr(made[0]), _ptr(made[1]), _ptr(made[2]), *(_ptr(t) for t in made[4:]), raw_stream(dev))
+    if rc != 0:
+        raise PPDError(rc, "ppd_paged_plan", load_library().ppd_last_hip_error(None))
+    return Plan(*made)
+
+
+def _paged_args_fp4(k_codes, k_scales, v_codes, v_scales, pages, q_start, kv_len, dtype, n_tokens):
+    """(cache, batch) as bytes, and the sizes that a workspace depends on."""
+    torch, codes = _step()[:2]
+    u8 = torch.uint8
+    if dtype not in codes:
+        raise ValueError("rows of float32, bfloat16 or float16")
+    shape = k_codes.shape
+    if len(shape) != 4 or v_codes.shape != shape or k_codes.dtype is not u8 or v_codes.dtype is not u8:
+        raise ValueError("k_codes, v_codes: uint8 [n_pages, page_size, n_kv_heads, head_dim / 2]")
+    n_pages, size, kv_heads, half = shape
+    if k_scales.shape != (n_pages, size, kv_heads, half // 16) or v_scales.shape != k_scales.shape or k_scales.dtype is not u8 or v_scales.dtype is not u8:
+        raise ValueError("k_scales, v_scales: uint8 [n_pages, page_size, n_kv_heads, head_dim / 32]")
+    strides = []
+    for t in (k_codes, v_codes, k_scales, v_scales):
+        s0, s1, s2, s3 = t.stride()
+        if s3 != 1:
+            raise ValueError("codes and scales of a row must be contiguous")
+        strides += (s0, s1, s2)
+    batch, most, n = _paged_batch(torch.int32, pages, q_start, kv_len, n_tokens)
+    code = codes[dtype]
+    return (_PACK_CACHE_FP4(k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), *strides, n_pages, size, kv_heads, 2 * half, code), batch,
+            (n_pages, size, kv_heads, 2 * half, code, most, n, n_tokens))
+
+
+def ppd_paged_append_fp4(k_codes, k_scales, v_codes, v_scales, pages, q_start, kv_len, q, k, v, q_gain=None, k_gain=None, norm_eps=1e-5, rotary_dim=0,
+                         rope_theta=10000.0, q_out=None, k_out=None, v_out=None, want_values=False, stream=None):
+    """ppd_paged_append into pages of 4-bit numbers: codes uint8 [n_pages, page_size, n_kv_heads, head_dim / 2], scales uint8 [..., head_dim / 32].
+    Returns (q_out, k_out, v_out); with want_values k_out and v_out, the keys and values as the pages have them now, are made here if not given (otherwise
+    they are None if not given).  Asynchronous."""
+    torch, _, device, raw_stream, _, append, _, _ = _step()
+    dev = k_codes.get_device()
+    if stream is not None or dev < 0 or dev != device():
+        return _on_device(k_codes, (k_scales, v_codes, v_scales, pages, q_start, kv_len, q, k, v, q_gain, k_gain, q_out, k_out, v_out), stream,
+                          lambda: ppd_paged_append_fp4(k_codes, k_scales, v_codes, v_scales, pages, q_start, kv_len, q, k, v, q_gain, k_gain, norm_eps,
+                                                       rotary_dim, rope_theta, q_out, k_out, v_out, want_values))
+    _same_gpu(dev, k_scales, v_codes, v_scales, pages, q_start, kv_len, q, k, v, q_gain, k_gain, q_out, k_out, v_out)
+    n, dtype = k.shape[0], k.dtype
+    cache, batch, sizes = _paged_args_fp4(k_codes, k_scales, v_codes, v_scales, pages, q_start, kv_len, dtype, n)
+    kv_heads, head_dim = sizes[2], sizes[3]
+    kr, vr = _rows(k, dtype, head_dim, "k", n, kv_heads)[0], _rows(v, dtype, head_dim, "v", n, kv_heads)[0]
+    qr, outr, heads = None, None, 0
+    if q is not None:
+        qr, heads = _rows(q, dtype, head_dim, "q", n)
+        if q_out is None:
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        outr = _rows(q_out, dtype, head_dim, "q_out", n, heads)[0]
+    if want_values:
+        if k_out is None:
+            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+        if v_out is None:
+            v_out = torch.empty_like(v, memory_format=torch.contiguous_format)
+    kor = None if k_out is None else _rows(k_out, dtype, head_dim, "k_out", n, kv_heads)[0]
+    vor = None if v_out is None else _rows(v_out, dtype, head_dim, "v_out", n, kv_heads)[0]
+    for g in (q_gain, k_gain):
+        if g is not None and (g.dtype is not dtype or g.numel() != head_dim or not g.is_contiguous()):
+            raise ValueError("gains: [head_dim] of the rows' type")
+    rc = append(cache, batch, heads, qr, outr, kr, vr, kor, vor, _ptr(q_gain), _ptr(k_gain), norm_eps, rotary_dim, rope_theta, raw_stream(dev))
+    if rc != 0:
+        raise PPDError(rc, "ppd_paged_append_fp4", load_library().ppd_last_hip_error(None))
+    return q_out if q is not None else None, k_out, v_out
+
+
+@functools.lru_cache(maxsize=4096)
+def _attention_fp4_workspace(sizes, heads):
+    """Bytes that ppd_paged_attention_fp4_workspace gives for these sizes (0 where it refuses: the call itself will)."""
+    pages, size, kv_heads, head_dim, code, max_pages, seqs, tokens = sizes
+    c = PagedCacheFp4(4096, 4096, 4096, 4096, *[0] * 12, pages, size, kv_heads, head_dim, code)
+    b = PagedBatch(4096, 4096, 4096, max_pages, max_pages, seqs, tokens)
+    need = ctypes.c_uint64()
+    return need.value if load_library().ppd_paged_attention_fp4_workspace(c, b, heads, need) == 0 else 0
+
+
+def ppd_paged_attention_fp4(q, k_codes, k_scales, v_codes, v_scales, pages, q_start, kv_len, scale=None, window=0, out=None, want_lse=False, workspace=None,
+                            stream=None):
+    """ppd_paged_attention over pages of 4-bit numbers (see ppd_paged_append_fp4): (out [n_tokens, n_heads, head_dim] of q's type, lse float32
+    [n_tokens, n_heads] or None).  Asynchronous."""
+    torch, _, device, raw_stream, _, _, attention, _ = _step()
+    dev = k_codes.get_device()
+    if stream is not None or dev < 0 or dev != device():
+        return _on_device(k_codes, (q, k_scales, v_codes, v_scales, pages, q_start, kv_len, out, workspace), stream, lambda: ppd_paged_attention_fp4(
+            q, k_codes, k_scales, v_codes, v_scales, pages, q_start, kv_len, scale, window, out, want_lse, workspace))
+    _same_gpu(dev, q, k_scales, v_codes, v_scales, pages, q_start, kv_len, out, workspace)
+    n, dtype = q.shape[0], q.dtype
+    cache, batch, sizes = _paged_args_fp4(k_codes, k_scales, v_codes, v_scales, pages, q_start, kv_len, dtype, n)
+    head_dim = sizes[3]
+    qr, heads = _rows(q, dtype, head_dim, "q", n)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    outr = _rows(out, dtype, head_dim, "out", n, heads)[0]
+    lse = torch.empty((n, heads), dtype=torch.float32, device=q.device) if want_lse else None
+    if workspace is None:
+        need = _attention_fp4_workspace(sizes, heads)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    rc = attention(cache, batch, heads, qr, outr, _ptr(lse), head_dim ** -0.5 if scale is None else scale, window, *_scratch(workspace), raw_stream(dev))
+    if rc != 0:
+        raise PPDError(rc, "ppd_paged_attention_fp4", load_library().ppd_last_hip_error(None))
+    return out, lse
+
+
+def ppd_adjust_logits(logits, row_start, ids=None, history=None, history_len=None, prompt_len=None, repetition=None, presence=None, frequency=None,
+                      bias_start=None, bias_ids=None, bias=None, mask=None, mask_row=None, out=None, stream=None):
+    """Penalties for tokens that a text has, biases and masks on logits [n_rows, vocab]; returns out, made here if not given (may be logits).
+    row_start int32 [n_seqs + 1], ids int32 [n_rows]; history int32 [n_seqs, most], history_len and prompt_len int32 [n_seqs]; repetition, presence and
+    frequency float32 [n_seqs]; bias_start int32 [n_seqs + 1], bias_ids int32 and bias float32 [n_bias]; mask int32 [n_masks, at least vocab / 32] with a
+    bit for every token that is allowed, mask_row int32 [n_rows].  Asynchronous."""
+    torch, codes, device, raw_stream, _, _, _, adjust = _step()
+    z = logits
+    dev = z.get_device()
+    others = (row_start, ids, history, history_len, prompt_len, repetition, presence, frequency, bias_start, bias_ids, bias, mask, mask_row, out)
+    if stream is not None or dev < 0 or dev != device():
+        return _on_device(z, others, stream, lambda: ppd_adjust_logits(z, *others))
+    _same_gpu(dev, *others)
+    i32, f32 = torch.int32, torch.float32
+    if z.dim() != 2 or z.dtype not in codes or (z.shape[1] > 1 and z.stride(1) != 1):
+        raise ValueError("logits: [n_rows, vocab], vocab contiguous, float32, bfloat16 or float16")
+    n, vocab = z.shape
+    if out is None:
+        out = torch.empty_like(z, memory_format=torch.contiguous_format)
+    elif out.shape != z.shape or out.dtype is not z.dtype or (vocab > 1 and out.stride(1) != 1):
+        raise ValueError("out: as logits")
+    seqs = row_start.numel() - 1
+    if row_start.dtype is not i32 or seqs < 1 or (ids is not None and (ids.dtype is not i32 or ids.numel() != n)):
+        raise ValueError("row_start int32 [n_seqs + 1], ids int32 [n_rows]")
+    for t, dtype in ((history_len, i32), (prompt_len, i32), (repetition, f32), (presence, f32), (frequency, f32)):
+        if t is not None and (t.dtype is not dtype or t.numel() != seqs):
+            raise ValueError("history_len, prompt_len int32 [n_seqs], repetition, presence, frequency float32 [n_seqs]")
+    if (history is None) != (history_len is None) or (bias is None) != (bias_ids is None) or (bias is None) != (bias_start is None) or (mask is None) != (mask_row is None):
+        raise ValueError("history with history_len, bias with bias_start and bias_ids, mask with mask_row")
+    most = many = masks = words = 0
+    if history is not None:
+        if history.dtype is not i32 or history.dim() != 2 or history.shape[0] != seqs:
+            raise ValueError("history int32 [n_seqs, most]")
+        most = history.shape[1]
+    if bias is not None:
+        many = bias.numel()
+        if bias.dtype is not f32 or bias_ids.dtype is not i32 or bias_ids.numel() != many or bias_start.dtype is not i32 or bias_start.numel() != seqs + 1:
+            raise ValueError("bias_start int32 [n_seqs + 1], bias_ids int32 [n_bias], bias float32 [n_bias]")
+    if mask is not None:
+        if mask.dtype is not i32 or mask.dim() != 2 or mask.shape[1] < (vocab + 31) // 32 or mask_row.dtype is not i32 or mask_row.numel() != n:
+            raise ValueError("mask int32 [n_masks, at least vocab / 32], mask_row int32 [n_rows]")
+        masks, words = mask.shape
+    if not all(t is None or t.is_contiguous() for t in others[:-1]):
+        raise ValueError("all but the logits must be contiguous")
+    if most == 0:                                           # (nothing in them: as if they were not given)
+        history = history_len = None
+    if many == 0:
+        bias_start = bias_ids = bias = None
+    if masks == 0:
+        mask = mask_row = None
+    rules = _PACK_RULES(_ptr(history) or 0, most, *(_ptr(t) or 0 for t in (history_len, prompt_len, repetition, presence, frequency, bias_start, bias_ids, bias, mask)),
+                        words, _ptr(mask_row) or 0, many, masks)
+    rc = adjust(seqs, n, vocab, codes[z.dtype], row_start.data_ptr(), _ptr(ids), z.data_ptr(), z.stride(0) if n > 1 else vocab, out.data_ptr(),
+                out.stride(0) if n > 1 else vocab, rules, raw_stream(dev))
+    if rc != 0:
+        raise PPDError(rc, "ppd_adjust_logits", load_library().ppd_last_hip_error(None))
+    return out
 
 
 class PPD:

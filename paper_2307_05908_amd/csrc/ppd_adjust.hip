@@ -1,0 +1,225 @@
+// ppd_adjust_logits: penalties for tokens that a text has, biases and masks on the logits of its rows.  Bound by reading and writing the
+// logits once.
+#include "ppd_layers_common.h"
+
+using namespace ppd;
+
+namespace {
+
+constexpr int ADJUST_MAX_VOCAB = 1 << 24;
+constexpr int AT = 256;                       // threads of a workgroup
+
+struct AdjustArgs {
+  const int32_t *row_start, *ids; const void* logits; void* out; int64_t stride, out_stride;
+  ppd_logit_rules r;
+  int n_seqs, n_rows, vocab;
+  bool in_place;
+};
+
+template <typename T> struct Logits;          // VEC of them are 16 bytes
+template <> struct Logits<float> {
+  static constexpr int VEC = 4;
+  typedef u32x4 loose __attribute__((aligned(4)));
+  __device__ static __forceinline__ void wide(u32x4 r, float* f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(r[e]);
+  }
+  __device__ static __forceinline__ u32x4 narrow(const float* f) { return (u32x4){__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])}; }
+};
+template <typename T> struct Logits16 {
+  static constexpr int VEC = 8;
+  typedef u32x4 loose __attribute__((aligned(2)));
+  __device__ static __forceinline__ void wide(u32x4 r, float* f) {
+    const f32x4 a = Quad<T>::wide((u32x2){r.x, r.y}), b = Quad<T>::wide((u32x2){r.z, r.w});
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { f[e] = a[e]; f[4 + e] = b[e]; }
+  }
+  __device__ static __forceinline__ u32x4 narrow(const float* f) {
+    const u32x2 a = Quad<T>::narrow((f32x4){f[0], f[1], f[2], f[3]}), b = Quad<T>::narrow((f32x4){f[4], f[5], f[6], f[7]});
+    return (u32x4){a.x, a.y, b.x, b.y};
+  }
+};
+template <> struct Logits<bf16_t> : Logits16<bf16_t> {};
+template <> struct Logits<f16_t> : Logits16<f16_t> {};
+
+// A workgroup has AT * NV * VEC tokens of the vocabulary and a share of one sequence's rows.  It counts the text before them in LDS (additions of
+// whole numbers, in any order), each thread takes the counts of its own tokens into registers, and from then on nothing crosses threads: a row's
+// own token is counted by the thread that has it.
+// grid: (pieces of the vocabulary, sequences, shares of rows)
+template <typename T, int NV>
+__global__ __launch_bounds__(AT) void adjust_kernel(AdjustArgs a) {
+  constexpr int VEC = Logits<T>::VEC, SIZE = 16 / VEC, PER = NV * VEC, CHUNK = AT * PER;
+  constexpr uint32_t IN_PROMPT = 1u << 31;
+  typedef typename Logits<T>::loose loose;
+  __shared__ __align__(16) uint32_t count[CHUNK];
+  __shared__ __align__(16) int entry[CHUNK];              // the bias list's entry for a token, and one more; 0: none
+  const int tid = threadIdx.x, s = blockIdx.y, first_id = blockIdx.x * CHUNK;
+  const int row0 = min(max(a.row_start[s], 0), a.n_rows), rows = min(max(a.row_start[s + 1], row0), a.n_rows) - row0;
+  const int share = (rows + gridDim.z - 1) / gridDim.z, begin = min((int)blockIdx.z * share, rows), end = min(begin + share, rows);
+  if (begin >= end) return;
+  const bool counts = a.r.repetition || a.r.presence || a.r.frequency;
+  const int before = counts && a.r.history ? min(max(a.r.history_len[s], 0), (int)a.r.history_stride) : 0;
+  const int prompt = a.r.prompt_len ? a.r.prompt_len[s] : 0;
+  // a thread's tokens: NV runs of VEC, run v at (v * AT + tid) * VEC
+  auto place = [&](int v) { return (v * AT + tid) * VEC; };
+  uint32_t n[PER];
+  float bias[PER];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) { n[e] = 0; bias[e] = -0.0f; }      // (what added to a number leaves it as it is)
+  if (counts || a.r.bias) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int e = 0; e < VEC; e += 4) {
+        *(u32x4*)(count + place(v) + e) = (u32x4){0u, 0u, 0u, 0u};
+        *(u32x4*)(entry + place(v) + e) = (u32x4){0u, 0u, 0u, 0u};
+      }
+    __syncthreads();
+    auto add = [&](int token, int at) {
+      const uint32_t t = (uint32_t)token - (uint32_t)first_id;
+      if (t < (uint32_t)CHUNK && token < a.vocab) { if (at < prompt) atomicOr(count + t, IN_PROMPT); else atomicAdd(count + t, 1u); }
+    };
+    auto scan = [&](const int32_t* text, int length, int at) {
+      for (int i0 = tid; i0 < length; i0 += 8 * AT) {      // eight loads under way
+        int token[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) token[u] = i0 + u * AT < length ? text[i0 + u * AT] : -1;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) if (token[u] >= 0) add(token[u], at + i0 + u * AT);
+      }
+    };
+    if (before > 0) scan(a.r.history + (int64_t)s * a.r.history_stride, before, 0);
+    if (counts && a.ids) scan(a.ids + row0, begin, before);
+    if (a.r.bias) {
+      const int from = min(max(a.r.bias_start[s], 0), a.r.n_bias), to = min(a.r.bias_start[s + 1], a.r.n_bias);
+      for (int e = from + tid; e < to; e += AT) {
+        const int token = a.r.bias_ids[e];
+        const uint32_t t = (uint32_t)token - (uint32_t)first_id;
+        if (t < (uint32_t)CHUNK && token >= 0 && token < a.vocab) atomicMax(entry + t, e + 1);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        n[v * VEC + e] = count[place(v) + e];
+        const int i = entry[place(v) + e];
+        if (i > 0) bias[v * VEC + e] = a.r.bias[i - 1];
+      }
+  }
+  const float again = a.r.repetition ? a.r.repetition[s] : 1.0f, factor = again > 0.f ? again : 1.0f, inverse = 1.0f / factor;
+  const float once = a.r.presence ? a.r.presence[s] : 0.0f, each = a.r.frequency ? a.r.frequency[s] : 0.0f;
+  // runs that something is done to where there is no mask; in place the others are neither read nor written
+  uint32_t touched = 0;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) if (n[e] != 0 || __float_as_uint(bias[e]) != 0x80000000u) touched |= 1u << e / VEC;
+  for (int i = begin; i < end; ++i) {
+    const int row = row0 + i;
+    if (counts && a.ids) {
+      const int token = a.ids[row];
+      const uint32_t t = (uint32_t)token - (uint32_t)first_id;
+      if (t < (uint32_t)CHUNK && token >= 0 && t / VEC % AT == (uint32_t)tid && token < a.vocab) {
+        const int mine = (int)(t / (VEC * AT) * VEC + t % VEC);
+        touched |= 1u << mine / VEC;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) if (e == mine) n[e] = before + i < prompt ? n[e] | IN_PROMPT : n[e] + 1;
+      }
+    }
+    const int which = a.r.mask ? a.r.mask_row[row] : -1;
+    const uint32_t* const mask = (unsigned)which < (unsigned)a.r.n_masks ? a.r.mask + (int64_t)which * a.r.mask_stride : nullptr;
+    const char* const src = (const char*)a.logits + (int64_t)row * a.stride * SIZE;
+    char* const dst = (char*)a.out + (int64_t)row * a.out_stride * SIZE;
+    u32x4 raw[NV];
+    uint32_t allowed[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int t = first_id + place(v);
+      const bool idle = a.in_place && !mask && !(touched >> v & 1);
+      raw[v] = (u32x4){0u, 0u, 0u, 0u};
+      allowed[v] = ~0u;
+      if (t >= a.vocab || idle) continue;
+      if (mask) allowed[v] = mask[t / 32] >> t % 32;
+      if (t + VEC <= a.vocab) raw[v] = *(const loose*)(src + (int64_t)t * SIZE);
+      else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (t + e < a.vocab) {
+            if constexpr (SIZE == 4) raw[v][e] = ((const uint32_t*)src)[t + e];
+            else raw[v][e / 2] |= (uint32_t)((const uint16_t*)src)[t + e] << 16 * (e % 2);
+          }
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int t = first_id + place(v);
+      if (t >= a.vocab || (a.in_place && !mask && !(touched >> v & 1))) continue;
+      float x[VEC];
+      Logits<T>::wide(raw[v], x);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const uint32_t c = n[v * VEC + e], said = c & ~IN_PROMPT;
+        const float y = x[e] * (x[e] > 0.f ? inverse : factor);
+        x[e] = c ? y : x[e];
+        const float less = x[e] - (each * (float)said + once);
+        x[e] = said ? less : x[e];
+        x[e] += bias[v * VEC + e];
+        x[e] = allowed[v] >> e & 1 ? x[e] : -INFINITY;
+      }
+      const u32x4 now = Logits<T>::narrow(x);
+      if (t + VEC <= a.vocab) *(loose*)(dst + (int64_t)t * SIZE) = now;
+      else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (t + e < a.vocab) {
+            if constexpr (SIZE == 4) ((uint32_t*)dst)[t + e] = now[e];
+            else ((uint16_t*)dst)[t + e] = (uint16_t)(now[e / 2] >> 16 * (e % 2));
+          }
+      }
+    }
+  }
+}
+
+template <typename T>
+hipError_t adjust_go(const AdjustArgs& a, hipStream_t stream) {
+  constexpr int VEC = Logits<T>::VEC, MANY = 16 / VEC;
+  const int per_seq = (a.n_rows + a.n_seqs - 1) / a.n_seqs;
+  constexpr int SHARES = 4096;      // (of rows, at most: a share may be any number of them)
+  const int64_t large = (a.vocab + AT * VEC * MANY - 1) / (AT * VEC * MANY), small = (a.vocab + AT * VEC - 1) / (AT * VEC);
+  if (large * a.n_seqs >= 512) {
+    const int shares = (per_seq + 15) / 16 < SHARES ? (per_seq + 15) / 16 : SHARES;
+    hipLaunchKernelGGL((adjust_kernel<T, MANY>), dim3(large, a.n_seqs, shares), dim3(AT), 0, stream, a);
+  } else {
+    int64_t shares = 512 / (small * a.n_seqs);
+    if (shares > per_seq) shares = per_seq;
+    if (shares < (per_seq + 15) / 16) shares = (per_seq + 15) / 16;
+    if (shares > SHARES) shares = SHARES;
+    hipLaunchKernelGGL((adjust_kernel<T, 1>), dim3(small, a.n_seqs, shares), dim3(AT), 0, stream, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+extern "C" int ppd_adjust_logits(int n_seqs, int n_rows, int vocab, int dtype, const int32_t* row_start, const int32_t* ids,
+                                 const void* logits, int64_t logits_stride, void* out, int64_t out_stride,
+                                 const ppd_logit_rules* rules, void* hip_stream) {
+  if (n_seqs < 1 || n_rows < 0 || vocab < 1 || dtype < PPD_FP32 || dtype > PPD_FP16 || !rules) return PPD_EINVAL;
+  if (n_seqs > PPD_MAX_SEQS || n_rows > PPD_MAX_TOKENS || vocab > ADJUST_MAX_VOCAB) return PPD_ELIMIT;
+  const ppd_logit_rules& r = *rules;
+  if (!r.history != !r.history_len || !r.mask != !r.mask_row || !r.bias != !r.bias_start || !r.bias != !r.bias_ids) return PPD_EINVAL;
+  if (((uintptr_t)row_start | (uintptr_t)ids | (uintptr_t)r.history | (uintptr_t)r.history_len | (uintptr_t)r.prompt_len | (uintptr_t)r.repetition |
+       (uintptr_t)r.presence | (uintptr_t)r.frequency | (uintptr_t)r.bias_start | (uintptr_t)r.bias_ids | (uintptr_t)r.bias | (uintptr_t)r.mask |
+       (uintptr_t)r.mask_row) & 3)
+    return PPD_EINVAL;
+  if (r.history && r.history_stride < 0) return PPD_EINVAL;
+  if (r.history && r.history_stride > 1 << 30) return PPD_ELIMIT;
+  if (r.bias && (r.n_bias < 0 || r.n_bias == INT32_MAX)) return PPD_EINVAL;
+  if (r.mask && (r.n_masks < 0 || (r.n_masks > 1 && r.mask_stride < (vocab + 31) / 32))) return PPD_EINVAL;
+  if (!row_start || !logits || !out || ((uintptr_t)logits | (uintptr_t)out) & (elem_size(dtype) - 1)) return PPD_EINVAL;
+  if (n_rows > 1 && (logits_stride < vocab || out_stride < vocab || (logits == out && logits_stride != out_stride))) return PPD_EINVAL;
+  if (n_rows == 0) return PPD_OK;
+  const AdjustArgs a = {row_start, ids, logits, out, logits_stride, out_stride, r, n_seqs, n_rows, vocab, logits == out};
+  hipStream_t st = (hipStream_t)hip_stream;
+  return launched(dtype == PPD_FP32 ? adjust_go<float>(a, st) : dtype == PPD_BF16 ? adjust_go<bf16_t>(a, st) : adjust_go<f16_t>(a, st));
+}

@@ -42,6 +42,10 @@ template <> struct Quad<f16_t> {
   }
 };
 
+template <int CTRL> __device__ __forceinline__ double dpp_f64(double v) {
+  return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xf, 0xf, false), __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xf, 0xf, false));
+}
+
 // A batch as the kernels take it.
 struct Batch {
   const int32_t* q_start; const int32_t* kv_len; const int32_t* pages;
@@ -78,7 +82,8 @@ __device__ __forceinline__ int page_of(const Batch& b, int s, int pos) {
   return (unsigned)page < (unsigned)b.n_pages ? page : -1;
 }
 
-inline Batch batch_of(const ppd_paged_cache& c, const ppd_paged_batch& b) {
+template <typename C>                                    // ppd_paged_cache, ppd_paged_cache_fp4
+inline Batch batch_of(const C& c, const ppd_paged_batch& b) {
   const int64_t room = (int64_t)b.max_pages * c.page_size;
   return {b.q_start, b.kv_len, b.pages, b.pages_stride, b.max_pages, b.n_seqs, b.n_tokens, c.n_pages, c.page_size, (int)room};
 }
@@ -87,6 +92,15 @@ inline int elem_size(int dtype) { return dtype == PPD_FP32 ? 4 : 2; }
 // strides (in elements) of `count` rows that begin at multiples of 16 bytes each
 inline bool good_stride(int64_t stride, int count, int dtype) { return count <= 1 || (stride >= 0 && stride % (16 / elem_size(dtype)) == 0); }
 
+// PPD_OK, or what is wrong with a batch over pages of this size
+inline int check_batch(const ppd_paged_batch* b, int kv_heads, int page_size) {
+  if (b->n_seqs < 1 || b->n_tokens < 0 || b->max_pages < 1 || !b->q_start || !b->kv_len || !b->pages) return PPD_EINVAL;
+  if (((uintptr_t)b->q_start | (uintptr_t)b->kv_len | (uintptr_t)b->pages) & 3) return PPD_EINVAL;
+  if (b->n_seqs > 1 && b->pages_stride < b->max_pages) return PPD_EINVAL;
+  if (b->n_seqs > PPD_MAX_SEQS || b->n_tokens > PPD_MAX_TOKENS || kv_heads > PPD_MAX_HEADS) return PPD_ELIMIT;
+  if ((int64_t)b->max_pages * page_size > 1 << 30) return PPD_ELIMIT;
+  return PPD_OK;
+}
 // PPD_OK, or what is wrong with a cache and a batch
 inline int check_paged(const ppd_paged_cache* c, const ppd_paged_batch* b) {
   if (!c || !b) return PPD_EINVAL;
@@ -95,12 +109,7 @@ inline int check_paged(const ppd_paged_cache* c, const ppd_paged_batch* b) {
   if (!good_stride(c->k_page, c->n_pages, c->dtype) || !good_stride(c->v_page, c->n_pages, c->dtype) || !good_stride(c->k_pos, c->page_size, c->dtype) ||
       !good_stride(c->v_pos, c->page_size, c->dtype) || !good_stride(c->k_head, c->n_kv_heads, c->dtype) || !good_stride(c->v_head, c->n_kv_heads, c->dtype))
     return PPD_EINVAL;
-  if (b->n_seqs < 1 || b->n_tokens < 0 || b->max_pages < 1 || !b->q_start || !b->kv_len || !b->pages) return PPD_EINVAL;
-  if (((uintptr_t)b->q_start | (uintptr_t)b->kv_len | (uintptr_t)b->pages) & 3) return PPD_EINVAL;
-  if (b->n_seqs > 1 && b->pages_stride < b->max_pages) return PPD_EINVAL;
-  if (b->n_seqs > PPD_MAX_SEQS || b->n_tokens > PPD_MAX_TOKENS || c->n_kv_heads > PPD_MAX_HEADS) return PPD_ELIMIT;
-  if ((int64_t)b->max_pages * c->page_size > 1 << 30) return PPD_ELIMIT;
-  return PPD_OK;
+  return check_batch(b, c->n_kv_heads, c->page_size);
 }
 // rows of a batch; written ones must not lie on each other
 inline bool good_rows(const ppd_rows* r, int tokens, int heads, int dtype, bool written) {

@@ -12,6 +12,7 @@
 namespace ppd {
 
 constexpr int SPLIT_ROWS = 16, TILE_ROWS = 128;   // rows of a tile of paged_split_kernel and of paged_tile_kernel
+constexpr int SPLIT_WAVES = 4, SPLIT_THREADS = SPLIT_WAVES * WAVE;
 constexpr int PLAN_BLOCK = 64;                    // positions that lengths are cut by
 
 struct PagedAttnArgs {
@@ -40,6 +41,14 @@ __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c, bf16_t) {
 }
 __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c, f16_t) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c, bf16_t) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c, f16_t) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 // two numbers rounded to the type, side by side, and what the rounding left of them
 __device__ __forceinline__ uint32_t pair(float a, float b, bf16_t) { const bf16x2 v = {(__bf16)a, (__bf16)b}; return __builtin_bit_cast(uint32_t, v); }
@@ -252,8 +261,192 @@ __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, bool 
   return true;
 }
 
+// Two weights as two terms of the type, side by side.  The first is cut off, not rounded, and the second is not zero where the weight is not (the
+// type's smallest normal number, or half floats' smallest one, 2^-31 of the row's largest weight): a value that is infinite has its sign in both
+// products.  (The rests of rounded first terms need a second pass without such values, 9 ms, not 0.6, for the two prompts where no value is a number;
+// else the same time.)
+__device__ __forceinline__ u32x2 two_terms(float x, float y, bf16_t) {
+  const uint32_t u = __float_as_uint(x), v = __float_as_uint(y);
+  const float a = x - __uint_as_float(u & 0xffff0000u), b = y - __uint_as_float(v & 0xffff0000u);
+  return (u32x2){__builtin_amdgcn_perm(v, u, 0x07060302u), pair(__builtin_amdgcn_fmed3f(a, x, 0x1p-126f), __builtin_amdgcn_fmed3f(b, y, 0x1p-126f), bf16_t())};
+}
+__device__ __forceinline__ u32x2 two_terms(float x, float y, f16_t) {
+  const auto h = __builtin_amdgcn_cvt_pkrtz(x, y);
+  const float a = x - (float)h[0], b = y - (float)h[1];
+  return (u32x2){__builtin_bit_cast(uint32_t, h), pair(__builtin_amdgcn_fmed3f(a, x, 0x1p-24f), __builtin_amdgcn_fmed3f(b, y, 0x1p-24f), f16_t())};
+}
+
+// ---- parts joined
+// A part's results: sums of a row's components, and its reference and total, past the L2, for whoever joins them.
+__device__ __forceinline__ void leave(float* to, f32x4 v) {
+  typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+  const u64x2 u = __builtin_bit_cast(u64x2, v);
+  __hip_atomic_store((uint64_t*)to, u.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store((uint64_t*)to + 1, u.y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void leave(float2* to, float m, float l) {
+  const f32x2 v = {m, l};
+  __hip_atomic_store((uint64_t*)to, __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2 left(const void* from) {
+  return __builtin_bit_cast(f32x2, __hip_atomic_load((const uint64_t*)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+// The waves of a workgroup joined: their results lie out_lds bytes apart, sums in rows of HD + 4 and behind them references and totals.  What comes of it
+// is the result, or a part's.
+template <typename T, int HD>
+__device__ __forceinline__ void join_waves(const PagedAttnArgs& a, const Item& it, int kvh, int tid, const char* lds, int out_lds) {
+  for (int x = tid; x < SPLIT_ROWS * HD / 4; x += SPLIT_THREADS) {
+    const int rr = x / (HD / 4), d = (x % (HD / 4)) * 4, ri = it.tile * SPLIT_ROWS + rr;
+    if (ri >= it.n * a.group) break;
+    float2 ml[SPLIT_WAVES];
+    float mx = -INFINITY, sum = 0.f;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < SPLIT_WAVES; ++w) { ml[w] = ((const float2*)((const float*)(lds + w * out_lds) + SPLIT_ROWS * (HD + 4)))[rr]; mx = fmaxf(mx, ml[w].x); }
+    const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+    for (int w = 0; w < SPLIT_WAVES; ++w) {
+      const float f = __builtin_amdgcn_exp2f(ml[w].x - ref);
+      sum = fmaf(f, ml[w].y, sum);
+      const f32x4 z = *(const f32x4*)((const float*)(lds + w * out_lds) + rr * (HD + 4) + d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = fmaf(f, z[e], y[e]);
+    }
+    if (it.parts > 1) {
+      const int64_t at = ((int64_t)it.slot * a.kv_heads + kvh) * SPLIT_ROWS + rr;
+      leave(a.part_o + at * HD + d, y);
+      if (d == 0) leave(a.part_ml + at, mx, sum);
+    } else {
+      const int t = ri / a.group, h = kvh * a.group + ri % a.group;
+      const bool none = mx == -INFINITY && sum == 0.f;    // nothing seen (a score that is no number leaves its mark on the sum)
+      const float inv = 1.0f / sum;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : y[e] * inv;
+      T* to = (T*)a.out + (int64_t)(it.rows0 + t) * a.o_tok + (int64_t)h * a.o_head + d;
+      *(typename Quad<T>::raw*)to = quad_out<T>(y);
+      if (a.lse && d == 0) a.lse[(int64_t)(it.rows0 + t) * a.heads + h] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718f;
+    }
+  }
+}
+// The end of a workgroup that had one of several parts (all of its threads, its results left): it puts the call's number beside them and
+// looks at the other parts' places; who finds the number everywhere joins them, in their order, and clears the places.  Nobody waits.
+// The number goes out, past the L2, before the others are looked at, so the last one to leave it finds all; two may, and write the
+// same bits.  Scratch memory needs nothing in it beforehand (numbers are 64 bits wide and never come twice, but for a replayed
+// launch's, and that one's own places are clear again by then).
+template <typename T, int HD>
+__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const Item& it, int kvh, int tid, int* s_flag) {
+  const int lane = tid & 63;
+  const int first = it.slot - it.part;                    // (the parts' places lie side by side)
+  uint64_t* const stamps = a.stamps + (int64_t)first * a.kv_heads + kvh;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid < WAVE) {
+    if (lane == 0) __hip_atomic_store(stamps + (int64_t)it.part * a.kv_heads, a.stamp, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    bool missing = false;
+    for (int p = lane; p < it.parts; p += WAVE) missing |= __hip_atomic_load(stamps + (int64_t)p * a.kv_heads, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != a.stamp;
+    missing = __ballot(missing) != 0;
+    if (lane == 0) *s_flag = !missing;
+  }
+  __syncthreads();
+  if (!*s_flag) return;
+  const int rows = min(SPLIT_ROWS, it.n * a.group - it.tile * SPLIT_ROWS);
+  for (int x = tid; x < rows * (HD / 4); x += SPLIT_THREADS) {
+    const int rr = x / (HD / 4), d = x % (HD / 4) * 4, ri = it.tile * SPLIT_ROWS + rr;
+    auto at = [&](int p) { return ((int64_t)(first + p) * a.kv_heads + kvh) * SPLIT_ROWS + rr; };
+    float mx = -INFINITY, sum = 0.f;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    for (int p0 = 0; p0 < it.parts; p0 += 4) {            // four parts at a time, their sums and totals in one go
+      f32x2 ml[4], u[4], w[4];
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const int64_t from = at(min(p0 + p, it.parts - 1));
+        ml[p] = left(a.part_ml + from); u[p] = left(a.part_o + from * HD + d); w[p] = left(a.part_o + from * HD + d + 2);
+      }
+      const float before = mx;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) mx = fmaxf(mx, ml[p].x);
+      const float ref = mx == -INFINITY ? 0.f : mx, keep = __builtin_amdgcn_exp2f(before - ref);
+      if (p0 > 0) {
+        sum *= keep;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] *= keep;
+      }
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        if (p0 + p >= it.parts) break;
+        const float f = __builtin_amdgcn_exp2f(ml[p].x - ref);
+        sum = fmaf(f, ml[p].y, sum);
+        y.x = fmaf(f, u[p].x, y.x); y.y = fmaf(f, u[p].y, y.y); y.z = fmaf(f, w[p].x, y.z); y.w = fmaf(f, w[p].y, y.w);
+      }
+    }
+    const bool none = mx == -INFINITY && sum == 0.f;      // nothing seen (a score that is no number leaves its mark on the sum)
+    const float inv = 1.0f / sum;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : y[e] * inv;
+    const int t = ri / a.group, h = kvh * a.group + ri % a.group;
+    *(typename Quad<T>::raw*)((T*)a.out + (int64_t)(it.rows0 + t) * a.o_tok + (int64_t)h * a.o_head + d) = quad_out<T>(y);
+    if (a.lse && d == 0) a.lse[(int64_t)(it.rows0 + t) * a.heads + h] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718f;
+  }
+  for (int p = tid; p < it.parts; p += SPLIT_THREADS) __hip_atomic_store(stamps + (int64_t)p * a.kv_heads, (uint64_t)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+
+namespace {      // (a kernel that two sources have)
+
+// The parts of a row joined, in their order: HD / 4 lanes for a row.  Bound by reading them (500 rows of 40 heads in 3 parts, 31 MB: 9 us).  A launch
+// of its own: joined by the workgroups that had the parts, as paged_split_kernel does, 500 tokens over 4000 positions took 143 us beside 86 then.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
+  constexpr int LPR = HD / 4, RPW = 256 / LPR;
+  const int row = blockIdx.x, lane = threadIdx.x & 63;
+  const int s = seq_of_row(a.b, row, lane);
+  if (s < 0) return;
+  const SeqRows sr = seq_rows(a.b, s);
+  if ((unsigned)(row - sr.row0) >= (unsigned)sr.rows) return;      // (q_start decreases: the sequence has other rows, or none and no plan)
+  const int2 plan = a.plan[s];
+  const int parts = plan.y, h = blockIdx.y * RPW + threadIdx.x / LPR, d = (threadIdx.x % LPR) * 4;
+  if (parts <= 1 || h >= a.heads) return;
+  const int kvh = h / a.group, r = (row - sr.row0) * a.group + h % a.group, first = plan.x + r / TILE_ROWS * parts;
+  if (!have_places(first, parts, a.items)) return;
+  float mx = -INFINITY, sum = 0.f;
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 0; p0 < parts; p0 += 4) {                  // four parts at a time, their sums and totals in one go
+    float2 ml[4];
+    f32x4 z[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const int64_t at = ((int64_t)(first + min(p0 + p, parts - 1)) * a.kv_heads + kvh) * TILE_ROWS + r % TILE_ROWS;
+      ml[p] = a.part_ml[at];
+      z[p] = *(const f32x4*)(a.part_o + at * HD + d);
+    }
+    const float before = mx;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) mx = fmaxf(mx, ml[p].x);
+    const float ref = mx == -INFINITY ? 0.f : mx, keep = __builtin_amdgcn_exp2f(before - ref);
+    if (p0 > 0) { sum *= keep; y *= keep; }
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      if (p0 + p >= parts) break;
+      const float f = __builtin_amdgcn_exp2f(ml[p].x - ref);
+      sum = fmaf(f, ml[p].y, sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = fmaf(f, z[p][e], y[e]);
+    }
+  }
+  const bool none = mx == -INFINITY && sum == 0.f;
+  const float inv = 1.0f / sum;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : y[e] * inv;
+  *(typename Quad<T>::raw*)((T*)a.out + (int64_t)row * a.o_tok + (int64_t)h * a.o_head + d) = quad_out<T>(y);
+  if (a.lse && d == 0) a.lse[(int64_t)row * a.heads + h] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718f;
+}
+
+}  // namespace
+
 // Whether 16 positions in a row that begin at a multiple of 16 lie in one page, within 2^31 bytes
 inline bool near_pages(const PagedAttnArgs& a) { return a.b.page_size % 16 == 0 && a.kc_pos < 1 << 25 && a.vc_pos < 1 << 25; }
 hipError_t launch_paged_tiles(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t stream);
+uint64_t next_stamp();      // of a call, see join_parts
 
 }  // namespace ppd

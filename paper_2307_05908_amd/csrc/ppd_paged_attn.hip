@@ -10,85 +10,6 @@ using namespace ppd;
 
 namespace {
 
-constexpr int SPLIT_WAVES = 4, SPLIT_THREADS = SPLIT_WAVES * WAVE;
-
-// A part's results: sums of a row's components, and its reference and total, past the L2, for whoever joins them.
-__device__ __forceinline__ void leave(float* to, f32x4 v) {
-  typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
-  const u64x2 u = __builtin_bit_cast(u64x2, v);
-  __hip_atomic_store((uint64_t*)to, u.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __hip_atomic_store((uint64_t*)to + 1, u.y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ void leave(float2* to, float m, float l) {
-  const f32x2 v = {m, l};
-  __hip_atomic_store((uint64_t*)to, __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ f32x2 left(const void* from) {
-  return __builtin_bit_cast(f32x2, __hip_atomic_load((const uint64_t*)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-}
-// The end of a workgroup that had one of several parts (all of its threads, its results left): it puts the call's number beside them and
-// looks at the other parts' places; who finds the number everywhere joins them, in their order, and clears the places.  Nobody waits.
-// The number goes out, past the L2, before the others are looked at, so the last one to leave it finds all; two may, and write the
-// same bits.  Scratch memory needs nothing in it beforehand (numbers are 64 bits wide and never come twice, but for a replayed
-// launch's, and that one's own places are clear again by then).
-template <typename T, int HD>
-__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const Item& it, int kvh, int tid, int* s_flag) {
-  const int lane = tid & 63;
-  const int first = it.slot - it.part;                    // (the parts' places lie side by side)
-  uint64_t* const stamps = a.stamps + (int64_t)first * a.kv_heads + kvh;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  if (tid < WAVE) {
-    if (lane == 0) __hip_atomic_store(stamps + (int64_t)it.part * a.kv_heads, a.stamp, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    bool missing = false;
-    for (int p = lane; p < it.parts; p += WAVE) missing |= __hip_atomic_load(stamps + (int64_t)p * a.kv_heads, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != a.stamp;
-    missing = __ballot(missing) != 0;
-    if (lane == 0) *s_flag = !missing;
-  }
-  __syncthreads();
-  if (!*s_flag) return;
-  const int rows = min(SPLIT_ROWS, it.n * a.group - it.tile * SPLIT_ROWS);
-  for (int x = tid; x < rows * (HD / 4); x += SPLIT_THREADS) {
-    const int rr = x / (HD / 4), d = x % (HD / 4) * 4, ri = it.tile * SPLIT_ROWS + rr;
-    auto at = [&](int p) { return ((int64_t)(first + p) * a.kv_heads + kvh) * SPLIT_ROWS + rr; };
-    float mx = -INFINITY, sum = 0.f;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    for (int p0 = 0; p0 < it.parts; p0 += 4) {            // four parts at a time, their sums and totals in one go
-      f32x2 ml[4], u[4], w[4];
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const int64_t from = at(min(p0 + p, it.parts - 1));
-        ml[p] = left(a.part_ml + from); u[p] = left(a.part_o + from * HD + d); w[p] = left(a.part_o + from * HD + d + 2);
-      }
-      const float before = mx;
-#pragma unroll
-      for (int p = 0; p < 4; ++p) mx = fmaxf(mx, ml[p].x);
-      const float ref = mx == -INFINITY ? 0.f : mx, keep = __builtin_amdgcn_exp2f(before - ref);
-      if (p0 > 0) {
-        sum *= keep;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] *= keep;
-      }
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        if (p0 + p >= it.parts) break;
-        const float f = __builtin_amdgcn_exp2f(ml[p].x - ref);
-        sum = fmaf(f, ml[p].y, sum);
-        y.x = fmaf(f, u[p].x, y.x); y.y = fmaf(f, u[p].y, y.y); y.z = fmaf(f, w[p].x, y.z); y.w = fmaf(f, w[p].y, y.w);
-      }
-    }
-    const bool none = mx == -INFINITY && sum == 0.f;      // nothing seen (a score that is no number leaves its mark on the sum)
-    const float inv = 1.0f / sum;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : y[e] * inv;
-    const int t = ri / a.group, h = kvh * a.group + ri % a.group;
-    *(typename Quad<T>::raw*)((T*)a.out + (int64_t)(it.rows0 + t) * a.o_tok + (int64_t)h * a.o_head + d) = quad_out<T>(y);
-    if (a.lse && d == 0) a.lse[(int64_t)(it.rows0 + t) * a.heads + h] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718f;
-  }
-  for (int p = tid; p < it.parts; p += SPLIT_THREADS) __hip_atomic_store(stamps + (int64_t)p * a.kv_heads, (uint64_t)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
 // ---- few rows, many positions: bound by the stream of keys and values, and, where these are few, by the chain of latencies (lengths, page
 // numbers, keys and values, the join).  64 bf16 tokens over 60 to 8000 positions each (411 MB) take 90 us: 4.6 TB/s, and with the products
 // taken out no less; 64 of 4000 (1 GB) 197, 5.3 TB/s; a large copy reaches 4.6, a plain stream of reads 7.1.  Long runs of fp32 come here, too: four
@@ -347,38 +268,7 @@ __global__ __launch_bounds__(SPLIT_THREADS, 2) void paged_split_kernel(PagedAttn
   for (int i = 0; i < HD / 16; ++i) *(f32x4*)(so + row * (HD + 4) + 16 * i + 4 * quad) = o[i];
   if (quad == 0) ((float2*)(so + SPLIT_ROWS * (HD + 4)))[row] = make_float2(m, l);
   __syncthreads();
-  for (int x = tid; x < SPLIT_ROWS * HD / 4; x += SPLIT_THREADS) {
-    const int rr = x / (HD / 4), d = (x % (HD / 4)) * 4, ri = it.tile * SPLIT_ROWS + rr;
-    if (ri >= all_rows) break;
-    float2 ml[SPLIT_WAVES];
-    float mx = -INFINITY, sum = 0.f;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < SPLIT_WAVES; ++w) { ml[w] = ((const float2*)((const float*)(lds + w * C::OUT_LDS) + SPLIT_ROWS * (HD + 4)))[rr]; mx = fmaxf(mx, ml[w].x); }
-    const float ref = mx == -INFINITY ? 0.f : mx;
-#pragma unroll
-    for (int w = 0; w < SPLIT_WAVES; ++w) {
-      const float f = __builtin_amdgcn_exp2f(ml[w].x - ref);
-      sum = fmaf(f, ml[w].y, sum);
-      const f32x4 z = *(const f32x4*)((const float*)(lds + w * C::OUT_LDS) + rr * (HD + 4) + d);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = fmaf(f, z[e], y[e]);
-    }
-    if (it.parts > 1) {
-      const int64_t at = ((int64_t)it.slot * a.kv_heads + kvh) * SPLIT_ROWS + rr;
-      leave(a.part_o + at * HD + d, y);
-      if (d == 0) leave(a.part_ml + at, mx, sum);
-    } else {
-      const int t = ri / a.group, h = kvh * a.group + ri % a.group;
-      const bool none = mx == -INFINITY && sum == 0.f;    // nothing seen (a score that is no number leaves its mark on the sum)
-      const float inv = 1.0f / sum;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : y[e] * inv;
-      T* to = (T*)a.out + (int64_t)(it.rows0 + t) * a.o_tok + (int64_t)h * a.o_head + d;
-      *(typename Quad<T>::raw*)to = quad_out<T>(y);
-      if (a.lse && d == 0) a.lse[(int64_t)(it.rows0 + t) * a.heads + h] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718f;
-    }
-  }
+  join_waves<T, HD>(a, it, kvh, tid, lds, C::OUT_LDS);
   if (it.parts > 1) join_parts<T, HD>(a, it, kvh, tid, &s_flag);
 }
 
@@ -428,12 +318,6 @@ int check_attention(const ppd_paged_cache* cache, const ppd_paged_batch* batch, 
   return PPD_OK;
 }
 
-// Numbers of calls: a product with an odd constant never comes twice in 2^64 calls, and looks like nothing that memory holds by chance.
-uint64_t next_stamp() {
-  static std::atomic<uint64_t> calls{0};
-  return (calls.fetch_add(1, std::memory_order_relaxed) + 1) * 0x9e3779b97f4a7c15ull;
-}
-
 template <typename T, int HD>
 hipError_t attn_go(const PagedAttnArgs& a, int dtype, hipStream_t stream) {
   if (a.tile_rows == TILE_ROWS) return launch_paged_tiles(a, dtype, HD, stream);
@@ -443,6 +327,12 @@ hipError_t attn_go(const PagedAttnArgs& a, int dtype, hipStream_t stream) {
 }
 
 }  // namespace
+
+// Numbers of calls: a product with an odd constant never comes twice in 2^64 calls, and looks like nothing that memory holds by chance.
+uint64_t ppd::next_stamp() {
+  static std::atomic<uint64_t> calls{0};
+  return (calls.fetch_add(1, std::memory_order_relaxed) + 1) * 0x9e3779b97f4a7c15ull;
+}
 
 extern "C" int ppd_paged_attention_workspace(const ppd_paged_cache* cache, const ppd_paged_batch* batch, int n_heads, uint64_t* bytes) {
   AttnPlan p;

@@ -13,28 +13,6 @@
 namespace ppd {
 namespace {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
-__device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c, bf16_t) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c, f16_t) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-// Two weights as two terms of the type, side by side.  The first is cut off, not rounded, and the second is not zero where the weight is not (the
-// type's smallest normal number, or half floats' smallest one, 2^-31 of the row's largest weight): a value that is infinite has its sign in both
-// products.  (The rests of rounded first terms need a second pass without such values, 9 ms, not 0.6, for the two prompts where no value is a number;
-// else the same time.)
-__device__ __forceinline__ u32x2 two_terms(float x, float y, bf16_t) {
-  const uint32_t u = __float_as_uint(x), v = __float_as_uint(y);
-  const float a = x - __uint_as_float(u & 0xffff0000u), b = y - __uint_as_float(v & 0xffff0000u);
-  return (u32x2){__builtin_amdgcn_perm(v, u, 0x07060302u), pair(__builtin_amdgcn_fmed3f(a, x, 0x1p-126f), __builtin_amdgcn_fmed3f(b, y, 0x1p-126f), bf16_t())};
-}
-__device__ __forceinline__ u32x2 two_terms(float x, float y, f16_t) {
-  const auto h = __builtin_amdgcn_cvt_pkrtz(x, y);
-  const float a = x - (float)h[0], b = y - (float)h[1];
-  return (u32x2){__builtin_bit_cast(uint32_t, h), pair(__builtin_amdgcn_fmed3f(a, x, 0x1p-24f), __builtin_amdgcn_fmed3f(b, y, 0x1p-24f), f16_t())};
-}
 // dma16 with the lanes' sources as 32-bit offsets from one address
 __device__ __forceinline__ void dma16_near(const void* base, int offset, void* lds_dst) {
   const unsigned la = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds_dst;
@@ -296,54 +274,6 @@ __global__ __launch_bounds__(256, HD == 64 ? 4 : 2) void paged_tile_kernel(Paged
       *(u32x2*)(to + 32 * d + 2 * e) = quad_out<T>(y);
     }
   if (a.lse && half == 0) a.lse[(int64_t)(it.rows0 + tok) * a.heads + head] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718f;
-}
-
-// The parts of a row joined, in their order: HD / 4 lanes for a row.  Bound by reading them (500 rows of 40 heads in 3 parts, 31 MB: 9 us).  A launch
-// of its own: joined by the workgroups that had the parts, as paged_split_kernel does, 500 tokens over 4000 positions took 143 us beside 86 then.
-template <typename T, int HD>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
-  constexpr int LPR = HD / 4, RPW = 256 / LPR;
-  const int row = blockIdx.x, lane = threadIdx.x & 63;
-  const int s = seq_of_row(a.b, row, lane);
-  if (s < 0) return;
-  const SeqRows sr = seq_rows(a.b, s);
-  if ((unsigned)(row - sr.row0) >= (unsigned)sr.rows) return;      // (q_start decreases: the sequence has other rows, or none and no plan)
-  const int2 plan = a.plan[s];
-  const int parts = plan.y, h = blockIdx.y * RPW + threadIdx.x / LPR, d = (threadIdx.x % LPR) * 4;
-  if (parts <= 1 || h >= a.heads) return;
-  const int kvh = h / a.group, r = (row - sr.row0) * a.group + h % a.group, first = plan.x + r / TILE_ROWS * parts;
-  if (!have_places(first, parts, a.items)) return;
-  float mx = -INFINITY, sum = 0.f;
-  f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  for (int p0 = 0; p0 < parts; p0 += 4) {                  // four parts at a time, their sums and totals in one go
-    float2 ml[4];
-    f32x4 z[4];
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const int64_t at = ((int64_t)(first + min(p0 + p, parts - 1)) * a.kv_heads + kvh) * TILE_ROWS + r % TILE_ROWS;
-      ml[p] = a.part_ml[at];
-      z[p] = *(const f32x4*)(a.part_o + at * HD + d);
-    }
-    const float before = mx;
-#pragma unroll
-    for (int p = 0; p < 4; ++p) mx = fmaxf(mx, ml[p].x);
-    const float ref = mx == -INFINITY ? 0.f : mx, keep = __builtin_amdgcn_exp2f(before - ref);
-    if (p0 > 0) { sum *= keep; y *= keep; }
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      if (p0 + p >= parts) break;
-      const float f = __builtin_amdgcn_exp2f(ml[p].x - ref);
-      sum = fmaf(f, ml[p].y, sum);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = fmaf(f, z[p][e], y[e]);
-    }
-  }
-  const bool none = mx == -INFINITY && sum == 0.f;
-  const float inv = 1.0f / sum;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : y[e] * inv;
-  *(typename Quad<T>::raw*)((T*)a.out + (int64_t)row * a.o_tok + (int64_t)h * a.o_head + d) = quad_out<T>(y);
-  if (a.lse && d == 0) a.lse[(int64_t)row * a.heads + h] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718f;
 }
 
 template <typename T, bool NEAR>

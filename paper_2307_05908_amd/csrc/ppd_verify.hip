@@ -117,9 +117,6 @@ __device__ __forceinline__ void fill_table(double* table) {
   table[i] = __hiloint2double(__double2hiint(p) - (i << 12), __double2loint(p));
 }
 
-template <int CTRL> __device__ __forceinline__ double dpp_f64(double v) {
-  return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xf, 0xf, false), __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xf, 0xf, false));
-}
 __device__ __forceinline__ double lane_f64(double v, int l) {
   return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), l), __builtin_amdgcn_readlane(__double2loint(v), l));
 }

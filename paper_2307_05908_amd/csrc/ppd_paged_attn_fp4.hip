@@ -101,6 +101,7 @@ __global__ __launch_bounds__(SPLIT_THREADS, sizeof(T) == 4 ? 2 : 3) void paged_s
   };
   f32x4 o[HD / 16];
   float m, l;                                             // the row's reference (its maximum of scores times to_log2; the same in its four lanes) and the lane's part of the sum
+  uint32_t nans = 0;                                      // blocks of 32 components with a value that is NaN and seen
   auto work = [&](int step, auto set) {
     constexpr int S = decltype(set)::value;
     const int base = it.lo + step * C::BP;
@@ -130,7 +131,7 @@ __global__ __launch_bounds__(SPLIT_THREADS, sizeof(T) == 4 ? 2 : 3) void paged_s
           s[t][e] = seen ? s[t][e] : -INFINITY;
         }
     }
-    // Values that are NaN go in as zeros, as a weight of zero does not silence them, and are put in below where they are seen.  (All others are
+    // Values that are NaN go in as zeros, as a weight of zero does not silence them, and are put in behind the loop where they are seen.  (All others are
     // finite, whatever lies where nothing is seen.)
     uint64_t nan[C::NT];
 #pragma unroll
@@ -182,14 +183,13 @@ __global__ __launch_bounds__(SPLIT_THREADS, sizeof(T) == 4 ? 2 : 3) void paged_s
 #pragma unroll
       for (int n = 0; n < NW; ++n) o[i] = mma16(vt, w[n], o[i], bf16_t());
     }
+    if (nan[0] | nan[1])
 #pragma unroll
-    for (int t = 0; t < C::NT; ++t)
-      for (uint64_t bits = nan[t]; bits; bits &= bits - 1) {      // (by position and quarter of the row)
-        const int at = __builtin_ctzll(bits), p = 16 * t + at / 4, first = at % 4 * (HD / 4) / FP4_BLOCK * 2;
-        if (((have >> p) & 1) && base + p <= pos && base + p >= from)
-#pragma unroll
-          for (int i = 0; i < HD / 16; ++i) if (i / 2 * 2 == first) o[i] = __builtin_nanf("");
-      }
+      for (int t = 0; t < C::NT; ++t)
+        for (uint64_t bits = nan[t]; bits; bits &= bits - 1) {      // (by position and quarter of the row)
+          const int at = __builtin_ctzll(bits), p = 16 * t + at / 4;
+          if (((have >> p) & 1) && base + p <= pos && base + p >= from) nans |= 1u << at % 4 * (HD / 4) / FP4_BLOCK;
+        }
   };
 #pragma unroll
   for (int i = 0; i < HD / 16; ++i) o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -209,6 +209,8 @@ __global__ __launch_bounds__(SPLIT_THREADS, sizeof(T) == 4 ? 2 : 3) void paged_s
     place(after + SPLIT_WAVES);
     work(next, uneven);
   }
+#pragma unroll
+  for (int i = 0; i < HD / 16; ++i) if (nans >> i / 2 & 1) o[i] = (f32x4){__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
   l += __shfl_xor(l, 16, WAVE);
   l += __shfl_xor(l, 32, WAVE);
   // ---- the waves' results

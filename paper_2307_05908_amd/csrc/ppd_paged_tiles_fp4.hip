@@ -13,7 +13,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_fp4_kernel(Fp4AttnArgs a) {
   constexpr int LANE = HD / 8, NC = LANE / 4;              // bytes of codes of a thread, and words of eight
   typedef typename std::conditional<HD == 128, u32x4, u32x2>::type words;
   __shared__ __align__(1024) char lds[4 * SIDE];           // [2 buffers][keys, values][64 positions][head_dim]
-  __shared__ uint64_t s_nan[2][4];                         // values that are NaN: by wave, a bit for each of its positions and quarters of the row
+  __shared__ __align__(16) uint64_t s_nan[2][4];                         // values that are NaN: by wave, a bit for each of its positions and quarters of the row
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int kvheads = a.kv_heads, idx = blockIdx.x / kvheads, kvh = blockIdx.x % kvheads;
   Item it;
@@ -92,6 +92,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_fp4_kernel(Fp4AttnArgs a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
   float m = -INFINITY, l = 0.f;
+  uint32_t nans = 0;                                       // blocks of 32 components with a value that is NaN and seen
   // where a lane's operands begin, see paged_tile_kernel
   int kat = col * ROWB + (half ^ (HD == 128 ? col & 15 : (col >> 1) & 7)) * 16;
   const int vrow = 4 * half + ((lane & 15) >> 2);
@@ -176,21 +177,18 @@ __global__ __launch_bounds__(256, 2) void paged_tile_fp4_kernel(Fp4AttnArgs a) {
         o[d] = mma32(w, lo, o[d], bf16_t());
       }
     }
-    // a weight of zero would not have silenced a value that is NaN: it is put in where it is seen
+    // a weight of zero would not have silenced a value that is NaN: it is put in, behind the loop, where it is seen
+    const u32x4 n0 = *(const u32x4*)&s_nan[n & 1][0], n1 = *(const u32x4*)&s_nan[n & 1][2];
+    if (__ballot((n0.x | n0.y | n0.z | n0.w | n1.x | n1.y | n1.z | n1.w) != 0))
 #pragma unroll 1
-    for (int w = 0; w < 4; ++w) {
-      const uint64_t some = s_nan[n & 1][w];
-      uint64_t bits = (uint64_t)__builtin_amdgcn_readfirstlane((int)(some >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)some);
-      for (; bits; bits &= bits - 1) {
-        const int at = __builtin_ctzll(bits), p = 16 * w + at / 4, block = at % 4 * (HD / 4) / FP4_BLOCK;
-        if (((have >> p) & 1) && base + p <= pos && base + p >= from)
-#pragma unroll
-          for (int d = 0; d < HD / 32; ++d)
-            if (d == block)
-#pragma unroll
-              for (int e = 0; e < 16; ++e) o[d][e] = __builtin_nanf("");
+      for (int w = 0; w < 4; ++w) {
+        const uint64_t some = s_nan[n & 1][w];
+        uint64_t bits = (uint64_t)__builtin_amdgcn_readfirstlane((int)(some >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)some);
+        for (; bits; bits &= bits - 1) {
+          const int at = __builtin_ctzll(bits), p = 16 * w + at / 4;
+          if (((have >> p) & 1) && base + p <= pos && base + p >= from) nans |= 1u << at % 4 * (HD / 4) / FP4_BLOCK;
+        }
       }
-    }
   };
   uint64_t have = 0, have_next = 0;
   if (blocks > 0) {
@@ -215,6 +213,11 @@ __global__ __launch_bounds__(256, 2) void paged_tile_fp4_kernel(Fp4AttnArgs a) {
     const bool whole = have == ~0ull && base + KV - 1 <= wave_first && base >= wave_all;
     step(n, base, have, whole);
   }
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d)
+    if (nans >> d & 1)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[d][e] = __builtin_nanf("");
   l += __shfl_xor(l, 32, WAVE);
   if (r >= all_rows) return;
   if (it.parts > 1) {

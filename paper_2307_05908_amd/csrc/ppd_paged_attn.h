@@ -23,6 +23,7 @@ struct PagedAttnArgs {
   int heads, kv_heads, group, window;
   int tile_rows, items;               // items: parts of a key/value head that there are workgroups and places for
   float to_log2;                      // scale * log2(e): a score's exponent of two
+  int wide_want; float wide_from;     // 0, or parts to aim at where all tiles together have this many blocks: wide workgroups then (paged_split_fp4_kernel)
   int want, fine, least, whole;       // parts per key/value head to aim at, and among sequences of unlike lengths; blocks of a part at least (0:
                                       // one part each), and up to which a tile is not cut
   float* part_o; float2* part_ml;     // [item][kv_heads][rows of a tile][head_dim], [item][kv_heads][rows of a tile]
@@ -84,6 +85,7 @@ struct Item {
   int tile, part, parts;
   int slot;                // where its partial results go
   int lo, hi;              // positions of the part, see span_of
+  bool wide;               // a workgroup has four heads, a wave each
 };
 
 // The first position that a row at `pos` sees.  Positions are negative where kv_len is below the rows, and windows go up to 2^31 - 1.
@@ -154,7 +156,7 @@ __device__ __forceinline__ bool find_whole(const PagedAttnArgs& a, int idx, int 
 // the one item that the grid has to spare.)  A lane looks at J sequences in turn, all lanes at once: up to 64 J sequences need one look.
 // False: there is no such item.
 template <int TILE, int J>
-__device__ __forceinline__ bool find_part(const PagedAttnArgs& a, int idx, bool tell, int lane, Item& it) {
+__device__ __forceinline__ bool find_part(const PagedAttnArgs& a, int idx, int wide_idx, bool tell, int lane, Item& it) {
   int tiles[J], blocks[J];
   SeqRows r1;                                               // (J 1: the lane's sequence)
   const bool few = a.b.n_seqs <= WAVE * J;
@@ -180,7 +182,9 @@ __device__ __forceinline__ bool find_part(const PagedAttnArgs& a, int idx, bool 
   // Two workgroups run on a unit, and where lengths differ and two long parts meet on one it is the last to end: then shorter parts, if they
   // are not too short for that.  bf16, us at `want` / `fine`: 64 sequences of 60 to 8000 positions 97 / 88, 32 of them 39.2 / 37.2, 64 of 60 to
   // 2000 32.1 / 34.2; of like lengths, 48 of 1000 38.6 / 45.1, 16 of 2000 29.3 / 32.9.
-  const float want = longest * count > 2.f * all && all >= 12.f * (float)a.fine ? (float)a.fine : (float)a.want;
+  it.wide = a.wide_want > 0 && all >= a.wide_from;
+  if (it.wide) idx = wide_idx;
+  const float want = it.wide ? (float)a.wide_want : longest * count > 2.f * all && all >= 12.f * (float)a.fine ? (float)a.fine : (float)a.want;
   int len = max(a.least, (int)ceilf(all / want));
   // few tiles: where their ends make it more parts than `want`, longer ones (a second round of workgroups for a few of them would cost more)
   for (int again = 0; again < 3 && few && J == 1; ++again) {
@@ -253,8 +257,10 @@ __device__ __forceinline__ bool find_part(const PagedAttnArgs& a, int idx, bool 
 __host__ __device__ __forceinline__ bool have_places(int first, int parts, int items) { return first >= 0 && parts <= items - first; }
 
 template <int TILE>
-__device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, bool tell, int lane, Item& it) {
-  if (!(a.least == 0 ? find_whole<TILE>(a, idx, lane, it) : a.b.n_seqs <= WAVE ? find_part<TILE, 1>(a, idx, tell, lane, it) : find_part<TILE, 8>(a, idx, tell, lane, it))) return false;
+__device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, int wide_idx, bool tell, int lane, Item& it) {
+  it.wide = false;
+  if (!(a.least == 0 ? find_whole<TILE>(a, idx, lane, it) : a.b.n_seqs <= WAVE ? find_part<TILE, 1>(a, idx, wide_idx, tell, lane, it)
+                                                                               : find_part<TILE, 8>(a, idx, wide_idx, tell, lane, it))) return false;
   if (!have_places(it.slot - it.part, it.parts, a.items)) return false;
   const Span span = span_of(it.pos0, it.n, it.tile, TILE, a.group, it.part, it.parts, a.b.room, a.window);
   it.lo = span.lo; it.hi = span.hi;
@@ -292,23 +298,24 @@ __device__ __forceinline__ f32x2 left(const void* from) {
   return __builtin_bit_cast(f32x2, __hip_atomic_load((const uint64_t*)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 // The waves of a workgroup joined: their results lie out_lds bytes apart, sums in rows of HD + 4 and behind them references and totals.  What comes of it
-// is the result, or a part's.
-template <typename T, int HD>
-__device__ __forceinline__ void join_waves(const PagedAttnArgs& a, const Item& it, int kvh, int tid, const char* lds, int out_lds) {
-  for (int x = tid; x < SPLIT_ROWS * HD / 4; x += SPLIT_THREADS) {
-    const int rr = x / (HD / 4), d = (x % (HD / 4)) * 4, ri = it.tile * SPLIT_ROWS + rr;
-    if (ri >= it.n * a.group) break;
-    float2 ml[SPLIT_WAVES];
+// is the result, or a part's.  WIDE: every wave has a key/value head of its own, kvh0 and on.
+template <typename T, int HD, bool WIDE = false>
+__device__ __forceinline__ void join_waves(const PagedAttnArgs& a, const Item& it, int kvh0, int tid, const char* lds, int out_lds) {
+  constexpr int HEADS = WIDE ? SPLIT_WAVES : 1, WAVES = SPLIT_WAVES / HEADS;
+  for (int x = tid; x < HEADS * SPLIT_ROWS * HD / 4; x += SPLIT_THREADS) {
+    const int own = x / (SPLIT_ROWS * HD / 4), kvh = kvh0 + own, rr = x / (HD / 4) % SPLIT_ROWS, d = (x % (HD / 4)) * 4, ri = it.tile * SPLIT_ROWS + rr;
+    if (ri >= it.n * a.group) continue;
+    float2 ml[WAVES];
     float mx = -INFINITY, sum = 0.f;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < SPLIT_WAVES; ++w) { ml[w] = ((const float2*)((const float*)(lds + w * out_lds) + SPLIT_ROWS * (HD + 4)))[rr]; mx = fmaxf(mx, ml[w].x); }
+    for (int w = 0; w < WAVES; ++w) { ml[w] = ((const float2*)((const float*)(lds + (own + w) * out_lds) + SPLIT_ROWS * (HD + 4)))[rr]; mx = fmaxf(mx, ml[w].x); }
     const float ref = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
-    for (int w = 0; w < SPLIT_WAVES; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       const float f = __builtin_amdgcn_exp2f(ml[w].x - ref);
       sum = fmaf(f, ml[w].y, sum);
-      const f32x4 z = *(const f32x4*)((const float*)(lds + w * out_lds) + rr * (HD + 4) + d);
+      const f32x4 z = *(const f32x4*)((const float*)(lds + (own + w) * out_lds) + rr * (HD + 4) + d);
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = fmaf(f, z[e], y[e]);
     }
@@ -333,64 +340,68 @@ __device__ __forceinline__ void join_waves(const PagedAttnArgs& a, const Item& i
 // The number goes out, past the L2, before the others are looked at, so the last one to leave it finds all; two may, and write the
 // same bits.  Scratch memory needs nothing in it beforehand (numbers are 64 bits wide and never come twice, but for a replayed
 // launch's, and that one's own places are clear again by then).
-template <typename T, int HD>
-__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const Item& it, int kvh, int tid, int* s_flag) {
-  const int lane = tid & 63;
+template <typename T, int HD, bool WIDE = false>
+__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const Item& it, int kvh0, int tid, int* s_flag) {      // s_flag: [heads]
+  constexpr int HEADS = WIDE ? SPLIT_WAVES : 1;
+  const int lane = tid & 63, own = WIDE ? tid >> 6 : 0;
   const int first = it.slot - it.part;                    // (the parts' places lie side by side)
-  uint64_t* const stamps = a.stamps + (int64_t)first * a.kv_heads + kvh;
+  uint64_t* const stamps = a.stamps + (int64_t)first * a.kv_heads + kvh0;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (tid < WAVE) {
-    if (lane == 0) __hip_atomic_store(stamps + (int64_t)it.part * a.kv_heads, a.stamp, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (tid < HEADS * WAVE) {
+    if (lane == 0) __hip_atomic_store(stamps + (int64_t)it.part * a.kv_heads + own, a.stamp, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     bool missing = false;
-    for (int p = lane; p < it.parts; p += WAVE) missing |= __hip_atomic_load(stamps + (int64_t)p * a.kv_heads, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != a.stamp;
+    for (int p = lane; p < it.parts; p += WAVE) missing |= __hip_atomic_load(stamps + (int64_t)p * a.kv_heads + own, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != a.stamp;
     missing = __ballot(missing) != 0;
-    if (lane == 0) *s_flag = !missing;
+    if (lane == 0) s_flag[own] = !missing;
   }
   __syncthreads();
-  if (!*s_flag) return;
-  const int rows = min(SPLIT_ROWS, it.n * a.group - it.tile * SPLIT_ROWS);
-  for (int x = tid; x < rows * (HD / 4); x += SPLIT_THREADS) {
-    const int rr = x / (HD / 4), d = x % (HD / 4) * 4, ri = it.tile * SPLIT_ROWS + rr;
-    auto at = [&](int p) { return ((int64_t)(first + p) * a.kv_heads + kvh) * SPLIT_ROWS + rr; };
-    float mx = -INFINITY, sum = 0.f;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    for (int p0 = 0; p0 < it.parts; p0 += 4) {            // four parts at a time, their sums and totals in one go
-      f32x2 ml[4], u[4], w[4];
+#pragma unroll 1
+  for (int head = 0; head < HEADS; ++head) {
+    if (!s_flag[head]) continue;
+    const int kvh = kvh0 + head;
+    const int rows = min(SPLIT_ROWS, it.n * a.group - it.tile * SPLIT_ROWS);
+    for (int x = tid; x < rows * (HD / 4); x += SPLIT_THREADS) {
+      const int rr = x / (HD / 4), d = x % (HD / 4) * 4, ri = it.tile * SPLIT_ROWS + rr;
+      auto at = [&](int p) { return ((int64_t)(first + p) * a.kv_heads + kvh) * SPLIT_ROWS + rr; };
+      float mx = -INFINITY, sum = 0.f;
+      f32x4 y = {0.f, 0.f, 0.f, 0.f};
+      for (int p0 = 0; p0 < it.parts; p0 += 4) {            // four parts at a time, their sums and totals in one go
+        f32x2 ml[4], u[4], w[4];
 #pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const int64_t from = at(min(p0 + p, it.parts - 1));
-        ml[p] = left(a.part_ml + from); u[p] = left(a.part_o + from * HD + d); w[p] = left(a.part_o + from * HD + d + 2);
+        for (int p = 0; p < 4; ++p) {
+          const int64_t from = at(min(p0 + p, it.parts - 1));
+          ml[p] = left(a.part_ml + from); u[p] = left(a.part_o + from * HD + d); w[p] = left(a.part_o + from * HD + d + 2);
+        }
+        const float before = mx;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) mx = fmaxf(mx, ml[p].x);
+        const float ref = mx == -INFINITY ? 0.f : mx, keep = __builtin_amdgcn_exp2f(before - ref);
+        if (p0 > 0) {
+          sum *= keep;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] *= keep;
+        }
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          if (p0 + p >= it.parts) break;
+          const float f = __builtin_amdgcn_exp2f(ml[p].x - ref);
+          sum = fmaf(f, ml[p].y, sum);
+          y.x = fmaf(f, u[p].x, y.x); y.y = fmaf(f, u[p].y, y.y); y.z = fmaf(f, w[p].x, y.z); y.w = fmaf(f, w[p].y, y.w);
+        }
       }
-      const float before = mx;
+      const bool none = mx == -INFINITY && sum == 0.f;      // nothing seen (a score that is no number leaves its mark on the sum)
+      const float inv = 1.0f / sum;
 #pragma unroll
-      for (int p = 0; p < 4; ++p) mx = fmaxf(mx, ml[p].x);
-      const float ref = mx == -INFINITY ? 0.f : mx, keep = __builtin_amdgcn_exp2f(before - ref);
-      if (p0 > 0) {
-        sum *= keep;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] *= keep;
-      }
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        if (p0 + p >= it.parts) break;
-        const float f = __builtin_amdgcn_exp2f(ml[p].x - ref);
-        sum = fmaf(f, ml[p].y, sum);
-        y.x = fmaf(f, u[p].x, y.x); y.y = fmaf(f, u[p].y, y.y); y.z = fmaf(f, w[p].x, y.z); y.w = fmaf(f, w[p].y, y.w);
-      }
+      for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : y[e] * inv;
+      const int t = ri / a.group, h = kvh * a.group + ri % a.group;
+      *(typename Quad<T>::raw*)((T*)a.out + (int64_t)(it.rows0 + t) * a.o_tok + (int64_t)h * a.o_head + d) = quad_out<T>(y);
+      if (a.lse && d == 0) a.lse[(int64_t)(it.rows0 + t) * a.heads + h] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718f;
     }
-    const bool none = mx == -INFINITY && sum == 0.f;      // nothing seen (a score that is no number leaves its mark on the sum)
-    const float inv = 1.0f / sum;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : y[e] * inv;
-    const int t = ri / a.group, h = kvh * a.group + ri % a.group;
-    *(typename Quad<T>::raw*)((T*)a.out + (int64_t)(it.rows0 + t) * a.o_tok + (int64_t)h * a.o_head + d) = quad_out<T>(y);
-    if (a.lse && d == 0) a.lse[(int64_t)(it.rows0 + t) * a.heads + h] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718f;
+    for (int p = tid; p < it.parts; p += SPLIT_THREADS) __hip_atomic_store(stamps + (int64_t)p * a.kv_heads + head, (uint64_t)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  for (int p = tid; p < it.parts; p += SPLIT_THREADS) __hip_atomic_store(stamps + (int64_t)p * a.kv_heads, (uint64_t)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-
 
 namespace {      // (a kernel that two sources have)
 

@@ -41,7 +41,7 @@ __global__ __launch_bounds__(SPLIT_THREADS, 2) void paged_split_kernel(PagedAttn
   // the heads of one part side by side: a position's keys are one run of memory, and its pieces then come at the same time
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kvh = blockIdx.x % a.kv_heads, row = lane & 15, quad = lane >> 4;
   Item it;
-  if (!find_item<SPLIT_ROWS>(a, blockIdx.x / a.kv_heads, false, lane, it)) return;
+  if (!find_item<SPLIT_ROWS>(a, blockIdx.x / a.kv_heads, 0, false, lane, it)) return;
   const int all_rows = it.n * a.group;
   const int r = it.tile * SPLIT_ROWS + row, rc = min(r, all_rows - 1), tok = rc / a.group, head = kvh * a.group + rc % a.group;
   const int pos = r < all_rows ? it.pos0 + tok : -1;                          // what the lane's row sees ends there
@@ -364,6 +364,7 @@ extern "C" int ppd_paged_attention(const ppd_paged_cache* cache, const ppd_paged
   a.tile_rows = p.tiles ? TILE_ROWS : SPLIT_ROWS; a.items = (int)p.items; a.want = p.want; a.fine = p.fine; a.least = p.least; a.whole = p.whole;
   a.part_o = (float*)workspace; a.part_ml = (float2*)((char*)workspace + p.o_bytes); a.stamps = (uint64_t*)((char*)workspace + p.o_bytes + p.ml_bytes);
   a.plan = (int2*)a.stamps;
+  a.wide_want = 0; a.wide_from = 0.f;
   a.stamp = next_stamp();
   hipStream_t st = (hipStream_t)hip_stream;
   if (cache->head_dim == 64)

@@ -13,6 +13,7 @@ namespace ppd {
 struct Fp4AttnArgs : PagedAttnArgs {
   const void *ks, *vs;
   int64_t ks_page, ks_pos, ks_head, vs_page, vs_pos, vs_head;
+  int side, wide_side; // workgroups of a part that follow each other on one XCD, and of four heads each
 };
 
 template <typename T> struct Terms;

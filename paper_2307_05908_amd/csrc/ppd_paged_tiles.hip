@@ -38,7 +38,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 4 : 2) void paged_tile_kernel(Paged
   __shared__ int s_odd[2];                                 // first and last block with a value that is infinite, or no number, where not every row sees it
   if (threadIdx.x == 0) { s_odd[0] = 0x7fffffff; s_odd[1] = -1; }
   Item it;
-  if (!find_item<TILE_ROWS>(a, idx, idx == 0 && kvh == 0 && wave == 0 && a.least > 0, lane, it)) return;
+  if (!find_item<TILE_ROWS>(a, idx, 0, idx == 0 && kvh == 0 && wave == 0 && a.least > 0, lane, it)) return;
   const int all_rows = it.n * a.group;
   const int r0 = it.tile * TILE_ROWS + 32 * wave, r = r0 + col, rc = min(r, all_rows - 1), tok = rc / a.group, head = kvh * a.group + rc % a.group;
   const int pos = r < all_rows ? it.pos0 + tok : -1, from = first_seen(pos, a.window);

@@ -33,12 +33,32 @@ def limits(b, ref, lse, size, reach):
     return size * (2 * w[..., None] + left) + ref.abs() * HALF_STEP[b.dtype] * (1 + 2.0 ** -9) + TINY[b.dtype] + gone, w + lse.abs() * 2.0 ** -23
 
 
+def long_runs(d):
+    """The same batch with so wide a table (of no pages) that its runs, if they are long enough, go through the kernel for long runs."""
+    if d.dtype == F32 or d.n * d.heads // d.kv_heads < 64 * d.pages.shape[0]:
+        return None
+    most = int(13e6 / (d.n * d.heads * d.page)) + 1
+    if most <= d.pages.shape[1]:
+        return None
+    e = object.__new__(Batch4)
+    e.__dict__ = dict(d.__dict__, pages=torch.cat([d.pages, torch.full((d.pages.shape[0], most - d.pages.shape[1]), -1, dtype=torch.int32, device="cuda")], 1))
+    return e
+
+
 def check(b, scale=None, window=0, d=None, ref=None):
     d = b.cuda() if d is None else d
+    ref = attention64(b, scale, window) if ref is None else ref
+    e = long_runs(d)
+    if e is not None:
+        check_one(b, scale, window, e, ref)
+    return check_one(b, scale, window, d, ref)
+
+
+def check_one(b, scale, window, d, ref):
     out, lse = call(d, scale=scale, window=window, out=torch.full_like(d.q, 7.0))
     torch.cuda.synchronize()
     o, z = out.cpu().double(), lse.cpu().double()
-    ref64, lse64, size, reach = attention64(b, scale, window) if ref is None else ref
+    ref64, lse64, size, reach = ref
     r = b.rows
     tol, ltol = limits(b, ref64, lse64, size, reach)
     gone = torch.isinf(lse64[:r])
@@ -151,9 +171,12 @@ def test_every_position_has_its_part(dtype, hd, new):
                 b.q[row, :, axis[p]] = 64.0                            # a score of 384, the others 0
                 want[row] = b.v_cache[b.slot(s, p)].repeat_interleave(2, 0).to(dtype)
             row += 1
-    out, _ = call(b.cuda(), scale=1.0)
     some = ~want.isnan().any(-1)
-    assert some.sum() > 150 and torch.equal(out.cpu()[:b.rows][some], want[some])
+    assert some.sum() > 150
+    d = b.cuda()
+    for e in (d, long_runs(d)):
+        if e is not None:
+            assert torch.equal(call(e, scale=1.0)[0].cpu()[:b.rows][some], want[some])
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -201,22 +224,27 @@ def test_what_is_not_seen_has_no_part(dtype, hd, bad, heads):
     # the last tokens of the two runs, and one in the middle: rows before them are as they were
     for s, back in ((1, 1), (1, 40), (3, 1), (3, 100)):
         spoil(d, b.slot(s, b.kv[s] - back))
-    out, lse = call(d)
     first, tol, ltol = b.rows - 140 - 4 - 60, *limits(b, *ref)
-    for lo, hi in ((0, first + 60 - 40), (first + 60, first + 64), (first + 64, first + 64 + 40)):
-        assert ((out.cpu().double() - ref[0]).abs() <= tol)[lo:hi].all()
-        assert ((lse.cpu().double() - ref[1]).abs() <= ltol)[lo:hi].all()
-    if bad >= 253:
-        assert out[first + 60 - 40:first + 60].isnan().all() and out[first + 64 + 40:].isnan().all() and lse[first + 64 + 40:].isnan().all()
+    for e in (d, long_runs(d)):
+        if e is None:
+            continue
+        out, lse = call(e)
+        for lo, hi in ((0, first + 60 - 40), (first + 60, first + 64), (first + 64, first + 64 + 40)):
+            assert ((out.cpu().double() - ref[0]).abs() <= tol)[lo:hi].all()
+            assert ((lse.cpu().double() - ref[1]).abs() <= ltol)[lo:hi].all()
+        if bad >= 253:
+            assert out[first + 60 - 40:first + 60].isnan().all() and out[first + 64 + 40:].isnan().all() and lse[first + 64 + 40:].isnan().all()
     # outside the window
     b = Batch4([1, 60, 4, 140], [90, 77, 30, 140], heads, 2, hd, dtype)
     ref = attention64(b, window=20)
     d = b.cuda()
     spoil(d, b.slot(3, 50))
-    out, lse = call(d, window=20)
     tol, ltol = limits(b, *ref)
     clean = [r for r in range(b.rows) if not (r >= 65 and 50 <= r - 65 < 70)]
-    assert ((out.cpu().double() - ref[0]).abs() <= tol)[clean].all() and ((lse.cpu().double() - ref[1]).abs() <= ltol)[clean].all()
+    for e in (d, long_runs(d)):
+        if e is not None:
+            out, lse = call(e, window=20)
+            assert ((out.cpu().double() - ref[0]).abs() <= tol)[clean].all() and ((lse.cpu().double() - ref[1]).abs() <= ltol)[clean].all()
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -236,9 +264,11 @@ def test_values_that_are_nan(dtype, hd, new, kv):
             d.v_codes[b.slot(s, p)][h, 16 * block:16 * block + 16] = 0
             hit[row + max(0, p - (x - m)):row + m, h, 32 * block:32 * block + 32] = True
         row += m
-    out, lse = call(d)
-    o = out.cpu().double()
-    assert o[hit].isnan().all() and ((o - ref[0]).abs() <= tol)[~hit].all() and ((lse.cpu().double() - ref[1]).abs() <= ltol).all()
+    for e in (d, long_runs(d)):
+        if e is not None:
+            out, lse = call(e)
+            o = out.cpu().double()
+            assert o[hit].isnan().all() and ((o - ref[0]).abs() <= tol)[~hit].all() and ((lse.cpu().double() - ref[1]).abs() <= ltol).all()
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -325,11 +355,13 @@ def test_strided_rows():
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_same_bits_every_time(dtype):
-    b = Batch4([1, 3, 40, 1], [2000, 800, 90, 1500], 8, 2, 128, dtype).cuda()
-    out, lse = call(b)
-    for _ in range(5):
-        o, z = call(b)
-        assert torch.equal(o, out) and torch.equal(z, lse)
+    for new in ([1, 3, 40, 1], [1, 3, 300, 1]):
+        b = Batch4(new, [2000, 800, 390, 1500], 8, 2, 128, dtype).cuda()
+        b = long_runs(b) or b
+        out, lse = call(b)
+        for _ in range(5):
+            o, z = call(b)
+            assert torch.equal(o, out) and torch.equal(z, lse)
 
 
 def test_offsets_beyond_32_bits():
@@ -339,6 +371,7 @@ def test_offsets_beyond_32_bits():
     scales = torch.zeros((n_pages, 64, 8, 4), dtype=torch.uint8, device="cuda")
     for new in ([3, 50], [150, 130]):
         d = b.cuda()
+        d.n = sum(new)
         d.new, d.q_start = new, torch.tensor([0, new[0], sum(new)], dtype=torch.int32, device="cuda")
         d.q = torch.randn((sum(new), 16, 128), device="cuda").to(BF16)
         move = torch.arange(n_pages - 2 * b.n_pages, n_pages, 2)[:b.n_pages]
@@ -350,6 +383,10 @@ def test_offsets_beyond_32_bits():
         d.k_codes, d.k_scales, d.v_codes, d.v_scales = far
         out, lse = call(d)
         assert torch.equal(out, ref) and torch.equal(lse, rl)
+        d.pages = torch.cat([d.pages, torch.full((2, 5000), -1, dtype=torch.int32, device="cuda")], 1)      # the kernel for long runs, where these are
+        tol, ltol = limits(b, ref.cpu().double(), rl.cpu().double(), torch.full(ref.shape, 5.0), torch.full(rl.shape, 40.0))
+        out, lse = call(d)
+        assert ((out - ref).cpu().double().abs() <= 2 * tol).all() and ((lse - rl).cpu().double().abs() <= 2 * ltol).all()
 
 
 def test_streams_replays_and_growing_lengths():
@@ -361,7 +398,7 @@ def test_streams_replays_and_growing_lengths():
             if int(b.pages[s, i]) < 0 and free:
                 b.pages[s, i] = free.pop()
     c = Batch4([20, 30], [900, 30], 8, 2, 128, BF16, seed=5).cuda()
-    e = Batch4([200, 1, 90], [2900, 5, 700], 8, 2, 128, F16, extra_pages=8).cuda()
+    e = Batch4([200, 1, 90], [2900, 5, 700], 8, 2, 128, F16, extra_pages=600).cuda()
     for s in range(3):
         e.pages[s] = torch.randint(0, e.n_pages, (e.pages.shape[1],), dtype=torch.int32)
     side = torch.cuda.Stream()
@@ -392,6 +429,7 @@ def test_scratch_memory_of_the_callers():
     """What lies in it does not matter, and no byte behind it is touched."""
     for dtype, new, kv in ((BF16, [1, 2], [3000, 700]), (F16, [200, 90], [2500, 700]), (F32, [4, 1], [900, 2000])):
         b = Batch4(new, kv, 8, 2, 128, dtype).cuda()
+        b = long_runs(b) or b
         ref, rl = call(b)
         sizes = binding._paged_args_fp4(*b.pool(), b.pages, b.q_start, b.kv_len, dtype, b.n)[2]
         need = binding._attention_fp4_workspace(sizes, 8)
@@ -412,6 +450,42 @@ def test_rows_that_are_no_runs(starts, dtype, kv):
     b, seqs = Batch4([30], [kv], 16, 2, 64, dtype, spare=5).cuda(), len(starts) - 1
     start, kv_len = torch.tensor(starts, dtype=torch.int32, device="cuda"), torch.full((seqs,), kv, dtype=torch.int32, device="cuda")
     outs = torch.full((40, 16, 64), 5.0, device="cuda").to(dtype)
-    binding.ppd_paged_attention_fp4(b.q, *b.pool(), b.pages.repeat(seqs, 1).contiguous(), start, kv_len, out=outs[5:-5])
-    torch.cuda.synchronize()
-    assert (outs[:5] == 5.0).all() and (outs[-5:] == 5.0).all()
+    for wide in (0, 3000):                                                     # (in a wide table the three sequences are long runs)
+        pages = torch.cat([b.pages, torch.full((1, wide), -1, dtype=torch.int32, device="cuda")], 1).repeat(seqs, 1).contiguous()
+        binding.ppd_paged_attention_fp4(b.q, *b.pool(), pages, start, kv_len, out=outs[5:-5])
+        torch.cuda.synchronize()
+        assert (outs[:5] == 5.0).all() and (outs[-5:] == 5.0).all()
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,hd,new", [(BF16, 32, 8, 128, 1), (F32, 8, 4, 64, 2), (F16, 12, 12, 64, 1), (BF16, 80, 16, 128, 3)])
+@pytest.mark.parametrize("page,window", [(16, 0), (20, 0), (16, 9000)])
+def test_more_than_the_caches_hold(dtype, heads, kv_heads, hd, new, page, window):
+    """Lengths of more than 320 MB together, which four heads a workgroup read; each sequence by itself, read by one head a workgroup, gives the same but
+    for the order of sums.  (The sequences share pages.)"""
+    rng = np.random.default_rng(heads)
+    kv = rng.integers(8000, 17000, int(330e6 / (12500 * kv_heads * 2 * 17 * hd / 32)) + 2)
+    kv[1], kv[2] = 30, 0
+    if window:
+        kv = np.concatenate([kv, kv])
+    n_pages, seqs = 300, len(kv)
+    g = torch.Generator(device="cuda").manual_seed(heads)
+    pool = []
+    for _ in range(2):
+        pool.append(torch.randint(0, 256, (n_pages, page, kv_heads, hd // 2), generator=g, device="cuda", dtype=torch.uint8))
+        pool.append(torch.randint(122, 128, (n_pages, page, kv_heads, hd // 32), generator=g, device="cuda", dtype=torch.uint8))
+    pool[3][7, 3, 1, 0] = 255                                                  # NaN where many see it
+    pages = torch.randint(0, n_pages, (seqs, -(-int(kv.max()) // page)), generator=g, device="cuda", dtype=torch.int32)
+    pages[0, 5] = -1
+    q = torch.randn((seqs * new, heads, hd), generator=g, device="cuda").to(dtype)
+    q_start = (torch.arange(seqs + 1, device="cuda") * new).int()
+    kv_len = torch.from_numpy(kv).int().cuda()
+    out, lse = binding.ppd_paged_attention_fp4(q, *pool, pages, q_start, kv_len, window=window, want_lse=True)
+    for s in range(seqs):
+        r = slice(s * new, s * new + new)
+        o, z = binding.ppd_paged_attention_fp4(q[r], *pool, pages[s:s + 1], q_start[:2], kv_len[s:s + 1], window=window, want_lse=True)
+        torch.cuda.synchronize()
+        # both as far off as a score of at most 6 * 3 * hd * 2^0 / sqrt(hd) may be, see limits; values are at most 6
+        w = ((QUERY_TERMS[dtype] * hd + 8) * 18 * hd ** 0.5 + WEIGHT_TERMS[dtype] * int(kv[s]) + 16) * 2.0 ** -24
+        tol = 2 * (6 * (2 * w + 2.0 ** (-9 * WEIGHT_TERMS[dtype])) + 6 * HALF_STEP[dtype])
+        assert torch.equal(o.isnan(), out[r].isnan()) and torch.equal(torch.isinf(z), torch.isinf(lse[r]))
+        assert ((o - out[r]).float().abs().nan_to_num() <= tol).all() and ((z - lse[r]).abs().nan_to_num() <= 2 * (w + 40 * 2.0 ** -23)).all()

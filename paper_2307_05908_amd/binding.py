@@ -503,22 +503,36 @@ def ppd_paged_plan(pages, free_pages, counters, held, wanted, page_size, n_rows,
             raise ValueError("held, wanted, kept: int32 [n_seqs]")
     if counters.dtype is not i64 or counters.numel() != 2:
         raise ValueError("counters: int64 [2]")
-    made = []
-    for t, size, dtype, make, name in ((q_start, n + 1, i32, True, "q_start"), (kv_len, n, i32, True, "kv_len"), (granted, n, i32, True, "granted"),
-                                       (counters_out, 2, i64, True, "counters_out"), (row_seq, n_rows, i32, want_rows, "row_seq"),
-                                       (positions, n_rows, i32, want_rows, "positions"), (slots, n_rows, i64, want_rows, "slots")):
-        if t is None and make:
-            t = torch.empty(size, dtype=dtype, device=pages.device)
-        elif t is not None and (t.dtype is not dtype or t.numel() != size):
-            raise ValueError(f"{name}: {dtype}, {size} numbers")
-        made.append(t)
-    if not all(t is None or t.is_contiguous() for t in (free_pages, counters, held, wanted, kept, *made)):
+    if not any(t is not None for t in given):               # (two allocations for all of them)
+        sizes32, sizes64 = ((n + 1, n, n, n_rows, n_rows), (2, n_rows)) if want_rows else ((n + 1, n, n), (2,))
+        made32 = torch.empty(sum(sizes32), dtype=i32, device=pages.device).split_with_sizes(sizes32)
+        made64 = torch.empty(sum(sizes64), dtype=i64, device=pages.device).split_with_sizes(sizes64)
+        made = (*made32[:3], made64[0], *made32[3:], made64[1]) if want_rows else (*made32, made64[0], None, None, None)
+    else:
+        made = []
+        for t, size, dtype, make, name in ((q_start, n + 1, i32, True, "q_start"), (kv_len, n, i32, True, "kv_len"), (granted, n, i32, True, "granted"),
+                                           (counters_out, 2, i64, True, "counters_out"), (row_seq, n_rows, i32, want_rows, "row_seq"),
+                                           (positions, n_rows, i32, want_rows, "positions"), (slots, n_rows, i64, want_rows, "slots")):
+            if t is None and make:
+                t = torch.empty(size, dtype=dtype, device=pages.device)
+            elif t is not None and (t.dtype is not dtype or t.numel() != size or not t.is_contiguous()):
+                raise ValueError(f"{name}: {dtype}, {size} numbers in a row")
+            made.append(t)
+    if not (free_pages.is_contiguous() and counters.is_contiguous() and held.is_contiguous() and wanted.is_contiguous() and (kept is None or kept.is_contiguous())):
         raise ValueError("all but pages must be contiguous")
     rc = plan(_PACK_TABLE(pages.data_ptr(), pages.stride(0), free_pages.data_ptr(), table[1], free_pages.numel(), page_size, n), counters.data_ptr(), _ptr(made[3]),
               held.data_ptr(), _ptr(kept), wanted.data_ptr(), n_rows, _ptr(made[0]), _ptr(made[1]), _ptr(made[2]), *(_ptr(t) for t in made[4:]), raw_stream(dev))
     if rc != 0:
         raise PPDError(rc, "ppd_paged_plan", load_library().ppd_last_hip_error(None))
     return Plan(*made)
+
+
+def _rows_made(out, like, dtype, head_dim, what, n_tokens, heads):
+    """`out`, made here as one piece if not given, and its rows as bytes."""
+    if out is None:
+        out = _layers()[0].empty_like(like, memory_format=_layers()[0].contiguous_format)
+        return out, _PACK_ROWS(out.data_ptr(), heads * head_dim, head_dim)
+    return out, _rows(out, dtype, head_dim, what, n_tokens, heads)[0]
 
 
 def _paged_args_fp4(k_codes, k_scales, v_codes, v_scales, pages, q_start, kv_len, dtype, n_tokens):
@@ -564,16 +578,12 @@ def ppd_paged_append_fp4(k_codes, k_scales, v_codes, v_scales, pages, q_start, k
     qr, outr, heads = None, None, 0
     if q is not None:
         qr, heads = _rows(q, dtype, head_dim, "q", n)
-        if q_out is None:
-            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        outr = _rows(q_out, dtype, head_dim, "q_out", n, heads)[0]
-    if want_values:
-        if k_out is None:
-            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
-        if v_out is None:
-            v_out = torch.empty_like(v, memory_format=torch.contiguous_format)
-    kor = None if k_out is None else _rows(k_out, dtype, head_dim, "k_out", n, kv_heads)[0]
-    vor = None if v_out is None else _rows(v_out, dtype, head_dim, "v_out", n, kv_heads)[0]
+        q_out, outr = _rows_made(q_out, q, dtype, head_dim, "q_out", n, heads)
+    kor = vor = None
+    if want_values or k_out is not None:
+        k_out, kor = _rows_made(k_out, k, dtype, head_dim, "k_out", n, kv_heads)
+    if want_values or v_out is not None:
+        v_out, vor = _rows_made(v_out, v, dtype, head_dim, "v_out", n, kv_heads)
     for g in (q_gain, k_gain):
         if g is not None and (g.dtype is not dtype or g.numel() != head_dim or not g.is_contiguous()):
             raise ValueError("gains: [head_dim] of the rows' type")
@@ -607,9 +617,7 @@ def ppd_paged_attention_fp4(q, k_codes, k_scales, v_codes, v_scales, pages, q_st
     cache, batch, sizes = _paged_args_fp4(k_codes, k_scales, v_codes, v_scales, pages, q_start, kv_len, dtype, n)
     head_dim = sizes[3]
     qr, heads = _rows(q, dtype, head_dim, "q", n)
-    if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    outr = _rows(out, dtype, head_dim, "out", n, heads)[0]
+    out, outr = _rows_made(out, q, dtype, head_dim, "out", n, heads)
     lse = torch.empty((n, heads), dtype=torch.float32, device=q.device) if want_lse else None
     if workspace is None:
         need = _attention_fp4_workspace(sizes, heads)

@@ -17,7 +17,7 @@ PROBE_PATH = os.path.join(HERE, "ppd_pmc_probe")
 N_INST = 8
 DEPS = [os.path.join(CSRC, f) for f in ("ppd_engine.hip", "ppd_ops.hip", "ppd_pmc_probe.cpp", "ppd_prefill.hip", "ppd_prefill.h", "ppd_fused.hip", "ppd_fused.h", "ppd_inst.hip", "ppd_kernels.h", "ppd_launch.h",
                                          "ppd_layers_common.h", "ppd_append.hip", "ppd_paged_attn.h", "ppd_paged_attn.hip", "ppd_paged_tiles.hip", "ppd_verify.hip",
-                                         "ppd_plan.hip", "ppd_paged_fp4.h", "ppd_append_fp4.hip", "ppd_paged_attn_fp4.h", "ppd_paged_attn_fp4.hip", "ppd_paged_tiles_fp4.hip", "ppd_adjust.hip")] + \
+                                         "ppd_plan.hip", "ppd_divide.h", "ppd_paged_fp4.h", "ppd_append_fp4.hip", "ppd_paged_attn_fp4.h", "ppd_paged_attn_fp4.hip", "ppd_paged_tiles_fp4.hip", "ppd_adjust.hip")] + \
        [os.path.join(os.path.dirname(HERE), "include", f) for f in ("ppd.h", "ppd_measure.h", "ppd_layers.h")]
 # -ffp-contract=off: every fused multiply-add in the kernels is an explicit fmaf, so a row's arithmetic
 # does not depend on which template instance it runs in.  Packed-fp32 code generation is switched off.

@@ -1,6 +1,7 @@
 // ppd_paged_plan: a step's row starts, lengths, pages and slots, from what each sequence keeps and wants.  Bound by latencies: one workgroup
 // reads the lengths, sums them up (sequences in their order, so that results do not depend on when a wave runs) and moves the pages' numbers;
 // the places of many rows are found by a launch of their own.
+#include "ppd_divide.h"
 #include "ppd_layers_common.h"
 
 using namespace ppd;
@@ -15,16 +16,9 @@ struct PlanArgs {
   int64_t pages_stride;
   int max_pages, n_pages, page_size, n_seqs, n_rows;
   bool rows_here;           // rows' places by plan_kernel
-  uint32_t by_size, shift;  // x / page_size = (2 x * by_size) >> (32 + shift) for x below 2^31, see divider
+  Divider by_size;          // (by page_size)
 };
-// For x below 2^31 and 2^(s - 1) < size <= 2^s, m = floor(2^(31 + s) / size) + 1: m size is above 2^(31 + s) by at most size <= 2^s, so that x m / 2^(31 + s) is
-// above x / size by at most x / (size 2^31), less than what parts x / size from the next whole number.
-inline void divider(PlanArgs& a) {
-  a.shift = 0;
-  while ((1u << a.shift) < (uint32_t)a.page_size) ++a.shift;
-  a.by_size = (uint32_t)((((uint64_t)1 << (31 + a.shift)) / (uint32_t)a.page_size) + 1);
-}
-__device__ __forceinline__ int pages_of(const PlanArgs& a, int positions) { return (int)(__umulhi(2u * ((uint32_t)positions + (uint32_t)a.page_size - 1u), a.by_size) >> a.shift); }
+__device__ __forceinline__ int pages_of(const PlanArgs& a, int positions) { return (int)a.by_size((uint32_t)positions + (uint32_t)a.page_size - 1u); }
 
 template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t dpp_plus(uint32_t v) { return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false); }
 __device__ __forceinline__ uint32_t wave_upto(uint32_t v) {      // sums up to the lane's
@@ -76,7 +70,7 @@ __device__ __forceinline__ void place_row(const PlanArgs& a, int row, int s, int
   if (!a.slots) return;
   int64_t slot = -1;
   if (s >= 0) {
-    const int i = (int)(__umulhi(2u * (uint32_t)pos, a.by_size) >> a.shift), page = a.pages[(int64_t)s * a.pages_stride + i];
+    const int i = (int)a.by_size((uint32_t)pos), page = a.pages[(int64_t)s * a.pages_stride + i];
     if ((unsigned)page < (unsigned)a.n_pages) slot = (int64_t)page * a.page_size + (pos - i * a.page_size);
   }
   a.slots[row] = slot;
@@ -258,8 +252,7 @@ extern "C" int ppd_paged_plan(const ppd_page_table* table, const int64_t* counte
   if (table->n_seqs > PPD_MAX_SEQS || n_rows > PPD_MAX_TOKENS || (int64_t)table->max_pages * table->page_size > 1 << 30) return PPD_ELIMIT;
   if ((int64_t)table->n_seqs * table->max_pages > 1 << 30) return PPD_ELIMIT;
   PlanArgs a = {counters, counters_out, held, kept, wanted, q_start, kv_len, granted, row_seq, positions, slots, table->pages, table->free_pages,
-                table->pages_stride, table->max_pages, table->n_pages, table->page_size, table->n_seqs, n_rows, false, 0, 0};
-  divider(a);
+                table->pages_stride, table->max_pages, table->n_pages, table->page_size, table->n_seqs, n_rows, false, Divider((uint32_t)table->page_size)};
   const bool rows = n_rows > 0 && (row_seq || positions || slots);
   a.rows_here = rows && n_rows <= 4096;
   hipStream_t st = (hipStream_t)hip_stream;

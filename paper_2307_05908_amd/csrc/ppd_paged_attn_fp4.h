@@ -21,7 +21,7 @@ template <> struct Terms<bf16_t> { static constexpr int Q = 1, W = 2; };
 template <> struct Terms<f16_t> { static constexpr int Q = 2, W = 2; };
 template <> struct Terms<float> { static constexpr int Q = 3, W = 3; };
 
-// eight numbers of a query as bf16 terms
+// eight numbers of a query as bf16 terms, each cut off, not rounded (so that the largest numbers stay finite): eight bits of the significand a term
 __device__ __forceinline__ void query_terms(const bf16_t* p, float, u32x4 (&t)[1]) { t[0] = *(const u32x4*)p; }
 template <typename T, int N>
 __device__ __forceinline__ void query_terms(const T* p, float factor, u32x4 (&t)[N]) {
@@ -34,10 +34,10 @@ __device__ __forceinline__ void query_terms(const T* p, float factor, u32x4 (&t)
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int e = 0; e < 4; e += 2) {
-        float a = x[h][e], b = x[h][e + 1];
-        const uint32_t w = pair(a, b, bf16_t());
-        rest(w, a, b, bf16_t());
-        t[n][2 * h + e / 2] = w; x[h][e] = a; x[h][e + 1] = b;
+        const uint32_t a = __float_as_uint(x[h][e]), b = __float_as_uint(x[h][e + 1]);
+        t[n][2 * h + e / 2] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        x[h][e] -= __uint_as_float(a & 0xffff0000u);
+        x[h][e + 1] -= __uint_as_float(b & 0xffff0000u);
       }
 }
 

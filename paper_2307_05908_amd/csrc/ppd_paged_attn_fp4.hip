@@ -296,7 +296,8 @@ int check_attention(const ppd_paged_cache_fp4* cache, const ppd_paged_batch* bat
   p->wide_want = !p->tiles && p->least && cache->n_kv_heads % SPLIT_WAVES == 0 && (float)tiles * (float)((capacity + PLAN_BLOCK - 1) / PLAN_BLOCK) >= p->wide_from
                      ? (2048 + cache->n_kv_heads - 1) / cache->n_kv_heads : 0;
   p->items = tiles + (p->least ? (p->fine > p->wide_want ? p->fine : p->wide_want) + 1 : 0);
-  if (p->items * cache->n_kv_heads >= (int64_t)1 << 24) return PPD_ELIMIT;      // (a launch has fewer than 2^32 threads, 256 to a workgroup)
+  // (a launch has fewer than 2^32 threads, 256 to a workgroup; workgroups are rounded up to eight rounds of up to eight heads, see attn_go)
+  if (p->items * cache->n_kv_heads >= ((int64_t)1 << 24) - 64) return PPD_ELIMIT;
   const uint64_t places = p->least ? (uint64_t)p->items * cache->n_kv_heads : 0;
   p->o_bytes = places * tile_rows * cache->head_dim * 4;
   p->ml_bytes = places * tile_rows * 8;

@@ -271,6 +271,16 @@ def test_values_that_are_nan(dtype, hd, new, kv):
             assert o[hit].isnan().all() and ((o - ref[0]).abs() <= tol)[~hit].all() and ((lse.cpu().double() - ref[1]).abs() <= ltol).all()
 
 
+@pytest.mark.parametrize("new,kv", [([1, 4, 2], [200, 130, 64]), ([150, 90], [200, 90])])
+def test_the_largest_queries(new, kv):
+    """Components next to fp32's largest number, above bf16's: their terms are finite."""
+    b = Batch4(new, kv, 4, 2, 64, F32)
+    b.k_scales[:] = 127 - 125
+    b.renew()
+    b.q[..., 5] = torch.where(b.q[..., 5] > 0, 3.4028e38, -3.4025e38)
+    check(b, scale=float(np.float32(math.log(2.0))))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_wide_ranges_of_scales(dtype):
     """Blocks of 2^-20 to 2^6 beside each other, as keys and as values."""

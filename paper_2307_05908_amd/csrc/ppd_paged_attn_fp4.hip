@@ -193,7 +193,8 @@ __global__ __launch_bounds__(SPLIT_THREADS, sizeof(T) == 4 ? 2 : 3) void paged_s
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 4; e += 2) {
-          const uint32_t p = pair(s[t][e], s[t][e + 1], bf16_t());
+          uint32_t p = pair(s[t][e], s[t][e + 1], bf16_t());
+          asm("" : "+v"(p));                              // (or each pair is rounded twice, once for what is taken off)
           w[n][2 * t + e / 2] = p;
           if (n + 1 < NW) { float x = s[t][e], y = s[t][e + 1]; rest(p, x, y, bf16_t()); s[t][e] = x; s[t][e + 1] = y; }
         }

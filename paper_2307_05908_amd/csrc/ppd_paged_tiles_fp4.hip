@@ -167,6 +167,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_fp4_kernel(Fp4AttnArgs a) {
       for (int e = 0; e < 4; ++e) {
         float x = s[t / 2][8 * (t % 2) + 2 * e], y = s[t / 2][8 * (t % 2) + 2 * e + 1];
         hi[e] = pair(x, y, bf16_t());
+        asm("" : "+v"(hi[e]));                             // (or each pair is rounded twice, once for what is taken off)
         rest(hi[e], x, y, bf16_t());
         lo[e] = pair(x, y, bf16_t());
       }

@@ -89,7 +89,9 @@ EXPORTS = ("ppd_create", "ppd_reset", "ppd_prefill", "ppd_step", "plain_greedy_s
            "ppd_time_ffn_in", "ppd_get_chain_rounds", "ppd_set_chain_wait", "ppd_stream_read_probe", "ppd_early_topk", "ppd_early_topk_noalloc", "ppd_destroy",
            "ppd_strerror", "ppd_last_hip_error",
            "ppd_paged_append", "ppd_paged_attention", "ppd_paged_attention_workspace", "ppd_verify_drafts", "ppd_verify_drafts_workspace",
-           "ppd_paged_plan", "ppd_paged_append_fp4", "ppd_paged_attention_fp4", "ppd_paged_attention_fp4_workspace", "ppd_adjust_logits")
+           "ppd_paged_plan", "ppd_adjust_logits")
+# (those with a digit in their names)
+FP4_EXPORTS = ("ppd_paged_append_fp4", "ppd_paged_attention_fp4", "ppd_paged_attention_fp4_workspace")
 
 _lib = None
 

@@ -1,5 +1,7 @@
 """What the operators around a step refuse, on the CPU: nothing is queued, nothing dereferenced."""
 import ctypes
+import os
+import re
 
 import pytest
 import torch
@@ -27,6 +29,15 @@ def attention(c=None, b=None, heads=16, q=None, out=None, lse=None, scale=0.125,
 def append(c=None, b=None, heads=16, q=None, q_out=None, k=None, v=None, k_out=None, v_out=None, qg=None, kg=None, eps=1e-5, rotary=64, theta=1e4):
     return binding.load_library().ppd_paged_append_fp4(c or cache(), b or batch(), heads, q or rows(), q_out or rows(p=1 << 20), k or rows(token=512), v or rows(token=512),
                                                        k_out, v_out, qg, kg, eps, rotary, theta, None)
+
+
+def test_declared_names_are_exported():
+    """All of them, with digits in their names or without."""
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "ppd_layers.h")).read()
+    names = set(re.findall(r"\b(ppd_\w+)\s*\(", re.sub(r"/\*.*?\*/", "", text, flags=re.S)))
+    assert {n for n in names if re.search(r"\d", n)} == set(binding.FP4_EXPORTS) and names <= {*binding.EXPORTS, *binding.FP4_EXPORTS}
+    for n in names:
+        assert getattr(binding.load_library(), n) is not None
 
 
 @pytest.mark.parametrize("kw", BAD_CACHE)

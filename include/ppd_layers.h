@@ -179,7 +179,8 @@ int ppd_paged_plan(const ppd_page_table *table, const int64_t *counters, int64_t
  * code is its sign, the others stand for 0, 0.5, 1, 1.5, 2, 3, 4, 6, and scale b multiplies by 2^(b - 127) (from 253 on: the 32
  * numbers are NaN).  k, v: [n_pages][page_size][n_kv_heads][head_dim / 2],
  * k_scales, v_scales: [n_pages][page_size][n_kv_heads][head_dim / 32], each in any order of the first three that its
- * strides (in BYTES) express, the last contiguous; strides of 0: for ppd_paged_attention_fp4 only.  Rows of codes begin at
+ * strides (in BYTES) express, the last contiguous (a head's positions side by side are read fastest); strides of 0: for
+ * ppd_paged_attention_fp4 only.  Rows of codes begin at
  * multiples of 16 bytes, rows of scales at multiples of head_dim / 32 (so do the tensors, and so do all strides). */
 typedef struct {
   void *k, *v, *k_scales, *v_scales;
@@ -208,7 +209,7 @@ int ppd_paged_append_fp4(const ppd_paged_cache_fp4 *cache, const ppd_paged_batch
 
 /* ppd_paged_attention over such pages: the same arguments, rules and limits.  Keys and values are taken as bf16 numbers,
  * which they are without rounding; queries of fp16 and fp32, and softmax weights, go into their products as two or three bf16 terms, so
- * that as there the result's own rounding is what counts (fp32: of 24 bits). */
+ * that as there the result's own rounding is what counts (fp32: of 24 bits).  Queries are finite numbers. */
 int ppd_paged_attention_fp4(const ppd_paged_cache_fp4 *cache, const ppd_paged_batch *batch, int n_heads, const ppd_rows *q,
                             const ppd_rows *out, float *lse, float scale, int window, void *workspace,
                             uint64_t workspace_bytes, void *hip_stream);

@@ -3,6 +3,7 @@
 // 4915 bf16 tokens of 40 + 2 * 40 heads, 329 MB, take 93 us, 3.5 TB/s (a copy 67); with the keys' scales and codes from 32 bits it were 79, but a key next to a border
 // would have a code that depends on the order of operations.  Bounds in 32 bits first, and 64 bits only where these leave it open, were no faster (94), and
 // no exchange between lanes or other order of the angles in LDS was either.
+#include "ppd_divide.h"
 #include "ppd_paged_fp4.h"
 
 #include <math.h>
@@ -20,11 +21,16 @@ struct AppendArgs {
   const void *q_gain, *k_gain;
   int heads, kv_heads, rotary;
   float eps;
+  int toks;              // tokens of a workgroup
+  Divider by_heads, by_kv_heads;
   double turns[64];      // angle of pair i per position, in whole turns
 };
 
 // Four sets of heads' rows a workgroup from this many sets on, see ppd_append.hip (4915 tokens of 8 sets: 93 us, one set a workgroup 112, two 96, eight 92).
 constexpr int MANY = 2048;
+// Of these, several tokens a workgroup, two sets together, where a token's rows fill no more than one (bf16, head_dim 128, us of one token / several: 35291 tokens of 2 + 2 * 1
+// heads 107 / 38, 2400 of 8 + 2 * 1 13.5 / 9.7, 16913 of 2 + 2 * 2 56 / 30, 7331 of 8 + 2 * 2 29 / 24; with rows for more than one set, 16 + 2 * 4, in four sets, 39 / 41).
+constexpr int TOKENS = 8;      // of a workgroup at most (16 were no faster)
 
 // sin and cos of 2 pi t in 64 bits: the nearest quarter turn taken off, the rest (at most pi / 4) by the Taylor series, whose next terms are
 // below 2^-53.
@@ -59,14 +65,15 @@ __device__ __forceinline__ float odd_f32(double d) {
 
 // A row of head_dim elements is HD / 8 lanes' work: lane l has elements 8 l .. 8 l + 7, an eighth of the row's code words and a quarter of a
 // block of 32, and brings the elements that its own are turned with, too, so that nothing crosses lanes but the norm's sum and a block's largest
-// magnitude.  A workgroup has one token and ITERS times 16 (32) of its heads' rows, all under way while the token's sequence, page and angles
-// are found.
-template <typename T, int HD, int ITERS>
+// magnitude.  A workgroup has one token and ITERS times 16 (32) of its heads' rows, or (SEVERAL) that many rows of a few tokens, all under way
+// while the tokens' sequences, pages and angles are found.
+template <typename T, int HD, int ITERS, bool SEVERAL>
 __global__ __launch_bounds__(256) void append_fp4_kernel(AppendArgs a) {
   typedef typename Quad<T>::raw raw;
-  constexpr int LPR = HD / 8, RPW = WAVE / LPR;
-  __shared__ double2 angles[HD / 2];
-  const int tok = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int LPR = HD / 8, RPW = WAVE / LPR, TOKS = SEVERAL ? TOKENS : 1;
+  __shared__ double2 angles[TOKS][HD / 2];
+  __shared__ int s_pos[TOKS], s_page[TOKS], s_slot[TOKS];      // (s_slot -1: a row of no sequence)
+  const int tok0 = SEVERAL ? blockIdx.x * a.toks : blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l = lane % LPR, half = a.rotary / 2;
   int own[2], other[2], angle[2];
 #pragma unroll
@@ -76,11 +83,25 @@ __global__ __launch_bounds__(256) void append_fp4_kernel(AppendArgs a) {
     angle[h] = e < half ? e : e - half;
     other[h] = e < half ? e + half : e < a.rotary ? e - half : e;
   }
-  const int rows = a.heads + 2 * a.kv_heads, first = blockIdx.y * ITERS * 4 * RPW + wave * RPW + lane / LPR;
+  const int rows = a.heads + 2 * a.kv_heads, first = (SEVERAL ? 0 : blockIdx.y * ITERS * 4 * RPW) + wave * RPW + lane / LPR;
+  const int toks = SEVERAL ? min(a.toks, a.b.n_tokens - tok0) : 1, all = toks * rows;
+  // number i of the workgroup's rows: its token, and its number r of the token's.  Of several tokens the queries come first, then the keys, and the values: a wave has
+  // rows of one kind, mostly (token by token, as one token's are, 54 us, not 44, for the first of TOKENS' sizes in four sets).
+  auto row_of = [&](int i, int& t, int& r) {
+    t = 0; r = i;
+    if constexpr (SEVERAL) {
+      const int k = i - toks * a.heads, v = k - toks * a.kv_heads;
+      t = (int)(k < 0 ? a.by_heads((uint32_t)i) : a.by_kv_heads((uint32_t)(v < 0 ? k : v)));
+      r = k < 0 ? i - t * a.heads : v < 0 ? a.heads + k - t * a.kv_heads : a.heads + a.kv_heads + v - t * a.kv_heads;
+    }
+  };
   raw ra[ITERS][2], rb[ITERS][2], gains[2][4] = {};
 #pragma unroll
   for (int it = 0; it < ITERS; ++it) {
-    const int r = first + it * 4 * RPW;
+    int t, r;
+    const int i = first + it * 4 * RPW;
+    row_of(i, t, r);
+    const int tok = tok0 + t;
     const bool turned = r < a.heads + a.kv_heads && half > 0;
     const T* const src = r < a.heads ? (const T*)a.q + tok * a.q_tok + r * a.q_head
                        : r < a.heads + a.kv_heads ? (const T*)a.k + tok * a.k_tok + (r - a.heads) * a.k_head
@@ -88,8 +109,8 @@ __global__ __launch_bounds__(256) void append_fp4_kernel(AppendArgs a) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       ra[it][h] = {}; rb[it][h] = {};
-      if (r < rows) ra[it][h] = *(const raw*)(src + own[h]);
-      if (r < rows && turned) rb[it][h] = *(const raw*)(src + other[h]);
+      if (i < all) ra[it][h] = *(const raw*)(src + own[h]);
+      if (i < all && turned) rb[it][h] = *(const raw*)(src + other[h]);
     }
   }
 #pragma unroll
@@ -99,19 +120,47 @@ __global__ __launch_bounds__(256) void append_fp4_kernel(AppendArgs a) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) { gains[g][h] = *(const raw*)(gain + own[h]); gains[g][2 + h] = *(const raw*)(gain + other[h]); }
   }
-  const int s = seq_of_row(a.b, tok, lane);
-  if (s < 0) return;                                       // (all of the workgroup)
-  const SeqRows sr = seq_rows(a.b, s);
-  const int pos = sr.pos0 + (tok - sr.row0), page = page_of(a.b, s, pos);
-  const int slot = page < 0 ? 0 : (int)((unsigned)pos % (unsigned)a.b.page_size);
-  if (half > 0) {
-    if ((int)threadIdx.x < half) angles[threadIdx.x] = sincos_turns((double)pos * a.turns[threadIdx.x]);
+  auto find = [&](int tok, int& pos, int& page, int& slot) {
+    const int s = seq_of_row(a.b, tok, lane);
+    if (s < 0) return false;
+    const SeqRows sr = seq_rows(a.b, s);
+    pos = sr.pos0 + (tok - sr.row0);
+    page = page_of(a.b, s, pos);
+    slot = page < 0 ? 0 : (int)((unsigned)pos % (unsigned)a.b.page_size);
+    return true;
+  };
+  int pos, page = -1, slot = 0;
+  if constexpr (SEVERAL) {
+    for (int t = wave; t < toks; t += 4) {
+      const bool there = find(tok0 + t, pos, page, slot);
+      if (lane == 0) { s_pos[t] = pos; s_page[t] = page; s_slot[t] = there ? slot : -1; }
+    }
     __syncthreads();
+    if (half > 0) {
+      for (int x = threadIdx.x; x < toks * (HD / 2); x += 256) {
+        const int t = x / (HD / 2), i = x % (HD / 2);
+        if (i < half && s_slot[t] >= 0) angles[t][i] = sincos_turns((double)s_pos[t] * a.turns[i]);
+      }
+      __syncthreads();
+    }
+  } else {
+    if (!find(tok0, pos, page, slot)) return;              // (all of the workgroup)
+    if (half > 0) {
+      if ((int)threadIdx.x < half) angles[0][threadIdx.x] = sincos_turns((double)pos * a.turns[threadIdx.x]);
+      __syncthreads();
+    }
   }
 #pragma unroll
   for (int it = 0; it < ITERS; ++it) {
-    const int r = first + it * 4 * RPW;
-    if (r >= rows) continue;
+    int t, r;
+    const int i = first + it * 4 * RPW;
+    row_of(i, t, r);
+    const int tok = tok0 + t;
+    if (i >= all) continue;
+    if constexpr (SEVERAL) {
+      page = s_page[t]; slot = s_slot[t];
+      if (slot < 0) continue;
+    }
     if (r < a.heads) {
       f32x4 x[2], y[2];
 #pragma unroll
@@ -138,7 +187,7 @@ __global__ __launch_bounds__(256) void append_fp4_kernel(AppendArgs a) {
         if (own[h] < a.rotary) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const double2 sc = angles[angle[h] + e];
+            const double2 sc = angles[t][angle[h] + e];
             const float sn = (float)sc.x, cs = (float)sc.y;
             x[h][e] = own[h] < half ? fmaf(x[h][e], cs, -(y[h][e] * sn)) : fmaf(x[h][e], cs, y[h][e] * sn);
           }
@@ -184,7 +233,7 @@ __global__ __launch_bounds__(256) void append_fp4_kernel(AppendArgs a) {
           const f32x4 u = Quad<T>::wide(rb[it][h]), g = Quad<T>::wide(gains[1][2 + h]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const double2 sc = angles[angle[h] + e];
+            const double2 sc = angles[t][angle[h] + e];
             const double y = a.k_gain ? u[e] * (rs * g[e]) : (double)u[e];
             d[4 * h + e] = fma(d[4 * h + e], sc.y, own[h] < half ? -(y * sc.x) : y * sc.x);
           }
@@ -230,10 +279,14 @@ __global__ __launch_bounds__(256) void append_fp4_kernel(AppendArgs a) {
 }
 
 template <typename T, int HD>
-hipError_t append_go(const AppendArgs& a, hipStream_t stream) {
-  const int rows = a.heads + 2 * a.kv_heads, per = 4 * (WAVE / (HD / 8)), sets = (rows + per - 1) / per;
-  if ((int64_t)a.b.n_tokens * sets <= MANY) hipLaunchKernelGGL((append_fp4_kernel<T, HD, 1>), dim3(a.b.n_tokens, sets), dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((append_fp4_kernel<T, HD, 4>), dim3(a.b.n_tokens, (sets + 3) / 4), dim3(256), 0, stream, a);
+hipError_t append_go(AppendArgs& a, hipStream_t stream) {
+  constexpr int PER = 4 * (WAVE / (HD / 8));               // rows of a set
+  const int rows = a.heads + 2 * a.kv_heads, sets = (rows + PER - 1) / PER;
+  a.toks = 2 * PER / rows < TOKENS ? 2 * PER / rows : TOKENS;
+  a.by_heads = Divider((uint32_t)(a.heads > 0 ? a.heads : 1)); a.by_kv_heads = Divider((uint32_t)a.kv_heads);
+  if ((int64_t)a.b.n_tokens * sets <= MANY) hipLaunchKernelGGL((append_fp4_kernel<T, HD, 1, false>), dim3(a.b.n_tokens, sets), dim3(256), 0, stream, a);
+  else if (a.toks > 1) hipLaunchKernelGGL((append_fp4_kernel<T, HD, 2, true>), dim3((a.b.n_tokens + a.toks - 1) / a.toks), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((append_fp4_kernel<T, HD, 4, false>), dim3(a.b.n_tokens, (sets + 3) / 4), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 

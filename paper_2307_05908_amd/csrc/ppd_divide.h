@@ -9,6 +9,7 @@ namespace ppd {
 // x m / 2^(31 + s) is above x / size by at most x / (size 2^31), less than what parts x / size from the next whole number.
 struct Divider {
   uint32_t by, shift;
+  Divider() : by(0), shift(0) {}
   explicit Divider(uint32_t size) : shift(0) {
     while ((1u << shift) < size) ++shift;
     by = (uint32_t)((((uint64_t)1 << (31 + shift)) / size) + 1);

@@ -98,6 +98,23 @@ def test_several_sets_of_rows_a_workgroup(dtype):
     check(Batch4([1300, 900], [1300, 1000], 3, 1, 64, dtype), (True, False), in_place=True)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("hd,heads,kv_heads", [(128, 2, 1), (128, 1, 1), (128, 4, 2), (128, 8, 4), (128, 14, 1), (64, 2, 1), (64, 12, 4), (64, 16, 8), (64, 5, 5)])
+def test_several_tokens_a_workgroup(dtype, hd, heads, kv_heads):
+    """Runs that begin and end inside a workgroup's tokens, and padded rows behind the last."""
+    check(Batch4([1200, 3, 0, 1, 1, 900, 45], [1210, 3, 4, 1, 70, 1300, 46], heads, kv_heads, hd, dtype, page=20, pad=11), (True, True), rotary=hd)
+    b = Batch4([2200, 1], [2200, 30], heads, kv_heads, hd, dtype)
+    b.pages[0, 3:60] = -1                                     # no page
+    check(b, rotary=hd // 2, keys_only=True)
+    check(b, (False, True), rotary=hd // 4, in_place=True)
+
+
+def test_several_tokens_of_many_sequences():
+    rng = np.random.default_rng(1)
+    new = rng.choice([0, 1, 3], 4096, p=[0.4, 0.3, 0.3])
+    check(Batch4(new.tolist(), (new + rng.integers(0, 20, 4096)).tolist(), 2, 1, 128, BF16, pad=2), rotary=128)
+
+
 @pytest.mark.parametrize("seqs", [64, 65, 200, 4096])
 def test_many_sequences(seqs):
     rng = np.random.default_rng(seqs)

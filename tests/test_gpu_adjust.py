@@ -211,6 +211,10 @@ def test_same_bits_every_time():
         assert torch.equal(c.call(), first)
 
 
+def test_the_largest_vocabulary():
+    Case([1, 2], 2 ** 24, BF16, biases=6, masks=2, seed=4).check()
+
+
 def test_offsets_beyond_32_bits():
     n, vocab = 70000, 33000
     z = torch.zeros((n, vocab), dtype=BF16, device="cuda")

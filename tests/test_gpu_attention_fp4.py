@@ -363,6 +363,29 @@ def test_strided_rows():
     assert torch.equal(got, ref)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("new", [[1, 1], [70, 90]])
+def test_lengths_behind_the_table(dtype, new):
+    """A row behind the table's last place sees what the table has, up to the largest length; with a window, what of it is left."""
+    b = Batch4(new, [160, 160], 4, 2, 64, dtype, page=16)
+    d = b.cuda()
+    e = long_runs(d)
+    for x in (d, e) if e is not None else (d,):
+        x.pages[:, 10:] = -1
+        room = x.pages.shape[1] * 16
+        want = []
+        for length in (room + max(new), 2 ** 31 - 1):
+            x.kv_len.fill_(length)
+            for window in (0, 2 ** 31 - 1):
+                want.append([t.clone() for t in call(x, window=window)])
+        assert not want[0][0][:b.rows].isnan().any() and torch.isfinite(want[0][1][:b.rows]).all()
+        for w in want[1:3]:
+            # (the same positions; a window that long may leave out the first of them, where lengths are largest)
+            assert all(torch.equal(x[:b.rows], y[:b.rows]) for x, y in zip(w, want[0]))
+        out, lse = call(x, window=5)
+        assert (out[:b.rows] == 0).all() and torch.isinf(lse[:b.rows]).all()
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_same_bits_every_time(dtype):
     for new in ([1, 3, 40, 1], [1, 3, 300, 1]):

@@ -168,6 +168,17 @@ def test_many_rows():
     check(pool, [0, 0, 70000, 0, 0], 70000, kept=[0] * 5)
 
 
+def test_the_largest_pages():
+    """2^30 places in a row of the table, slots beyond 32 bits."""
+    page = 2 ** 20
+    pool = Pool([2 ** 30 - 5, 3 * page, 0, 2 ** 30], page, 1024, 2000)
+    assert pool.n_pages * page > 2 ** 31
+    check(pool, [5, 4, 30000, 1], 40000, kept=None)
+    check(pool, [0, 2 ** 30 - 3 * page - 4, 2, 0], 40000)              # (more than the rows)
+    check(pool, [6, 1, 0, 2 ** 30], 40000, kept=[0, page, 30000, 0])
+    check(Pool([2 ** 30, 0], 2 ** 30, 1, 3), [1, 4], 10, kept=[2 ** 30 - 1, 0])
+
+
 def test_tables_wider_than_what_is_used():
     pool = Pool([20, 30, 40], 16, 6, 9)
     whole = torch.full((5, 50), 77, dtype=torch.int32, device="cuda")

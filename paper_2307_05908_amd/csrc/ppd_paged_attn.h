@@ -299,17 +299,17 @@ __device__ __forceinline__ f32x2 left(const void* from) {
 }
 // The waves of a workgroup joined: their results lie out_lds bytes apart, sums in rows of HD + 4 and behind them references and totals.  What comes of it
 // is the result, or a part's.  WIDE: every wave has a key/value head of its own, kvh0 and on.
-template <typename T, int HD, bool WIDE = false>
+template <typename T, int HD, bool WIDE = false, int ROWS = SPLIT_ROWS>
 __device__ __forceinline__ void join_waves(const PagedAttnArgs& a, const Item& it, int kvh0, int tid, const char* lds, int out_lds) {
   constexpr int HEADS = WIDE ? SPLIT_WAVES : 1, WAVES = SPLIT_WAVES / HEADS;
-  for (int x = tid; x < HEADS * SPLIT_ROWS * HD / 4; x += SPLIT_THREADS) {
-    const int own = x / (SPLIT_ROWS * HD / 4), kvh = kvh0 + own, rr = x / (HD / 4) % SPLIT_ROWS, d = (x % (HD / 4)) * 4, ri = it.tile * SPLIT_ROWS + rr;
+  for (int x = tid; x < HEADS * ROWS * HD / 4; x += SPLIT_THREADS) {
+    const int own = x / (ROWS * HD / 4), kvh = kvh0 + own, rr = x / (HD / 4) % ROWS, d = (x % (HD / 4)) * 4, ri = it.tile * ROWS + rr;
     if (ri >= it.n * a.group) continue;
     float2 ml[WAVES];
     float mx = -INFINITY, sum = 0.f;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) { ml[w] = ((const float2*)((const float*)(lds + (own + w) * out_lds) + SPLIT_ROWS * (HD + 4)))[rr]; mx = fmaxf(mx, ml[w].x); }
+    for (int w = 0; w < WAVES; ++w) { ml[w] = ((const float2*)((const float*)(lds + (own + w) * out_lds) + ROWS * (HD + 4)))[rr]; mx = fmaxf(mx, ml[w].x); }
     const float ref = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
@@ -320,7 +320,7 @@ __device__ __forceinline__ void join_waves(const PagedAttnArgs& a, const Item& i
       for (int e = 0; e < 4; ++e) y[e] = fmaf(f, z[e], y[e]);
     }
     if (it.parts > 1) {
-      const int64_t at = ((int64_t)it.slot * a.kv_heads + kvh) * SPLIT_ROWS + rr;
+      const int64_t at = ((int64_t)it.slot * a.kv_heads + kvh) * ROWS + rr;
       leave(a.part_o + at * HD + d, y);
       if (d == 0) leave(a.part_ml + at, mx, sum);
     } else {
@@ -340,7 +340,7 @@ __device__ __forceinline__ void join_waves(const PagedAttnArgs& a, const Item& i
 // The number goes out, past the L2, before the others are looked at, so the last one to leave it finds all; two may, and write the
 // same bits.  Scratch memory needs nothing in it beforehand (numbers are 64 bits wide and never come twice, but for a replayed
 // launch's, and that one's own places are clear again by then).
-template <typename T, int HD, bool WIDE = false>
+template <typename T, int HD, bool WIDE = false, int ROWS = SPLIT_ROWS>
 __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const Item& it, int kvh0, int tid, int* s_flag) {      // s_flag: [heads]
   constexpr int HEADS = WIDE ? SPLIT_WAVES : 1;
   const int lane = tid & 63, own = WIDE ? tid >> 6 : 0;
@@ -361,10 +361,10 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const Item& i
   for (int head = 0; head < HEADS; ++head) {
     if (!s_flag[head]) continue;
     const int kvh = kvh0 + head;
-    const int rows = min(SPLIT_ROWS, it.n * a.group - it.tile * SPLIT_ROWS);
+    const int rows = min(ROWS, it.n * a.group - it.tile * ROWS);
     for (int x = tid; x < rows * (HD / 4); x += SPLIT_THREADS) {
-      const int rr = x / (HD / 4), d = x % (HD / 4) * 4, ri = it.tile * SPLIT_ROWS + rr;
-      auto at = [&](int p) { return ((int64_t)(first + p) * a.kv_heads + kvh) * SPLIT_ROWS + rr; };
+      const int rr = x / (HD / 4), d = x % (HD / 4) * 4, ri = it.tile * ROWS + rr;
+      auto at = [&](int p) { return ((int64_t)(first + p) * a.kv_heads + kvh) * ROWS + rr; };
       float mx = -INFINITY, sum = 0.f;
       f32x4 y = {0.f, 0.f, 0.f, 0.f};
       for (int p0 = 0; p0 < it.parts; p0 += 4) {            // four parts at a time, their sums and totals in one go

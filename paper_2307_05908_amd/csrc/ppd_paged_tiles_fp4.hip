@@ -20,7 +20,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_fp4_kernel(Fp4AttnArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int kvheads = a.kv_heads, idx = blockIdx.x / kvheads, kvh = blockIdx.x % kvheads;
   Item it;
-  if (!find_item<TILE_ROWS>(a, idx, 0, idx == 0 && kvh == 0 && wave == 0 && a.least > 0, lane, it)) return;
+  if (!find_item_fp4<TILE_ROWS>(a, idx, 0, idx == 0 && kvh == 0 && wave == 0 && a.least > 0, lane, it)) return;
   const int all_rows = it.n * a.group;
   const int r0 = it.tile * TILE_ROWS + 32 * wave, r = r0 + col, rc = min(r, all_rows - 1), tok = rc / a.group, head = kvh * a.group + rc % a.group;
   const int pos = r < all_rows ? it.pos0 + tok : -1, from = first_seen(pos, a.window);

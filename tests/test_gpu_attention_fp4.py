@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from fp4_common import Batch4
+from fp4_common import NAMES, Batch4
 from paged_common import HALF_STEP, TINY, attention64
 from paper_2307_05908_amd import binding
 
@@ -45,19 +45,52 @@ def long_runs(d):
     return e
 
 
+def many_heads(d):
+    """The same batch with its heads so many times that sequences of more than 16 rows go through tiles of 32, and the number of times."""
+    group, some = d.heads // d.kv_heads, min(d.n, len(d.new))
+    rows = d.n * group
+    sixteens = -(-rows // (16 * some)) if some else 0
+    if d.dtype == F32 or sixteens < 2:
+        return None, 0
+    times = -(-(1024 if sixteens % 2 else 256) // ((rows // 32 + some) * d.kv_heads))
+    if times < 2 or times * d.heads > 1024:
+        return None, 0
+    e = object.__new__(Batch4)
+    e.__dict__ = dict(d.__dict__, heads=times * d.heads, kv_heads=times * d.kv_heads, **{n: getattr(d, n).repeat_interleave(times, 2) for n in NAMES})
+    e.q = d.q.unflatten(1, (d.kv_heads, group)).repeat_interleave(times, 1).flatten(1, 2)
+    return e, times
+
+
+def variants(d):
+    """The batch as it is and as other kernels take it, and what makes a result (of any of these) the batch's."""
+    yield d, lambda x: x
+    e = long_runs(d)
+    if e is not None:
+        yield e, lambda x: x
+    e, times = many_heads(d)
+    if e is not None:
+        def back(x):
+            y = x.unflatten(1, (d.kv_heads, times, d.heads // d.kv_heads))
+            z = y[:d.rows].nan_to_num(7.0)                   # (log sums of other rows are not written)
+            assert torch.equal(z, z[:, :, :1].expand_as(z))  # (every copy of a head, to the bit)
+            return y[:, :, 0].flatten(1, 2)
+        yield e, back
+
+
 def check(b, scale=None, window=0, d=None, ref=None):
     d = b.cuda() if d is None else d
     ref = attention64(b, scale, window) if ref is None else ref
-    e = long_runs(d)
-    if e is not None:
-        check_one(b, scale, window, e, ref)
-    return check_one(b, scale, window, d, ref)
+    for i, (e, back) in enumerate(variants(d)):
+        got = check_one(b, scale, window, e, back, ref)
+        if i == 0:
+            first = got
+    return first
 
 
-def check_one(b, scale, window, d, ref):
+def check_one(b, scale, window, d, back, ref):
     out, lse = call(d, scale=scale, window=window, out=torch.full_like(d.q, 7.0))
     torch.cuda.synchronize()
-    o, z = out.cpu().double(), lse.cpu().double()
+    o, z = back(out).cpu().double(), back(lse).cpu().double()
     ref64, lse64, size, reach = ref
     r = b.rows
     tol, ltol = limits(b, ref64, lse64, size, reach)
@@ -174,9 +207,8 @@ def test_every_position_has_its_part(dtype, hd, new):
     some = ~want.isnan().any(-1)
     assert some.sum() > 150
     d = b.cuda()
-    for e in (d, long_runs(d)):
-        if e is not None:
-            assert torch.equal(call(e, scale=1.0)[0].cpu()[:b.rows][some], want[some])
+    for e, back in variants(d):
+        assert torch.equal(back(call(e, scale=1.0)[0]).cpu()[:b.rows][some], want[some])
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -225,10 +257,8 @@ def test_what_is_not_seen_has_no_part(dtype, hd, bad, heads):
     for s, back in ((1, 1), (1, 40), (3, 1), (3, 100)):
         spoil(d, b.slot(s, b.kv[s] - back))
     first, tol, ltol = b.rows - 140 - 4 - 60, *limits(b, *ref)
-    for e in (d, long_runs(d)):
-        if e is None:
-            continue
-        out, lse = call(e)
+    for e, back in variants(d):
+        out, lse = map(back, call(e))
         for lo, hi in ((0, first + 60 - 40), (first + 60, first + 64), (first + 64, first + 64 + 40)):
             assert ((out.cpu().double() - ref[0]).abs() <= tol)[lo:hi].all()
             assert ((lse.cpu().double() - ref[1]).abs() <= ltol)[lo:hi].all()
@@ -241,10 +271,9 @@ def test_what_is_not_seen_has_no_part(dtype, hd, bad, heads):
     spoil(d, b.slot(3, 50))
     tol, ltol = limits(b, *ref)
     clean = [r for r in range(b.rows) if not (r >= 65 and 50 <= r - 65 < 70)]
-    for e in (d, long_runs(d)):
-        if e is not None:
-            out, lse = call(e, window=20)
-            assert ((out.cpu().double() - ref[0]).abs() <= tol)[clean].all() and ((lse.cpu().double() - ref[1]).abs() <= ltol)[clean].all()
+    for e, back in variants(d):
+        out, lse = map(back, call(e, window=20))
+        assert ((out.cpu().double() - ref[0]).abs() <= tol)[clean].all() and ((lse.cpu().double() - ref[1]).abs() <= ltol)[clean].all()
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -264,11 +293,10 @@ def test_values_that_are_nan(dtype, hd, new, kv):
             d.v_codes[b.slot(s, p)][h, 16 * block:16 * block + 16] = 0
             hit[row + max(0, p - (x - m)):row + m, h, 32 * block:32 * block + 32] = True
         row += m
-    for e in (d, long_runs(d)):
-        if e is not None:
-            out, lse = call(e)
-            o = out.cpu().double()
-            assert o[hit].isnan().all() and ((o - ref[0]).abs() <= tol)[~hit].all() and ((lse.cpu().double() - ref[1]).abs() <= ltol).all()
+    for e, back in variants(d):
+        out, lse = map(back, call(e))
+        o = out.cpu().double()
+        assert o[hit].isnan().all() and ((o - ref[0]).abs() <= tol)[~hit].all() and ((lse.cpu().double() - ref[1]).abs() <= ltol).all()
 
 
 @pytest.mark.parametrize("new,kv", [([1, 4, 2], [200, 130, 64]), ([150, 90], [200, 90])])
@@ -311,6 +339,50 @@ def test_many_sequences(dtype):
     new = rng.integers(0, 4, 150)
     check(Batch4(new.tolist(), (new + rng.integers(0, 120, 150)).tolist(), 4, 2, 64, dtype, pad=5))
     check(Batch4([1] * 300, rng.integers(1, 50, 300).tolist(), 2, 2, 64, dtype))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("page,window", [(16, 0), (20, 0), (16, 70)])
+@pytest.mark.parametrize("heads,kv_heads,new,ctx", [(32, 8, (5, 8), (0, 900)), (16, 16, (17, 32), (0, 300)), (24, 8, (0, 16), (0, 200)), (7, 1, (3, 20), (300, 3000)), (16, 2, (1, 8), (0, 100))])
+def test_tiles_of_32_rows(dtype, hd, page, window, heads, kv_heads, new, ctx):
+    """Drafts of sequences that share heads, and short runs."""
+    rng = np.random.default_rng(heads)
+    new = rng.integers(new[0], new[1] + 1, 13)
+    check(Batch4(new.tolist(), (new + rng.integers(ctx[0], ctx[1] + 1, 13)).tolist(), heads, kv_heads, hd, dtype, page=page, pad=3), window=window)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("seqs,heads,kv_heads,new,page", [(40, 4, 4, 16, 16), (70, 8, 8, 16, 16), (130, 16, 4, 4, 20), (261, 4, 1, 4, 16), (300, 2, 2, 1, 16), (700, 8, 2, 4, 16)])
+def test_tiles_that_are_not_cut(dtype, seqs, heads, kv_heads, new, page):
+    """Whole tiles, of sequences of one tile each and a few without any, more than a look finds."""
+    rng = np.random.default_rng(seqs)
+    n = np.where(rng.random(seqs) < 0.1, 0, new)
+    b = Batch4(n.tolist(), (n + rng.integers(0, 150, seqs)).tolist(), heads, kv_heads, 64, dtype, page=page, pad=2)
+    check(b)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("seqs", [5, 66, 130])
+def test_long_runs_that_are_not_cut(hd, seqs):
+    rng = np.random.default_rng(seqs)
+    new = np.where(rng.random(seqs) < 0.1, 0, rng.choice([17, 32, 33, 70], seqs))
+    group = 8 if seqs < 100 else 4
+    b = Batch4(new.tolist(), (new + rng.integers(0, 40, seqs)).tolist(), group, 1, hd, BF16, pad=1)
+    d = b.cuda()
+    ref = attention64(b)
+    e = object.__new__(Batch4)                             # so many heads that every tile is one part, whatever the table's width
+    times = 64
+    e.__dict__ = dict(d.__dict__, heads=times * group, kv_heads=times, **{n: getattr(d, n).repeat_interleave(times, 2) for n in NAMES})
+    e.q = d.q.repeat(1, times, 1)
+    wide = long_runs(e) or e
+    out, lse = call(wide, out=torch.full_like(e.q, 7.0))
+    tol, ltol = limits(b, *ref)
+    r = b.rows
+    o, z = out.unflatten(1, (times, group)), lse.unflatten(1, (times, group))
+    assert torch.equal(o, o[:, :1].expand_as(o)) and torch.equal(z[:r], z[:r, :1].expand_as(z[:r]))
+    assert ((o[:r, 0].cpu().double() - ref[0][:r]).abs() <= tol[:r]).all() and ((z[:r, 0].cpu().double() - ref[1][:r]).abs() <= ltol[:r]).all()
+    assert (out[r:] == 7.0).all()
 
 
 @pytest.mark.parametrize("seqs,kv_heads,most", [(65, 2, 900), (130, 2, 600), (530, 1, 400), (4096, 1, 40)])
@@ -490,7 +562,7 @@ def test_rows_that_are_no_runs(starts, dtype, kv):
         assert (outs[:5] == 5.0).all() and (outs[-5:] == 5.0).all()
 
 
-@pytest.mark.parametrize("dtype,heads,kv_heads,hd,new", [(BF16, 32, 8, 128, 1), (F32, 8, 4, 64, 2), (F16, 12, 12, 64, 1), (BF16, 80, 16, 128, 3)])
+@pytest.mark.parametrize("dtype,heads,kv_heads,hd,new", [(BF16, 32, 8, 128, 1), (F32, 8, 4, 64, 2), (F16, 12, 12, 64, 1), (BF16, 80, 16, 128, 3), (F16, 32, 8, 64, 8), (BF16, 64, 8, 128, 6)])
 @pytest.mark.parametrize("page,window", [(16, 0), (20, 0), (16, 9000)])
 def test_more_than_the_caches_hold(dtype, heads, kv_heads, hd, new, page, window):
     """Lengths of more than 320 MB together, which four heads a workgroup read; each sequence by itself, read by one head a workgroup, gives the same but

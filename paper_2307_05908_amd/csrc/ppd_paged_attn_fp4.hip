@@ -307,11 +307,14 @@ int check_attention(const ppd_paged_cache_fp4* cache, const ppd_paged_batch* bat
   // tile kernel: 64 sequences of 64 rows over 4000 positions 168 / 174, of 80 253 / 193, of 96 265 / 192; 24 over 2000 of 64 43 / 56, of 80 58 / 60, of 96 65 / 61;
   // one of 128 over 8000 27.2 / 32.5, of 256 over 500 12.7 / 19.1, over 2000 19.3 / 25.5, over 8000 42.7 / 34.8.
   p->tiles = cache->dtype != PPD_FP32 && rows > 64 * (int64_t)batch->n_seqs && (double)rows * cache->n_kv_heads * (double)capacity >= 12e6;
-  // The split kernel's tiles of 32 rows for more than 16 rows of a 16-bit type a sequence, where there are many: us of 16 / 32 rows a tile: 64 sequences of 20
-  // rows over 1000 positions 37 / 29, of 4000 120 / 77, of 8000 243 / 194, 24 over 2000 32.7 / 30.7, 8 over 2000 18.7 / 17.8, 4 over 500 11.4 / 12.9, one over 8000 18.8 / 27;
-  // of 48 rows, three tiles or two that are not full, 64 over 1000 59 / 52, 24 over 200 to 4000 26 / 31.
+  // The split kernel's tiles of 32 rows where there are many and most of them are full, as far as the host can know, or where there is more to read than the memory-side cache
+  // holds.  16-bit types, 32 / 8 heads, us of 16 / 32 rows a tile: 64 sequences of 20 rows over 4000 positions 120 / 77, over 8000 243 / 194; of 32 rows over
+  // 1000 37 / 30, 24 of them over 2000 33 / 32, 4 over 500 11.4 / 14.4, one over 8000 20 / 32; of 48 rows over 1000 47 / 52, over 400 to 32000 465 / 309; of 64 rows over 1000
+  // 60 / 53, over 4000 212 / 182.  Of 4 to 32 rows, over 100 to 4000 72 / 85, over 400 to 32000 174 to 194 / 192.
   const int64_t wide_tiles = (rows / (2 * SPLIT_ROWS) + some) * cache->n_kv_heads, sixteens = some ? (rows + SPLIT_ROWS * some - 1) / (SPLIT_ROWS * some) : 0;
-  p->tile_rows = p->tiles ? TILE_ROWS : cache->dtype != PPD_FP32 && sixteens > 1 && wide_tiles >= (sixteens % 2 ? 1024 : 256) ? 2 * SPLIT_ROWS : SPLIT_ROWS;
+  const bool full = sixteens % 2 == 0 && 2 * (rows - (sixteens - 1) * SPLIT_ROWS * some) > SPLIT_ROWS * some;
+  const bool much = (double)some * (double)capacity * cache->n_kv_heads * (cache->head_dim + cache->head_dim / 16) >= 320e6;
+  p->tile_rows = p->tiles ? TILE_ROWS : cache->dtype != PPD_FP32 && sixteens > 1 && sixteens <= 4 && wide_tiles >= 256 && (full || much) ? 2 * SPLIT_ROWS : SPLIT_ROWS;
   const int tile_rows = p->tile_rows;
   const int64_t tiles = rows / tile_rows + some;
   const int slots = p->tiles ? 512 : 256;                   // (see ppd_paged_attn.hip; 512 for few rows: one sequence of 60000 positions 30.6 us, not 28.3, 8 of 4 rows over 2000 18 / 15)

@@ -46,17 +46,20 @@ def long_runs(d):
 
 
 def many_heads(d):
-    """The same batch with its heads so many times that sequences of more than 16 rows go through tiles of 32, and the number of times."""
+    """The same batch with its heads so many times, and so wide a table, that sequences of 17 to 64 rows go through tiles of 32, and the number of times."""
     group, some = d.heads // d.kv_heads, min(d.n, len(d.new))
     rows = d.n * group
     sixteens = -(-rows // (16 * some)) if some else 0
-    if d.dtype == F32 or sixteens < 2:
+    if d.dtype == F32 or sixteens not in (2, 3, 4):
         return None, 0
-    times = -(-(1024 if sixteens % 2 else 256) // ((rows // 32 + some) * d.kv_heads))
-    if times < 2 or times * d.heads > 1024:
+    times = max(1, -(-256 // ((rows // 32 + some) * d.kv_heads)))
+    if times * d.heads > 1024:
         return None, 0
+    # so wide a table (of no pages) that there may be more to read than caches hold
+    most = max(d.pages.shape[1], int(321e6 / (some * d.page * times * d.kv_heads * d.hd * 17 / 16)) + 1)
+    pages = torch.cat([d.pages, torch.full((d.pages.shape[0], most - d.pages.shape[1]), -1, dtype=torch.int32, device=d.pages.device)], 1)
     e = object.__new__(Batch4)
-    e.__dict__ = dict(d.__dict__, heads=times * d.heads, kv_heads=times * d.kv_heads, **{n: getattr(d, n).repeat_interleave(times, 2) for n in NAMES})
+    e.__dict__ = dict(d.__dict__, pages=pages, heads=times * d.heads, kv_heads=times * d.kv_heads, **{n: getattr(d, n).repeat_interleave(times, 2) for n in NAMES})
     e.q = d.q.unflatten(1, (d.kv_heads, group)).repeat_interleave(times, 1).flatten(1, 2)
     return e, times
 
@@ -353,7 +356,7 @@ def test_tiles_of_32_rows(dtype, hd, page, window, heads, kv_heads, new, ctx):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("seqs,heads,kv_heads,new,page", [(40, 4, 4, 16, 16), (70, 8, 8, 16, 16), (130, 16, 4, 4, 20), (261, 4, 1, 4, 16), (300, 2, 2, 1, 16), (700, 8, 2, 4, 16)])
+@pytest.mark.parametrize("seqs,heads,kv_heads,new,page", [(40, 4, 4, 16, 16), (70, 8, 8, 16, 16), (130, 16, 4, 4, 20), (40, 64, 32, 16, 16), (70, 32, 16, 16, 20), (261, 4, 1, 4, 16), (300, 2, 2, 1, 16), (700, 8, 2, 4, 16)])
 def test_tiles_that_are_not_cut(dtype, seqs, heads, kv_heads, new, page):
     """Whole tiles, of sequences of one tile each and a few without any, more than a look finds."""
     rng = np.random.default_rng(seqs)

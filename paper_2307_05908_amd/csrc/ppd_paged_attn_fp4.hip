@@ -310,11 +310,11 @@ int check_attention(const ppd_paged_cache_fp4* cache, const ppd_paged_batch* bat
   // The split kernel's tiles of 32 rows where there are many and most of them are full, as far as the host can know, or where there is more to read than the memory-side cache
   // holds.  16-bit types, 32 / 8 heads, us of 16 / 32 rows a tile: 64 sequences of 20 rows over 4000 positions 120 / 77, over 8000 243 / 194; of 32 rows over
   // 1000 37 / 30, 24 of them over 2000 33 / 32, 4 over 500 11.4 / 14.4, one over 8000 20 / 32; of 48 rows over 1000 47 / 52, over 400 to 32000 465 / 309; of 64 rows over 1000
-  // 60 / 53, over 4000 212 / 182.  Of 4 to 32 rows, over 100 to 4000 72 / 85, over 400 to 32000 174 to 194 / 192.
+  // 60 / 53, over 4000 212 / 182.  Where sequences have from 4 to 32 rows, 17 of them on average, over 100 to 4000 81 / 86, over 400 to 32000 178 / 203.
   const int64_t wide_tiles = (rows / (2 * SPLIT_ROWS) + some) * cache->n_kv_heads, sixteens = some ? (rows + SPLIT_ROWS * some - 1) / (SPLIT_ROWS * some) : 0;
   const bool full = sixteens % 2 == 0 && 2 * (rows - (sixteens - 1) * SPLIT_ROWS * some) > SPLIT_ROWS * some;
   const bool much = (double)some * (double)capacity * cache->n_kv_heads * (cache->head_dim + cache->head_dim / 16) >= 320e6;
-  p->tile_rows = p->tiles ? TILE_ROWS : cache->dtype != PPD_FP32 && sixteens > 1 && sixteens <= 4 && wide_tiles >= 256 && (full || much) ? 2 * SPLIT_ROWS : SPLIT_ROWS;
+  p->tile_rows = p->tiles ? TILE_ROWS : cache->dtype != PPD_FP32 && rows >= 20 * some && sixteens <= 4 && wide_tiles >= 256 && (full || much) ? 2 * SPLIT_ROWS : SPLIT_ROWS;
   const int tile_rows = p->tile_rows;
   const int64_t tiles = rows / tile_rows + some;
   const int slots = p->tiles ? 512 : 256;                   // (see ppd_paged_attn.hip; 512 for few rows: one sequence of 60000 positions 30.6 us, not 28.3, 8 of 4 rows over 2000 18 / 15)

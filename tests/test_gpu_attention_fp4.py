@@ -50,7 +50,7 @@ def many_heads(d):
     group, some = d.heads // d.kv_heads, min(d.n, len(d.new))
     rows = d.n * group
     sixteens = -(-rows // (16 * some)) if some else 0
-    if d.dtype == F32 or sixteens not in (2, 3, 4):
+    if d.dtype == F32 or rows < 20 * some or sixteens not in (2, 3, 4):
         return None, 0
     times = max(1, -(-256 // ((rows // 32 + some) * d.kv_heads)))
     if times * d.heads > 1024:

@@ -500,12 +500,11 @@ def ppd_paged_plan(pages, free_pages, counters, held, wanted, page_size, n_rows,
     table = pages.shape
     if pages.dtype is not i32 or len(table) != 2 or table[0] != n or (table[1] > 1 and pages.stride(1) != 1) or free_pages.dtype is not i32 or free_pages.dim() != 1:
         raise ValueError("pages int32 [n_seqs, max_pages], its rows contiguous, free_pages int32 [n_pages]")
-    for t in (held, wanted, kept):
-        if t is not None and (t.dtype is not i32 or t.numel() != n):
-            raise ValueError("held, wanted, kept: int32 [n_seqs]")
+    if held.dtype is not i32 or wanted.dtype is not i32 or wanted.numel() != n or (kept is not None and (kept.dtype is not i32 or kept.numel() != n)):
+        raise ValueError("held, wanted, kept: int32 [n_seqs]")
     if counters.dtype is not i64 or counters.numel() != 2:
         raise ValueError("counters: int64 [2]")
-    if not any(t is not None for t in given):               # (two allocations for all of them)
+    if q_start is kv_len is granted is counters_out is row_seq is positions is slots is None:      # (two allocations for all of them)
         sizes32, sizes64 = ((n + 1, n, n, n_rows, n_rows), (2, n_rows)) if want_rows else ((n + 1, n, n), (2,))
         made32 = torch.empty(sum(sizes32), dtype=i32, device=pages.device).split_with_sizes(sizes32)
         made64 = torch.empty(sum(sizes64), dtype=i64, device=pages.device).split_with_sizes(sizes64)
@@ -526,13 +525,13 @@ def ppd_paged_plan(pages, free_pages, counters, held, wanted, page_size, n_rows,
               held.data_ptr(), _ptr(kept), wanted.data_ptr(), n_rows, _ptr(made[0]), _ptr(made[1]), _ptr(made[2]), *(_ptr(t) for t in made[4:]), raw_stream(dev))
     if rc != 0:
         raise PPDError(rc, "ppd_paged_plan", load_library().ppd_last_hip_error(None))
-    return Plan(*made)
+    return Plan._make(made)
 
 
 def _rows_made(out, like, dtype, head_dim, what, n_tokens, heads):
     """`out`, made here as one piece if not given, and its rows as bytes."""
     if out is None:
-        out = _layers()[0].empty_like(like, memory_format=_layers()[0].contiguous_format)
+        out = like.new_empty((n_tokens, heads, head_dim))
         return out, _PACK_ROWS(out.data_ptr(), heads * head_dim, head_dim)
     return out, _rows(out, dtype, head_dim, what, n_tokens, heads)[0]
 
@@ -549,16 +548,16 @@ def _paged_args_fp4(k_codes, k_scales, v_codes, v_scales, pages, q_start, kv_len
     n_pages, size, kv_heads, half = shape
     if k_scales.shape != (n_pages, size, kv_heads, half // 16) or v_scales.shape != k_scales.shape or k_scales.dtype is not u8 or v_scales.dtype is not u8:
         raise ValueError("k_scales, v_scales: uint8 [n_pages, page_size, n_kv_heads, head_dim / 32]")
-    strides = []
-    for t in (k_codes, v_codes, k_scales, v_scales):
-        s0, s1, s2, s3 = t.stride()
-        if s3 != 1:
-            raise ValueError("codes and scales of a row must be contiguous")
-        strides += (s0, s1, s2)
+    k0, k1, k2, k3 = k_codes.stride()
+    v0, v1, v2, v3 = v_codes.stride()
+    x0, x1, x2, x3 = k_scales.stride()
+    y0, y1, y2, y3 = v_scales.stride()
+    if not k3 == v3 == x3 == y3 == 1:
+        raise ValueError("codes and scales of a row must be contiguous")
     batch, most, n = _paged_batch(torch.int32, pages, q_start, kv_len, n_tokens)
-    code = codes[dtype]
-    return (_PACK_CACHE_FP4(k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), *strides, n_pages, size, kv_heads, 2 * half, code), batch,
-            (n_pages, size, kv_heads, 2 * half, code, most, n, n_tokens))
+    code, head_dim = codes[dtype], 2 * half
+    return (_PACK_CACHE_FP4(k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), k0, k1, k2, v0, v1, v2, x0, x1, x2, y0, y1, y2,
+                            n_pages, size, kv_heads, head_dim, code), batch, (n_pages, size, kv_heads, head_dim, code, most, n, n_tokens))
 
 
 def ppd_paged_append_fp4(k_codes, k_scales, v_codes, v_scales, pages, q_start, kv_len, q, k, v, q_gain=None, k_gain=None, norm_eps=1e-5, rotary_dim=0,

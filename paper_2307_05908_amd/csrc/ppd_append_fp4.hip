@@ -1,6 +1,6 @@
 // ppd_paged_append_fp4: queries and keys normalised per head and rotated to their positions, keys and values into pages of 4-bit numbers.
 // Bound by reading the rows and writing queries (and, where asked for, the values that the pages have now), and, close behind, by the keys' arithmetic in 64 bits:
-// 4915 bf16 tokens of 40 + 2 * 40 heads, 329 MB, take 93 us, 3.5 TB/s (a copy 67); with the keys' scales and codes from 32 bits it were 79, but a key next to a border
+// 4915 bf16 tokens of 40 + 2 * 40 heads, 329 MB, take 88 us, 3.7 TB/s (a copy 67); with the keys' scales and codes from 32 bits it were 79, but a key next to a border
 // would have a code that depends on the order of operations.  Bounds in 32 bits first, and 64 bits only where these leave it open, were no faster (94), and
 // no exchange between lanes or other order of the angles in LDS was either.
 #include "ppd_divide.h"
@@ -56,10 +56,11 @@ __device__ __forceinline__ uint32_t most_of_block(uint32_t m) {      // over the
   m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xf, 0xf, false));
   return max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xf, 0xf, false));
 }
-// A 64-bit number of at most 8 as fp32, cut off and with its last bit set where something was: on the same side of every border between codes.
+// A 64-bit number below 2^128 as fp32, cut off and with its last bit set where something was: on the same side of every border between codes.  (One below
+// 2^-126 as one below 2^-126.)
 __device__ __forceinline__ float odd_f32(double d) {
-  const uint32_t hi = (uint32_t)__double2hiint(d), lo = (uint32_t)__double2loint(d), a = hi & 0x7fffffffu;
-  const uint32_t f = a < 897u << 20 ? 0u : (a - (896u << 20)) << 3 | lo >> 29 | ((lo & 0x1fffffffu) != 0);
+  const uint32_t hi = (uint32_t)__double2hiint(d), lo = (uint32_t)__double2loint(d);
+  const uint32_t f = __builtin_amdgcn_alignbit(max(hi & 0x7fffffffu, 896u << 20) - (896u << 20), lo, 29) | min(lo << 3, 1u);
   return __uint_as_float(f | (hi & 0x80000000u));
 }
 
@@ -246,9 +247,15 @@ __global__ __launch_bounds__(256) void append_fp4_kernel(AppendArgs a) {
       const bool endless = most >= 0x7ff00000u;
       const int exponent = min(max((int)((most + 0x3ffffu) >> 20) - 1023 - 2, FP4_LEAST), FP4_MOST);
       byte = endless ? 255 : 127 + exponent;
-      scale = 1.0f;
+      if (__ballot(!endless && (exponent < -110 || exponent > 110))) {      // (where fp32 ends: divided by the scale, and cut to what its numbers are)
+        scale = 1.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = odd_f32(endless ? 0.0 : fmin(fmax(ldexp(d[e], -exponent), -8.0), 8.0));
+        for (int e = 0; e < 8; ++e) x[e] = odd_f32(fmin(fmax(ldexp(d[e], -exponent), -8.0), 8.0));
+      } else {
+        scale = __uint_as_float((uint32_t)(127 + exponent) << 23);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = odd_f32(d[e]);
+      }
     } else {
       const f32x4 u = Quad<T>::wide(ra[it][0]), w = Quad<T>::wide(ra[it][1]);
 #pragma unroll
@@ -256,12 +263,9 @@ __global__ __launch_bounds__(256) void append_fp4_kernel(AppendArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(x[e]) & 0x7fffffffu);
       byte = fp4_scale_of(most_of_block(most));
-      scale = fp4_scale(byte);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = byte == 255 ? 0.f : x[e];
-      if (byte == 255) scale = 1.0f;
+      scale = byte == 255 ? 1.0f : fp4_scale(byte);
     }
-    const uint32_t codes = fp4_narrow(x, scale);
+    const uint32_t codes = byte == 255 ? 0u : fp4_narrow(x, scale);
     if (page >= 0) {
       uint8_t* const c = is_k ? a.kc + page * a.kc_page + slot * a.kc_pos + kvh * a.kc_head : a.vc + page * a.vc_page + slot * a.vc_pos + kvh * a.vc_head;
       uint8_t* const b = is_k ? a.ks + page * a.ks_page + slot * a.ks_pos + kvh * a.ks_head : a.vs + page * a.vs_page + slot * a.vs_pos + kvh * a.vs_head;

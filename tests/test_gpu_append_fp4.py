@@ -148,7 +148,7 @@ def test_positions_without_a_page():
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
-@pytest.mark.parametrize("scale", [0, 9, -9, 100, -100, 123, -122])
+@pytest.mark.parametrize("scale", [0, 9, -9, 100, -100, 108, 109, 110, 111, 112, -108, -109, -110, -111, -112, -113, 123, -122])
 def test_borders(dtype, scale):
     """Numbers on the borders between codes and beside them, and largest ones on the borders between scales and beside them."""
     if dtype == F16 and abs(scale) > 9:

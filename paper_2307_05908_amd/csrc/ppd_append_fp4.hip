@@ -26,7 +26,7 @@ struct AppendArgs {
   double turns[64];      // angle of pair i per position, in whole turns
 };
 
-// Four sets of heads' rows a workgroup from this many sets on, see ppd_append.hip (4915 tokens of 8 sets: 93 us, one set a workgroup 112, two 96, eight 92).
+// Four sets of heads' rows a workgroup from this many sets on, see ppd_append.hip (4915 tokens of 8 sets, keys' codes then a little slower: 93 us, one set a workgroup 112, two 96, eight 92).
 constexpr int MANY = 2048;
 // Of these, several tokens a workgroup, two sets together, where a token's rows fill no more than one (bf16, head_dim 128, us of one token / several: 35291 tokens of 2 + 2 * 1
 // heads 107 / 38, 2400 of 8 + 2 * 1 13.5 / 9.7, 16913 of 2 + 2 * 2 56 / 30, 7331 of 8 + 2 * 2 29 / 24; with rows for more than one set, 16 + 2 * 4, in four sets, 39 / 41).

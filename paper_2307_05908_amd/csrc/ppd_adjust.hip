@@ -8,11 +8,22 @@ namespace {
 
 constexpr int ADJUST_MAX_VOCAB = 1 << 24;
 constexpr int AT = 256;                       // threads of a workgroup
+constexpr int LOOK = 4;                       // sequences of a lane at a look
+
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t dpp_plus(uint32_t v) { return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ uint32_t runs_upto(uint32_t v) {      // sums up to the lane's
+  v = dpp_plus<0x111, 0xf>(v);
+  v = dpp_plus<0x112, 0xf>(v);
+  v = dpp_plus<0x114, 0xf>(v);
+  v = dpp_plus<0x118, 0xf>(v);
+  v = dpp_plus<0x142, 0xa>(v);
+  return dpp_plus<0x143, 0xc>(v);
+}
 
 struct AdjustArgs {
   const int32_t *row_start, *ids; const void* logits; void* out; int64_t stride, out_stride;
   ppd_logit_rules r;
-  int n_seqs, n_rows, vocab;
+  int n_seqs, n_rows, vocab, run;      // run: rows of a workgroup, as a power of two
   bool in_place;
 };
 
@@ -42,12 +53,14 @@ template <typename T> struct Logits16 {
 template <> struct Logits<bf16_t> : Logits16<bf16_t> {};
 template <> struct Logits<f16_t> : Logits16<f16_t> {};
 
-// A workgroup has 16 bytes' worth of tokens of the vocabulary a thread, and a share of one sequence's rows.  It counts the text before them in LDS
+// A workgroup has 16 bytes' worth of tokens of the vocabulary a thread, and a run of one sequence's rows.  It counts the text before them in LDS
 // (additions of whole numbers, in any order), each thread takes the counts of its own tokens into registers, and from then on nothing crosses
 // threads: a row's own token is counted by the thread that has it.  Rows follow each other; what hides their waits is the other workgroups on the unit
 // (the next row's logits under way while one is worked on: 30.7 us, not 31.7, for 901 bf16 rows of 32000 logits, 115 MB; pieces of the vocabulary four
-// times as large 34.9; five, three, two rows a share 33.7, 37.8, 40.0, as each reads the text anew.  A copy takes 25).
-// grid: (pieces of the vocabulary, sequences, shares of rows)
+// times as large 34.9; five, three, two rows a run 33.7, 37.8, 40.0, as each reads the text anew.  A copy takes 25).
+// Every wave counts the runs for itself, 256 sequences at a look: a workgroup has sixteen rows at most, however rows are spread over sequences (800 rows of
+// one and one of each of 63 others 33 us, by equal shares for all 882), and none without a run lies between others.
+// grid: (pieces of the vocabulary, runs of rows, and what is left of them)
 template <typename T>
 __global__ __launch_bounds__(AT) void adjust_kernel(AdjustArgs a) {
   constexpr int VEC = Logits<T>::VEC, SIZE = 16 / VEC, PIECE = AT * VEC;
@@ -55,10 +68,32 @@ __global__ __launch_bounds__(AT) void adjust_kernel(AdjustArgs a) {
   typedef typename Logits<T>::loose loose;
   __shared__ __align__(16) uint32_t count[PIECE];
   __shared__ __align__(16) int entry[PIECE];              // the bias list's entry for a token, and one more; 0: none
-  const int tid = threadIdx.x, s = blockIdx.y, first_id = blockIdx.x * PIECE, first = first_id + tid * VEC;      // (of the workgroup's tokens, of the thread's)
-  const int row0 = min(max(a.row_start[s], 0), a.n_rows), rows = min(max(a.row_start[s + 1], row0), a.n_rows) - row0;
-  const int share = (rows + gridDim.z - 1) / gridDim.z, begin = min((int)blockIdx.z * share, rows), end = min(begin + share, rows);
-  if (begin >= end) return;
+  const int tid = threadIdx.x, lane = tid & 63, idx = blockIdx.z * gridDim.y + blockIdx.y, first_id = blockIdx.x * PIECE, first = first_id + tid * VEC;      // (of the workgroup's tokens, of the thread's)
+  auto start_of = [&](int t) { return min(max(a.row_start[min(t, a.n_seqs)], 0), a.n_rows); };
+  int s = -1, row0 = 0, rows = 0, r = 0, before_runs = 0;   // (r: of the sequence's runs)
+  for (int from = 0; s < 0; from += LOOK * WAVE) {
+    if (from >= a.n_seqs) return;
+    int lo[LOOK + 1], runs[LOOK], mine = 0;
+#pragma unroll
+    for (int j = 0; j <= LOOK; ++j) lo[j] = start_of(from + LOOK * lane + j);
+#pragma unroll
+    for (int j = 0; j < LOOK; ++j) { lo[j + 1] = max(lo[j + 1], lo[j]); runs[j] = (lo[j + 1] - lo[j] + (1 << a.run) - 1) >> a.run; mine += runs[j]; }
+    const int upto = before_runs + (int)runs_upto((uint32_t)mine);
+    const unsigned long long past = __ballot(upto > idx);
+    before_runs = __builtin_amdgcn_readlane(upto, 63);
+    if (!past) continue;
+    const int w = __builtin_ctzll(past);
+    int at = idx - (upto - mine), j0 = 0, l = lo[0], h = lo[1];
+    bool there = false;
+#pragma unroll
+    for (int j = 0; j < LOOK; ++j) {
+      if (there) continue;
+      if (at < runs[j]) { there = true; j0 = j; l = lo[j]; h = lo[j + 1]; } else at -= runs[j];
+    }
+    s = from + LOOK * w + __builtin_amdgcn_readlane(j0, w);
+    row0 = __builtin_amdgcn_readlane(l, w); rows = __builtin_amdgcn_readlane(h, w) - row0; r = __builtin_amdgcn_readlane(at, w);
+  }
+  const int begin = r << a.run, end = min(begin + (1 << a.run), rows);
   const bool counts = a.r.repetition || a.r.presence || a.r.frequency;
   const int before = counts && a.r.history ? min(max(a.r.history_len[s], 0), (int)a.r.history_stride) : 0;
   const int prompt = a.r.prompt_len ? a.r.prompt_len[s] : 0;
@@ -162,15 +197,13 @@ __global__ __launch_bounds__(AT) void adjust_kernel(AdjustArgs a) {
 }
 
 template <typename T>
-hipError_t adjust_go(const AdjustArgs& a, hipStream_t stream) {
-  constexpr int SHARES = 4096;      // (of rows, at most: a share may be any number of them)
-  const int per_seq = (a.n_rows + a.n_seqs - 1) / a.n_seqs;
-  const int64_t pieces = (a.vocab + AT * Logits<T>::VEC - 1) / (AT * Logits<T>::VEC);
-  int64_t shares = 512 / (pieces * a.n_seqs);              // sixteen rows a share, or fewer where workgroups are few
-  if (shares > per_seq) shares = per_seq;
-  if (shares < (per_seq + 15) / 16) shares = (per_seq + 15) / 16;
-  if (shares > SHARES) shares = SHARES;
-  hipLaunchKernelGGL((adjust_kernel<T>), dim3(pieces, a.n_seqs, shares), dim3(AT), 0, stream, a);
+hipError_t adjust_go(AdjustArgs& a, hipStream_t stream) {
+  const int64_t pieces = (a.vocab + AT * Logits<T>::VEC - 1) / (AT * Logits<T>::VEC), some = a.n_rows < a.n_seqs ? a.n_rows : a.n_seqs;
+  a.run = 4;                                               // sixteen rows a run, or fewer where workgroups are few
+  while (a.run > 0 && pieces * ((a.n_rows >> a.run) + some) < 512) --a.run;
+  const int64_t runs = (a.n_rows >> a.run) + some;
+  const int64_t side = runs < 32768 ? runs : 32768;        // (a grid's second size ends at 65535)
+  hipLaunchKernelGGL((adjust_kernel<T>), dim3(pieces, side, (runs + side - 1) / side), dim3(AT), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -194,7 +227,7 @@ extern "C" int ppd_adjust_logits(int n_seqs, int n_rows, int vocab, int dtype, c
   if (!row_start || !logits || !out || ((uintptr_t)logits | (uintptr_t)out) & (elem_size(dtype) - 1)) return PPD_EINVAL;
   if (n_rows > 1 && (logits_stride < vocab || out_stride < vocab || (logits == out && logits_stride != out_stride))) return PPD_EINVAL;
   if (n_rows == 0) return PPD_OK;
-  const AdjustArgs a = {row_start, ids, logits, out, logits_stride, out_stride, r, n_seqs, n_rows, vocab, logits == out};
+  AdjustArgs a = {row_start, ids, logits, out, logits_stride, out_stride, r, n_seqs, n_rows, vocab, 0, logits == out};
   hipStream_t st = (hipStream_t)hip_stream;
   return launched(dtype == PPD_FP32 ? adjust_go<float>(a, st) : dtype == PPD_BF16 ? adjust_go<bf16_t>(a, st) : adjust_go<f16_t>(a, st));
 }

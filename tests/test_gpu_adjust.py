@@ -215,6 +215,26 @@ def test_the_largest_vocabulary():
     Case([1, 2], 2 ** 24, BF16, biases=6, masks=2, seed=4).check()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_spread_unevenly(dtype):
+    """A sequence with most of the rows, others with one or none, and more sequences than are looked at at once."""
+    Case([1, 0, 77, 1, 0, 16, 17], 1500, dtype, before=30, biases=5, masks=3, seed=2, start=3, pad=2).check()
+    rows = [0, 1] * 150 + [100] + [1, 2, 0] * 70
+    Case(rows, 40, dtype, before=5, biases=2, masks=2, seed=3, pad=1).check()
+
+
+def test_very_many_rows():
+    """More runs of rows than a grid's second size."""
+    n = 1200000
+    z = torch.zeros(n, 3, device="cuda")
+    start = torch.tensor([0, 5, 5, n - 7, n], dtype=torch.int32, device="cuda")
+    bias = torch.tensor([1.0, 2.0, 3.0, 4.0], device="cuda")
+    out = binding.ppd_adjust_logits(z, start, bias_start=torch.arange(5, dtype=torch.int32, device="cuda"), bias_ids=torch.tensor([0, 1, 2, 0], dtype=torch.int32, device="cuda"), bias=bias)
+    want = torch.zeros_like(z)
+    want[:5, 0], want[5:n - 7, 2], want[n - 7:, 0] = 1.0, 3.0, 4.0
+    assert torch.equal(out, want)
+
+
 def test_offsets_beyond_32_bits():
     n, vocab = 70000, 33000
     z = torch.zeros((n, vocab), dtype=BF16, device="cuda")

@@ -8,7 +8,6 @@ namespace {
 
 constexpr int ADJUST_MAX_VOCAB = 1 << 24;
 constexpr int AT = 256;                       // threads of a workgroup
-constexpr int LOOK = 4;                       // sequences of a lane at a look
 
 template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t dpp_plus(uint32_t v) { return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false); }
 __device__ __forceinline__ uint32_t runs_upto(uint32_t v) {      // sums up to the lane's
@@ -53,12 +52,43 @@ template <typename T> struct Logits16 {
 template <> struct Logits<bf16_t> : Logits16<bf16_t> {};
 template <> struct Logits<f16_t> : Logits16<f16_t> {};
 
+// A run's sequence, that one's rows, and which of its runs it is, LOOK sequences of a lane at a time; false: there are not so many.
+template <int LOOK>
+__device__ __forceinline__ bool find_run(const AdjustArgs& a, int idx, int lane, int& s, int& row0, int& rows, int& r) {
+  auto start_of = [&](int t) { return min(max(a.row_start[min(t, a.n_seqs)], 0), a.n_rows); };
+  int before = 0;
+  for (int from = 0; from < a.n_seqs; from += LOOK * WAVE) {
+    int lo[LOOK + 1], runs[LOOK], mine = 0;
+#pragma unroll
+    for (int j = 0; j <= LOOK; ++j) lo[j] = start_of(from + LOOK * lane + j);
+#pragma unroll
+    for (int j = 0; j < LOOK; ++j) { lo[j + 1] = max(lo[j + 1], lo[j]); runs[j] = (lo[j + 1] - lo[j] + (1 << a.run) - 1) >> a.run; mine += runs[j]; }
+    const int upto = before + (int)runs_upto((uint32_t)mine);
+    const unsigned long long past = __ballot(upto > idx);
+    if (past) {
+      const int w = __builtin_ctzll(past);
+      int at = idx - (upto - mine), j0 = 0, l = lo[0], h = lo[1];
+      bool there = false;
+#pragma unroll
+      for (int j = 0; j < LOOK; ++j) {
+        if (there) continue;
+        if (at < runs[j]) { there = true; j0 = j; l = lo[j]; h = lo[j + 1]; } else at -= runs[j];
+      }
+      s = from + LOOK * w + __builtin_amdgcn_readlane(j0, w);
+      row0 = __builtin_amdgcn_readlane(l, w); rows = __builtin_amdgcn_readlane(h, w) - row0; r = __builtin_amdgcn_readlane(at, w);
+      return true;
+    }
+    before = __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
 // A workgroup has 16 bytes' worth of tokens of the vocabulary a thread, and a run of one sequence's rows.  It counts the text before them in LDS
 // (additions of whole numbers, in any order), each thread takes the counts of its own tokens into registers, and from then on nothing crosses
 // threads: a row's own token is counted by the thread that has it.  Rows follow each other; what hides their waits is the other workgroups on the unit
 // (the next row's logits under way while one is worked on: 30.7 us, not 31.7, for 901 bf16 rows of 32000 logits, 115 MB; pieces of the vocabulary four
 // times as large 34.9; five, three, two rows a run 33.7, 37.8, 40.0, as each reads the text anew.  A copy takes 25).
-// Every wave counts the runs for itself, 256 sequences at a look: a workgroup has sixteen rows at most, however rows are spread over sequences (800 rows of
+// Every wave counts the runs for itself: a workgroup has sixteen rows at most, however rows are spread over sequences (800 rows of
 // one and one of each of 63 others 33 us, by equal shares for all 882), and none without a run lies between others.
 // grid: (pieces of the vocabulary, runs of rows, and what is left of them)
 template <typename T>
@@ -69,30 +99,8 @@ __global__ __launch_bounds__(AT) void adjust_kernel(AdjustArgs a) {
   __shared__ __align__(16) uint32_t count[PIECE];
   __shared__ __align__(16) int entry[PIECE];              // the bias list's entry for a token, and one more; 0: none
   const int tid = threadIdx.x, lane = tid & 63, idx = blockIdx.z * gridDim.y + blockIdx.y, first_id = blockIdx.x * PIECE, first = first_id + tid * VEC;      // (of the workgroup's tokens, of the thread's)
-  auto start_of = [&](int t) { return min(max(a.row_start[min(t, a.n_seqs)], 0), a.n_rows); };
-  int s = -1, row0 = 0, rows = 0, r = 0, before_runs = 0;   // (r: of the sequence's runs)
-  for (int from = 0; s < 0; from += LOOK * WAVE) {
-    if (from >= a.n_seqs) return;
-    int lo[LOOK + 1], runs[LOOK], mine = 0;
-#pragma unroll
-    for (int j = 0; j <= LOOK; ++j) lo[j] = start_of(from + LOOK * lane + j);
-#pragma unroll
-    for (int j = 0; j < LOOK; ++j) { lo[j + 1] = max(lo[j + 1], lo[j]); runs[j] = (lo[j + 1] - lo[j] + (1 << a.run) - 1) >> a.run; mine += runs[j]; }
-    const int upto = before_runs + (int)runs_upto((uint32_t)mine);
-    const unsigned long long past = __ballot(upto > idx);
-    before_runs = __builtin_amdgcn_readlane(upto, 63);
-    if (!past) continue;
-    const int w = __builtin_ctzll(past);
-    int at = idx - (upto - mine), j0 = 0, l = lo[0], h = lo[1];
-    bool there = false;
-#pragma unroll
-    for (int j = 0; j < LOOK; ++j) {
-      if (there) continue;
-      if (at < runs[j]) { there = true; j0 = j; l = lo[j]; h = lo[j + 1]; } else at -= runs[j];
-    }
-    s = from + LOOK * w + __builtin_amdgcn_readlane(j0, w);
-    row0 = __builtin_amdgcn_readlane(l, w); rows = __builtin_amdgcn_readlane(h, w) - row0; r = __builtin_amdgcn_readlane(at, w);
-  }
+  int s, row0, rows, r;
+  if (!(a.n_seqs <= WAVE ? find_run<1>(a, idx, lane, s, row0, rows, r) : find_run<4>(a, idx, lane, s, row0, rows, r))) return;
   const int begin = r << a.run, end = min(begin + (1 << a.run), rows);
   const bool counts = a.r.repetition || a.r.presence || a.r.frequency;
   const int before = counts && a.r.history ? min(max(a.r.history_len[s], 0), (int)a.r.history_stride) : 0;

@@ -229,7 +229,8 @@ int ppd_paged_attention_fp4_workspace(const ppd_paged_cache_fp4 *cache, const pp
  * sequence are not touched (row_start must not decrease, as q_start there).
  * All of it DEVICE, contiguous but for the rows' strides (in elements), and each of these may be NULL: ids (the text is the history), history
  * and history_len (both: the text is the batch's rows), prompt_len (0), repetition (1), presence (0),
- * frequency (0), bias_start, bias_ids and bias (all three), mask and mask_row (both). */
+ * frequency (0), bias_start, bias_ids and bias (all three), mask and mask_row (both).  With n_rows 0 nothing is done, and logits, out and
+ * mask_row may be NULL, too. */
 typedef struct {
   const int32_t *history;       /* [n_seqs][history_stride] */
   int64_t history_stride;       /* at most 2^30 */

@@ -223,7 +223,8 @@ extern "C" int ppd_adjust_logits(int n_seqs, int n_rows, int vocab, int dtype, c
   if (n_seqs < 1 || n_rows < 0 || vocab < 1 || dtype < PPD_FP32 || dtype > PPD_FP16 || !rules) return PPD_EINVAL;
   if (n_seqs > PPD_MAX_SEQS || n_rows > PPD_MAX_TOKENS || vocab > ADJUST_MAX_VOCAB) return PPD_ELIMIT;
   const ppd_logit_rules& r = *rules;
-  if (!r.history != !r.history_len || !r.mask != !r.mask_row || !r.bias != !r.bias_start || !r.bias != !r.bias_ids) return PPD_EINVAL;
+  if (!r.history != !r.history_len || !r.bias != !r.bias_start || !r.bias != !r.bias_ids) return PPD_EINVAL;
+  if (n_rows > 0 && (!logits || !out || !r.mask != !r.mask_row)) return PPD_EINVAL;      // (what has no rows has no address, either)
   if (((uintptr_t)row_start | (uintptr_t)ids | (uintptr_t)r.history | (uintptr_t)r.history_len | (uintptr_t)r.prompt_len | (uintptr_t)r.repetition |
        (uintptr_t)r.presence | (uintptr_t)r.frequency | (uintptr_t)r.bias_start | (uintptr_t)r.bias_ids | (uintptr_t)r.bias | (uintptr_t)r.mask |
        (uintptr_t)r.mask_row) & 3)
@@ -232,7 +233,7 @@ extern "C" int ppd_adjust_logits(int n_seqs, int n_rows, int vocab, int dtype, c
   if (r.history && r.history_stride > 1 << 30) return PPD_ELIMIT;
   if (r.bias && (r.n_bias < 0 || r.n_bias == INT32_MAX)) return PPD_EINVAL;
   if (r.mask && (r.n_masks < 0 || (r.n_masks > 1 && r.mask_stride < (vocab + 31) / 32))) return PPD_EINVAL;
-  if (!row_start || !logits || !out || ((uintptr_t)logits | (uintptr_t)out) & (elem_size(dtype) - 1)) return PPD_EINVAL;
+  if (!row_start || ((uintptr_t)logits | (uintptr_t)out) & (elem_size(dtype) - 1)) return PPD_EINVAL;
   if (n_rows > 1 && (logits_stride < vocab || out_stride < vocab || (logits == out && logits_stride != out_stride))) return PPD_EINVAL;
   if (n_rows == 0) return PPD_OK;
   AdjustArgs a = {row_start, ids, logits, out, logits_stride, out_stride, r, n_seqs, n_rows, vocab, 0, logits == out};

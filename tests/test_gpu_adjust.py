@@ -270,3 +270,15 @@ def test_streams_and_replays():
         got = out.clone()
         torch.cuda.synchronize()
         assert torch.equal(got, binding.ppd_adjust_logits(z, start, **rest))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("masks", [0, 3])
+def test_no_rows(dtype, masks):
+    """Tensors without elements have no address."""
+    c = Case([0, 0], 300, dtype, biases=4, masks=masks)
+    assert c.n == 0
+    for out in (None, torch.empty((0, 300), dtype=dtype, device="cuda"), "in place"):
+        assert c.call(out).shape == (0, 300)
+    assert Case([0], 1, dtype, without=RULES).call().shape == (0, 1)
+    torch.cuda.synchronize()

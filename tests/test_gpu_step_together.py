@@ -272,3 +272,25 @@ def test_two_captured_steps_on_two_streams_at_once():
     for t in threads:
         t.join(60)
     assert got == want
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_a_step_in_which_nobody_has_a_row(dtype):
+    """Every operator takes the batch that the plan makes of it, and leaves the pages as they were."""
+    def ints(*x):
+        return torch.tensor(x, dtype=torch.int32, device="cuda")
+    pages, counters = torch.full((2, 4), -1, dtype=torch.int32, device="cuda"), torch.tensor([0, 9], device="cuda")
+    plan = binding.ppd_paged_plan(pages, torch.arange(9, dtype=torch.int32, device="cuda"), counters, ints(0, 0), ints(0, 3), PAGE, 0)
+    assert plan.q_start.tolist() == [0, 0, 0] and plan.granted.tolist() == [0, 0] and plan.counters.tolist() == [0, 9] and plan.slots.shape == (0,)
+    pool = [torch.full((9, PAGE, KV_HEADS, x), 3, dtype=torch.uint8, device="cuda") for x in (HD // 2, HD // 32) * 2]
+    where = (*pool, pages, plan.q_start, plan.kv_len)
+    q, k, z = (torch.empty(0, *shape, dtype=dtype, device="cuda") for shape in ((HEADS, HD), (KV_HEADS, HD), (VOCAB,)))
+    q, *values = binding.ppd_paged_append_fp4(*where, q, k, k.clone(), rotary_dim=HD, want_values=True)
+    out, lse = binding.ppd_paged_attention_fp4(q, *where, want_lse=True)
+    assert q.shape == out.shape == (0, HEADS, HD) and all(x.shape == (0, KV_HEADS, HD) for x in values) and lse.shape == (0, HEADS)
+    mask = torch.full((1, (VOCAB + 31) // 32), -1, dtype=torch.int32, device="cuda")
+    for rules in ({}, dict(repetition=torch.ones(2, device="cuda")), dict(mask=mask, mask_row=ints())):
+        assert binding.ppd_adjust_logits(z, plan.q_start, ids=ints(), **rules).shape == (0, VOCAB)
+    tokens, accepted = binding.ppd_verify_drafts(z, ints(), plan.q_start, torch.empty(0, 2, device="cuda"))
+    torch.cuda.synchronize()
+    assert tokens.shape == (0,) and accepted.shape == (2,) and all((t == 3).all() for t in pool)

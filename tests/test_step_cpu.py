@@ -157,6 +157,16 @@ def test_bad_adjust_arguments():
     assert adjust(n_bias=-1) == EINVAL and adjust(n_bias=2 ** 31 - 1) == EINVAL and adjust(n_masks=-1) == EINVAL and adjust(mask_stride=31) == EINVAL
 
 
+@pytest.mark.parametrize("mask", [4096, None])
+def test_no_rows_have_no_tensors(mask):
+    """What has no elements has no address, either: a call of no rows takes NULL for all that has a number a row."""
+    assert adjust(n=0, z=None, out=None, ids=None, mask=mask, mask_row=None) == 0
+    assert adjust(n=0, z=None, out=None, ids=None, mask=mask, mask_row=None, zs=0, outs=0) == 0
+    assert adjust(n=1, z=None, mask=mask, mask_row=None) == EINVAL and adjust(n=1, out=None, mask=mask, mask_row=mask) == EINVAL
+    for kw in (dict(rules=False), dict(start=None), dict(seqs=0), dict(vocab=0), dict(dtype=3), dict(history=None), dict(bias_ids=None), dict(n_bias=-1), dict(z=ctypes.c_void_p(4097))):
+        assert adjust(n=0, **kw) == EINVAL                                                           # (what is wrong with rows or without)
+
+
 def test_binding_refuses_what_the_library_cannot_see():
     t, i32, u8 = torch.zeros, torch.int32, torch.uint8
     codes, scales = t(3, 16, 4, 32, dtype=u8), t(3, 16, 4, 2, dtype=u8)

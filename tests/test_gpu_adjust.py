@@ -282,3 +282,35 @@ def test_no_rows(dtype, masks):
         assert c.call(out).shape == (0, 300)
     assert Case([0], 1, dtype, without=RULES).call().shape == (0, 1)
     torch.cuda.synchronize()
+
+
+def same_as_with(c, **inside):
+    """The call's result, which is to the bit that of the same numbers inside their ranges, and that the definition's."""
+    got = c.call()
+    for name, values in inside.items():
+        assert not torch.equal(getattr(c, name), torch.tensor(values, dtype=torch.int32))
+        setattr(c, name, torch.tensor(values, dtype=torch.int32))
+    assert torch.equal(got, c.check())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_numbers_outside_their_range_count_as_the_next_inside(dtype):
+    def case(**numbers):
+        c = Case([2, 3, 1], 300, dtype, biases=5, masks=3, without=("mask", "mask_row"))
+        c.repetition, c.presence, c.frequency = torch.tensor([1.5, 0.75, 2.0]), torch.tensor([0.5, -0.25, 1.0]), torch.tensor([0.25, 0.5, -0.125])
+        for name, values in numbers.items():
+            setattr(c, name, torch.tensor(values, dtype=torch.int32))
+        return c
+
+    whole = case().history.shape[1]
+    many = case().bias.numel()
+    same_as_with(case(history_len=[-5, 2 ** 31 - 1, -2 ** 31], prompt_len=[0, 3, 1]), history_len=[0, whole, 0])
+    same_as_with(case(history_len=[whole, 7, whole], prompt_len=[2 ** 31 - 1, -2 ** 31, whole + 5]), prompt_len=[whole + 2, 0, whole + 1])
+    same_as_with(case(history_len=[-1, whole + 1, 4], prompt_len=[2 ** 31 - 1, -2 ** 31, -1]), history_len=[0, whole, 4], prompt_len=[2, 0, 0])
+    same_as_with(case(bias_start=[-9, 2 ** 31 - 1, -2 ** 31, 3]), bias_start=[0, many, 0, 3])
+    same_as_with(case(bias_start=[-2 ** 31, 1, many + 1, 2 ** 31 - 1]), bias_start=[0, 1, many, many])
+    c = case(ids=[2 ** 31 - 1, -2 ** 31, 300, -1, 299, 0])
+    got = c.call()
+    assert torch.equal(got, c.check())
+    c.ids = torch.tensor([-1, -1, -1, -1, 299, 0], dtype=torch.int32)
+    assert torch.equal(got, c.call())

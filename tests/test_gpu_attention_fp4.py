@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from fp4_common import NAMES, Batch4
+from fp4_common import NAMES, Batch4, values64
 from paged_common import HALF_STEP, TINY, attention64
 from paper_2307_05908_amd import binding
 
@@ -597,3 +597,106 @@ def test_more_than_the_caches_hold(dtype, heads, kv_heads, hd, new, page, window
         tol = 2 * (6 * (2 * w + 2.0 ** (-9 * WEIGHT_TERMS[dtype])) + 6 * HALF_STEP[dtype])
         assert torch.equal(o.isnan(), out[r].isnan()) and torch.equal(torch.isinf(z), torch.isinf(lse[r]))
         assert ((o - out[r]).float().abs().nan_to_num() <= tol).all() and ((z - lse[r]).abs().nan_to_num() <= 2 * (w + 40 * 2.0 ** -23)).all()
+
+
+class Large:
+    """Lengths of more than 320 MB together over pages that sequences share, as in test_more_than_the_caches_hold."""
+
+    def __init__(self, dtype, heads, kv_heads, hd, new, page, window):
+        rng = np.random.default_rng(hd + heads + new)
+        kv = rng.integers(8000, 17000, int(400e6 / (12500 * kv_heads * 2 * 17 * hd / 32)) + 2)
+        kv[1], kv[2] = 30, 0
+        self.kv = np.concatenate([kv, kv]) if window else kv
+        self.dtype, self.heads, self.kv_heads, self.hd, self.new, self.page, self.window, self.n_pages = dtype, heads, kv_heads, hd, new, page, window, 300
+        self.pages = torch.from_numpy(rng.integers(0, self.n_pages, (len(self.kv), -(-int(self.kv.max()) // page)))).int()
+        self.pages[0, 5], self.pages[-1, 250], self.pages[-1, 251] = -1, self.n_pages, -7
+        lo = np.maximum(self.kv - new + 1 - window, 0) if window else 0
+        blocks = np.maximum(self.kv - lo, 0) / 64
+        assert blocks.sum() * 64 * kv_heads * (hd + hd // 16) > 320e6          # (so that workgroups have four heads)
+        # Parts of all tiles (of 16 rows, or of 32) have about the same length, of 2048 / kv_heads parts at most together: positions of one, and parts of one tile.
+        self.longest = 64 * (math.ceil(-(-new * heads // kv_heads // 16) * (blocks + 2).sum() / (2048 // kv_heads)) + 1)
+        self.parts = 2048 // kv_heads
+
+    def call(self, q, k_codes, k_scales, v_codes, v_scales, scale):
+        up = lambda t: t.cuda()  # noqa: E731
+        q_start = (torch.arange(len(self.kv) + 1) * self.new).int()
+        out, lse = binding.ppd_paged_attention_fp4(up(q), up(k_codes), up(k_scales), up(v_codes), up(v_scales), up(self.pages), up(q_start), up(torch.from_numpy(self.kv).int()),
+                                                   scale=scale, window=self.window, want_lse=True)
+        torch.cuda.synchronize()
+        return out.cpu().double(), lse.cpu().double()
+
+    def weights_off(self, reach):
+        """limits' w, but for the sums over positions: those of a part, and then of the parts (three roundings each)."""
+        return ((QUERY_TERMS[self.dtype] * self.hd + 8) * reach + WEIGHT_TERMS[self.dtype] * self.longest + 3 * self.parts + 16) * 2.0 ** -24
+
+
+LARGE = pytest.mark.parametrize("dtype,heads,kv_heads,hd,new", [(BF16, 32, 8, 128, 1), (F32, 8, 4, 64, 2), (F16, 12, 12, 64, 1), (F32, 16, 16, 128, 1), (BF16, 80, 16, 128, 3), (F16, 32, 8, 64, 8),
+                                                              (BF16, 64, 8, 128, 6)])
+LARGE_PAGES = pytest.mark.parametrize("page,window", [(16, 0), (20, 0), (16, 9000)])
+
+
+@LARGE
+@LARGE_PAGES
+@pytest.mark.parametrize("score", [0.0, 87 / 64])
+def test_every_position_of_more_than_the_caches_hold(dtype, heads, kv_heads, hd, new, page, window, score):
+    """Positions of two kinds, with scores 0 and -score: the log sum tells how many there are of each, and component c of the values, 6 in pages c modulo hd and else 0,
+    how many of these.  With equal scores the counts are exact; the other weight, e^-1.359, is no bf16 number by 1/267 of it, nearly the most that there is."""
+    x = Large(dtype, heads, kv_heads, hd, new, page, window)
+    q = torch.zeros(len(x.kv) * new, heads, hd, dtype=dtype)
+    q[..., 33] = score
+    k_codes, v_codes = (torch.zeros(x.n_pages, page, kv_heads, hd // 2, dtype=torch.uint8) for _ in "kv")
+    scales = torch.full((x.n_pages, page, kv_heads, hd // 32), 127, dtype=torch.uint8)
+    k_codes[1::2, ..., 16] = 10 << 4                                           # (component 33: -1)
+    for p in range(x.n_pages):
+        v_codes[p, ..., p % hd // 2] = 7 << 4 * (p % hd % 2)
+    out, lse = x.call(q, k_codes, scales, v_codes, scales, 1.0)
+    of_kind = torch.tensor([1.0, math.exp(-score)], dtype=torch.float64)[torch.arange(hd) % 2]
+    for s, kv in enumerate(x.kv.tolist()):
+        page_of = x.pages[s][torch.arange(max(kv, 1)) // page]
+        bucket = torch.where((page_of >= 0) & (page_of < x.n_pages), page_of % hd, hd)
+        for i in range(new):
+            at, r = kv - new + i, s * new + i
+            if at < 0:
+                assert (out[r] == 0).all() and (lse[r] == -math.inf).all()
+                continue
+            count = torch.bincount(bucket[max(0, at - window + 1) if window else 0:at + 1], minlength=hd + 1)[:hd].double()
+            total = float((count * of_kind).sum())
+            if score == 0:
+                # exact sums; the reciprocal, the product, and the rounding to the type
+                assert (torch.exp(lse[r]) - total).abs().max() < 0.25
+                off = 4 * 2.0 ** -24
+            else:
+                w = x.weights_off(score)
+                assert (lse[r] - math.log(total)).abs().max() <= w + math.log(total) * 2.0 ** -23
+                off = 2 * w + 2.0 ** (-9 * WEIGHT_TERMS[dtype])
+            want = 6 * count * of_kind / total
+            assert ((out[r] - want).abs() <= want * (off + HALF_STEP[dtype] * (1 + 2.0 ** -9))).all(), (s, i, float(((out[r] - want).abs() / want.clamp(min=1e-9)).max()))
+
+
+@LARGE
+@LARGE_PAGES
+def test_more_than_the_caches_hold_against_64_bits(dtype, heads, kv_heads, hd, new, page, window):
+    """Some sequences and heads of such a batch: holes in the table, a value that is NaN, the first heads and the last."""
+    x = Large(dtype, heads, kv_heads, hd, new, page, window)
+    g = torch.Generator().manual_seed(heads)
+    codes = [torch.randint(0, 256, (x.n_pages, page, kv_heads, hd // 2), generator=g, dtype=torch.uint8) for _ in "kv"]
+    scales = [torch.randint(122, 128, (x.n_pages, page, kv_heads, hd // 32), generator=g, dtype=torch.uint8) for _ in "kv"]
+    scales[1][7, 3, 1, 0] = 255
+    q = torch.randn(len(x.kv) * new, heads, hd, generator=g).to(dtype)
+    out, lse = x.call(q, codes[0], scales[0], codes[1], scales[1], hd ** -0.5)
+    group = heads // kv_heads
+    some = [0, 1, 2, 3, kv_heads - 1] if kv_heads > 4 else list(range(kv_heads))
+    k, v = (values64(c[:, :, some], z[:, :, some]) for c, z in zip(codes, scales))
+    for s in (0, 1, 2, 3, len(x.kv) - 1):
+        r = slice(s * new, s * new + new)
+        b = object.__new__(Batch4)
+        b.__dict__ = dict(new=[new], kv=[int(x.kv[s])], heads=len(some) * group, kv_heads=len(some), hd=hd, dtype=dtype, page=page, n=new, n_pages=x.n_pages, pages=x.pages[s:s + 1],
+                          k_cache=k, v_cache=v, q=q[r].unflatten(1, (kv_heads, group))[:, some].flatten(1, 2))
+        ref, z, size, reach = attention64(b, window=window)
+        o, l = (t[r].unflatten(1, (kv_heads, group))[:, some].flatten(1, 2) for t in (out, lse))
+        assert torch.equal(o.isnan(), ref.isnan()) and torch.equal(torch.isinf(l), torch.isinf(z))
+        w = x.weights_off(reach)
+        tol = size * (2 * w[..., None] + 2.0 ** (-9 * WEIGHT_TERMS[dtype])) + ref.abs() * HALF_STEP[dtype] * (1 + 2.0 ** -9) + TINY[dtype]
+        seen = ~torch.isinf(z)
+        assert ((l - z).abs() <= w + z.abs() * 2.0 ** -23)[seen].all(), float((l - z).abs()[seen].max())
+        assert ((o - ref).abs() <= tol)[~ref.isnan()].all(), float(((o - ref).abs() / tol)[~ref.isnan()].max())

@@ -9,16 +9,6 @@ namespace {
 constexpr int ADJUST_MAX_VOCAB = 1 << 24;
 constexpr int AT = 256;                       // threads of a workgroup
 
-template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t dpp_plus(uint32_t v) { return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false); }
-__device__ __forceinline__ uint32_t runs_upto(uint32_t v) {      // sums up to the lane's
-  v = dpp_plus<0x111, 0xf>(v);
-  v = dpp_plus<0x112, 0xf>(v);
-  v = dpp_plus<0x114, 0xf>(v);
-  v = dpp_plus<0x118, 0xf>(v);
-  v = dpp_plus<0x142, 0xa>(v);
-  return dpp_plus<0x143, 0xc>(v);
-}
-
 struct AdjustArgs {
   const int32_t *row_start, *ids; const void* logits; void* out; int64_t stride, out_stride;
   ppd_logit_rules r;
@@ -63,7 +53,7 @@ __device__ __forceinline__ bool find_run(const AdjustArgs& a, int idx, int lane,
     for (int j = 0; j <= LOOK; ++j) lo[j] = start_of(from + LOOK * lane + j);
 #pragma unroll
     for (int j = 0; j < LOOK; ++j) { lo[j + 1] = max(lo[j + 1], lo[j]); runs[j] = (lo[j + 1] - lo[j] + (1 << a.run) - 1) >> a.run; mine += runs[j]; }
-    const int upto = before + (int)runs_upto((uint32_t)mine);
+    const int upto = before + scan_up(mine);
     const unsigned long long past = __ballot(upto > idx);
     if (past) {
       const int w = __builtin_ctzll(past);

@@ -115,15 +115,6 @@ __device__ __forceinline__ void seq_plan(const PagedAttnArgs& a, int s, SeqPlan&
   const int hi = min(p.r.pos0 + p.r.rows, a.b.room), lo = first_seen(p.r.pos0, a.window) & -PLAN_BLOCK;
   p.blocks = max(1, (hi - lo + PLAN_BLOCK - 1) / PLAN_BLOCK);
 }
-template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_add(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
-__device__ __forceinline__ int scan_up(int v) {          // sums up to the lane's: within rows of 16, then of the rows before
-  v = dpp_add<0x111, 0xf>(v);
-  v = dpp_add<0x112, 0xf>(v);
-  v = dpp_add<0x114, 0xf>(v);
-  v = dpp_add<0x118, 0xf>(v);
-  v = dpp_add<0x142, 0xa>(v);
-  return dpp_add<0x143, 0xc>(v);
-}
 // One part for each tile: sequence s has items from q_start[s] * group / TILE + min(s, q_start[s]) on.  That leaves room for its tiles (and sometimes
 // for one more), is known without the lengths before it, and never decreases: the last sequence that begins at or before the item has it.
 template <int TILE>
@@ -265,21 +256,6 @@ __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, int w
   const Span span = span_of(it.pos0, it.n, it.tile, TILE, a.group, it.part, it.parts, a.b.room, a.window);
   it.lo = span.lo; it.hi = span.hi;
   return true;
-}
-
-// Two weights as two terms of the type, side by side.  The first is cut off, not rounded, and the second is not zero where the weight is not (the
-// type's smallest normal number, or half floats' smallest one, 2^-31 of the row's largest weight): a value that is infinite has its sign in both
-// products.  (The rests of rounded first terms need a second pass without such values, 9 ms, not 0.6, for the two prompts where no value is a number;
-// else the same time.)
-__device__ __forceinline__ u32x2 two_terms(float x, float y, bf16_t) {
-  const uint32_t u = __float_as_uint(x), v = __float_as_uint(y);
-  const float a = x - __uint_as_float(u & 0xffff0000u), b = y - __uint_as_float(v & 0xffff0000u);
-  return (u32x2){__builtin_amdgcn_perm(v, u, 0x07060302u), pair(__builtin_amdgcn_fmed3f(a, x, 0x1p-126f), __builtin_amdgcn_fmed3f(b, y, 0x1p-126f), bf16_t())};
-}
-__device__ __forceinline__ u32x2 two_terms(float x, float y, f16_t) {
-  const auto h = __builtin_amdgcn_cvt_pkrtz(x, y);
-  const float a = x - (float)h[0], b = y - (float)h[1];
-  return (u32x2){__builtin_bit_cast(uint32_t, h), pair(__builtin_amdgcn_fmed3f(a, x, 0x1p-24f), __builtin_amdgcn_fmed3f(b, y, 0x1p-24f), f16_t())};
 }
 
 // ---- parts joined

@@ -21,15 +21,6 @@ struct PlanArgs {
 };
 __device__ __forceinline__ int pages_of(const PlanArgs& a, int positions) { return (int)a.by_size((uint32_t)positions + (uint32_t)a.page_size - 1u); }
 
-template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t dpp_plus(uint32_t v) { return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false); }
-__device__ __forceinline__ uint32_t wave_upto(uint32_t v) {      // sums up to the lane's
-  v = dpp_plus<0x111, 0xf>(v);
-  v = dpp_plus<0x112, 0xf>(v);
-  v = dpp_plus<0x114, 0xf>(v);
-  v = dpp_plus<0x118, 0xf>(v);
-  v = dpp_plus<0x142, 0xa>(v);
-  return dpp_plus<0x143, 0xc>(v);
-}
 // K sums of the threads before this one, and of all, at most 2^30 of either but for a wave's own share.  `to`: words of no other call's.
 template <int THREADS, int K>
 __device__ __forceinline__ void block_before(uint32_t (&v)[K], uint32_t (*to)[THREADS / WAVE], uint32_t (&all)[K]) {
@@ -38,7 +29,7 @@ __device__ __forceinline__ void block_before(uint32_t (&v)[K], uint32_t (*to)[TH
   uint32_t upto[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    upto[k] = wave_upto(v[k]);
+    upto[k] = (uint32_t)scan_up((int)v[k]);
     if (lane == 63) to[k][wave] = upto[k];
   }
   __syncthreads();

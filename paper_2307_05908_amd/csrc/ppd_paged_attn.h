@@ -23,12 +23,12 @@ struct PagedAttnArgs {
   int heads, kv_heads, group, window;
   int tile_rows, items;               // items: parts of a key/value head that there are workgroups and places for
   float to_log2;                      // scale * log2(e): a score's exponent of two
-  int wide_want; float wide_from;     // 0, or parts to aim at where all tiles together have this many blocks: wide workgroups then (paged_split_fp4_kernel)
   int want, fine, least, whole;       // parts per key/value head to aim at, and among sequences of unlike lengths; blocks of a part at least (0:
                                       // one part each), and up to which a tile is not cut
   float* part_o; float2* part_ml;     // [item][kv_heads][rows of a tile][head_dim], [item][kv_heads][rows of a tile]
   uint64_t* stamps; uint64_t stamp;   // paged_split_kernel, [item][kv_heads]: this call's number, once the part is there (see join_parts)
   int2* plan;                         // paged_tile_kernel, [n_seqs]: first item of a sequence, parts of its tiles
+  int wide_want; float wide_from;     // 0, or parts to aim at where all tiles together have this many blocks: wide workgroups then (paged_split_fp4_kernel)
 };
 
 // ---- element types as matrix operands
@@ -145,8 +145,9 @@ __device__ __forceinline__ bool find_whole(const PagedAttnArgs& a, int idx, int 
 // Every wave makes the plan for itself, from the lengths on the device: all tiles' blocks of positions together are cut into about
 // `want` parts of equal length, a tile at its own ends.  (The sum is in fp32, one order: every wave has the same; its error is far below
 // the one item that the grid has to spare.)  A lane looks at J sequences in turn, all lanes at once: up to 64 J sequences need one look.
-// False: there is no such item.
-template <int TILE, int J>
+// False: there is no such item.  WIDE: workgroups of four heads where there is so much to read (as a part of every kernel this cost one token's attention over 16-bit pages
+// 0.2 us of 10.8).
+template <int TILE, int J, bool WIDE>
 __device__ __forceinline__ bool find_part(const PagedAttnArgs& a, int idx, int wide_idx, bool tell, int lane, Item& it) {
   int tiles[J], blocks[J];
   SeqRows r1;                                               // (J 1: the lane's sequence)
@@ -173,7 +174,7 @@ __device__ __forceinline__ bool find_part(const PagedAttnArgs& a, int idx, int w
   // Two workgroups run on a unit, and where lengths differ and two long parts meet on one it is the last to end: then shorter parts, if they
   // are not too short for that.  bf16, us at `want` / `fine`: 64 sequences of 60 to 8000 positions 97 / 88, 32 of them 39.2 / 37.2, 64 of 60 to
   // 2000 32.1 / 34.2; of like lengths, 48 of 1000 38.6 / 45.1, 16 of 2000 29.3 / 32.9.
-  it.wide = a.wide_want > 0 && all >= a.wide_from;
+  it.wide = WIDE && a.wide_want > 0 && all >= a.wide_from;
   if (it.wide) idx = wide_idx;
   const float want = it.wide ? (float)a.wide_want : longest * count > 2.f * all && all >= 12.f * (float)a.fine ? (float)a.fine : (float)a.want;
   int len = max(a.least, (int)ceilf(all / want));
@@ -247,11 +248,11 @@ __device__ __forceinline__ bool find_part(const PagedAttnArgs& a, int idx, int w
 // the host has counted.
 __host__ __device__ __forceinline__ bool have_places(int first, int parts, int items) { return first >= 0 && parts <= items - first; }
 
-template <int TILE>
+template <int TILE, bool WIDE = false>
 __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int idx, int wide_idx, bool tell, int lane, Item& it) {
   it.wide = false;
-  if (!(a.least == 0 ? find_whole<TILE>(a, idx, lane, it) : a.b.n_seqs <= WAVE ? find_part<TILE, 1>(a, idx, wide_idx, tell, lane, it)
-                                                                               : find_part<TILE, 8>(a, idx, wide_idx, tell, lane, it))) return false;
+  if (!(a.least == 0 ? find_whole<TILE>(a, idx, lane, it) : a.b.n_seqs <= WAVE ? find_part<TILE, 1, WIDE>(a, idx, wide_idx, tell, lane, it)
+                                                                               : find_part<TILE, 8, WIDE>(a, idx, wide_idx, tell, lane, it))) return false;
   if (!have_places(it.slot - it.part, it.parts, a.items)) return false;
   const Span span = span_of(it.pos0, it.n, it.tile, TILE, a.group, it.part, it.parts, a.b.room, a.window);
   it.lo = span.lo; it.hi = span.hi;

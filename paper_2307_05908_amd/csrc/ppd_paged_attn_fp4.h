@@ -87,7 +87,7 @@ __device__ __forceinline__ bool find_tile(const PagedAttnArgs& a, int idx, int l
 template <int TILE>
 __device__ __forceinline__ bool find_item_fp4(const PagedAttnArgs& a, int idx, int wide_idx, bool tell, int lane, Item& it) {
   // (over 256 sequences of half a tile or less, gaps are few, and counting takes longer: 1000 of one token over 700 positions 207 us, not 226)
-  if (a.least > 0 || (a.b.n_seqs > 4 * WAVE && 2 * (int64_t)a.b.n_tokens * a.group <= (int64_t)TILE * a.b.n_seqs)) return find_item<TILE>(a, idx, wide_idx, tell, lane, it);
+  if (a.least > 0 || (a.b.n_seqs > 4 * WAVE && 2 * (int64_t)a.b.n_tokens * a.group <= (int64_t)TILE * a.b.n_seqs)) return find_item<TILE, TILE != TILE_ROWS>(a, idx, wide_idx, tell, lane, it);
   return a.b.n_seqs <= WAVE ? find_tile<TILE, 1>(a, idx, lane, it) : find_tile<TILE, 4>(a, idx, lane, it);
 }
 

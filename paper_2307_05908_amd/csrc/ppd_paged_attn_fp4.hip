@@ -13,7 +13,7 @@ namespace {
 // that order, too.  Values are widened in rows, too, and go through LDS rows of the wave's own, from where the transposing reads take them.
 // The next step's codes and scales are under way while one is worked on.  (Two steps were no faster, at two workgroups a unit or three, nor was a copy of the step's
 // codes through LDS.)  Bound by the reads, of half a line each where heads are neighbours: 64 bf16 tokens of 32 / 8 heads over 400 to 32000 positions,
-// 488 MB, take 125 us, 3.9 TB/s (bf16 pages of the same positions are 1.8 GB), 64 over 4000 63, 4.4 TB/s; the same with the loads taken out half of that.  With 4.25
+// 488 MB, take 123 us, 4.0 TB/s (bf16 pages of the same positions are 1.8 GB), 64 over 4000 63, 4.4 TB/s; the same with the loads taken out half of that.  With 4.25
 // bits a number widening counts, too: 38 % of the cycles are vector instructions.
 template <int HD, int G>
 struct Split4 {

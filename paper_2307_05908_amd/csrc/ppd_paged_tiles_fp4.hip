@@ -7,8 +7,8 @@ namespace {
 // Four waves of 32 rows each, see paged_tile_kernel: the same operands, orders and exchanged places in LDS.  Codes and scales of the block after the
 // next are under way in registers (a thread has a quarter of a row of keys and one of values), and the next block's are widened into the other
 // LDS buffer beside this one's products: one barrier a block.  Bound as paged_tile_kernel is, by the products and the vector instructions beside them, which are
-// issued in turns (46 and 51 % of the cycles): two bf16 prompts of 3937 and 4013 tokens, 32 / 8 heads, take 370 us, 1050 TFLOP/s with the second
-// terms of the weights, 700 without; a chunk of 500 fp16 rows over 4000 positions, 40 heads, 94 with the join of its parts.  Half of what is written to LDS meets
+// issued in turns (46 and 51 % of the cycles): two bf16 prompts of 3937 and 4013 tokens, 32 / 8 heads, take 366 us, 1050 TFLOP/s with the second
+// terms of the weights, 700 without; a chunk of 500 fp16 rows over 4000 positions, 40 heads, 96 with the join of its parts.  Half of what is written to LDS meets
 // another lane's on the same banks; without that (lanes' words in another order) it was no faster.
 template <typename T, int HD, bool NEAR>
 __global__ __launch_bounds__(256, 2) void paged_tile_fp4_kernel(Fp4AttnArgs a) {

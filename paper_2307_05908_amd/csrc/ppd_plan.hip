@@ -1,7 +1,7 @@
 // ppd_paged_plan: a step's row starts, lengths, pages and slots, from what each sequence keeps and wants.  Bound by latencies: one workgroup
 // reads the lengths, sums them up (sequences in their order, so that results do not depend on when a wave runs) and moves the pages' numbers;
 // the places of many rows are found by a launch of their own.  24 sequences 6.3 us, an empty kernel takes 2 to 3; 2048 sequences that move 16000 pages' numbers and
-// have 131000 rows 18.7 + 6.0 (which sequence a page or a row belongs to by searches instead of marks, see owners: 38 together).
+// have 131000 rows 18.6 + 6.0 (which sequence a page or a row belongs to by searches instead of marks, see owners: 38 together).
 #include "ppd_divide.h"
 #include "ppd_layers_common.h"
 

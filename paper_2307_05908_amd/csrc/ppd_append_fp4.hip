@@ -1,7 +1,7 @@
 // ppd_paged_append_fp4: queries and keys normalised per head and rotated to their positions, keys and values into pages of 4-bit numbers.
 // Bound by reading the rows and writing queries (and, where asked for, the values that the pages have now), and, close behind, by the keys' arithmetic in 64 bits:
 // 4915 bf16 tokens of 40 + 2 * 40 heads, 329 MB, take 84 us among others, 3.9 TB/s (a copy 67; a launch under a trace, or replayed, 94); with the keys' scales and codes from 32 bits
-// a trace had 79, but a key next to a border would have a code that depends on the order of operations.  Bounds in 32 bits first, and 64 bits only where these leave it open, were no faster (94 of then 91), and
+// a trace had 79, but a key next to a border would have a code that depends on the order of operations.  Bounds in 32 bits first, and 64 bits only where these leave it open, were no faster (94 of then 93), and
 // no exchange between lanes or other order of the angles in LDS was either.
 #include "ppd_divide.h"
 #include "ppd_paged_fp4.h"

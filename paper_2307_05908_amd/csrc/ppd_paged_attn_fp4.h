@@ -1,7 +1,8 @@
 // What the kernels of ppd_paged_attention_fp4 share, beside what they have from ppd_paged_attention's.
 //
 // Codes become bf16 numbers in registers, without rounding, and from there on both products are those of bf16 keys and values.  What is not bf16
-// goes in as a sum of bf16 terms: queries of fp16 in two (11 bits of significand in 8 + 8) and of fp32 in three (24 in 8 + 8 + 8), exactly;
+// goes in as a sum of bf16 terms: queries of fp16 in two (11 bits of significand in 8 + 8) and of fp32 in three (24 in 8 + 8 + 8), exactly (fp32 ones
+// times scale * log2(e), rounded to fp32);
 // softmax weights in two for 16-bit results (2^-17 of each is lost, and the result's own rounding is 2^-9 or 2^-12), in three for fp32.
 #pragma once
 #include "ppd_paged_attn.h"
